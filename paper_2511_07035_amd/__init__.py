@@ -547,5 +547,19 @@ def gockpt_load(ctx, path: str, host_ptr: int, host_bytes: int, nthreads: int = 
 
 from .session import Session, StateSlab  # noqa: E402  (torch-backed buffers around the C-ABI)
 
+# Operators around the step (torch tensors in and out): loaded at their first
+# use, since this module itself is imported without torch.
+_OPS = ("GradList", "GradResult", "embedding", "embedding_grad", "gockpt_embedding_grad_bytes", "gockpt_scale_ptr",
+        "GOCKPT_BF16", "GOCKPT_FP16", "GOCKPT_FP32")
+
+
+def __getattr__(name: str):
+    if name in _OPS:
+        from . import ops
+        globals().update({n: getattr(ops, n) for n in _OPS})
+        return globals()[name]
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+
+
 __all__ = [n for n in dir() if n.startswith(("gockpt_", "GOCKPT_"))] + ["Session", "StateSlab", "GockptError", "lib",
-                                                           "RECORD_DTYPE"]
+                                                           "RECORD_DTYPE", *_OPS]

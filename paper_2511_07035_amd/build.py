@@ -3,7 +3,7 @@
     python -m paper_2511_07035_amd.build
 
 Produces ``paper_2511_07035_amd/libgockpt.so`` (the C-ABI declared in
-``include/gockpt.h``) and ``paper_2511_07035_amd/libgockpt_bench.so`` (device
+``include/gockpt.h`` and ``include/gockpt_ops.h``) and ``paper_2511_07035_amd/libgockpt_bench.so`` (device
 helpers of the benchmark harness and tests: the forward/backward stand-in,
 HBM probes, a kernel that holds every wave slot, and a device division and
 square root for bitwise checks).
@@ -39,7 +39,7 @@ HIP_FLAGS = [
 HOST_FLAGS = ["-O3", "-std=c++17", "-fPIC", "-ffp-contract=off", "-fno-math-errno", "-mavx2", "-msse4.2", "-Wall",
               f"-I{INCLUDE}"]
 
-LIB_HIP = ["gockpt_kernels.hip", "gockpt_cast.hip", "gockpt_runtime.hip"]
+LIB_HIP = ["gockpt_kernels.hip", "gockpt_cast.hip", "gockpt_runtime.hip", "gockpt_grads.hip", "gockpt_embed.hip"]
 LIB_HOST = ["gockpt_plan.cpp", "gockpt_planner.cpp", "gockpt_restore.cpp", "gockpt_persist.cpp"]
 BENCH_HIP = ["bench_kernels.hip"]
 

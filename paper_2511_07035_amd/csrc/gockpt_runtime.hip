@@ -64,6 +64,7 @@
 #include <thread>
 #include <vector>
 
+#include "../../include/gockpt_ops.h"
 #include "gockpt_internal.h"
 
 namespace gockpt {
@@ -1918,6 +1919,14 @@ int gockpt_get_scaler(gockpt_ctx* c, int64_t* t, float* scale, int64_t* tracker)
     if (t) *t = h.t;
     if (scale) *scale = h.scale;
     if (tracker) *tracker = h.tracker;
+    return GOCKPT_OK;
+}
+
+int gockpt_scale_ptr(const gockpt_ctx* c, const float** out) {
+    if (out == nullptr) return GOCKPT_EINVAL;
+    *out = nullptr;
+    if (c == nullptr) return GOCKPT_EINVAL;
+    *out = reinterpret_cast<const float*>(c->ws + kWsScalerOff + offsetof(DevScaler, scale));
     return GOCKPT_OK;
 }
 

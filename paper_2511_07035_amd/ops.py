@@ -1,0 +1,355 @@
+"""Operators around the optimizer step -- binding of ``include/gockpt_ops.h``.
+
+``GradList``        norm and clipping of a list of gradient tensors
+``embedding``       rows of a table by token id, scaled (differentiable)
+``embedding_grad``  the table's gradient
+
+Checks of shapes and types are made here or in the library and raise
+ValueError or GockptError; all arithmetic runs in the library's kernels.
+Calls are queued on the current torch stream, or on ``stream``; as with any
+torch operation, tensors written on another stream have to be waited for.
+"""
+from __future__ import annotations
+
+import ctypes
+import struct
+
+import torch
+
+from . import GOCKPT_EINVAL, GockptError, _check, lib
+
+GOCKPT_BF16, GOCKPT_FP16, GOCKPT_FP32 = 0, 1, 2
+NO_PADDING = -(1 << 63)
+
+_DTYPE = {torch.bfloat16: GOCKPT_BF16, torch.float16: GOCKPT_FP16, torch.float32: GOCKPT_FP32}
+_BITS = {torch.int32: 32, torch.int64: 64}
+
+# The structs of gockpt_ops.h as packed bytes.
+GRAD_TENSOR = struct.Struct("<QQqqqii")   # data, dst, rows, cols, stride, dtype, dst_dtype
+MATRIX = struct.Struct("<Qqqqii")         # data, rows, cols, stride, dtype, reserved
+TOKEN_IDS = struct.Struct("<Qqqqqii")     # ids, batch, length, stride, first_id, bits, reserved
+GRAD_RESULT = struct.Struct("<dfff3f")    # sumsq, norm, found_inf, coef, reserved
+
+_P = ctypes.c_void_p
+_B = ctypes.c_char_p
+_SZ = ctypes.POINTER(ctypes.c_size_t)
+_ops = None
+
+
+def _lib():
+    global _ops
+    if _ops is None:
+        L = lib()
+        for name, args in (
+                ("gockpt_grads_bytes", [_B, ctypes.c_int64, _SZ]),
+                ("gockpt_grads_create", [_B, ctypes.c_int64, _P, ctypes.c_size_t, _P, ctypes.POINTER(_P)]),
+                ("gockpt_grads_destroy", [_P]),
+                ("gockpt_grads_norm", [_P, _P, ctypes.c_double, _P, _P]),
+                ("gockpt_grads_scale", [_P, _P, _P]),
+                ("gockpt_grads_clip", [_P, _P, ctypes.c_double, _P, _P]),
+                ("gockpt_grads_result", [_P, _P, ctypes.c_double, _P]),
+                ("gockpt_scale_ptr", [_P, ctypes.POINTER(_P)]),
+                ("gockpt_embedding", [_B, _B, ctypes.c_float, _B, _P]),
+                ("gockpt_embedding_grad_bytes", [ctypes.c_int64, ctypes.c_int64, ctypes.c_int64, _SZ]),
+                ("gockpt_embedding_grad", [_B, _B, ctypes.c_int64, ctypes.c_float, ctypes.c_int, _B, _P,
+                                           ctypes.c_size_t, _P])):
+            f = getattr(L, name)
+            f.argtypes, f.restype = args, ctypes.c_int
+        _ops = L
+    return _ops
+
+
+def gockpt_scale_ptr(ctx) -> int:
+    """Device address of a context's loss scale."""
+    out = _P()
+    _check(_lib().gockpt_scale_ptr(ctx, ctypes.byref(out)), "gockpt_scale_ptr", None)
+    return out.value
+
+
+def gockpt_embedding_grad_bytes(tokens: int, rows: int, cols: int) -> int:
+    n = ctypes.c_size_t()
+    _check(_lib().gockpt_embedding_grad_bytes(int(tokens), int(rows), int(cols), ctypes.byref(n)),
+           "gockpt_embedding_grad_bytes", None)
+    return n.value
+
+
+def _here(t, what: str) -> None:
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{what}: expected a tensor on the current GPU, got one on {t.device}")
+
+
+def _dtype(t, what: str) -> int:
+    d = _DTYPE.get(t.dtype)
+    if d is None:
+        raise ValueError(f"{what}: expected bfloat16, float16 or float32, got {t.dtype}")
+    return d
+
+
+def _stream(stream, device) -> int:
+    return (torch.cuda.current_stream(device) if stream is None else stream).cuda_stream
+
+
+def _rows(shape, stride):
+    """(rows, cols, row stride) of elements in row-major order, or None where
+    they are not rows of adjacent elements at one distance."""
+    dims = []
+    for n, s in zip(shape, stride):
+        if n == 0:
+            return 0, 0, 0
+        if n == 1:
+            continue
+        if dims and dims[-1][1] == n * s:
+            dims[-1] = (dims[-1][0] * n, s)
+        else:
+            dims.append((n, s))
+    if not dims:
+        return 1, 1, 1
+    if dims[-1][1] != 1:
+        dims.append((1, 1))
+    if len(dims) == 1:
+        return 1, dims[0][0], dims[0][0]
+    if len(dims) == 2 and dims[0][1] >= dims[1][0]:
+        return dims[0][0], dims[1][0], dims[0][1]
+    return None
+
+
+class GradResult:
+    """The device-resident outcome of a norm: one-element tensors ``norm``
+    (of the unscaled gradients), ``found_inf`` (1.0 or 0.0; what
+    ``Session(found_inf=...)`` takes), ``coef`` (the clipping coefficient) and
+    ``sumsq`` (float64, of the elements as stored: what ranks add up)."""
+
+    def __init__(self, device="cuda"):
+        self.buffer = torch.zeros(8, dtype=torch.float32, device=device)
+        self.sumsq = self.buffer[:2].view(torch.float64)
+        self.norm = self.buffer[2:3]
+        self.found_inf = self.buffer[3:4]
+        self.coef = self.buffer[4:5]
+        self.ptr = self.buffer.data_ptr()
+
+    def update(self, max_norm: float = float("inf"), scale=None, stream=None) -> "GradResult":
+        """norm, found_inf and coef again from ``sumsq``, after ranks that hold
+        different parameters have added theirs up."""
+        _here(self.buffer, "result")
+        _check(_lib().gockpt_grads_result(self.ptr, _scale_ptr(scale), max_norm,
+                                          _stream(stream, self.buffer.device)), "gockpt_grads_result", None)
+        return self
+
+
+def _scale_ptr(scale):
+    """Address of a one-element float32 device tensor, or of the loss scale of
+    a Session."""
+    if scale is None:
+        return None
+    if isinstance(scale, torch.Tensor):
+        if scale.dtype != torch.float32 or scale.numel() != 1:
+            raise ValueError("scale: expected a one-element float32 tensor or a Session")
+        _here(scale, "scale")
+        return scale.data_ptr()
+    return gockpt_scale_ptr(scale.ctx)
+
+
+class GradList:
+    """A handle over gradient tensors (bfloat16, float16 and float32 mixed, any
+    sizes, any alignment of their elements; rows may lie apart).
+
+    out: destinations of ``clip`` and ``scale``, one for each tensor (contiguous,
+    as many elements, any of the three types: views of ``Session.grad``, say);
+    None, or None in a place: in place.  Writing in place also takes a tensor
+    whose dimensions are permuted.  The handle keeps the tensors alive and
+    holds their addresses: make a new one when they move.  Its calls run one
+    at a time, in stream order."""
+
+    def __init__(self, tensors, out=None, stream=None):
+        self.handle = None
+        self.tensors = list(tensors)
+        self.out = [None] * len(self.tensors) if out is None else list(out)
+        if len(self.out) != len(self.tensors):
+            raise ValueError(f"{len(self.tensors)} tensors, {len(self.out)} destinations")
+        table = bytearray()
+        for i, (t, o) in enumerate(zip(self.tensors, self.out)):
+            _here(t, f"tensor {i}")
+            d = _dtype(t, f"tensor {i}")
+            r = _rows(t.shape, t.stride())
+            if r is None and o is None:  # element by element in place: the order does not matter
+                r = _rows(*zip(*sorted(zip(t.shape, t.stride()), key=lambda x: -x[1])))
+            if r is None:
+                raise ValueError(f"tensor {i}: shape {tuple(t.shape)} with strides {t.stride()} is not rows of "
+                                 "adjacent elements")
+            if o is not None:
+                _here(o, f"out {i}")
+                if o.numel() != t.numel() or not o.is_contiguous():
+                    raise ValueError(f"out {i}: expected {t.numel()} contiguous elements, got {tuple(o.shape)}")
+            table += GRAD_TENSOR.pack(t.data_ptr(), 0 if o is None else o.data_ptr(), *r, d,
+                                      d if o is None else _dtype(o, f"out {i}"))
+        table, n, size = bytes(table), len(self.tensors), ctypes.c_size_t()
+        _check(_lib().gockpt_grads_bytes(table, n, ctypes.byref(size)), "gockpt_grads_bytes", None)
+        self.device = self.tensors[0].device if n else torch.device("cuda", torch.cuda.current_device())
+        with torch.cuda.stream(stream):
+            self.workspace = torch.empty(size.value, dtype=torch.uint8, device=self.device)
+            self.result = GradResult(self.device)
+        handle = _P()
+        _check(_lib().gockpt_grads_create(table, n, self.workspace.data_ptr(), size.value,
+                                          _stream(stream, self.device), ctypes.byref(handle)),
+               "gockpt_grads_create", None)
+        self.handle = handle.value
+
+    def _open(self):
+        if self.handle is None:
+            raise GockptError(GOCKPT_EINVAL, "GradList", "closed")
+        return self.handle
+
+    def norm(self, max_norm: float = float("inf"), *, scale=None, result=None, stream=None) -> GradResult:
+        """The norm over all tensors, divided by ``scale`` (the loss scale the
+        gradients carry: a device tensor or a Session), into ``result`` (the
+        list's own, overwritten by its next call, if None)."""
+        r = self.result if result is None else result
+        _check(_lib().gockpt_grads_norm(self._open(), _scale_ptr(scale), max_norm, r.ptr,
+                                        _stream(stream, self.device)), "gockpt_grads_norm", None)
+        return r
+
+    def clip(self, max_norm: float, *, scale=None, result=None, stream=None) -> GradResult:
+        """``norm``, then every element times min(1, max_norm / (norm + 1e-6))
+        in place or into ``out``.  With an inf or NaN among the gradients they
+        are left, or copied, as they are, and ``found_inf`` tells."""
+        r = self.result if result is None else result
+        _check(_lib().gockpt_grads_clip(self._open(), _scale_ptr(scale), max_norm, r.ptr,
+                                        _stream(stream, self.device)), "gockpt_grads_clip", None)
+        return r
+
+    def scale(self, result=None, *, stream=None) -> None:
+        """Every element times ``result.coef``: the second half of ``clip``."""
+        r = self.result if result is None else result
+        _check(_lib().gockpt_grads_scale(self._open(), r.ptr, _stream(stream, self.device)), "gockpt_grads_scale",
+               None)
+
+    def close(self) -> None:
+        if self.handle is not None:
+            _lib().gockpt_grads_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def _matrix(t, what: str, cols=None) -> bytes:
+    """A 2-D tensor, or with cols the rows of that many elements of any."""
+    _here(t, what)
+    d = _dtype(t, what)
+    if t.dim() == 2:
+        (rows, n), (stride, step) = t.shape, t.stride()
+    elif cols is not None and t.dim() > 0:
+        n, step = t.shape[-1], t.stride(-1)
+        r = _rows(t.shape[:-1], t.stride()[:-1])
+        if n and r is not None and r[0] and r[1] != 1 and r[0] != 1:
+            r = None
+        if r is None:
+            raise ValueError(f"{what}: shape {tuple(t.shape)} with strides {t.stride()} is not rows at one distance")
+        rows = t.numel() // n if n else 0
+        stride = r[2] if r[1] == 1 else 1
+    else:
+        raise ValueError(f"{what}: expected a matrix, got shape {tuple(t.shape)}")
+    if (step != 1 and n > 1) or (cols is not None and n != cols):
+        raise ValueError(f"{what}: expected rows of {cols if cols is not None else n} adjacent elements, got shape "
+                         f"{tuple(t.shape)} with strides {t.stride()}")
+    return MATRIX.pack(t.data_ptr(), rows, n, stride, d, 0)
+
+
+def _token_ids(ids, first_id: int) -> bytes:
+    _here(ids, "ids")
+    bits = _BITS.get(ids.dtype)
+    if bits is None:
+        raise ValueError(f"ids: expected int32 or int64, got {ids.dtype}")
+    r = _rows(ids.shape, ids.stride())
+    if r is None:
+        raise ValueError(f"ids: shape {tuple(ids.shape)} with strides {ids.stride()} is not rows of adjacent ids")
+    return TOKEN_IDS.pack(ids.data_ptr(), *r, first_id, bits, 0)
+
+
+def _lookup(weight, ids, scale, out, out_dtype, first_id, stream):
+    shape = (*ids.shape, weight.shape[1]) if weight.dim() == 2 else None
+    if out is None and shape is not None:
+        dtype = weight.dtype if out_dtype is None else out_dtype
+        if stream is None:
+            out = torch.empty(shape, dtype=dtype, device=weight.device)
+        else:
+            with torch.cuda.stream(stream):
+                out = torch.empty(shape, dtype=dtype, device=weight.device)
+    elif out is not None and (tuple(out.shape) != shape or (out_dtype is not None and out.dtype != out_dtype)):
+        raise ValueError(f"out: expected shape {shape}, got {tuple(out.shape)} of {out.dtype}")
+    w = _matrix(weight, "weight")
+    _check(_lib().gockpt_embedding(w, _token_ids(ids, first_id), scale, _matrix(out, "out", weight.shape[1]),
+                                   _stream(stream, weight.device)), "gockpt_embedding", None)
+    return out
+
+
+def embedding(weight, ids, *, scale: float = 1.0, out=None, out_dtype=None, first_id: int = 0, padding_id=None,
+              grad_weight=None, accumulate: bool = False, stream=None):
+    """scale * weight[ids - first_id] of shape (*ids.shape, dim), rounded once
+    to out_dtype (default: the weight's).  Ids outside [first_id, first_id +
+    rows) are masked: zeros, and no gradient.
+
+    Differentiable in weight, with the gradient of ``embedding_grad``: returned
+    to autograd in the weight's type, or, with grad_weight (the weight's part
+    of ``Session.grad``), written or accumulated there and not returned.  Tokens
+    with padding_id add no gradient.  out and stream are for calls that need
+    no gradient."""
+    if weight.requires_grad and torch.is_grad_enabled():
+        if out is not None or stream is not None:
+            raise ValueError("out and stream: for calls without a gradient")
+        return _Embedding.apply(weight, ids, scale, out_dtype, first_id, padding_id, grad_weight, accumulate)
+    return _lookup(weight, ids, scale, out, out_dtype, first_id, stream)
+
+
+def embedding_grad(grad_out, ids, grad_weight, *, scale: float = 1.0, accumulate: bool = False, first_id: int = 0,
+                   padding_id=None, workspace=None, stream=None):
+    """grad_weight[v] = scale * (sum of the rows of grad_out whose id is
+    first_id + v), summed in fp32 and rounded once; every row is written.  With
+    accumulate the sums are added to what grad_weight holds and rows without a
+    token are left alone.  workspace: a uint8 tensor of at least
+    gockpt_embedding_grad_bytes(tokens, rows, dim) (None: allocated)."""
+    m = _matrix(grad_weight, "grad_weight")
+    if tuple(grad_out.shape[:-1]) != tuple(ids.shape):
+        raise ValueError(f"grad_out of shape {tuple(grad_out.shape)} for ids of shape {tuple(ids.shape)}")
+    rows, cols = grad_weight.shape
+    tokens = ids.numel()
+    device = grad_weight.device
+    if workspace is None:
+        size = gockpt_embedding_grad_bytes(tokens, rows, cols)
+        if size and stream is None:
+            workspace = torch.empty(size, dtype=torch.uint8, device=device)
+        elif size:
+            with torch.cuda.stream(stream):
+                workspace = torch.empty(size, dtype=torch.uint8, device=device)
+    else:
+        _here(workspace, "workspace")
+        if workspace.dtype != torch.uint8 or not workspace.is_contiguous():
+            raise ValueError("workspace: expected a contiguous uint8 tensor")
+    _check(_lib().gockpt_embedding_grad(
+        _matrix(grad_out, "grad_out", cols), _token_ids(ids, first_id), NO_PADDING if padding_id is None else padding_id,
+        scale, accumulate, m, None if workspace is None else workspace.data_ptr(),
+        0 if workspace is None else workspace.numel(), _stream(stream, device)), "gockpt_embedding_grad", None)
+    return grad_weight
+
+
+class _Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, weight, ids, scale, out_dtype, first_id, padding_id, grad_weight, accumulate):
+        ctx.save_for_backward(ids)
+        ctx.args = dict(scale=scale, first_id=first_id, padding_id=padding_id)
+        ctx.into, ctx.accumulate = grad_weight, accumulate
+        ctx.like = (weight.shape, weight.dtype, weight.device)
+        return _lookup(weight.detach(), ids, scale, None, out_dtype, first_id, None)
+
+    @staticmethod
+    def backward(ctx, grad_out):
+        (ids,) = ctx.saved_tensors
+        into = ctx.into
+        if into is None:
+            shape, dtype, device = ctx.like
+            into = torch.empty(shape, dtype=dtype, device=device)
+        embedding_grad(grad_out.contiguous(), ids, into, accumulate=ctx.accumulate and ctx.into is not None, **ctx.args)
+        return (into if ctx.into is None else None,) + (None,) * 7

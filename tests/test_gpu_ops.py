@@ -1,0 +1,552 @@
+"""Norm, clipping, embedding lookup and its gradient on the GPU, against plain
+implementations in float64.
+
+Tolerances, with u = 2^-24:
+  norm      a sum of squares groups at most 32 fp32 products, each sum off by
+            32 u at most, so the norm by 16 u, and its rounding to fp32 by u:
+            17 u.  The coefficient inherits that and rounds once more: 18 u.
+  clip, embedding   one fp32 product rounded once: the same bits as torch.
+  embedding_grad    fp32 sums of n terms are off by n u sum|x|; the product
+            with the scale, the sum with the old value and the rounding to
+            the output's type (half an ulp) come on top.
+"""
+import math
+
+import numpy as np
+import pytest
+
+import paper_2511_07035_amd as g
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+DT = {"bf16": torch.bfloat16, "fp16": torch.float16, "fp32": torch.float32}
+HALF_ULP = {torch.bfloat16: (2.0 ** -8, 2.0 ** -134), torch.float16: (2.0 ** -11, 2.0 ** -25),
+            torch.float32: (U, 2.0 ** -150)}
+
+
+def bits(t):
+    return t.contiguous().view({2: torch.int16, 4: torch.int32}[t.element_size()])
+
+
+def same(a, b):
+    """The same bits; a NaN equals a NaN."""
+    nan = torch.isnan(a) & torch.isnan(b)
+    return bool(((bits(a) == bits(b)) | nan).all())
+
+
+def randn(shape, dtype, seed, sigma=1e-3):
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(seed)
+    return torch.empty(shape, device="cuda").normal_(0.0, sigma, generator=gen).to(dtype)
+
+
+# ---- lists of gradients --------------------------------------------------------
+
+
+def tensors_of(kind, dtype, seed):
+    sizes = {"one": [1], "tiny": [1, 2, 3, 7, 8, 9, 15, 17], "edge": [8191, 8192, 8193, 4096, 4097, 16385],
+             "many": [(i * 37) % 501 + 1 for i in range(3000)], "big": [3_000_001, 5, 1_234_567], "none": []}
+    if kind in sizes:
+        return [randn((n,), dtype, seed + n) for n in sizes[kind]]
+    if kind == "offsets":  # views that start and end anywhere in one buffer
+        buf, out, at = randn((200_000,), dtype, seed), [], 1
+        for n in (1, 5, 1023, 1, 20_001, 8192, 16, 3, 70_000, 11):
+            out.append(buf[at:at + n])
+            at += n + (n % 3)
+        return out
+    if kind == "strided":
+        return [randn((50, 70), dtype, seed)[:, 3:30], randn((3, 20_000), dtype, seed + 1)[:, :9001],
+                randn((40_000, 2), dtype, seed + 2)[:, 1], randn((700, 33), dtype, seed + 3)[:, :1],
+                randn((5, 6, 130), dtype, seed + 4)[:, :, :129], randn((64, 4097), dtype, seed + 5)[:, :4096],
+                randn((9, 11, 13), dtype, seed + 6)[:, :11], randn((1100, 16), dtype, seed + 7)[:, 8:]]
+    if kind == "empty":
+        return [randn((0,), dtype, seed), randn((4, 0), dtype, seed), randn((100,), dtype, seed)]
+    raise ValueError(kind)
+
+
+def norm64(tensors, scale=1.0):
+    return math.sqrt(sum(float(t.double().square().sum()) for t in tensors)) / scale
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("kind", ["one", "tiny", "edge", "many", "big", "none", "offsets", "strided", "empty"])
+def test_norm(kind, dtype):
+    ts = tensors_of(kind, DT[dtype], 11)
+    gl = g.GradList(ts)
+    scale = torch.full((1,), 256.0, device="cuda")
+    want = norm64(ts, 256.0)
+    r = gl.norm(want / 3 if want else 1.0, scale=scale)
+    first = r.buffer.clone()
+    assert float(r.found_inf) == 0.0
+    assert abs(float(r.norm) - want) <= 17 * U * want
+    coef = min(1.0, (want / 3 if want else 1.0) / (want + 1e-6))
+    assert abs(float(r.coef) - coef) <= 18 * U * coef
+    assert float(gl.norm(scale=scale).coef) == 1.0
+    for _ in range(3):  # the same bits every time
+        assert torch.equal(gl.norm(want / 3 if want else 1.0, scale=scale).buffer, first)
+
+
+def test_norm_of_mixed_types():
+    ts = [randn((999,), torch.bfloat16, 1), randn((65, 129), torch.float32, 2), randn((4001,), torch.float16, 3)] * 5
+    assert abs(float(g.GradList(ts).norm().norm) - norm64(ts)) <= 17 * U * norm64(ts)
+
+
+@pytest.mark.parametrize("value", [3e38, 1e25, 1.5e19, 1e-15, 1e-22, 1e-38, 1e-40])
+def test_norm_where_fp32_squares_leave_the_range(value):
+    # every element within the type's range counts, however large or small
+    for ts in ([torch.full((10_007,), value, device="cuda")],
+               [torch.full((10_007,), value, device="cuda"), torch.zeros(5000, device="cuda")]):
+        x = float(ts[0][0].double())
+        want = x * math.sqrt(10_007)
+        r = g.GradList(ts).norm()
+        assert float(r.found_inf) == 0.0
+        assert abs(float(r.sumsq) - want * want) <= 34 * U * want * want
+        if want < 3e38:
+            assert abs(float(r.norm) - want) <= 17 * U * want + 2.0 ** -150
+        else:
+            assert math.isinf(float(r.norm))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+def test_found_inf_and_clip_of_non_finite_gradients(dtype, value):
+    for at in (0, 7, 8191, 8192, 12_344, 20_000):
+        t = randn((20_001,), DT[dtype], 5)
+        t[at] = value
+        keep, out = t.clone(), torch.zeros(20_001, dtype=torch.float32, device="cuda")
+        r = g.GradList([randn((64,), DT[dtype], 6), t]).clip(1e-3)
+        assert float(r.found_inf) == 1.0 and float(r.coef) == 1.0
+        assert not math.isfinite(float(r.norm)) and math.isnan(float(r.norm)) == math.isnan(value)
+        assert same(t, keep)
+        g.GradList([t], [out]).clip(1e-3)
+        assert same(out, keep.float())
+
+
+def test_all_zero_gradients():
+    t = torch.zeros(5000, device="cuda")
+    t[::2] = -0.0
+    r = g.GradList([t]).clip(0.0)
+    assert float(r.norm) == 0.0 and float(r.found_inf) == 0.0 and float(r.coef) == 0.0
+
+
+@pytest.mark.parametrize("dst", ["bf16", "fp16", "fp32", None])
+@pytest.mark.parametrize("src", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("kind", ["tiny", "edge", "many", "offsets", "strided", "empty"])
+def test_clip(kind, src, dst):
+    ts = tensors_of(kind, DT[src], 23)
+    keep = [t.clone() for t in ts]
+    flat = None
+    if dst is not None:  # a flat buffer, tensors one after another from an odd place on
+        flat = torch.full((sum(t.numel() for t in ts) + 9,), 7.0, dtype=DT[dst], device="cuda")
+        outs = list(torch.split(flat[3:-6], [t.numel() for t in ts]))
+    want = norm64(ts)
+    gl = g.GradList(ts, outs if dst is not None else None)
+    r = gl.clip(0.37 * want)
+    assert abs(float(r.norm) - want) <= 17 * U * want
+    got = [o.view(t.shape) for o, t in zip(outs, ts)] if dst is not None else ts
+    for a, k in zip(got, keep):
+        assert same(a, (k.float() * r.coef).to(a.dtype))
+    if dst is not None:
+        assert bool((flat[:3] == 7.0).all()) and bool((flat[-6:] == 7.0).all())
+        for t, k in zip(ts, keep):
+            assert same(t, k)
+        gl.clip(2.0 * want)  # under the limit: rounded, not scaled
+        for a, k in zip(got, keep):
+            assert same(a, k.to(a.dtype))
+
+
+def test_clip_writes_nothing_between_strided_rows():
+    buf = randn((300, 64), torch.bfloat16, 3)
+    keep = buf.clone()
+    view = buf[:, 5:44]
+    r = g.GradList([view]).clip(1e-4)
+    want = keep.clone()
+    want[:, 5:44] = (keep[:, 5:44].float() * r.coef).to(torch.bfloat16)
+    assert float(r.coef) < 1.0 and same(buf, want)
+
+
+def test_clip_in_place_of_permuted_dimensions():
+    t = randn((30, 50, 4), torch.float32, 9).permute(2, 0, 1)
+    keep = t.clone()
+    r = g.GradList([t]).clip(1e-3)
+    assert same(t, keep * r.coef)
+
+
+def test_norm_then_scale_and_ranks():
+    """Two ranks hold different parameters: their sums of squares are added
+    up, and both clip by the norm of all."""
+    a, b = [randn((30_001,), torch.bfloat16, 1)], [randn((77, 501), torch.bfloat16, 2)]
+    la, lb = g.GradList(a), g.GradList(b)
+    keep = [a[0].clone(), b[0].clone()]
+    scale = torch.full((1,), 8.0, device="cuda")
+    ra, rb = la.norm(1e-3, scale=scale), lb.norm(1e-3, scale=scale)
+    total = ra.sumsq + rb.sumsq
+    want = norm64(a + b, 8.0)
+    for r, gl in ((ra, la), (rb, lb)):
+        r.sumsq.copy_(total)
+        r.update(1e-3, scale=scale)
+        assert abs(float(r.norm) - want) <= 17 * U * want
+        gl.scale(r)
+    assert torch.equal(ra.buffer, rb.buffer)
+    for t, k in zip(a + b, keep):
+        assert same(t, (k.float() * ra.coef).to(t.dtype))
+
+
+def test_list_refusals():
+    t = torch.zeros(64, device="cuda")
+    for bad in (t.double(), t.expand(3, 64), torch.zeros(8, 8, 8, device="cuda")[:, :4, :4]):
+        with pytest.raises(ValueError):
+            g.GradList([bad])
+    for out in ([], [torch.zeros(63, device="cuda")], [torch.zeros(128, device="cuda")[::2]],
+                [torch.zeros(64, device="cuda", dtype=torch.float64)]):
+        with pytest.raises(ValueError):
+            g.GradList([t], out)
+    with pytest.raises(ValueError):
+        g.GradList([torch.zeros(8, 9, device="cuda").t()], [torch.zeros(72, device="cuda")])
+    gl = g.GradList([t])
+    for scale in (torch.zeros(2, device="cuda"), torch.zeros(1, device="cuda", dtype=torch.float64), torch.zeros(1)):
+        with pytest.raises(ValueError):
+            gl.norm(scale=scale)
+    for most in (-1.0, float("nan")):
+        with pytest.raises(g.GockptError):
+            gl.clip(most)
+    gl.close()
+    gl.close()
+    with pytest.raises(g.GockptError):
+        gl.norm()
+
+
+# ---- embedding -----------------------------------------------------------------
+
+
+def ids_of(kind, tokens, vocab, seed):
+    r = np.random.default_rng(seed)
+    if kind == "uniform":
+        ids = r.integers(0, vocab, tokens)
+    elif kind == "zipf":
+        p = 1.0 / (np.arange(vocab) + 2.7)
+        ids = r.choice(vocab, tokens, p=p / p.sum())
+    elif kind == "same":
+        ids = np.full(tokens, vocab // 2)
+    elif kind == "masked":
+        ids = np.where(r.random(tokens) < 0.5, r.integers(0, vocab, tokens),
+                       r.choice([-1, -100, vocab, vocab + 5, 2 ** 31 - 1, -(2 ** 31)], tokens))
+    elif kind == "none":
+        ids = np.full(tokens, -1)
+    elif kind == "ends":
+        ids = r.choice([0, vocab - 1], tokens)
+    elif kind == "sorted":
+        ids = np.sort(r.integers(0, vocab, tokens))[::-1].copy()
+    return torch.from_numpy(np.ascontiguousarray(ids, dtype=np.int64)).cuda()
+
+
+def lookup_plain(weight, ids, scale, dtype, first=0):
+    at = ids - first
+    there = (ids >= first) & (at < weight.shape[0])
+    rows = weight[at.clamp(0, max(weight.shape[0] - 1, 0))].float() * torch.tensor(scale, dtype=torch.float32,
+                                                                                  device="cuda")
+    return torch.where(there[..., None], rows, torch.zeros_like(rows)).to(dtype)
+
+
+@pytest.mark.parametrize("out", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("weight", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("tokens,vocab,dim", [(1, 300, 4096), (1, 7, 1), (3, 50, 8), (129, 1000, 513), (1025, 321, 64),
+                                              (700, 97, 2056), (17, 33, 5121), (4099, 5000, 24)])
+def test_embedding(tokens, vocab, dim, weight, out):
+    w = randn((vocab, dim), DT[weight], 4, 0.02)
+    for kind, bits_ in (("uniform", torch.int64), ("masked", torch.int32)):
+        ids = ids_of(kind, tokens, vocab, 8).to(bits_)
+        got = g.embedding(w, ids, scale=7.3, out_dtype=DT[out])
+        assert got.shape == (tokens, dim) and same(got, lookup_plain(w, ids.long(), 7.3, DT[out]))
+
+
+def test_embedding_strides_shards_and_special_values():
+    wide = randn((100, 80), torch.float32, 5)
+    wide[3, 10:14] = torch.tensor([float("inf"), float("-inf"), float("nan"), -0.0], device="cuda")
+    w = wide[:, 7:74]
+    ids = torch.arange(-4, 108, device="cuda").view(8, 14)
+    buf = torch.full((8, 11, 90), 5.0, device="cuda")
+    # sequences cut from longer ones, rows of a wider output, the table a slice
+    out = g.embedding(w, ids[:, :11], scale=-2.0, out=buf.view(88, 90)[:, 9:76].view(8, 11, 67))
+    assert same(out, lookup_plain(w, ids[:, :11], -2.0, torch.float32))
+    assert bool((buf[..., :9] == 5.0).all()) and bool((buf[..., 76:] == 5.0).all())
+    # masked tokens are +0 whatever the scale
+    for scale in (-1.0, float("inf"), float("nan")):
+        z = g.embedding(w, torch.full((3,), -1, device="cuda"), scale=scale)
+        assert bool((bits(z) == 0).all())
+    # a shard of the vocabulary: the other ranks' ids are masked
+    whole = lookup_plain(w, ids, 1.5, torch.bfloat16)
+    parts = [g.embedding(w[a:b], ids, scale=1.5, first_id=a, out_dtype=torch.bfloat16) for a, b in ((0, 31), (31, 100))]
+    both = parts[0] + parts[1]  # -0 + 0 is 0: values, not bits
+    assert bool(((both == whole) | (torch.isnan(both) & torch.isnan(whole))).all())
+    # ids at the ends of their type
+    far = torch.tensor([2 ** 63 - 1, -(2 ** 63), 2 ** 63 - 1 - 5], device="cuda")
+    got = g.embedding(w, far, first_id=2 ** 63 - 1 - 5)
+    assert same(got, torch.stack([w[5], torch.zeros(67, device="cuda"), w[0]]))
+    assert bool((bits(g.embedding(w, far[1:2], first_id=2 ** 63 - 1)) == 0).all())
+    assert g.embedding(w, ids[:0]).shape == (0, 14, 67)
+    assert same(g.embedding(w, ids[2, 6]), w[30])
+
+
+def grad_plain(grad_out, ids, rows, first=0, padding=None):
+    """(sum, sum of magnitudes, number of terms) of each row, float64."""
+    flat = ids.reshape(-1)
+    there = (flat >= first) & (flat - first < rows)
+    if padding is not None:
+        there &= flat != padding
+    at, x = flat[there] - first, grad_out.reshape(flat.numel(), -1)[there].double()
+    total = torch.zeros(rows, x.shape[1], dtype=torch.float64, device="cuda").index_add_(0, at, x)
+    size = torch.zeros_like(total).index_add_(0, at, x.abs())
+    n = torch.zeros(rows, dtype=torch.float64, device="cuda").index_add_(0, at, torch.ones_like(at, dtype=torch.float64))
+    return total, size, n[:, None]
+
+
+def check_grad(got, total, size, n, scale, old=None):
+    want = total * scale
+    slack = abs(scale) * (n + 2.0) * U * size
+    if old is not None:
+        want = want + torch.where(n > 0, old.double(), torch.zeros_like(want))
+        slack = slack + U * (want.abs() + slack)
+    rel, least = HALF_ULP[got.dtype]
+    err = (got.double() - (want if old is None else torch.where(n > 0, want, old.double()))).abs()
+    bound = slack + rel * (want.abs() + slack) + least
+    bound = torch.where(n > 0, bound, torch.zeros_like(bound))
+    assert bool((err <= bound).all()), float((err - bound).max())
+
+
+GRAD_SHAPES = [(1, 10, 8), (1, 1, 1), (2, 70, 3), (48, 320, 64), (97, 64, 513), (130, 65, 2048), (2048, 50, 40),
+               (2049, 50, 40), (2049, 3000, 24), (5000, 1000, 264), (5000, 129, 5121), (20_001, 4001, 136),
+               (70_000, 300_001, 16), (66_000, 64, 8), (3001, 263_000, 9)]
+
+
+@pytest.mark.parametrize("kind", ["uniform", "zipf", "same", "masked", "none", "ends", "sorted"])
+@pytest.mark.parametrize("tokens,vocab,dim", GRAD_SHAPES)
+def test_embedding_grad(tokens, vocab, dim, kind):
+    ids = ids_of(kind, tokens, vocab, 31)
+    x = randn((tokens, dim), torch.float32, 17)
+    total, size, n = grad_plain(x, ids, vocab)
+    out = torch.full((vocab, dim), 9.0, device="cuda")
+    assert g.embedding_grad(x, ids, out, scale=3.5) is out
+    check_grad(out, total, size, n, 3.5)
+    assert bool((bits(out)[n[:, 0] == 0] == 0).all())
+    for _ in range(2):  # the same bits every time
+        again = torch.empty_like(out)
+        assert same(g.embedding_grad(x, ids, again, scale=3.5), out)
+    old = randn((vocab, dim), torch.float32, 18)
+    added = g.embedding_grad(x, ids.int(), old.clone(), scale=-0.25, accumulate=True)
+    check_grad(added, total, size, n, -0.25, old)
+
+
+@pytest.mark.parametrize("dst", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("src", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("tokens,vocab,dim", [(300, 200, 75), (6000, 500, 520)])
+def test_embedding_grad_types(tokens, vocab, dim, src, dst):
+    ids = ids_of("zipf", tokens, vocab, 3)
+    x = randn((tokens, dim), DT[src], 7)
+    total, size, n = grad_plain(x, ids, vocab)
+    check_grad(g.embedding_grad(x, ids, torch.full((vocab, dim), 5.0, dtype=DT[dst], device="cuda"), scale=11.0),
+               total, size, n, 11.0)
+    old = randn((vocab, dim), DT[dst], 8)
+    check_grad(g.embedding_grad(x, ids, old.clone(), accumulate=True), total, size, n, 1.0, old)
+
+
+@pytest.mark.parametrize("length", [40, 900])
+def test_embedding_grad_strides_shards_and_padding(length):
+    batch, vocab, dim = 7, 333, 130
+    ids = ids_of("zipf", batch * (length + 1), vocab, 5).view(batch, length + 1)[:, 1:]
+    x = randn((batch * length, dim + 9), torch.bfloat16, 6)[:, 4:dim + 4].view(batch, length, dim)
+    x[0, 0] = float("nan")  # a masked token's gradient is not read
+    ids = ids.clone() if length == 40 else ids
+    ids[0, 0] = -1
+    wide = torch.full((vocab, 200), 5.0, device="cuda")
+    total, size, n = grad_plain(torch.nan_to_num(x), ids, vocab, padding=1)
+    g.embedding_grad(x, ids, wide[:, 3:dim + 3], padding_id=1)
+    check_grad(wide[:, 3:dim + 3], total, size, n, 1.0)
+    assert bool((wide[:, :3] == 5.0).all()) and bool((wide[:, dim + 3:] == 5.0).all())
+    assert bool((wide[1, 3:dim + 3] == 0.0).all())
+    shards = [torch.empty(r, dim, device="cuda") for r in (100, 233)]
+    g.embedding_grad(x, ids, shards[0], padding_id=1)
+    g.embedding_grad(x, ids, shards[1], padding_id=1, first_id=100)
+    check_grad(torch.cat(shards), total, size, n, 1.0)
+
+
+def test_embedding_grad_of_non_finite_rows():
+    for tokens in (64, 4000):
+        ids = torch.arange(tokens, device="cuda") % 50
+        x = randn((tokens, 16), torch.float32, 1)
+        x[3, 2], x[4, 5] = float("inf"), float("nan")
+        out = g.embedding_grad(x, ids, torch.zeros(60, 16, device="cuda"))
+        bad = ~torch.isfinite(out)
+        assert int(bad.sum()) == 2 and math.isinf(float(out[3, 2])) and math.isnan(float(out[4, 5]))
+
+
+def test_no_tokens():
+    ids = torch.zeros(0, 5, dtype=torch.int64, device="cuda")
+    x = torch.zeros(0, 5, 24, device="cuda")
+    out = torch.full((70, 24), 3.0, device="cuda")
+    g.embedding_grad(x, ids, out, accumulate=True)
+    assert bool((out == 3.0).all())
+    g.embedding_grad(x, ids, out)
+    assert bool((out == 0.0).all())
+
+
+def test_embedding_refusals():
+    w, ids = torch.zeros(10, 8, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda")
+    for bad in (dict(weight=w.double()), dict(weight=w[0]), dict(weight=w.t()), dict(ids=ids.float()),
+                dict(ids=torch.zeros(8, 8, dtype=torch.int64, device="cuda").t()),
+                dict(out=torch.zeros(3, 8, device="cuda")), dict(out=torch.zeros(8, 4, device="cuda").t()),
+                dict(out=torch.zeros(4, 8, device="cuda"), out_dtype=torch.float16)):
+        with pytest.raises(ValueError):
+            g.embedding(**(dict(weight=w, ids=ids) | bad))
+    x = torch.zeros(4, 8, device="cuda")
+    for bad in (dict(grad_out=x[:3]), dict(grad_out=x[:, :7]), dict(grad_weight=w.t()), dict(grad_out=x.double()),
+                dict(ids=ids.double()), dict(workspace=torch.zeros(9, device="cuda"))):
+        with pytest.raises(ValueError):
+            g.embedding_grad(**(dict(grad_out=x, ids=ids, grad_weight=w.clone()) | bad))
+    with pytest.raises(g.GockptError):  # a workspace too small
+        g.embedding_grad(torch.zeros(4000, 8, device="cuda"), torch.zeros(4000, dtype=torch.int64, device="cuda"),
+                         w.clone(), workspace=torch.zeros(512, dtype=torch.uint8, device="cuda"))
+
+
+def test_autograd_against_differences_and_the_formula():
+    """The loss sum(c * y^2) of y = s * W[ids] is quadratic in W: its central
+    difference is exact but for rounding.  In float32 with W, c, s of about 1
+    and y^2 up to 30 the loss of 200 terms is off by 200 * 30 u ~ 4e-4 at most,
+    a difference over 2 h = 1 as much again twice: 8e-4."""
+    torch.manual_seed(2)
+    vocab, dim = 12, 5
+    w = torch.randn(vocab, dim, device="cuda", requires_grad=True)
+    ids = torch.tensor([[1, 5, 5, -1, 11], [0, 5, 3, 1, 1], [2, 2, 2, 2, 7], [5, 99, 1, 0, 0]], device="cuda")
+    c = torch.rand(4, 5, dim, device="cuda")
+
+    def loss(weight):
+        return (c * g.embedding(weight, ids, scale=1.25, padding_id=2).square()).sum()
+
+    loss(w).backward()
+    y = lookup_plain(w.detach(), ids, 1.25, torch.float32)
+    total, size, n = grad_plain(2.0 * c * y, ids, vocab, padding=2)
+    check_grad(w.grad, total, size * (1 + 4 * U), n, 1.25)
+    for v, d in ((5, 0), (1, 3), (0, 4), (11, 2), (8, 1), (2, 0)):
+        h = torch.zeros_like(w)
+        h[v, d] = 0.5
+        with torch.no_grad():
+            diff = float(loss(w + h)) - float(loss(w - h))
+        if v == 2:  # the padding id is looked up but learns nothing
+            assert float(w.grad[v, d]) == 0.0 and diff != 0.0
+        else:
+            assert abs(float(w.grad[v, d]) - diff) <= 8e-4
+    # into the caller's buffer, added to what a tied head left there
+    into = torch.ones(vocab, dim, dtype=torch.bfloat16, device="cuda")
+    w2 = w.detach().clone().requires_grad_()
+    (c * g.embedding(w2, ids, scale=1.25, padding_id=2, grad_weight=into, accumulate=True).square()).sum().backward()
+    assert w2.grad is None
+    check_grad(into, total, size * (1 + 4 * U), n, 1.25, torch.ones(vocab, dim, device="cuda"))
+
+
+# ---- streams and graphs ----------------------------------------------------------
+
+
+def test_on_another_stream():
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        x = torch.zeros(9000, 64, device="cuda")
+        ids = torch.arange(9000, device="cuda") % 77
+        torch.cuda._sleep(20_000_000)  # the inputs are written late on this stream
+        x.fill_(1.0)
+    w = torch.empty(77, 64, dtype=torch.bfloat16, device="cuda")
+    s.wait_stream(torch.cuda.current_stream())
+    g.embedding_grad(x, ids, w, stream=s)
+    gl = g.GradList([w], stream=s)
+    r = gl.clip(1.0, stream=s)
+    y = g.embedding(w, ids, stream=s)
+    s.synchronize()
+    n = torch.bincount(ids, minlength=77).double()
+    want = math.sqrt(float((n.square() * 64).sum()))
+    assert abs(float(r.norm) - want) <= 17 * U * want
+    assert same(y, w[ids])
+
+
+@pytest.mark.parametrize("tokens", [200, 6000])
+def test_captured_in_a_graph(tokens):
+    vocab, dim = 500, 96
+    w, ids = randn((vocab, dim), torch.bfloat16, 1, 0.02), ids_of("zipf", tokens, vocab, 2)
+    x = randn((tokens, dim), torch.bfloat16, 3)
+    y, gw = torch.empty(tokens, dim, dtype=torch.bfloat16, device="cuda"), torch.empty_like(w)
+    flat = torch.empty(vocab * dim + 700, dtype=torch.bfloat16, device="cuda")
+    main = randn((700,), torch.float32, 4)
+    gl = g.GradList([gw, main], [flat[:vocab * dim], flat[vocab * dim:]])
+    ws = torch.empty(max(g.gockpt_embedding_grad_bytes(tokens, vocab, dim), 256), dtype=torch.uint8, device="cuda")
+    s = torch.cuda.Stream()
+    torch.cuda.synchronize()
+
+    def step():
+        g.embedding(w, ids, scale=2.0, out=y)
+        g.embedding_grad(x, ids, gw, scale=2.0, workspace=ws)
+        gl.clip(1e-3)
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        step()
+    torch.cuda.synchronize()
+    for k in range(4):
+        x.copy_(randn((tokens, dim), torch.bfloat16, 30 + k))
+        ids.copy_(ids_of("zipf", tokens, vocab, 40 + k))
+        main.copy_(randn((700,), torch.float32, 50 + k))
+        step()
+        want = [t.clone() for t in (y, gw, flat, gl.result.buffer)]
+        for t in (y, gw, flat):
+            t.fill_(3.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip((y, gw, flat, gl.result.buffer), want):
+            assert same(a, b)
+
+
+# ---- with a Session ----------------------------------------------------------------
+
+
+def test_a_clipped_window_and_the_loss_scale_on_the_device():
+    """The flat gradient is clipped, with the Session's own loss scale read on
+    the device, before each step of a save window; found_inf skips the step
+    whose gradients overflow; the restored checkpoint equals the state."""
+    n, K = 40_000, 4
+    result = g.GradResult()
+    sess = g.Session(n, ring_bytes=1 << 20, dynamic_scale=True, init_scale=1024.0, found_inf=result.found_inf,
+                     grad_norm=False)
+    try:
+        with torch.cuda.stream(sess.compute):
+            sess.master.normal_(0.0, 0.02)
+            sess.weight.copy_(sess.master)
+            gl = g.GradList([sess.grad[:12_345], sess.grad[12_345:]], stream=sess.compute)
+        sess.begin_window([0, 8000, 16_000, 24_000, n])
+        scale = 1024.0
+        for s in range(1, K + 1):
+            sess.backward_begin()
+            with torch.cuda.stream(sess.compute):
+                sess.grad.copy_(randn((n,), torch.float32, s, 1e-3 * scale))
+                if s == 2:
+                    sess.grad[30_000] = float("inf")
+                before = sess.grad.clone()
+                r = gl.clip(0.1, scale=sess, result=result)
+                sess.compute.synchronize()
+                want = norm64([before], scale)
+                if s == 2:
+                    assert float(r.found_inf) == 1.0
+                    scale *= 0.5
+                else:
+                    assert abs(float(r.norm) - want) <= 17 * U * want and float(r.coef) < 1.0
+                assert same(sess.grad, (before.float() * r.coef).to(torch.bfloat16))
+            sess.step(1e-4)
+        sess.drain()
+        assert list(sess.records()["skip"]) == [0, 1, 0, 0]
+        meta = sess.restore()
+        dev = sess.state_to_host()
+        assert meta.t == 3 and meta.scale == 512.0
+        for a, b in zip(sess.arena_state(), dev[:3]):
+            assert np.array_equal(a.view(np.uint32), b.view(np.uint32))
+    finally:
+        sess.close()
