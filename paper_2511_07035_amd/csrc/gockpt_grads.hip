@@ -6,11 +6,20 @@
 //                  norm = sqrt(S) / scale, found_inf, and the clipping
 //                  coefficient min(1, max_norm / (norm + 1e-6)).
 //   scale_kernel   element * coef, rounded to the destination's type.
+//   whole_kernel   all of it in one launch for a list of at most 8 MiB.
 //
 // The host cuts the tensors into tiles of at most 1024 units of 16 source
 // bytes (16 KiB) once, when the list is made; a tensor of any size, type,
 // stride or start is a few entries of one table, and one launch covers all.
+//
+// Memory bounds all of it: 2 flops an element against 2 or 4 bytes read.  On
+// the 1.31e9 bf16 gradients of GPT 1.3B (2.62 GB in 195 tensors) the norm takes
+// 374 us, 7.0 TB/s, which is what a read-only probe reaches.  Clipping reads
+// twice, since no element can be scaled before the last one is squared: 5.2 GB
+// of fp32 gradients rounded into bf16 take 1992 us, 6.6 TB/s over the 13.1 GB
+// moved.  Up to 8 MiB a launch costs more than the data, hence whole_kernel.
 #include <math.h>
+#include <stdlib.h>
 
 #include <new>
 #include <vector>
@@ -26,11 +35,39 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kUnitsPerThread = 4;
 constexpr int kTileUnits = kThreads * kUnitsPerThread;
-constexpr int kMaxBlocks = 2048;  // 8 blocks of 4 wavefronts on each of 256 compute units
+
+// Blocks of sumsq_kernel.  Each keeps the next tile's loads in flight during
+// the arithmetic of the current one, so 4 blocks a compute unit are enough and
+// fewer partials are left to add (GPT 1.3B in bf16 376 us, with 2048 390).
+constexpr int kSumBlocks = 1024;
+
+// Lists of up to this many tiles (8 MiB) take one launch, a tile a block.  us
+// a call in one launch and in two (norm) or three (clip): 2^17 bf16 elements
+// 5.6 and 8.6, 6.0 and 11.1; 2^21 5.5 and 8.7, 8.6 and 11.4; 2^22, the limit,
+// 5.5 and 8.4, 11.3 and 11.4.  Above it, blocks of two or four tiles that keep
+// them in registers gained nothing (2^23 8.2 and 8.5, 16.3 and 16.2).
+constexpr int kWholeTiles = 512;
+// Polls (about 0.5 us each) before a block computes the partials it misses;
+// none with GOCKPT_TEST_GRADS_AGAIN=1 in the environment when the list is made,
+// with which tests reach that path.
+constexpr int kWholeSpins = 64;
+
+// Clipping up to this many source bytes: the sums leave what they read in the
+// last-level cache, and scale_kernel, last tiles first, finds part of it there
+// (us cached and with nontemporal loads: 1.3e8 bf16 elements 128 and 134,
+// 2.7e8 256 and 260; 1.3e9 fp32 2086 and 1992).  The norm alone always reads
+// with the hint (1.3e9 bf16 390 against 436).
+constexpr int64_t kCachedSumBytes = int64_t{512} << 20;
+// scale_kernel has the hint on loads and stores where it moves more than this
+// (us without and with it: 64 MiB in and out 36.5 and 37.8, 128 MiB 79.7 and
+// 68.1; fp32 to bf16 64 + 32 MiB 30.7 and 32.5, 128 + 64 MiB 63.0 and 56.2).
+constexpr int64_t kCachedScaleBytes = int64_t{144} << 20;
 constexpr double kClipEps = 1e-6;
 
 // Rows of one tensor, or a piece of one row.  Unit u of a tile is unit u %
-// per_row of row u / per_row; every unit but a row's last holds 16 bytes.
+// per_row of row u / per_row.  A unit is 16 bytes of source; a row's last one
+// is the 16 bytes that end with the row, of which the first `skip` belong to
+// the unit before (or, in a row of under 16 bytes, to nothing).
 struct GradTile {
     const uint8_t* src;
     uint8_t* dst;
@@ -39,7 +76,7 @@ struct GradTile {
     int32_t units;     // of the tile, at most kTileUnits
     int32_t per_row;   // units of a row
     uint32_t magic;    // per_row > 1: floor(2^32 / per_row) + 1, u / per_row is the high word of u * magic
-    int16_t last;      // bytes in a row's last unit, 2 to 16
+    int16_t skip;      // of a row's last unit: 0 to 14
     int8_t dtype, dst_dtype;
 };
 static_assert(sizeof(GradTile) == 48, "table entry");
@@ -59,26 +96,53 @@ __device__ __forceinline__ void unit_place(const GradTile& t, uint32_t u, uint32
     }
 }
 
-// Unit u of the tile; zeros in the places behind the row's end.
-__device__ __forceinline__ u32x4 load_unit(const GradTile& t, uint32_t u) {
-    uint32_t row, k;
-    unit_place(t, u, row, k);
-    const uint8_t* p = t.src + row * t.stride + k * 16u;
-    if (k + 1 < static_cast<uint32_t>(t.per_row) || t.last == 16) return *reinterpret_cast<const u32x4_any*>(p);
-    const uint16_t* h = reinterpret_cast<const uint16_t*>(p);
-    u32x4 raw = {0u, 0u, 0u, 0u};
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (2 * i < t.last) raw[i / 2] |= static_cast<uint32_t>(h[i]) << (16 * (i & 1));
-    return raw;
+__device__ __forceinline__ uint32_t unit_skip(const GradTile& t, uint32_t k) {
+    return k + 1 == static_cast<uint32_t>(t.per_row) ? t.skip : 0;
 }
 
+// The units of this thread, zeros beyond the tile's end.  What a last unit
+// skips is not cleared: that would wait for the load.
+template <bool kNT>
 __device__ __forceinline__ void load_tile(const GradTile& t, u32x4 (&raw)[kUnitsPerThread]) {
+    if (t.per_row == 1 && t.skip > 0) {  // rows of under 16 bytes
+#pragma unroll
+        for (int i = 0; i < kUnitsPerThread; ++i) {
+            const uint32_t u = i * kThreads + threadIdx.x;
+            raw[i] = (u32x4){0u, 0u, 0u, 0u};
+            if (u >= static_cast<uint32_t>(t.units)) continue;
+            const uint16_t* h = reinterpret_cast<const uint16_t*>(t.src + u * t.stride - t.skip);
+#pragma unroll
+            for (int j = 1; j < 8; ++j)
+                if (2 * j >= t.skip) raw[i][j / 2] |= static_cast<uint32_t>(h[j]) << (16 * (j & 1));
+        }
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < kUnitsPerThread; ++i) {
         const uint32_t u = i * kThreads + threadIdx.x;
         raw[i] = (u32x4){0u, 0u, 0u, 0u};
-        if (u < static_cast<uint32_t>(t.units)) raw[i] = load_unit(t, u);
+        if (u >= static_cast<uint32_t>(t.units)) continue;
+        uint32_t row, k;
+        unit_place(t, u, row, k);
+        const u32x4_any* p =
+            reinterpret_cast<const u32x4_any*>(t.src + row * t.stride + k * 16u - unit_skip(t, k));
+        raw[i] = kNT ? __builtin_nontemporal_load(p) : *p;
+    }
+}
+
+// Clears what a tile's last units skip.
+__device__ __forceinline__ void clear_skipped(const GradTile& t, u32x4 (&raw)[kUnitsPerThread]) {
+    if (t.skip == 0) return;
+#pragma unroll
+    for (int i = 0; i < kUnitsPerThread; ++i) {
+        uint32_t row, k;
+        unit_place(t, i * kThreads + threadIdx.x, row, k);
+        const int skip = static_cast<int>(unit_skip(t, k));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (skip >= 4 * j + 2) raw[i][j] &= 0xFFFF0000u;
+            if (skip >= 4 * j + 4) raw[i][j] = 0u;
+        }
     }
 }
 
@@ -97,7 +161,8 @@ __device__ __forceinline__ void each_elem(u32x4 raw, F&& f) {
 
 // Sum of squares of a thread's units (at most 32 elements).  In fp32 unless
 // that may have lost something: an fp32 sum in [2^-100, 2^126) has overflowed
-// nowhere, and what its terms lost below 2^-149 is under 2^-44 of it.
+// nowhere, and what its terms lost below 2^-149 is under 2^-44 of it.  (All in
+// fp64 would be two more operations an element at a lower rate.)
 // Otherwise (or where it is NaN), and if some element is not zero, the squares
 // are added again in fp64, where those of fp32 values neither overflow nor
 // vanish and the sum is finite exactly when every element is.
@@ -122,24 +187,39 @@ __device__ __forceinline__ double block_sum(double x) {
     __shared__ double part[kThreads / 64];
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+    __syncthreads();  // an earlier sum has been read
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
     __syncthreads();
     return (part[0] + part[1]) + (part[2] + part[3]);
 }
 
+// raw -> the sum of its squares.
+__device__ __forceinline__ double tile_sum(const GradTile& t, u32x4 (&raw)[kUnitsPerThread]) {
+    clear_skipped(t, raw);
+    if (t.dtype == kBF16) return square_sum<kBF16>(raw);
+    if (t.dtype == kFP16) return square_sum<kFP16>(raw);
+    return square_sum<kFP32>(raw);
+}
+
+template <bool kNT>
 __global__ __launch_bounds__(kThreads) void sumsq_kernel(const GradTile* __restrict__ tiles, int ntiles,
                                                          double* __restrict__ parts) {
     double acc = 0.0;
-    for (int i = blockIdx.x; i < ntiles; i += gridDim.x) {
-        const GradTile t = tiles[i];
+    u32x4 next[kUnitsPerThread];
+    int i = blockIdx.x;
+    GradTile t = tiles[i];
+    load_tile<kNT>(t, next);
+    while (i < ntiles) {
         u32x4 raw[kUnitsPerThread];
-        load_tile(t, raw);
-        if (t.dtype == kBF16)
-            acc += square_sum<kBF16>(raw);
-        else if (t.dtype == kFP16)
-            acc += square_sum<kFP16>(raw);
-        else
-            acc += square_sum<kFP32>(raw);
+#pragma unroll
+        for (int k = 0; k < kUnitsPerThread; ++k) raw[k] = next[k];
+        const GradTile now = t;
+        i += gridDim.x;
+        if (i < ntiles) {
+            t = tiles[i];
+            load_tile<kNT>(t, next);
+        }
+        acc += tile_sum(now, raw);
     }
     acc = block_sum(acc);
     if (threadIdx.x == 0) parts[blockIdx.x] = acc;
@@ -170,75 +250,225 @@ __global__ void result_again_kernel(gockpt_grad_result* out, const float* scale,
     finish_result(out->sumsq, scale, max_norm, out);
 }
 
-// One unit times coef to its place in dst.
-template <int kS, int kD>
-__device__ __forceinline__ void scale_unit(u32x4 raw, float coef, uint8_t* d, int last) {
+// One element, or two, four or eight, at any address.
+template <int kT, int kN, bool kNT>
+__device__ __forceinline__ void store_n(uint8_t* p, const float* x) {
+    if constexpr (kT == kFP32) {
+        if constexpr (kN > 4) {
+            store_n<kT, 4, kNT>(p, x);
+            store_n<kT, kN - 4, kNT>(p + 16, x + 4);
+        } else {
+            typedef float vec __attribute__((ext_vector_type(kN)));
+            typedef vec vec_any __attribute__((aligned(2)));
+            vec v;
+#pragma unroll
+            for (int i = 0; i < kN; ++i) {
+                if constexpr (kN == 1)
+                    v = x[i];
+                else
+                    v[i] = x[i];
+            }
+            if constexpr (kNT)
+                __builtin_nontemporal_store(v, reinterpret_cast<vec_any*>(p));
+            else
+                *reinterpret_cast<vec_any*>(p) = v;
+        }
+    } else if constexpr (kN == 1) {
+        store_elem<kT>(p, x[0]);
+    } else {
+        typedef uint32_t vec __attribute__((ext_vector_type(kN / 2)));
+        typedef vec vec_any __attribute__((aligned(2)));
+        vec v;
+#pragma unroll
+        for (int i = 0; i < kN / 2; ++i) {
+            if constexpr (kN == 2)
+                v = pack2<kT>(x[0], x[1]);
+            else
+                v[i] = pack2<kT>(x[2 * i], x[2 * i + 1]);
+        }
+        if constexpr (kNT)
+            __builtin_nontemporal_store(v, reinterpret_cast<vec_any*>(p));
+        else
+            *reinterpret_cast<vec_any*>(p) = v;
+    }
+}
+
+// One unit times coef to its place in dst (d: of its first byte, skipped or
+// not).
+template <int kS, int kD, bool kNT>
+__device__ __forceinline__ void scale_unit(u32x4 raw, float coef, uint8_t* d, uint32_t skip) {
     constexpr int kN = kS == kFP32 ? 4 : 8;
     constexpr int kB = kD == kFP32 ? 4 : 2;
     float x[kN];
     int n = 0;
     each_elem<kS>(raw, [&](float v) { x[n++] = v * coef; });
-    if (last == 16) {
-        if constexpr (kD == kFP32) {
-#pragma unroll
-            for (int i = 0; i < kN; i += 4)
-                *reinterpret_cast<u32x4_any*>(d + 4 * i) =
-                    (u32x4){__float_as_uint(x[i]), __float_as_uint(x[i + 1]), __float_as_uint(x[i + 2]),
-                            __float_as_uint(x[i + 3])};
-        } else if constexpr (kN == 8) {
-            *reinterpret_cast<u32x4_any*>(d) = (u32x4){pack2<kD>(x[0], x[1]), pack2<kD>(x[2], x[3]),
-                                                       pack2<kD>(x[4], x[5]), pack2<kD>(x[6], x[7])};
-        } else {
-            *reinterpret_cast<u32x2_any*>(d) = (u32x2){pack2<kD>(x[0], x[1]), pack2<kD>(x[2], x[3])};
-        }
+    if (skip == 0) {
+        store_n<kD, kN, kNT>(d, x);
     } else {
-        const int m = last / (kS == kFP32 ? 4 : 2);
+        const int from = skip / (kS == kFP32 ? 4 : 2);
 #pragma unroll
-        for (int i = 0; i < kN; ++i)
-            if (i < m) store_elem<kD>(d + kB * i, x[i]);
+        for (int i = 1; i < kN; ++i)
+            if (i >= from) store_elem<kD>(d + kB * i, x[i]);
     }
 }
 
-template <int kS, int kD>
-__device__ __forceinline__ void scale_tile(const GradTile& t, float coef) {
-    u32x4 raw[kUnitsPerThread];
-    load_tile(t, raw);
+template <int kS, int kD, bool kNT>
+__device__ __forceinline__ void scale_units(const GradTile& t, const u32x4 (&raw)[kUnitsPerThread], float coef) {
 #pragma unroll
     for (int i = 0; i < kUnitsPerThread; ++i) {
         const uint32_t u = i * kThreads + threadIdx.x;
         if (u >= static_cast<uint32_t>(t.units)) break;
         uint32_t row, k;
         unit_place(t, u, row, k);
-        const int last = k + 1 < static_cast<uint32_t>(t.per_row) ? 16 : t.last;
-        constexpr uint32_t kUnitOut = 16u * (kD == kFP32 ? 4 : 2) / (kS == kFP32 ? 4 : 2);
-        scale_unit<kS, kD>(raw[i], coef, t.dst + row * t.dst_row + k * kUnitOut, last);
+        constexpr int kSrcBytes = kS == kFP32 ? 4 : 2, kDstBytes = kD == kFP32 ? 4 : 2;
+        const int skip = static_cast<int>(unit_skip(t, k));
+        const int at = (static_cast<int>(k) * 16 - skip) / kSrcBytes * kDstBytes;
+        scale_unit<kS, kD, kNT>(raw[i], coef, t.dst + row * t.dst_row + at, skip);
     }
 }
 
+// raw * coef to the tile's places in dst.
+template <bool kNT>
+__device__ __forceinline__ void scale_tile(const GradTile& t, const u32x4 (&raw)[kUnitsPerThread], float coef) {
+    if (t.dst == t.src && coef == 1.0f) return;
+    switch (t.dtype * 3 + t.dst_dtype) {
+        case kBF16 * 3 + kBF16: scale_units<kBF16, kBF16, kNT>(t, raw, coef); break;
+        case kBF16 * 3 + kFP16: scale_units<kBF16, kFP16, kNT>(t, raw, coef); break;
+        case kBF16 * 3 + kFP32: scale_units<kBF16, kFP32, kNT>(t, raw, coef); break;
+        case kFP16 * 3 + kBF16: scale_units<kFP16, kBF16, kNT>(t, raw, coef); break;
+        case kFP16 * 3 + kFP16: scale_units<kFP16, kFP16, kNT>(t, raw, coef); break;
+        case kFP16 * 3 + kFP32: scale_units<kFP16, kFP32, kNT>(t, raw, coef); break;
+        case kFP32 * 3 + kBF16: scale_units<kFP32, kBF16, kNT>(t, raw, coef); break;
+        case kFP32 * 3 + kFP16: scale_units<kFP32, kFP16, kNT>(t, raw, coef); break;
+        default: scale_units<kFP32, kFP32, kNT>(t, raw, coef); break;
+    }
+}
+
+// One tile a block, the last tiles first (sumsq_kernel read them last).  A
+// launch of all tiles is faster than 2048 blocks that walk over them: 1.3e9
+// fp32 elements into bf16 2145 us a clip against 2292.
+template <bool kNT>
 __global__ __launch_bounds__(kThreads) void scale_kernel(const GradTile* __restrict__ tiles, int ntiles,
                                                          const gockpt_grad_result* __restrict__ result) {
     const float coef = result->coef;
-    for (int i = blockIdx.x; i < ntiles; i += gridDim.x) {
-        const GradTile t = tiles[i];
-        if (t.dst == t.src && coef == 1.0f) continue;
-        switch (t.dtype * 3 + t.dst_dtype) {
-            case kBF16 * 3 + kBF16: scale_tile<kBF16, kBF16>(t, coef); break;
-            case kBF16 * 3 + kFP16: scale_tile<kBF16, kFP16>(t, coef); break;
-            case kBF16 * 3 + kFP32: scale_tile<kBF16, kFP32>(t, coef); break;
-            case kFP16 * 3 + kBF16: scale_tile<kFP16, kBF16>(t, coef); break;
-            case kFP16 * 3 + kFP16: scale_tile<kFP16, kFP16>(t, coef); break;
-            case kFP16 * 3 + kFP32: scale_tile<kFP16, kFP32>(t, coef); break;
-            case kFP32 * 3 + kBF16: scale_tile<kFP32, kBF16>(t, coef); break;
-            case kFP32 * 3 + kFP16: scale_tile<kFP32, kFP16>(t, coef); break;
-            default: scale_tile<kFP32, kFP32>(t, coef); break;
+    const GradTile t = tiles[ntiles - 1 - static_cast<int>(blockIdx.x)];
+    if (t.dst == t.src && coef == 1.0f) return;
+    u32x4 raw[kUnitsPerThread];
+    load_tile<kNT>(t, raw);
+    scale_tile<kNT>(t, raw, coef);
+}
+
+// ---- small lists: one launch ---------------------------------------------------
+//
+// Block b squares tile b, publishes its partial and, to clip, waits for the
+// partials of all blocks, adds them in the fixed order that every block uses,
+// and scales the tile, which it still has in registers.  For a norm only block
+// 0 waits.
+//
+// A partial is one 64-bit word: a double, and in the place of its sign, which
+// a sum of squares has no use for, the call's epoch modulo two.  Every call on
+// a list writes every slot, so a slot with the other tag is the last call's:
+// value and flag are one word, and no fence is needed, which on this chip would
+// write back an XCD's L2.  Block 0 moves the epoch on once it has seen every
+// partial, that is after every block has read it.
+//
+// No block but block 0 depends on another one running: after `spins`
+// polls it computes the missing partials itself, and block 0 thus waits only
+// for blocks that all finish on their own.  A missing partial's tile may be
+// scaled in place by its owner while it is read here, but the owner scales
+// only after it has seen its own partial published: if the slot is still empty
+// after the tile has been read, what was read is unscaled, and if it is not,
+// the slot's value is taken.
+
+constexpr uint64_t kSlotTag = uint64_t{1} << 63;
+
+__device__ __forceinline__ uint64_t slot_tag(uint32_t epoch) { return epoch & 1u ? kSlotTag : 0u; }
+
+__device__ __forceinline__ uint64_t read_slot(const uint64_t* p) {
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+template <bool kClip>
+__global__ __launch_bounds__(kThreads) void whole_kernel(const GradTile* __restrict__ tiles, uint32_t* sync,
+                                                         uint64_t* slots, int spins,
+                                                         const float* __restrict__ scale, double max_norm,
+                                                         gockpt_grad_result* __restrict__ out) {
+    __shared__ double all[kWholeTiles];
+    __shared__ float coef;
+    const int blocks = gridDim.x;
+    const uint32_t epoch = *sync;
+    const GradTile t = tiles[blockIdx.x];
+    u32x4 raw[kUnitsPerThread];
+    load_tile<false>(t, raw);
+    const double mine = block_sum(tile_sum(t, raw));
+    if (threadIdx.x == 0)
+        __hip_atomic_store(slots + blockIdx.x, (__builtin_bit_cast(uint64_t, mine) & ~kSlotTag) | slot_tag(epoch),
+                           __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (!kClip && blockIdx.x != 0) return;
+
+    // thread i waits for slots i and i + kThreads
+    constexpr int kPer = kWholeTiles / kThreads;
+    uint64_t word[kPer];
+    auto missing = [&]() {
+        bool m = false;
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            const int b = k * kThreads + static_cast<int>(threadIdx.x);
+            word[k] = b < blocks ? read_slot(slots + b) : slot_tag(epoch);
+            m |= (word[k] & kSlotTag) != slot_tag(epoch);
         }
+        return m;
+    };
+    bool wait = missing();
+    for (int i = 0; wait && (blockIdx.x == 0 || i < spins); ++i) {
+        __builtin_amdgcn_s_sleep(2);
+        wait = missing();
+    }
+#pragma unroll
+    for (int k = 0; k < kPer; ++k)  // -1: missing
+        all[k * kThreads + threadIdx.x] =
+            (word[k] & kSlotTag) == slot_tag(epoch) ? __builtin_bit_cast(double, word[k] & ~kSlotTag) : -1.0;
+    if (__syncthreads_or(wait)) {
+        for (int b = 0; b < blocks; ++b) {
+            if (all[b] != -1.0) continue;  // the same for all threads
+            const GradTile other = tiles[b];
+            u32x4 again[kUnitsPerThread];
+            load_tile<false>(other, again);
+            double x = block_sum(tile_sum(other, again));
+            if (threadIdx.x == 0) {
+                const uint64_t w = read_slot(slots + b);
+                if ((w & kSlotTag) == slot_tag(epoch)) x = __builtin_bit_cast(double, w & ~kSlotTag);
+                all[b] = x;
+            }
+            __syncthreads();
+        }
+    }
+    double acc = 0.0;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) acc += all[k * kThreads + threadIdx.x];
+    acc = block_sum(acc);
+    if (threadIdx.x == 0) {
+        gockpt_grad_result r;
+        finish_result(acc, scale, max_norm, &r);
+        coef = r.coef;
+        if (blockIdx.x == 0) {
+            *out = r;
+            *sync = epoch + 1u;
+        }
+    }
+    if constexpr (kClip) {
+        __syncthreads();
+        scale_tile<false>(t, raw, coef);
     }
 }
 
 // ---- host: the table ---------------------------------------------------------
 
 constexpr int64_t kMaxElems = int64_t{1} << 46;
-constexpr size_t kPartsBytes = kMaxBlocks * sizeof(double);
+// Workspace: sync word, slots of the one-launch form, partials, table.
+constexpr size_t kSlotsOff = 256;
+constexpr size_t kPartsOff = kSlotsOff + kWholeTiles * sizeof(uint64_t);
+constexpr size_t kTableOff = kPartsOff + kSumBlocks * sizeof(double);
 
 // A tensor as the tiles see it: rows that follow one another are one row.
 struct Flat {
@@ -302,7 +532,7 @@ int count_list(const char* name, const gockpt_grad_tensor* tensors, int64_t coun
         const int rc = check_tensor(name, i, tensors[i], &x);
         if (rc != GOCKPT_OK) return rc;
         *ntiles += count_tiles(x, tensors[i].dtype);
-        if (*ntiles > (int64_t{1} << 30)) return ops_fail(GOCKPT_EINVAL, "%s: too many elements", name);
+        if (*ntiles >= (int64_t{1} << 24)) return ops_fail(GOCKPT_EINVAL, "%s: too many elements", name);
     }
     return GOCKPT_OK;
 }
@@ -314,9 +544,10 @@ int count_list(const char* name, const gockpt_grad_tensor* tensors, int64_t coun
 using namespace gockpt;
 
 struct gockpt_grads {
-    double* parts;
+    uint8_t* ws;
     const GradTile* tiles;
-    int ntiles, blocks;
+    int ntiles, spins;
+    int64_t src_bytes, dst_bytes;  // of all tensors
 };
 
 extern "C" {
@@ -326,7 +557,7 @@ int gockpt_grads_bytes(const gockpt_grad_tensor* tensors, int64_t count, size_t*
     *bytes = 0;
     int64_t ntiles;
     const int rc = count_list("gockpt_grads_bytes", tensors, count, &ntiles);
-    if (rc == GOCKPT_OK) *bytes = (kPartsBytes + ntiles * sizeof(GradTile) + 255) / 256 * 256;
+    if (rc == GOCKPT_OK) *bytes = (kTableOff + ntiles * sizeof(GradTile) + 255) / 256 * 256;
     return rc;
 }
 
@@ -340,11 +571,14 @@ int gockpt_grads_create(const gockpt_grad_tensor* tensors, int64_t count, void* 
     if (rc != GOCKPT_OK) return rc;
     if (workspace == nullptr || reinterpret_cast<uintptr_t>(workspace) % 256 != 0)
         return ops_fail(GOCKPT_EINVAL, "%s: the workspace must be 256-byte aligned", name);
-    if (workspace_bytes < kPartsBytes + ntiles * sizeof(GradTile))
+    if (workspace_bytes < kTableOff + ntiles * sizeof(GradTile))
         return ops_fail(GOCKPT_ENOMEM, "%s: workspace of %zu bytes", name, workspace_bytes);
-    std::vector<GradTile> table;
+    std::vector<uint8_t> head;  // the workspace's contents
+    int64_t src_bytes = 0, dst_bytes = 0;
     try {
-        table.reserve(static_cast<size_t>(ntiles));
+        head.resize(kTableOff + ntiles * sizeof(GradTile));
+        *reinterpret_cast<uint32_t*>(head.data()) = 1u;  // the first epoch: cleared slots are not of it
+        GradTile* next = reinterpret_cast<GradTile*>(head.data() + kTableOff);
         for (int64_t i = 0; i < count; ++i) {
             const gockpt_grad_tensor& t = tensors[i];
             Flat x;
@@ -364,10 +598,12 @@ int gockpt_grads_create(const gockpt_grad_tensor* tensors, int64_t count, void* 
                 g.per_row = static_cast<int32_t>((cols * sb + 15) / 16);
                 g.units = static_cast<int32_t>(rows) * g.per_row;
                 g.magic = g.per_row > 1 ? static_cast<uint32_t>((uint64_t{1} << 32) / g.per_row) + 1u : 0u;
-                g.last = static_cast<int16_t>(cols * sb - (g.per_row - 1) * 16);
+                g.skip = static_cast<int16_t>(g.per_row * 16 - cols * sb);
                 g.dtype = static_cast<int8_t>(t.dtype);
                 g.dst_dtype = static_cast<int8_t>(dst_dtype);
-                table.push_back(g);
+                *next++ = g;
+                src_bytes += rows * cols * sb;
+                dst_bytes += rows * cols * db;
             });
         }
     } catch (...) {
@@ -375,20 +611,20 @@ int gockpt_grads_create(const gockpt_grad_tensor* tensors, int64_t count, void* 
     }
     gockpt_grads* list = new (std::nothrow) gockpt_grads;
     if (list == nullptr) return ops_fail(GOCKPT_ENOMEM, "%s: out of host memory", name);
-    list->parts = static_cast<double*>(workspace);
-    list->tiles = reinterpret_cast<const GradTile*>(static_cast<uint8_t*>(workspace) + kPartsBytes);
-    list->ntiles = static_cast<int>(table.size());
-    list->blocks = list->ntiles < kMaxBlocks ? list->ntiles : kMaxBlocks;
-    if (!table.empty()) {
-        hipStream_t s = static_cast<hipStream_t>(stream);
-        hipError_t e = hipMemcpyAsync(const_cast<GradTile*>(list->tiles), table.data(),
-                                      table.size() * sizeof(GradTile), hipMemcpyHostToDevice, s);
-        const hipError_t w = hipStreamSynchronize(s);
-        if (e == hipSuccess) e = w;
-        if (e != hipSuccess) {
-            delete list;
-            return ops_fail(GOCKPT_EHIP, "%s: %s", name, hipGetErrorString(e));
-        }
+    list->ws = static_cast<uint8_t*>(workspace);
+    list->tiles = reinterpret_cast<const GradTile*>(list->ws + kTableOff);
+    list->ntiles = static_cast<int>(ntiles);
+    const char* again = getenv("GOCKPT_TEST_GRADS_AGAIN");
+    list->spins = again != nullptr && again[0] == '1' ? 0 : kWholeSpins;
+    list->src_bytes = src_bytes;
+    list->dst_bytes = dst_bytes;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    hipError_t e = hipMemcpyAsync(workspace, head.data(), head.size(), hipMemcpyHostToDevice, s);
+    const hipError_t w = hipStreamSynchronize(s);
+    if (e == hipSuccess) e = w;
+    if (e != hipSuccess) {
+        delete list;
+        return ops_fail(GOCKPT_EHIP, "%s: %s", name, hipGetErrorString(e));
     }
     *out = list;
     return GOCKPT_OK;
@@ -407,19 +643,47 @@ static int check_norm(const char* name, const void* scale, double max_norm, cons
     return GOCKPT_OK;
 }
 
-int gockpt_grads_norm(gockpt_grads* list, const float* scale, double max_norm, gockpt_grad_result* result,
-                      void* stream) {
-    const char* name = "gockpt_grads_norm";
+static void launch_scale(const gockpt_grads* list, const gockpt_grad_result* result, hipStream_t s) {
+    if (list->ntiles == 0) return;
+    const bool nt = list->src_bytes + list->dst_bytes > kCachedScaleBytes;
+    hipLaunchKernelGGL(nt ? scale_kernel<true> : scale_kernel<false>, dim3(list->ntiles), dim3(kThreads), 0, s,
+                       list->tiles, list->ntiles, result);
+}
+
+// The norm, and with clip the scaling.
+static int run_list(const char* name, gockpt_grads* list, const float* scale, double max_norm,
+                    gockpt_grad_result* result, bool clip, void* stream) {
     if (list == nullptr) return ops_fail(GOCKPT_EINVAL, "%s: null list", name);
     const int rc = check_norm(name, scale, max_norm, result);
     if (rc != GOCKPT_OK) return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (list->blocks > 0)
-        hipLaunchKernelGGL(sumsq_kernel, dim3(list->blocks), dim3(kThreads), 0, s, list->tiles, list->ntiles,
-                           list->parts);
-    hipLaunchKernelGGL(result_kernel, dim3(1), dim3(kThreads), 0, s, list->parts, list->blocks, scale, max_norm,
-                       result);
+    const int n = list->ntiles;
+    if (n > 0 && n <= kWholeTiles) {
+        hipLaunchKernelGGL(clip ? whole_kernel<true> : whole_kernel<false>, dim3(n), dim3(kThreads), 0, s,
+                           list->tiles, reinterpret_cast<uint32_t*>(list->ws),
+                           reinterpret_cast<uint64_t*>(list->ws + kSlotsOff), list->spins, scale, max_norm, result);
+        return ops_launched(name);
+    }
+    double* parts = reinterpret_cast<double*>(list->ws + kPartsOff);
+    const int blocks = n < kSumBlocks ? n : kSumBlocks;
+    if (blocks > 0) {
+        const bool nt = !clip || list->src_bytes > kCachedSumBytes;
+        hipLaunchKernelGGL(nt ? sumsq_kernel<true> : sumsq_kernel<false>, dim3(blocks), dim3(kThreads), 0, s,
+                           list->tiles, n, parts);
+    }
+    hipLaunchKernelGGL(result_kernel, dim3(1), dim3(kThreads), 0, s, parts, blocks, scale, max_norm, result);
+    if (clip) launch_scale(list, result, s);
     return ops_launched(name);
+}
+
+int gockpt_grads_norm(gockpt_grads* list, const float* scale, double max_norm, gockpt_grad_result* result,
+                      void* stream) {
+    return run_list("gockpt_grads_norm", list, scale, max_norm, result, false, stream);
+}
+
+int gockpt_grads_clip(gockpt_grads* list, const float* scale, double max_norm, gockpt_grad_result* result,
+                      void* stream) {
+    return run_list("gockpt_grads_clip", list, scale, max_norm, result, true, stream);
 }
 
 int gockpt_grads_scale(gockpt_grads* list, const gockpt_grad_result* result, void* stream) {
@@ -427,16 +691,8 @@ int gockpt_grads_scale(gockpt_grads* list, const gockpt_grad_result* result, voi
     if (list == nullptr) return ops_fail(GOCKPT_EINVAL, "%s: null list", name);
     const int rc = check_norm(name, nullptr, 0.0, result);
     if (rc != GOCKPT_OK) return rc;
-    if (list->blocks > 0)
-        hipLaunchKernelGGL(scale_kernel, dim3(list->blocks), dim3(kThreads), 0, static_cast<hipStream_t>(stream),
-                           list->tiles, list->ntiles, result);
+    launch_scale(list, result, static_cast<hipStream_t>(stream));
     return ops_launched(name);
-}
-
-int gockpt_grads_clip(gockpt_grads* list, const float* scale, double max_norm, gockpt_grad_result* result,
-                      void* stream) {
-    const int rc = gockpt_grads_norm(list, scale, max_norm, result, stream);
-    return rc != GOCKPT_OK ? rc : gockpt_grads_scale(list, result, stream);
 }
 
 int gockpt_grads_result(gockpt_grad_result* result, const float* scale, double max_norm, void* stream) {
