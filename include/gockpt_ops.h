@@ -138,9 +138,9 @@ int gockpt_embedding_grad_bytes(int64_t tokens, int64_t rows, int64_t cols, size
  * no token has it); 1 adds to what the row holds, round(old + scale * sum), and
  * touches only rows that some token has (a head that shares the table has
  * written its gradient there).  Tokens with padding_id add nothing (INT64_MIN:
- * none).  Sums are fp32, over at most a few hundred tokens in token order,
- * those sums then in order; no atomics.  grad_out has batch * length rows; table at most
- * 4194304 rows.  workspace: 256-byte aligned, gockpt_embedding_grad_bytes; in
+ * none).  Sums are fp32, in token order over chunks of at most 128 tokens, those
+ * sums then in order; no atomics.  grad_out has batch * length rows, the table
+ * at most 4194304.  workspace: 256-byte aligned, gockpt_embedding_grad_bytes; in
  * use until the call's kernels have run.  Errors: EINVAL, ENOMEM (workspace),
  * EHIP. */
 int gockpt_embedding_grad(const gockpt_matrix* grad_out, const gockpt_token_ids* tokens, int64_t padding_id,

@@ -344,9 +344,10 @@ def embedding_grad(grad_out, ids, grad_weight, *, scale: float = 1.0, accumulate
         if workspace.dtype != torch.uint8 or not workspace.is_contiguous():
             raise ValueError("workspace: expected a contiguous uint8 tensor")
         ptr, size = workspace.data_ptr(), workspace.numel()
-    _check(_lib().gockpt_embedding_grad(
-        _matrix(grad_out, "grad_out", cols), _token_ids(ids, first_id), NO_PADDING if padding_id is None else padding_id,
-        scale, accumulate, m, ptr, size, _stream(stream, grad_weight.get_device())), "gockpt_embedding_grad", None)
+    x, t = _matrix(grad_out, "grad_out", cols), _token_ids(ids, first_id)
+    _check(_lib().gockpt_embedding_grad(x, t, NO_PADDING if padding_id is None else padding_id, scale, accumulate, m,
+                                        ptr, size, _stream(stream, grad_weight.get_device())),
+           "gockpt_embedding_grad", None)
     return grad_weight
 
 

@@ -342,7 +342,8 @@ def check_grad(got, total, size, n, scale, old=None):
 
 GRAD_SHAPES = [(1, 10, 8), (1, 1, 1), (2, 70, 3), (48, 320, 64), (97, 64, 513), (130, 65, 2048), (2048, 50, 40),
                (2049, 50, 40), (2049, 3000, 24), (5000, 1000, 264), (5000, 129, 5121), (20_001, 4001, 136),
-               (70_000, 300_001, 16), (66_000, 64, 8), (3001, 263_000, 9)]
+               (70_000, 300_001, 16), (66_000, 64, 8), (3001, 263_000, 9),
+               (16_384, 2500, 72), (16_385, 2049, 40), (33_000, 1_100_000, 8), (17_001, 1, 20)]
 
 
 @pytest.mark.parametrize("kind", ["uniform", "zipf", "same", "masked", "none", "ends", "sorted"])
