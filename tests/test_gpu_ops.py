@@ -575,3 +575,19 @@ def test_a_clipped_window_and_the_loss_scale_on_the_device():
             assert np.array_equal(a.view(np.uint32), b.view(np.uint32))
     finally:
         sess.close()
+
+
+def test_the_example_learns_and_its_checkpoint_is_whole():
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "clipped_training.py")
+    spec = importlib.util.spec_from_file_location("clipped_training", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    losses, norms, coefs, equal = example.main(steps=40, verbose=False)
+    assert equal and all(math.isfinite(x) for x in losses + norms)
+    # ids at random have a loss of ln 500 = 6.2, the language's own entropy is ln 4
+    assert sum(losses[-5:]) < 0.9 * sum(losses[:5]), losses
+    assert min(coefs) < 1.0
+    for n, c in zip(norms, coefs):
+        assert abs(c - min(1.0, 0.2 / (n + 1e-6))) <= 1e-5
