@@ -12,6 +12,7 @@ torch operation, tensors written on another stream have to be waited for.
 from __future__ import annotations
 
 import ctypes
+import functools
 import struct
 
 import torch
@@ -66,6 +67,7 @@ def gockpt_scale_ptr(ctx) -> int:
     return out.value
 
 
+@functools.lru_cache(maxsize=256)
 def gockpt_embedding_grad_bytes(tokens: int, rows: int, cols: int) -> int:
     n = ctypes.c_size_t()
     _check(_lib().gockpt_embedding_grad_bytes(int(tokens), int(rows), int(cols), ctypes.byref(n)),
@@ -73,9 +75,13 @@ def gockpt_embedding_grad_bytes(tokens: int, rows: int, cols: int) -> int:
     return n.value
 
 
-def _here(t, what: str) -> None:
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+def _here(t, what: str, device: int | None = None) -> int:
+    """The current GPU (`device`, where the caller knows it), which t is on."""
+    if device is None and t.is_cuda:
+        device = torch.cuda.current_device()
+    if not t.is_cuda or t.get_device() != device:
         raise ValueError(f"{what}: expected a tensor on the current GPU, got one on {t.device}")
+    return device
 
 
 def _dtype(t, what: str) -> int:
@@ -168,25 +174,28 @@ class GradList:
         self.out = [None] * len(self.tensors) if out is None else list(out)
         if len(self.out) != len(self.tensors):
             raise ValueError(f"{len(self.tensors)} tensors, {len(self.out)} destinations")
+        self.device = None
         table = bytearray()
         for i, (t, o) in enumerate(zip(self.tensors, self.out)):
-            _here(t, f"tensor {i}")
+            self.device = _here(t, f"tensor {i}", self.device)
             d = _dtype(t, f"tensor {i}")
-            r = _rows(t.shape, t.stride())
+            size = t.numel()
+            r = (1, size, size) if t.is_contiguous() else _rows(t.shape, t.stride())
             if r is None and o is None:  # element by element in place: the order does not matter
                 r = _rows(*zip(*sorted(zip(t.shape, t.stride()), key=lambda x: -x[1])))
             if r is None:
                 raise ValueError(f"tensor {i}: shape {tuple(t.shape)} with strides {t.stride()} is not rows of "
                                  "adjacent elements")
             if o is not None:
-                _here(o, f"out {i}")
-                if o.numel() != t.numel() or not o.is_contiguous():
+                _here(o, f"out {i}", self.device)
+                if o.numel() != size or not o.is_contiguous():
                     raise ValueError(f"out {i}: expected {t.numel()} contiguous elements, got {tuple(o.shape)}")
             table += GRAD_TENSOR.pack(t.data_ptr(), 0 if o is None else o.data_ptr(), *r, d,
                                       d if o is None else _dtype(o, f"out {i}"))
         table, n, size = bytes(table), len(self.tensors), ctypes.c_size_t()
         _check(_lib().gockpt_grads_bytes(table, n, ctypes.byref(size)), "gockpt_grads_bytes", None)
-        self.device = torch.cuda.current_device()
+        if self.device is None:
+            self.device = torch.cuda.current_device()
         with torch.cuda.stream(stream):
             self.workspace = torch.empty(size.value, dtype=torch.uint8, device=self.device)
             self.result = GradResult(self.device)
@@ -237,9 +246,9 @@ class GradList:
             pass
 
 
-def _matrix(t, what: str, cols=None) -> bytes:
+def _matrix(t, what: str, device: int, cols=None) -> bytes:
     """A 2-D tensor, or with cols the rows of that many elements of any."""
-    _here(t, what)
+    _here(t, what, device)
     d = _dtype(t, what)
     shape = t.shape
     if cols is not None and len(shape) > 0 and shape[-1] == cols and t.is_contiguous():
@@ -263,8 +272,8 @@ def _matrix(t, what: str, cols=None) -> bytes:
     return MATRIX.pack(t.data_ptr(), rows, n, stride, d, 0)
 
 
-def _token_ids(ids, first_id: int) -> bytes:
-    _here(ids, "ids")
+def _token_ids(ids, first_id: int, device: int) -> bytes:
+    _here(ids, "ids", device)
     bits = _BITS.get(ids.dtype)
     if bits is None:
         raise ValueError(f"ids: expected int32 or int64, got {ids.dtype}")
@@ -277,16 +286,17 @@ def _token_ids(ids, first_id: int) -> bytes:
     return TOKEN_IDS.pack(ids.data_ptr(), *r, first_id, bits, 0)
 
 
-def _empty(shape, dtype, device, stream):
-    """Allocated for use on the stream that the call runs on."""
+def _empty(like, shape, dtype, stream):
+    """On like's GPU, allocated for use on the stream that the call runs on."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
     with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
 
 
 def _lookup(weight, ids, scale, out, out_dtype, first_id, stream):
-    w, t = _matrix(weight, "weight"), _token_ids(ids, first_id)
+    device = _here(weight, "weight")
+    w, t = _matrix(weight, "weight", device), _token_ids(ids, first_id, device)
     dim = weight.shape[1]
     shape = (*ids.shape, dim)
     if out is None:
@@ -294,13 +304,13 @@ def _lookup(weight, ids, scale, out, out_dtype, first_id, stream):
         code = _DTYPE.get(dtype)
         if code is None:
             raise ValueError(f"out_dtype: expected bfloat16, float16 or float32, got {dtype}")
-        out = _empty(shape, dtype, weight.device, stream)
+        out = _empty(weight, shape, dtype, stream)
         o = MATRIX.pack(out.data_ptr(), ids.numel(), dim, dim, code, 0)
     else:
         if out.shape != shape or (out_dtype is not None and out.dtype != out_dtype):
             raise ValueError(f"out: expected shape {shape}, got {tuple(out.shape)} of {out.dtype}")
-        o = _matrix(out, "out", dim)
-    _check(_lib().gockpt_embedding(w, t, scale, o, _stream(stream, weight.get_device())), "gockpt_embedding", None)
+        o = _matrix(out, "out", device, dim)
+    _check(_lib().gockpt_embedding(w, t, scale, o, _stream(stream, device)), "gockpt_embedding", None)
     return out
 
 
@@ -329,7 +339,8 @@ def embedding_grad(grad_out, ids, grad_weight, *, scale: float = 1.0, accumulate
     accumulate the sums are added to what grad_weight holds and rows without a
     token are left alone.  workspace: a uint8 tensor of at least
     gockpt_embedding_grad_bytes(tokens, rows, dim) (None: allocated)."""
-    m = _matrix(grad_weight, "grad_weight")
+    device = _here(grad_weight, "grad_weight")
+    m = _matrix(grad_weight, "grad_weight", device)
     if grad_out.shape[:-1] != ids.shape:
         raise ValueError(f"grad_out of shape {tuple(grad_out.shape)} for ids of shape {tuple(ids.shape)}")
     rows, cols = grad_weight.shape
@@ -337,16 +348,16 @@ def embedding_grad(grad_out, ids, grad_weight, *, scale: float = 1.0, accumulate
     if workspace is None:
         size = gockpt_embedding_grad_bytes(ids.numel(), rows, cols)
         if size:
-            workspace = _empty((size,), torch.uint8, grad_weight.device, stream)
+            workspace = _empty(grad_weight, (size,), torch.uint8, stream)
             ptr = workspace.data_ptr()
     else:
-        _here(workspace, "workspace")
+        _here(workspace, "workspace", device)
         if workspace.dtype != torch.uint8 or not workspace.is_contiguous():
             raise ValueError("workspace: expected a contiguous uint8 tensor")
         ptr, size = workspace.data_ptr(), workspace.numel()
-    x, t = _matrix(grad_out, "grad_out", cols), _token_ids(ids, first_id)
+    x, t = _matrix(grad_out, "grad_out", device, cols), _token_ids(ids, first_id, device)
     _check(_lib().gockpt_embedding_grad(x, t, NO_PADDING if padding_id is None else padding_id, scale, accumulate, m,
-                                        ptr, size, _stream(stream, grad_weight.get_device())),
+                                        ptr, size, _stream(stream, device)),
            "gockpt_embedding_grad", None)
     return grad_weight
 
