@@ -85,7 +85,8 @@ int gockpt_grads_norm(gockpt_grads* list, const float* scale, double max_norm,
                       gockpt_grad_result* result, void* stream);
 
 /* dst = round(element * result->coef) for every element, one fp32 product
- * rounded once to the destination's type, to nearest even.  In place, a
+ * rounded once to the destination's type, to nearest even (beyond fp16's
+ * range: infinity, which no found_inf of this norm tells).  In place, a
  * coefficient of 1 leaves the memory untouched.  Errors: EINVAL, EHIP. */
 int gockpt_grads_scale(gockpt_grads* list, const gockpt_grad_result* result, void* stream);
 

@@ -869,7 +869,7 @@ int check_matrix(const char* name, const char* what, const gockpt_matrix* m) {
     if (m->rows < 0 || m->cols < 0 || m->rows > kMaxTokens || m->cols > kMaxCols)
         return ops_fail(GOCKPT_EINVAL, "%s: %s of %lld x %lld", name, what, static_cast<long long>(m->rows),
                         static_cast<long long>(m->cols));
-    if (m->rows > 1 && (m->stride < m->cols || m->stride > int64_t{1} << 40))
+    if (m->rows > 1 && (m->stride < m->cols || m->stride > (int64_t{1} << 46) / m->rows))
         return ops_fail(GOCKPT_EINVAL, "%s: %s stride %lld for rows of %lld", name, what,
                         static_cast<long long>(m->stride), static_cast<long long>(m->cols));
     if (m->rows > 0 && m->cols > 0 && (m->data == nullptr || !elem_aligned(m->data, m->dtype)))

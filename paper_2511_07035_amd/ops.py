@@ -165,8 +165,8 @@ class GradList:
     as many elements, any of the three types: views of ``Session.grad``, say);
     None, or None in a place: in place.  Writing in place also takes a tensor
     whose dimensions are permuted.  The handle keeps the tensors alive and
-    holds their addresses: make a new one when they move.  Its calls run one
-    at a time, in stream order."""
+    holds their addresses: make a new one when they move.  Its calls use its
+    workspace one at a time: on several streams they have to be ordered."""
 
     def __init__(self, tensors, out=None, stream=None):
         self.handle = None
@@ -200,42 +200,50 @@ class GradList:
             self.workspace = torch.empty(size.value, dtype=torch.uint8, device=self.device)
             self.result = GradResult(self.device)
         handle = _P()
-        _check(_lib().gockpt_grads_create(table, n, self.workspace.data_ptr(), size.value,
-                                          _stream(stream, self.device), ctypes.byref(handle)),
-               "gockpt_grads_create", None)
+        self.home, self.strayed = _stream(stream, self.device), False
+        _check(_lib().gockpt_grads_create(table, n, self.workspace.data_ptr(), size.value, self.home,
+                                          ctypes.byref(handle)), "gockpt_grads_create", None)
         self.handle = handle.value
 
-    def _open(self):
+    def _on(self, stream) -> int:
+        """The stream of a call, on the list's GPU."""
         if self.handle is None:
             raise GockptError(GOCKPT_EINVAL, "GradList", "closed")
-        return self.handle
+        if torch.cuda.current_device() != self.device:
+            raise ValueError(f"the list is on GPU {self.device}, which is not the current one")
+        s = _stream(stream, self.device)
+        if s != self.home:  # not the stream that the workspace was allocated for
+            self.strayed = True
+        return s
 
     def norm(self, max_norm: float = float("inf"), *, scale=None, result=None, stream=None) -> GradResult:
         """The norm over all tensors, divided by ``scale`` (the loss scale the
         gradients carry: a device tensor or a Session), into ``result`` (the
         list's own, overwritten by its next call, if None)."""
-        r = self.result if result is None else result
-        _check(_lib().gockpt_grads_norm(self._open(), _scale_ptr(scale), max_norm, r.ptr,
-                                        _stream(stream, self.device)), "gockpt_grads_norm", None)
+        r, s = self.result if result is None else result, self._on(stream)
+        _check(_lib().gockpt_grads_norm(self.handle, _scale_ptr(scale), max_norm, r.ptr, s), "gockpt_grads_norm", None)
         return r
 
     def clip(self, max_norm: float, *, scale=None, result=None, stream=None) -> GradResult:
         """``norm``, then every element times min(1, max_norm / (norm + 1e-6))
         in place or into ``out``.  With an inf or NaN among the gradients they
         are left, or copied, as they are, and ``found_inf`` tells."""
-        r = self.result if result is None else result
-        _check(_lib().gockpt_grads_clip(self._open(), _scale_ptr(scale), max_norm, r.ptr,
-                                        _stream(stream, self.device)), "gockpt_grads_clip", None)
+        r, s = self.result if result is None else result, self._on(stream)
+        _check(_lib().gockpt_grads_clip(self.handle, _scale_ptr(scale), max_norm, r.ptr, s), "gockpt_grads_clip", None)
         return r
 
     def scale(self, result=None, *, stream=None) -> None:
         """Every element times ``result.coef``: the second half of ``clip``."""
-        r = self.result if result is None else result
-        _check(_lib().gockpt_grads_scale(self._open(), r.ptr, _stream(stream, self.device)), "gockpt_grads_scale",
-               None)
+        r, s = self.result if result is None else result, self._on(stream)
+        _check(_lib().gockpt_grads_scale(self.handle, r.ptr, s), "gockpt_grads_scale", None)
 
     def close(self) -> None:
+        """Releases the handle.  Waits for the GPU if calls ran on other
+        streams than the one the list was made on, which torch's allocator
+        does not know of."""
         if self.handle is not None:
+            if self.strayed:
+                torch.cuda.synchronize(self.device)
             _lib().gockpt_grads_destroy(self.handle)
             self.handle = None
 
@@ -325,6 +333,8 @@ def embedding(weight, ids, *, scale: float = 1.0, out=None, out_dtype=None, firs
     of ``Session.grad``), written or accumulated there and not returned.  Tokens
     with padding_id add no gradient.  out and stream are for calls that need
     no gradient."""
+    if accumulate and grad_weight is None:
+        raise ValueError("accumulate: into a grad_weight")
     if weight.requires_grad and torch.is_grad_enabled():
         if out is not None or stream is not None:
             raise ValueError("out and stream: for calls without a gradient")
@@ -372,6 +382,7 @@ class _Embedding(torch.autograd.Function):
         return _lookup(weight.detach(), ids, scale, None, out_dtype, first_id, None)
 
     @staticmethod
+    @torch.autograd.function.once_differentiable
     def backward(ctx, grad_out):
         (ids,) = ctx.saved_tensors
         into = ctx.into

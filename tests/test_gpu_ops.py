@@ -251,7 +251,7 @@ def ids_of(kind, tokens, vocab, seed):
         ids = r.integers(0, vocab, tokens)
     elif kind == "zipf":
         p = 1.0 / (np.arange(vocab) + 2.7)
-        ids = r.choice(vocab, tokens, p=p / p.sum())
+        ids = np.minimum(np.searchsorted(np.cumsum(p / p.sum()), r.random(tokens)), vocab - 1)
     elif kind == "same":
         ids = np.full(tokens, vocab // 2)
     elif kind == "masked":
@@ -418,6 +418,8 @@ def test_no_tokens():
 
 
 def test_embedding_refusals():
+    with pytest.raises(ValueError):
+        g.embedding(torch.zeros(10, 8, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda"), accumulate=True)
     w, ids = torch.zeros(10, 8, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda")
     for bad in (dict(weight=w.double()), dict(weight=w[0]), dict(weight=w.t()), dict(ids=ids.float()),
                 dict(ids=torch.zeros(8, 8, dtype=torch.int64, device="cuda").t()),
@@ -470,6 +472,64 @@ def test_autograd_against_differences_and_the_formula():
     check_grad(into, total, size * (1 + 4 * U), n, 1.25, torch.ones(vocab, dim, device="cuda"))
 
 
+@pytest.mark.parametrize("tokens,vocab,dim", [(129, 70, 9), (2049, 3000, 24), (9000, 50, 515), (20_001, 4001, 136),
+                                              (70_000, 300_001, 16)])
+def test_embedding_grad_stays_within_its_workspace_and_table(tokens, vocab, dim):
+    size = g.gockpt_embedding_grad_bytes(tokens, vocab, dim)
+    around = torch.full((size + 8192,), 0xA5, dtype=torch.uint8, device="cuda")
+    at = -around.data_ptr() % 256 + 4096
+    for dst in (torch.bfloat16, torch.float32):
+        table = torch.full((vocab + 20, dim), 5.0, dtype=dst, device="cuda")
+        for kind in ("zipf", "same", "masked"):
+            ids = ids_of(kind, tokens, vocab, 3)
+            x = randn((tokens, dim), torch.float32, 4)
+            g.embedding_grad(x, ids, table[10:-10], workspace=around[at:at + size])
+            check_grad(table[10:-10], *grad_plain(x, ids, vocab), 1.0)
+            assert bool((around[:at] == 0xA5).all()) and bool((around[at + size:] == 0xA5).all())
+            assert bool((table[:10] == 5.0).all()) and bool((table[-10:] == 5.0).all())
+
+
+def test_embedding_grad_of_an_expanded_gradient():
+    w = randn((40, 24), torch.float32, 1).requires_grad_()
+    ids = ids_of("masked", 500, 40, 2)
+    g.embedding(w, ids, scale=0.5).sum().backward()  # autograd hands over one element with strides of 0
+    n = torch.bincount(ids[(ids >= 0) & (ids < 40)], minlength=40)
+    assert torch.equal(w.grad, (n[:, None] * 0.5).expand(40, 24).float())
+    with pytest.raises((ValueError, g.GockptError)):
+        g.embedding_grad(torch.ones(1, 24, device="cuda").expand(500, 24), ids, torch.zeros(40, 24, device="cuda"))
+
+
+def test_offsets_beyond_32_bits():
+    n = 2 ** 32 + 5
+    t = torch.ones(n, dtype=torch.bfloat16, device="cuda")
+    gl = g.GradList([t, t[:7]])
+    r = gl.norm(1.0)
+    assert float(r.sumsq) == n + 7
+    r = g.GradList([t]).clip(float(np.sqrt(np.float64(n))) / 2)
+    assert abs(float(r.coef) - 0.5) <= 18 * U
+    half = (torch.ones(1, device="cuda") * r.coef).to(torch.bfloat16)
+    for a in (0, 2 ** 31 - 3, 2 ** 31 + 8191, 2 ** 32 - 8):
+        assert bool((t[a:a + 13] == half).all())
+    assert bool((t[-13:] == half).all())
+    gl.close()
+    del gl, t
+    # a table of 4.9 GB, rows of a gradient 4 MiB apart
+    rows, dim = 600_000, 4096
+    table = torch.zeros(rows, dim, dtype=torch.bfloat16, device="cuda")
+    table[-3:] = randn((3, dim), torch.bfloat16, 1, 1.0)
+    ids = torch.tensor([rows - 1, 5, rows - 3, rows - 2, -1], device="cuda")
+    assert same(g.embedding(table, ids), lookup_plain(table, ids, 1.0, torch.bfloat16))
+    apart = torch.zeros(1500 * 2 ** 21, dtype=torch.bfloat16, device="cuda").view(1500, 2 ** 21)[:, :64]
+    apart.copy_(randn((1500, 64), torch.bfloat16, 2))
+    for tokens in (100, 1500):  # both forms
+        ids = rows - 1 - ids_of("zipf", tokens, 400, 3)
+        x = apart[-tokens:]
+        out = g.embedding_grad(x, ids, table[:, 100:164])
+        total, size, n = grad_plain(x, ids - (rows - 400), 400)
+        check_grad(out[-400:], total, size, n, 1.0)
+        assert bool((out[:-400].abs().amax() == 0).all())
+
+
 # ---- streams and graphs ----------------------------------------------------------
 
 
@@ -488,6 +548,8 @@ def test_on_another_stream():
     r = gl.clip(1.0, stream=s)
     y = g.embedding(w, ids, stream=s)
     s.synchronize()
+    gl.norm(result=g.GradResult())  # on the current stream, after the other has finished
+    gl.close()
     n = torch.bincount(ids, minlength=77).double()
     want = math.sqrt(float((n.square() * 64).sum()))
     assert abs(float(r.norm) - want) <= 17 * U * want
