@@ -321,9 +321,17 @@ def grad_plain(grad_out, ids, rows, first=0, padding=None):
     if padding is not None:
         there &= flat != padding
     at, x = flat[there] - first, grad_out.reshape(flat.numel(), -1)[there].double()
-    total = torch.zeros(rows, x.shape[1], dtype=torch.float64, device="cuda").index_add_(0, at, x)
-    size = torch.zeros_like(total).index_add_(0, at, x.abs())
-    n = torch.zeros(rows, dtype=torch.float64, device="cuda").index_add_(0, at, torch.ones_like(at, dtype=torch.float64))
+    total = torch.zeros(rows, x.shape[1], dtype=torch.float64, device="cuda")
+    size, n = torch.zeros_like(total), torch.zeros(rows, dtype=torch.float64, device="cuda")
+    few = at.unique()
+    if few.numel() <= 16:  # index_add_ would queue up at these rows
+        for v in few.tolist():
+            mine = x[at == v]
+            total[v], size[v], n[v] = mine.sum(0), mine.abs().sum(0), len(mine)
+    else:
+        total.index_add_(0, at, x)
+        size.index_add_(0, at, x.abs())
+        n.index_add_(0, at, torch.ones_like(at, dtype=torch.float64))
     return total, size, n[:, None]
 
 
