@@ -15,9 +15,9 @@
 //
 //   Memory bounds it: grad_out read once, every row of the table written.
 //   131072 tokens x 4096 fp16 into 32000 rows, a tenth masked (0.97 GB + 0.26
-//   GB): 272 us, of which the sort 42 (it writes half of the table's zeros
-//   meanwhile), the sums 215 at 5.6 TB/s, the join 16.  16384 x 2048 bf16 into
-//   50304 rows (67 + 206 MB): 71 us, of which the sort 37, the sums 30.
+//   GB): 272 us, of which the sort 42 (half of the table is cleared meanwhile),
+//   the sums 215 at 5.6 TB/s, the join 16.  16384 x 2048 bf16 into 50304 rows
+//   (67 + 206 MB): 65 us.  A copy moves the same bytes in 260 and 58.
 #include <limits.h>
 
 #include "gockpt_ops_internal.h"
@@ -144,46 +144,54 @@ __device__ __forceinline__ void store_cols(uint8_t* p, int64_t c, int64_t cols, 
     }
 }
 
-// A lane takes 16 bytes of output columns (so that a wavefront's stores are one
-// contiguous KiB: fp32 output at 8 columns a lane, two stores 32 bytes apart,
-// ran at half the rate), a block kThreads / lanes rows at a time, kRows times,
-// whose loads are all in flight before the first store.  The column blocks of
-// the same rows follow one another.
+// A lane takes 16 bytes of output columns, so that a wavefront's stores are one
+// contiguous KiB (fp32 output at 8 columns a lane, two stores 32 bytes apart,
+// ran at half the rate).  A piece is kThreads / lanes rows in one column block;
+// a block takes kPieces of them, all columns of a row before the next row, and
+// has all their loads in flight before its first store.
 //
 // Bound by the writes, and by the reads of rows that the caches do not hold:
-// 65536 x 5120 fp32 from a bf16 table in 333 us with the table's rows in HBM
-// and 250 with them in the last-level cache (1.34 GB written: 195 us at the
-// rate of a fill), 16384 x 2048 bf16 in 18 us.  Tried without gain:
-// the column blocks of a row on one XCD each, so that its L2 holds a part of
-// more rows; contiguous tokens on each XCD; stores written through the L2.
-template <int kW, int kO, int kRows, bool kNT>
+// 65536 x 5120 fp32 from a bf16 table whose rows lie in HBM 345 us, with them
+// in the last-level cache 250 (1.34 GB written: 195 us at the rate of a fill,
+// 312 at a copy's over all 1.48 GB); 131072 x 4096 bf16 287, 16384 x 2048 bf16
+// 19.  us with 2, 3, 4 and 8 pieces: 396, 338, 345, 355; 310, 302, 287, 325;
+// 18.8, 19.0, 19.3, 21.9.  Slower: the same column block of several rows in a
+// block (357, 310); a row's column blocks on one XCD each, so that its L2 holds
+// parts of more rows; contiguous tokens on each XCD; loads past the caches
+// (389); stores written through the L2.
+constexpr int kPieces = 4;
+
+template <int kW, int kO, bool kNT>
 __global__ __launch_bounds__(kThreads) void lookup_kernel(LookupArgs a) {
     constexpr int kV = kO == kFP32 ? 4 : 8;
     const uint32_t lane = threadIdx.x & (a.lanes - 1);
     const uint32_t per = kThreads / a.lanes;
-    const uint32_t group = blockIdx.x / a.col_blocks, col = blockIdx.x - group * a.col_blocks;
-    const int64_t c = (static_cast<int64_t>(col) * a.lanes + lane) * kV;
-    if (c >= a.cols) return;
-    const uint32_t t0 = group * per * kRows + threadIdx.x / a.lanes;
-    int32_t row[kRows];
+    uint32_t group = blockIdx.x * kPieces / a.col_blocks, col = blockIdx.x * kPieces - group * a.col_blocks;
+    int32_t row[kPieces];
+    uint32_t t[kPieces];
+    int64_t c[kPieces];
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-        const uint32_t t = t0 + i * per;
-        row[i] = t < a.ids.tokens ? token_row(a.ids, t, false) : -1;
+    for (int i = 0; i < kPieces; ++i) {
+        t[i] = group * per + threadIdx.x / a.lanes;
+        c[i] = (static_cast<int64_t>(col) * a.lanes + lane) * kV;
+        row[i] = t[i] < a.ids.tokens ? token_row(a.ids, t[i], false) : -1;
+        if (++col == a.col_blocks) {
+            col = 0;
+            ++group;
+        }
     }
-    Piece<kW, kV> x[kRows] = {};
+    Piece<kW, kV> x[kPieces] = {};
 #pragma unroll
-    for (int i = 0; i < kRows; ++i)
-        if (row[i] >= 0) x[i].load(a.table + row[i] * a.table_stride, c, a.cols);
+    for (int i = 0; i < kPieces; ++i)
+        if (row[i] >= 0) x[i].load(a.table + row[i] * a.table_stride, c[i], a.cols);
 #pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-        const uint32_t t = t0 + i * per;
-        if (t >= a.ids.tokens) continue;
+    for (int i = 0; i < kPieces; ++i) {
+        if (t[i] >= a.ids.tokens) continue;
         float y[kV];
         // a masked token's zeros stay +0 whatever the scale
 #pragma unroll
         for (int k = 0; k < kV; ++k) y[k] = row[i] >= 0 ? x[i][k] * a.scale : 0.0f;
-        store_cols<kO, kV, kNT>(a.out + t * a.out_stride, c, a.cols, y);
+        store_cols<kO, kV, kNT>(a.out + t[i] * a.out_stride, c[i], a.cols, y);
     }
 }
 
@@ -206,11 +214,13 @@ constexpr int kBucketDigits = 512;
 // Bytes of the table that are cleared beside the sort: 96 MiB beside
 // bucket_kernel, 32 beside each of the four radix launches.  The rows that have
 // a token are written again, and the writes slow the sort, so more is not
-// better: 16384 tokens into 206 MB 78.8 us without, 69.9 with 24 a launch, 72.3
-// with 36, 70.9 with 50; 131072 tokens into 262 MB 281, 273, 272, 273.
+// better: us with 24, 32 and 48 MiB a launch, 16384 tokens into 206 MB 65.8,
+// 65.3, 68.8, 131072 into 262 MB 273, 272, 278; with 64, 96 and 128, 8192 tokens
+// 54.8, 50.9, 52.1.  A table above kCachedOutBytes is cleared past the caches
+// (with plain stores 72.8, 273 and 54.7).
 constexpr int64_t kClearBucketBytes = int64_t{96} << 20;
 constexpr int64_t kClearRadixBytes = int64_t{32} << 20;
-// Blocks that do it: enough to keep the memory busy (32: 78 us, 512: 73).
+// Blocks that do it (64, 256 and 512: 68.2, 68.9, 66.7 us for the 16384).
 constexpr int kClearBlocks = 128;
 
 // A token and its row.
@@ -237,6 +247,7 @@ struct GradArgs {
     // known which have a token; the others, where none has, by sum_kernel's
     // blocks from sum_blocks on.
     int64_t clear_from;
+    bool clear_nt;
     int32_t part, parts;
     uint32_t sum_blocks;
     int32_t chunk;                         // sorted tokens that one group of lanes sums
@@ -249,10 +260,16 @@ struct GradArgs {
     int64_t wide;                          // cols rounded up to 8
 };
 
-// Zeros `bytes` at p (2-byte aligned, a multiple of 2) with n threads.
-__device__ __forceinline__ void clear_span(uint8_t* p, int64_t bytes, uint32_t i, uint32_t n) {
+// Zeros `bytes` at p (2-byte aligned, a multiple of 2) with n threads, this one
+// number i; past the caches with nt.
+__device__ __forceinline__ void clear_span(uint8_t* p, int64_t bytes, uint32_t i, uint32_t n, bool nt) {
     const u32x4 zero = {0u, 0u, 0u, 0u};
-    for (int64_t at = i * 16; at + 16 <= bytes; at += n * 16) *reinterpret_cast<u32x4_any*>(p + at) = zero;
+    if (nt) {
+        for (int64_t at = i * 16; at + 16 <= bytes; at += n * 16)
+            __builtin_nontemporal_store(zero, reinterpret_cast<u32x4_any*>(p + at));
+    } else {
+        for (int64_t at = i * 16; at + 16 <= bytes; at += n * 16) *reinterpret_cast<u32x4_any*>(p + at) = zero;
+    }
     const int64_t tail = bytes / 16 * 16 + i * 2;
     if (tail < bytes) *reinterpret_cast<uint16_t*>(p + tail) = 0;
 }
@@ -265,10 +282,10 @@ __device__ __forceinline__ void clear_table(const GradArgs& a) {
     const int64_t r0 = lo + (hi - lo) * i / blocks, r1 = lo + (hi - lo) * (i + 1) / blocks;
     const int64_t bytes = a.cols * (a.dst_dtype == kFP32 ? 4 : 2);
     if (a.dst_stride == bytes) {
-        clear_span(a.dst + r0 * bytes, (r1 - r0) * bytes, threadIdx.x, kSortThreads);
+        clear_span(a.dst + r0 * bytes, (r1 - r0) * bytes, threadIdx.x, kSortThreads, a.clear_nt);
     } else {
         for (int64_t r = r0 + threadIdx.x / 64; r < r1; r += kSortWaves)
-            clear_span(a.dst + r * a.dst_stride, bytes, threadIdx.x & 63, 64);
+            clear_span(a.dst + r * a.dst_stride, bytes, threadIdx.x & 63, 64, a.clear_nt);
     }
 }
 
@@ -650,7 +667,7 @@ __device__ __forceinline__ void clear_absent(const GradArgs& a, uint32_t block) 
     const uint64_t there = __ballot(lo < n && a.sorted[lo].row == row);
     const int64_t bytes = a.cols * (a.dst_dtype == kFP32 ? 4 : 2);
     for (int r = threadIdx.x / 64; r < kClearRows && row0 + r < a.clear_from; r += kThreads / 64)
-        if (!(there >> r & 1u)) clear_span(a.dst + (row0 + r) * a.dst_stride, bytes, lane, 64);
+        if (!(there >> r & 1u)) clear_span(a.dst + (row0 + r) * a.dst_stride, bytes, lane, 64, a.clear_nt);
 }
 
 // Sorted tokens q * chunk to q * chunk + chunk - 1, summed row by row by
@@ -910,33 +927,18 @@ int check_ids(const char* name, const gockpt_token_ids* t, int64_t rows, int64_t
 // that reads its output, with plain and with nontemporal stores: 32 MiB 23.2
 // and 24.1, 64 MiB 39.4 and 40.2, 128 MiB 80.9 and 80.1, 512 MiB 339 and 324.
 constexpr int64_t kCachedOutBytes = int64_t{96} << 20;
-// Rows of a thread: 4, and 8 in launches of more than this many blocks whose
-// lanes load only 8 bytes of a row (a 16-bit table, fp32 output).  us with 2, 4
-// and 8 rows: fp32 from bf16, 4096 x 5120 25.5, 23.8, 27.4, 65536 x 5120 355,
-// 342, 333; bf16 from bf16, 131072 x 4096 294, 288, 293.
-constexpr int64_t kManyLookupBlocks = 16384;
-
-template <int kW, int kO, int kRows>
-int launch_lookup_rows(const LookupArgs& a, const char* name, hipStream_t s) {
-    const int64_t per = kThreads / a.lanes * kRows;
-    const int64_t blocks = (a.ids.tokens + per - 1) / per * a.col_blocks;
-    if (blocks >= kMaxGrid) return ops_fail(GOCKPT_EINVAL, "%s: out is too large", name);
-    const bool nt = a.ids.tokens * a.cols * dtype_bytes(kO) > kCachedOutBytes;
-    hipLaunchKernelGGL((nt ? lookup_kernel<kW, kO, kRows, true> : lookup_kernel<kW, kO, kRows, false>),
-                       dim3(static_cast<uint32_t>(blocks)), dim3(kThreads), 0, s, a);
-    return ops_launched(name);
-}
-
 template <int kW, int kO>
 int launch_lookup(LookupArgs& a, const char* name, hipStream_t s) {
     constexpr int kV = kO == kFP32 ? 4 : 8;
     a.lanes = lanes_for(a.cols, kV, 1, kThreads);
     a.col_blocks = col_blocks(a.cols, kV, a.lanes);
-    if constexpr (kO == kFP32 && kW != kFP32) {
-        if (int64_t{a.ids.tokens} * a.lanes / (4 * kThreads) * a.col_blocks > kManyLookupBlocks)
-            return launch_lookup_rows<kW, kO, 8>(a, name, s);
-    }
-    return launch_lookup_rows<kW, kO, 4>(a, name, s);
+    const int64_t per = kThreads / a.lanes;
+    const int64_t blocks = ((a.ids.tokens + per - 1) / per * a.col_blocks + kPieces - 1) / kPieces;
+    if (blocks >= kMaxGrid) return ops_fail(GOCKPT_EINVAL, "%s: out is too large", name);
+    const bool nt = a.ids.tokens * a.cols * dtype_bytes(kO) > kCachedOutBytes;
+    hipLaunchKernelGGL((nt ? lookup_kernel<kW, kO, true> : lookup_kernel<kW, kO, false>),
+                       dim3(static_cast<uint32_t>(blocks)), dim3(kThreads), 0, s, a);
+    return ops_launched(name);
 }
 
 template <int kW>
@@ -998,7 +1000,8 @@ int launch_grad(GradArgs& a, const GradPlan& p, const char* name, hipStream_t s)
     int64_t clear_blocks = 0;
     if (!a.accumulate) {
         const int64_t bytes = p.bucket ? kClearBucketBytes : 2 * p.passes * kClearRadixBytes;
-        const int64_t early = bytes / (a.cols * dtype_bytes(a.dst_dtype));
+        const int64_t row_bytes = a.cols * dtype_bytes(a.dst_dtype), early = bytes / row_bytes;
+        a.clear_nt = a.clear_from * row_bytes > kCachedOutBytes;
         a.clear_from = early < a.clear_from ? a.clear_from - early : 0;
         clear_blocks = (a.clear_from + kClearRows - 1) / kClearRows;
     }
