@@ -240,8 +240,15 @@ __device__ __forceinline__ void finish_result(double sumsq, const float* scale, 
 __global__ __launch_bounds__(kThreads) void result_kernel(const double* __restrict__ parts, int nparts,
                                                           const float* __restrict__ scale, double max_norm,
                                                           gockpt_grad_result* __restrict__ out) {
+    double v[kSumBlocks / kThreads];
+#pragma unroll
+    for (int k = 0; k < kSumBlocks / kThreads; ++k) {
+        const int i = k * kThreads + static_cast<int>(threadIdx.x);
+        v[k] = i < nparts ? parts[i] : 0.0;
+    }
     double acc = 0.0;
-    for (int i = threadIdx.x; i < nparts; i += kThreads) acc += parts[i];
+#pragma unroll
+    for (int k = 0; k < kSumBlocks / kThreads; ++k) acc += v[k];
     acc = block_sum(acc);
     if (threadIdx.x == 0) finish_result(acc, scale, max_norm, out);
 }
