@@ -1,8 +1,7 @@
 // gockpt_grads.hip -- norm and clipping of a list of gradient tensors.
 //
 //   sumsq_kernel   reads every tensor once: S = sum of squares, one fp64
-//                  partial a block.
-//   result_kernel  one block: adds the partials in a fixed order;
+//                  partial a block; block 0 adds them in a fixed order:
 //                  norm = sqrt(S) / scale, found_inf, and the clipping
 //                  coefficient min(1, max_norm / (norm + 1e-6)).
 //   scale_kernel   element * coef, rounded to the destination's type.
@@ -42,10 +41,9 @@ constexpr int kTileUnits = kThreads * kUnitsPerThread;
 constexpr int kSumBlocks = 1024;
 
 // Lists of up to this many tiles (8 MiB) take one launch, a tile a block.  us
-// a call in one launch and in two (norm) or three (clip): 2^17 bf16 elements
-// 5.6 and 8.6, 6.0 and 11.1; 2^21 5.5 and 8.7, 8.6 and 11.4; 2^22, the limit,
-// 5.5 and 8.4, 11.3 and 11.4.  Above it, blocks of two or four tiles that keep
-// them in registers gained nothing (2^23 8.2 and 8.5, 16.3 and 16.2).
+// a clip in one launch and in three: 2^17 bf16 elements 6.0 and 11.1, 2^21 8.6
+// and 11.4, 2^22, the limit, 11.3 and 11.4.  Above it, blocks of two or four
+// tiles that keep them in registers gained nothing (2^23 16.3 and 16.2).
 constexpr int kWholeTiles = 512;
 // Polls (about 0.5 us each) before a block computes the partials it misses;
 // none with GOCKPT_TEST_GRADS_AGAIN=1 in the environment when the list is made,
@@ -201,9 +199,63 @@ __device__ __forceinline__ double tile_sum(const GradTile& t, u32x4 (&raw)[kUnit
     return square_sum<kFP32>(raw);
 }
 
+// ---- exchange of the blocks' partials ------------------------------------------
+//
+// A partial is one 64-bit word: a double, and in the place of its sign, which
+// a sum of squares has no use for, the call's epoch modulo two.  Every call on
+// a list writes every slot, so a slot with the other tag is the last call's:
+// value and flag are one word, and no fence is needed, which on this chip would
+// write back an XCD's L2.  Block 0 adds the partials in a fixed order and moves
+// the epoch on once it has seen every one of them, that is after every block
+// has read it.  (As a launch of its own that cost 1 us more: 2^23 bf16 elements
+// 6.5 and 7.5, 2^25 14.1 and 15.2.)
+
+constexpr uint64_t kSlotTag = uint64_t{1} << 63;
+
+__device__ __forceinline__ uint64_t slot_tag(uint32_t epoch) { return epoch & 1u ? kSlotTag : 0u; }
+
+__device__ __forceinline__ uint64_t read_slot(const uint64_t* p) {
+    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+__device__ __forceinline__ void publish(uint64_t* slot, uint32_t epoch, double x) {
+    __hip_atomic_store(slot, (__builtin_bit_cast(uint64_t, x) & ~kSlotTag) | slot_tag(epoch), __ATOMIC_RELAXED,
+                       __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// This thread's slots, i, i + kThreads and so on below `blocks`; true while one
+// is not of this epoch.
+template <int kPer>
+__device__ __forceinline__ bool read_slots(const uint64_t* slots, int blocks, uint32_t epoch, uint64_t (&word)[kPer]) {
+    bool missing = false;
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        const int b = k * kThreads + static_cast<int>(threadIdx.x);
+        word[k] = b < blocks ? read_slot(slots + b) : slot_tag(epoch);
+        missing |= (word[k] & kSlotTag) != slot_tag(epoch);
+    }
+    return missing;
+}
+
+__device__ __forceinline__ void finish_result(double sumsq, const float* scale, double max_norm,
+                                              gockpt_grad_result* out) {
+    const double norm = sqrt(sumsq) / (scale != nullptr ? static_cast<double>(*scale) : 1.0);
+    const bool finite = isfinite(sumsq);
+    const double coef = max_norm / (norm + kClipEps);
+    out->sumsq = sumsq;
+    out->norm = static_cast<float>(norm);
+    out->found_inf = finite ? 0.0f : 1.0f;
+    out->coef = finite && coef < 1.0 ? static_cast<float>(coef) : 1.0f;
+    out->reserved_[0] = out->reserved_[1] = out->reserved_[2] = 0.0f;
+}
+
+// Block 0 waits for the others, none of which waits for anything.
 template <bool kNT>
 __global__ __launch_bounds__(kThreads) void sumsq_kernel(const GradTile* __restrict__ tiles, int ntiles,
-                                                         double* __restrict__ parts) {
+                                                         uint32_t* sync, uint64_t* slots,
+                                                         const float* __restrict__ scale, double max_norm,
+                                                         gockpt_grad_result* __restrict__ out) {
+    const uint32_t epoch = *sync;
     double acc = 0.0;
     u32x4 next[kUnitsPerThread];
     int i = blockIdx.x;
@@ -222,39 +274,23 @@ __global__ __launch_bounds__(kThreads) void sumsq_kernel(const GradTile* __restr
         acc += tile_sum(now, raw);
     }
     acc = block_sum(acc);
-    if (threadIdx.x == 0) parts[blockIdx.x] = acc;
-}
-
-__device__ __forceinline__ void finish_result(double sumsq, const float* scale, double max_norm,
-                                              gockpt_grad_result* out) {
-    const double norm = sqrt(sumsq) / (scale != nullptr ? static_cast<double>(*scale) : 1.0);
-    const bool finite = isfinite(sumsq);
-    const double coef = max_norm / (norm + kClipEps);
-    out->sumsq = sumsq;
-    out->norm = static_cast<float>(norm);
-    out->found_inf = finite ? 0.0f : 1.0f;
-    out->coef = finite && coef < 1.0 ? static_cast<float>(coef) : 1.0f;
-    out->reserved_[0] = out->reserved_[1] = out->reserved_[2] = 0.0f;
-}
-
-__global__ __launch_bounds__(kThreads) void result_kernel(const double* __restrict__ parts, int nparts,
-                                                          const float* __restrict__ scale, double max_norm,
-                                                          gockpt_grad_result* __restrict__ out) {
-    double v[kSumBlocks / kThreads];
+    if (threadIdx.x == 0) publish(slots + blockIdx.x, epoch, acc);
+    if (blockIdx.x != 0) return;
+    uint64_t word[kSumBlocks / kThreads];
+    while (read_slots(slots, gridDim.x, epoch, word)) __builtin_amdgcn_s_sleep(2);
+    acc = 0.0;
 #pragma unroll
-    for (int k = 0; k < kSumBlocks / kThreads; ++k) {
-        const int i = k * kThreads + static_cast<int>(threadIdx.x);
-        v[k] = i < nparts ? parts[i] : 0.0;
-    }
-    double acc = 0.0;
-#pragma unroll
-    for (int k = 0; k < kSumBlocks / kThreads; ++k) acc += v[k];
+    for (int k = 0; k < kSumBlocks / kThreads; ++k) acc += __builtin_bit_cast(double, word[k] & ~kSlotTag);
     acc = block_sum(acc);
-    if (threadIdx.x == 0) finish_result(acc, scale, max_norm, out);
+    if (threadIdx.x == 0) {
+        finish_result(acc, scale, max_norm, out);
+        *sync = epoch + 1u;
+    }
 }
 
-__global__ void result_again_kernel(gockpt_grad_result* out, const float* scale, double max_norm) {
-    finish_result(out->sumsq, scale, max_norm, out);
+// The result of an empty list, or again from its sumsq.
+__global__ void result_kernel(gockpt_grad_result* out, const float* scale, double max_norm, bool empty) {
+    finish_result(empty ? 0.0 : out->sumsq, scale, max_norm, out);
 }
 
 // One element, or two, four or eight, at any address.
@@ -368,16 +404,9 @@ __global__ __launch_bounds__(kThreads) void scale_kernel(const GradTile* __restr
 // ---- small lists: one launch ---------------------------------------------------
 //
 // Block b squares tile b, publishes its partial and, to clip, waits for the
-// partials of all blocks, adds them in the fixed order that every block uses,
-// and scales the tile, which it still has in registers.  For a norm only block
-// 0 waits.
-//
-// A partial is one 64-bit word: a double, and in the place of its sign, which
-// a sum of squares has no use for, the call's epoch modulo two.  Every call on
-// a list writes every slot, so a slot with the other tag is the last call's:
-// value and flag are one word, and no fence is needed, which on this chip would
-// write back an XCD's L2.  Block 0 moves the epoch on once it has seen every
-// partial, that is after every block has read it.
+// partials of all blocks, adds them in the order that every block uses, and
+// scales the tile, which it still has in registers.  For a norm only block 0
+// waits.
 //
 // No block but block 0 depends on another one running: after `spins`
 // polls it computes the missing partials itself, and block 0 thus waits only
@@ -386,14 +415,6 @@ __global__ __launch_bounds__(kThreads) void scale_kernel(const GradTile* __restr
 // only after it has seen its own partial published: if the slot is still empty
 // after the tile has been read, what was read is unscaled, and if it is not,
 // the slot's value is taken.
-
-constexpr uint64_t kSlotTag = uint64_t{1} << 63;
-
-__device__ __forceinline__ uint64_t slot_tag(uint32_t epoch) { return epoch & 1u ? kSlotTag : 0u; }
-
-__device__ __forceinline__ uint64_t read_slot(const uint64_t* p) {
-    return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
 
 template <bool kClip>
 __global__ __launch_bounds__(kThreads) void whole_kernel(const GradTile* __restrict__ tiles, uint32_t* sync,
@@ -408,28 +429,15 @@ __global__ __launch_bounds__(kThreads) void whole_kernel(const GradTile* __restr
     u32x4 raw[kUnitsPerThread];
     load_tile<false>(t, raw);
     const double mine = block_sum(tile_sum(t, raw));
-    if (threadIdx.x == 0)
-        __hip_atomic_store(slots + blockIdx.x, (__builtin_bit_cast(uint64_t, mine) & ~kSlotTag) | slot_tag(epoch),
-                           __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (threadIdx.x == 0) publish(slots + blockIdx.x, epoch, mine);
     if (!kClip && blockIdx.x != 0) return;
 
-    // thread i waits for slots i and i + kThreads
     constexpr int kPer = kWholeTiles / kThreads;
     uint64_t word[kPer];
-    auto missing = [&]() {
-        bool m = false;
-#pragma unroll
-        for (int k = 0; k < kPer; ++k) {
-            const int b = k * kThreads + static_cast<int>(threadIdx.x);
-            word[k] = b < blocks ? read_slot(slots + b) : slot_tag(epoch);
-            m |= (word[k] & kSlotTag) != slot_tag(epoch);
-        }
-        return m;
-    };
-    bool wait = missing();
+    bool wait = read_slots(slots, blocks, epoch, word);
     for (int i = 0; wait && (blockIdx.x == 0 || i < spins); ++i) {
         __builtin_amdgcn_s_sleep(2);
-        wait = missing();
+        wait = read_slots(slots, blocks, epoch, word);
     }
 #pragma unroll
     for (int k = 0; k < kPer; ++k)  // -1: missing
@@ -472,10 +480,10 @@ __global__ __launch_bounds__(kThreads) void whole_kernel(const GradTile* __restr
 // ---- host: the table ---------------------------------------------------------
 
 constexpr int64_t kMaxElems = int64_t{1} << 46;
-// Workspace: sync word, slots of the one-launch form, partials, table.
+// Workspace: sync word, the blocks' partials, table.
 constexpr size_t kSlotsOff = 256;
-constexpr size_t kPartsOff = kSlotsOff + kWholeTiles * sizeof(uint64_t);
-constexpr size_t kTableOff = kPartsOff + kSumBlocks * sizeof(double);
+constexpr size_t kTableOff = kSlotsOff + kSumBlocks * sizeof(uint64_t);
+static_assert(kWholeTiles <= kSumBlocks, "slots");
 
 // A tensor as the tiles see it: rows that follow one another are one row.
 struct Flat {
@@ -665,21 +673,19 @@ static int run_list(const char* name, gockpt_grads* list, const float* scale, do
     if (rc != GOCKPT_OK) return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const int n = list->ntiles;
-    if (n > 0 && n <= kWholeTiles) {
+    uint32_t* sync = reinterpret_cast<uint32_t*>(list->ws);
+    uint64_t* slots = reinterpret_cast<uint64_t*>(list->ws + kSlotsOff);
+    if (n == 0) {
+        hipLaunchKernelGGL(result_kernel, dim3(1), dim3(1), 0, s, result, scale, max_norm, true);
+    } else if (n <= kWholeTiles) {
         hipLaunchKernelGGL(clip ? whole_kernel<true> : whole_kernel<false>, dim3(n), dim3(kThreads), 0, s,
-                           list->tiles, reinterpret_cast<uint32_t*>(list->ws),
-                           reinterpret_cast<uint64_t*>(list->ws + kSlotsOff), list->spins, scale, max_norm, result);
-        return ops_launched(name);
-    }
-    double* parts = reinterpret_cast<double*>(list->ws + kPartsOff);
-    const int blocks = n < kSumBlocks ? n : kSumBlocks;
-    if (blocks > 0) {
+                           list->tiles, sync, slots, list->spins, scale, max_norm, result);
+    } else {
         const bool nt = !clip || list->src_bytes > kCachedSumBytes;
-        hipLaunchKernelGGL(nt ? sumsq_kernel<true> : sumsq_kernel<false>, dim3(blocks), dim3(kThreads), 0, s,
-                           list->tiles, n, parts);
+        hipLaunchKernelGGL(nt ? sumsq_kernel<true> : sumsq_kernel<false>, dim3(n < kSumBlocks ? n : kSumBlocks),
+                           dim3(kThreads), 0, s, list->tiles, n, sync, slots, scale, max_norm, result);
+        if (clip) launch_scale(list, result, s);
     }
-    hipLaunchKernelGGL(result_kernel, dim3(1), dim3(kThreads), 0, s, parts, blocks, scale, max_norm, result);
-    if (clip) launch_scale(list, result, s);
     return ops_launched(name);
 }
 
@@ -706,8 +712,8 @@ int gockpt_grads_result(gockpt_grad_result* result, const float* scale, double m
     const char* name = "gockpt_grads_result";
     const int rc = check_norm(name, scale, max_norm, result);
     if (rc != GOCKPT_OK) return rc;
-    hipLaunchKernelGGL(result_again_kernel, dim3(1), dim3(1), 0, static_cast<hipStream_t>(stream), result, scale,
-                       max_norm);
+    hipLaunchKernelGGL(result_kernel, dim3(1), dim3(1), 0, static_cast<hipStream_t>(stream), result, scale, max_norm,
+                       false);
     return ops_launched(name);
 }
 
