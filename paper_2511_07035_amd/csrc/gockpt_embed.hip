@@ -237,10 +237,10 @@ struct GradArgs {
     int32_t dst_dtype, accumulate;
     int32_t lanes;                         // of a row, a power of two
     uint32_t col_blocks;
-    // sort: blocks that sort, and tokens of each; the others of the launch
-    // clear a part of the table
+    // blocks of a launch that sort, and tokens of each; the others clear a part
+    // of the table
     int32_t sort_blocks, sort_tokens;
-    int32_t low_bits, digits;              // of the running pass
+    int32_t digits;                        // of the running radix pass
     uint32_t shift;
     // Rows from clear_from on are cleared in `parts` parts by the launches that
     // sort (whose blocks alone leave most of the device idle), before it is
@@ -375,15 +375,15 @@ __device__ __forceinline__ void place_round(uint32_t (&next)[kDigits], WaveCount
     }
 }
 
-// Sort of at most kBucketTokens tokens in one launch: a block takes the rows
-// of one bucket of 1 << bits, at most kBucketDigits.  It looks through
-// all ids, counts the tokens of smaller rows, which is where its own begin,
-// lists its own in token order and sorts them by row in one counting pass.
+// Sort of at most kBucketTokens tokens in one launch: a block takes the rows of
+// one bucket of 1 << bits, at most kBucketDigits.  It looks through all ids,
+// counts the tokens of smaller rows, which is where its own begin, lists its own
+// in token order and sorts them by row in one counting pass.
 constexpr uint32_t kIdsAhead = 8;
 
 __global__ __launch_bounds__(kSortThreads, 8) void bucket_kernel(GradArgs a, int bits) {
     constexpr int kDigits = kBucketDigits;
-    __shared__ uint32_t list[kBucketTokens];        // row within the bucket << 16 | token
+    __shared__ uint32_t list[kBucketTokens];  // row within the bucket << 16 | token
     __shared__ uint32_t next[kDigits];
     __shared__ alignas(16) WaveCounts<kDigits> in_wave;
     __shared__ uint32_t found[kSortWaves], below[kSortWaves], valid[kSortWaves];
