@@ -611,13 +611,20 @@ __global__ __launch_bounds__(kThreads) void direct_kernel(GradArgs a) {
     __syncthreads();
 
     const int lane = threadIdx.x & (a.lanes - 1), g = threadIdx.x / a.lanes;
-    const int64_t c = (static_cast<int64_t>(col) * a.lanes + lane) * kV;
-    if (c >= a.cols) return;
-    if (!a.accumulate) {
-        const float zero[kV] = {};
-        for (int r = g * group_rows; r < (g + 1) * group_rows && r < kBucketRows && row0 + r < a.ids.rows; ++r)
-            if (!(seen[r / 32] >> r % 32 & 1u)) finish_row<kV>(a, row0 + r, c, zero, false);
+    const int64_t c0 = static_cast<int64_t>(col) * a.lanes * kV, c = c0 + lane * kV;
+    if (!a.accumulate) {  // rows without a token, a wavefront each
+        const int64_t wide = a.lanes * kV, size = a.dst_dtype == kFP32 ? 4 : 2;
+        const int64_t bytes = (a.cols - c0 < wide ? a.cols - c0 : wide) * size;
+        const int64_t here = a.ids.rows - row0 < kBucketRows ? a.ids.rows - row0 : kBucketRows;
+        if (n == 0 && bytes == a.dst_stride) {
+            clear_span(a.dst + row0 * bytes, here * bytes, threadIdx.x, kThreads, a.clear_nt);
+            return;
+        }
+        for (int r = threadIdx.x / 64; r < here; r += kThreads / 64)
+            if (!(seen[r / 32] >> r % 32 & 1u))
+                clear_span(a.dst + (row0 + r) * a.dst_stride + c0 * size, bytes, threadIdx.x & 63, 64, a.clear_nt);
     }
+    if (c >= a.cols) return;
     int at = 0;
     for (int k = 0; k < g; ++k) at = max(at, group_end[k]);
     const int end = max(at, group_end[g]);
@@ -666,7 +673,12 @@ __device__ __forceinline__ void clear_absent(const GradArgs& a, uint32_t block) 
     }
     const uint64_t there = __ballot(lo < n && a.sorted[lo].row == row);
     const int64_t bytes = a.cols * (a.dst_dtype == kFP32 ? 4 : 2);
-    for (int r = threadIdx.x / 64; r < kClearRows && row0 + r < a.clear_from; r += kThreads / 64)
+    const int64_t here = a.clear_from - row0 < kClearRows ? a.clear_from - row0 : kClearRows;
+    if ((there & (here < 64 ? (uint64_t{1} << here) - 1 : ~uint64_t{0})) == 0 && bytes == a.dst_stride) {
+        clear_span(a.dst + row0 * bytes, here * bytes, threadIdx.x, kThreads, a.clear_nt);
+        return;
+    }
+    for (int r = threadIdx.x / 64; r < here; r += kThreads / 64)
         if (!(there >> r & 1u)) clear_span(a.dst + (row0 + r) * a.dst_stride, bytes, lane, 64, a.clear_nt);
 }
 
@@ -683,11 +695,12 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(GradArgs a) {
         return;
     }
     const int lane = threadIdx.x & (a.lanes - 1), g = threadIdx.x / a.lanes;
-    const int groups = kThreads / a.lanes;
-    const uint32_t block = blockIdx.x / a.col_blocks, col = blockIdx.x - block * a.col_blocks;
-    const uint32_t n = a.heads[0];
-    uint32_t q = block * groups + g;
+    // a block's groups take the column blocks of a chunk, then the next chunk:
+    // groups of one wavefront mostly end rows together
+    const uint32_t n = a.heads[0], item = blockIdx.x * (kThreads / a.lanes) + g;
+    uint32_t q = item / a.col_blocks;
     if constexpr (kWave) q = __builtin_amdgcn_readfirstlane(q);
+    const uint32_t col = item - q * a.col_blocks;
     const uint32_t first = q * a.chunk;
     const int left = first < n ? static_cast<int>(n - first) : 0, count = left < a.chunk ? left : a.chunk;
     const uint32_t none = 0xFFFFFFFFu;
@@ -812,15 +825,16 @@ constexpr int64_t kMaxTokens = INT32_MAX;
 constexpr int64_t kMaxCols = int64_t{1} << 24;
 constexpr int64_t kMaxGrid = int64_t{1} << 24;  // blocks of kThreads that a launch can have
 
-// Lanes of a row: the power of two from `least` to `most` with the fewest idle
-// lanes over all column blocks, the larger one of equals.
-int lanes_for(int64_t cols, int per_lane, int least, int most) {
+// Lanes of a row: the power of two from `least` to `most` that one column block
+// needs, or, where it takes several, down to `down_to`, the one with the fewest
+// idle lanes over all of them, the larger one of equals.
+int lanes_for(int64_t cols, int per_lane, int least, int most, int down_to) {
     const int64_t need = (cols + per_lane - 1) / per_lane;
     int lanes = least;
     while (lanes < most && lanes < need) lanes *= 2;
     if (need > lanes) {
         int64_t best = (need + lanes - 1) / lanes * lanes;
-        for (int l = lanes / 2; l >= 64; l /= 2) {
+        for (int l = lanes / 2; l >= down_to; l /= 2) {
             const int64_t all = (need + l - 1) / l * l;
             if (all < best) {
                 best = all;
@@ -856,13 +870,14 @@ GradPlan plan_grad(int64_t tokens, int64_t rows, int64_t cols) {
     per = (per + kSortThreads - 1) / kSortThreads * kSortThreads;
     p.sort_tokens = static_cast<int>(per);
     p.sort_blocks = static_cast<int>((tokens + per - 1) / per);
-    const int l = lanes_for(cols, 8, kMinLanes, 64);
+    const int l = lanes_for(cols, 8, kMinLanes, 64, kMinLanes);
     const int64_t waves = tokens * col_blocks(cols, 8, l) * l / 64;
     // Longer chunks have fewer partials, shorter ones keep more loads in flight
-    // (us with chunks of 16, 32 and 64, bf16 but the last to fp32: 2048 tokens into 1000 x
-    // 256 17.8, 24, 38, 8192 into 50304 x 2048 60, 62, 75, 16384 76, 75, 80,
-    // 131072 into 32000 x 4096 406, 377, 362, 30000 into 20011 x 1001 64, 74, 95).
-    p.chunk = tokens > 65536 ? 64 : waves < 65536 ? 16 : 32;
+    // (us with chunks of 16, 32 and 64, bf16, text's law: 2048 tokens into 1000 x
+    // 256 17.8, 24, 38, 8192 into 50304 x 2048 60, 62, 75, 16384 76, 75, 80, 30000
+    // into 20011 x 1001 64, 74, 95, 91000 into 883 x 640 -, 54, 65, 131072 into
+    // 32000 x 4096 406, 377, 362, into 1000 x 64 61, 46, 46).
+    p.chunk = waves >= 524288 ? 64 : waves >= 65536 || tokens > 65536 ? 32 : 16;
     p.chunks = (tokens + p.chunk - 1) / p.chunk;
     const int64_t wide = (cols + 7) / 8 * 8;
     size_t at = 0;
@@ -930,7 +945,7 @@ constexpr int64_t kCachedOutBytes = int64_t{96} << 20;
 template <int kW, int kO>
 int launch_lookup(LookupArgs& a, const char* name, hipStream_t s) {
     constexpr int kV = kO == kFP32 ? 4 : 8;
-    a.lanes = lanes_for(a.cols, kV, 1, kThreads);
+    a.lanes = lanes_for(a.cols, kV, 1, kThreads, 64);
     a.col_blocks = col_blocks(a.cols, kV, a.lanes);
     const int64_t per = kThreads / a.lanes;
     const int64_t blocks = ((a.ids.tokens + per - 1) / per * a.col_blocks + kPieces - 1) / kPieces;
@@ -982,18 +997,23 @@ template <int kS>
 int launch_grad(GradArgs& a, const GradPlan& p, const char* name, hipStream_t s) {
     constexpr int kV = kS == kFP32 ? 4 : 8;
     if (p.direct) {
-        a.lanes = lanes_for(a.cols, kV, 1, kThreads);
+        a.lanes = lanes_for(a.cols, kV, 1, kThreads, 64);
         a.col_blocks = col_blocks(a.cols, kV, a.lanes);
+        a.clear_nt = a.ids.rows * a.cols * dtype_bytes(a.dst_dtype) > kCachedOutBytes;
         const int64_t blocks = (int64_t{a.ids.rows} + kBucketRows - 1) / kBucketRows * a.col_blocks;
         if (blocks >= kMaxGrid) return ops_fail(GOCKPT_EINVAL, "%s: the table is too large", name);
         hipLaunchKernelGGL(direct_kernel<kS>, dim3(static_cast<uint32_t>(blocks)), dim3(kThreads), 0, s, a);
         return ops_launched(name);
     }
-    a.lanes = lanes_for(a.cols, kV, kMinLanes, 64);
+    // Whole wavefronts where there are few tokens (narrow rows then leave lanes
+    // idle, but rows end together: 2304 x 77 23.6 us, 24.4 in groups of 16); with
+    // many, the groups with the fewest idle lanes (102016 x 637 80, 100).
+    const int least = p.bucket ? 64 : kMinLanes;
+    a.lanes = lanes_for(a.cols, kV, least, 64, least);
     a.col_blocks = col_blocks(a.cols, kV, a.lanes);
     a.chunk = p.chunk;
     const int groups = kThreads / a.lanes;
-    const int64_t blocks = (p.chunks + groups - 1) / groups * a.col_blocks;
+    const int64_t blocks = (p.chunks * a.col_blocks + groups - 1) / groups;
     if (2 * blocks >= kMaxGrid) return ops_fail(GOCKPT_EINVAL, "%s: too many tokens", name);
     a.clear_from = a.ids.rows;
     a.sum_blocks = static_cast<uint32_t>(blocks);
@@ -1012,7 +1032,7 @@ int launch_grad(GradArgs& a, const GradPlan& p, const char* name, hipStream_t s)
         hipLaunchKernelGGL((sum_kernel<kS, true>), grid, dim3(kThreads), 0, s, a);
     else
         hipLaunchKernelGGL((sum_kernel<kS, false>), grid, dim3(kThreads), 0, s, a);
-    a.lanes = lanes_for(a.cols, kJoinCols, kMinLanes, 64);
+    a.lanes = lanes_for(a.cols, kJoinCols, kMinLanes, 64, kMinLanes);
     a.col_blocks = col_blocks(a.cols, kJoinCols, a.lanes);
     const int64_t jblocks = (p.chunks + kThreads / a.lanes - 1) / (kThreads / a.lanes) * a.col_blocks;
     hipLaunchKernelGGL(join_kernel, dim3(static_cast<uint32_t>(jblocks)), dim3(kThreads), 0, s, a);
