@@ -564,14 +564,14 @@ def test_on_another_stream():
     assert same(y, w[ids])
 
 
-@pytest.mark.parametrize("tokens", [200, 6000])
-def test_captured_in_a_graph(tokens):
-    vocab, dim = 500, 96
+@pytest.mark.parametrize("tokens,more", [(100, 700), (6000, 700), (20_000, 6_000_001)])
+def test_captured_in_a_graph(tokens, more):
+    vocab, dim = 3000, 96  # every form of the sort, and of the norm
     w, ids = randn((vocab, dim), torch.bfloat16, 1, 0.02), ids_of("zipf", tokens, vocab, 2)
     x = randn((tokens, dim), torch.bfloat16, 3)
     y, gw = torch.empty(tokens, dim, dtype=torch.bfloat16, device="cuda"), torch.empty_like(w)
-    flat = torch.empty(vocab * dim + 700, dtype=torch.bfloat16, device="cuda")
-    main = randn((700,), torch.float32, 4)
+    flat = torch.empty(vocab * dim + more, dtype=torch.bfloat16, device="cuda")
+    main = randn((more,), torch.float32, 4)
     gl = g.GradList([gw, main], [flat[:vocab * dim], flat[vocab * dim:]])
     ws = torch.empty(max(g.gockpt_embedding_grad_bytes(tokens, vocab, dim), 256), dtype=torch.uint8, device="cuda")
     s = torch.cuda.Stream()
@@ -589,7 +589,7 @@ def test_captured_in_a_graph(tokens):
     for k in range(4):
         x.copy_(randn((tokens, dim), torch.bfloat16, 30 + k))
         ids.copy_(ids_of("zipf", tokens, vocab, 40 + k))
-        main.copy_(randn((700,), torch.float32, 50 + k))
+        main.copy_(randn((more,), torch.float32, 50 + k))
         step()
         want = [t.clone() for t in (y, gw, flat, gl.result.buffer)]
         for t in (y, gw, flat):
