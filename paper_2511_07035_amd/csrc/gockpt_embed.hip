@@ -17,7 +17,7 @@
 //   131072 tokens x 4096 fp16 into 32000 rows, a tenth masked (0.97 GB + 0.26
 //   GB): 272 us, of which the sort 42 (half of the table is cleared meanwhile),
 //   the sums 215 at 5.6 TB/s, the join 16.  16384 x 2048 bf16 into 50304 rows
-//   (67 + 206 MB): 65 us.  A copy moves the same bytes in 260 and 58.
+//   (67 + 206 MB): 62 us.  A copy moves the same bytes in 260 and 58.
 #include <limits.h>
 
 #include "gockpt_ops_internal.h"
@@ -685,8 +685,11 @@ __device__ __forceinline__ void clear_absent(const GradArgs& a, uint32_t block) 
 // Sorted tokens q * chunk to q * chunk + chunk - 1, summed row by row by
 // `lanes` lanes, kV columns each.  A row that lies in this chunk alone is
 // finished here; of one that began before, the sum goes to partial 2 q, of one
-// that begins here and goes on, to 2 q + 1.
-template <int kS, bool kWave>
+// that begins here and goes on, to 2 q + 1.  Sums that are added to what the table
+// holds (kAdd) are a kernel apart, which keeps the plain one's registers at 70, not
+// 90: 16384 tokens into 50304 x 2048 62 us, 64.5 as one.  What a row holds is loaded
+// when the row ends; loading it when the row begins was no faster (59 us, 58).
+template <int kS, bool kWave, bool kAdd>
 __global__ __launch_bounds__(kThreads) void sum_kernel(GradArgs a) {
     constexpr int kV = kS == kFP32 ? 4 : 8;
     __shared__ Pair pairs[kWave ? 1 : kThreads / kMinLanes * kMaxChunk];
@@ -742,7 +745,7 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(GradArgs a) {
                 *reinterpret_cast<u32x4*>(p + k) = (u32x4){__float_as_uint(acc[k]), __float_as_uint(acc[k + 1]),
                                                            __float_as_uint(acc[k + 2]), __float_as_uint(acc[k + 3])};
         } else {
-            finish_row<kV>(a, cur, c, acc, a.accumulate != 0);
+            finish_row<kV>(a, cur, c, acc, kAdd);
         }
     };
     Piece<kS, kV> x[kAhead];
@@ -1029,9 +1032,11 @@ int launch_grad(GradArgs& a, const GradPlan& p, const char* name, hipStream_t s)
     const dim3 grid(static_cast<uint32_t>(blocks + clear_blocks));
     a.wide = (a.cols + 7) / 8 * 8;
     if (a.lanes == 64)
-        hipLaunchKernelGGL((sum_kernel<kS, true>), grid, dim3(kThreads), 0, s, a);
+        hipLaunchKernelGGL((a.accumulate ? sum_kernel<kS, true, true> : sum_kernel<kS, true, false>), grid,
+                           dim3(kThreads), 0, s, a);
     else
-        hipLaunchKernelGGL((sum_kernel<kS, false>), grid, dim3(kThreads), 0, s, a);
+        hipLaunchKernelGGL((a.accumulate ? sum_kernel<kS, false, true> : sum_kernel<kS, false, false>), grid,
+                           dim3(kThreads), 0, s, a);
     a.lanes = lanes_for(a.cols, kJoinCols, kMinLanes, 64, kMinLanes);
     a.col_blocks = col_blocks(a.cols, kJoinCols, a.lanes);
     const int64_t jblocks = (p.chunks + kThreads / a.lanes - 1) / (kThreads / a.lanes) * a.col_blocks;
