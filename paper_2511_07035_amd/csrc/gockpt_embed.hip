@@ -1115,7 +1115,9 @@ int gockpt_embedding_grad(const gockpt_matrix* grad_out, const gockpt_token_ids*
     a.dst = static_cast<uint8_t*>(const_cast<void*>(grad_table->data));
     a.cols = grad_table->cols;
     a.src_stride = grad_out->stride * dtype_bytes(grad_out->dtype);
-    a.dst_stride = grad_table->stride * dtype_bytes(grad_table->dtype);
+    // a single row may come with any stride; the kernels take rows whose stride
+    // is their width as one span
+    a.dst_stride = (grad_table->rows > 1 ? grad_table->stride : grad_table->cols) * dtype_bytes(grad_table->dtype);
     a.scale = scale;
     a.dst_dtype = grad_table->dtype;
     a.accumulate = accumulate != 0;
