@@ -329,15 +329,24 @@ def embedding(weight, ids, *, scale: float = 1.0, out=None, out_dtype=None, firs
     rows) are masked: zeros, and no gradient.
 
     Differentiable in weight, with the gradient of ``embedding_grad``: returned
-    to autograd in the weight's type, or, with grad_weight (the weight's part
-    of ``Session.grad``), written or accumulated there and not returned.  Tokens
-    with padding_id add no gradient.  out and stream are for calls that need
-    no gradient."""
+    to autograd in the weight's type, or, with grad_weight (of the weight's
+    shape: its part of ``Session.grad``), written or accumulated there and not
+    returned; where the weight requires no gradient, nothing is written.  Each
+    backward writes every row of grad_weight: with several lookups of one table
+    in a step, clear it first and let all of them accumulate.  Tokens with
+    padding_id add no gradient.  out and stream are for calls that need no
+    gradient."""
     if accumulate and grad_weight is None:
         raise ValueError("accumulate: into a grad_weight")
     if weight.requires_grad and torch.is_grad_enabled():
         if out is not None or stream is not None:
             raise ValueError("out and stream: for calls without a gradient")
+        if grad_weight is not None:
+            # the backward takes the table's rows, and so which ids count, from it
+            if grad_weight.shape != weight.shape:
+                raise ValueError(f"grad_weight of shape {tuple(grad_weight.shape)} for a weight of shape "
+                                 f"{tuple(weight.shape)}")
+            _matrix(grad_weight, "grad_weight", _here(weight, "weight"))
         return _Embedding.apply(weight, ids, scale, out_dtype, first_id, padding_id, grad_weight, accumulate)
     return _lookup(weight, ids, scale, out, out_dtype, first_id, stream)
 

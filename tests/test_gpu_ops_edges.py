@@ -27,3 +27,20 @@ def test_the_gradient_of_a_table_of_one_row_is_written_whole(cols, dtype, tokens
         ids[0] = 0
         g.embedding_grad(torch.ones(tokens, cols, dtype=dtype, device="cuda"), ids, into)
         assert bool((into == 1.0).all()) and bool((buf[cols:] == 9.0).all())
+
+
+@pytest.mark.parametrize("rows", [6, 11])
+def test_a_gradient_of_another_shape_than_the_table_is_refused(rows):
+    table = torch.randn(10, 8, device="cuda").requires_grad_()
+    ids = torch.tensor([1, 7, 9, 10], device="cuda")
+    with pytest.raises(ValueError):
+        g.embedding(table, ids, grad_weight=torch.zeros(rows, 8, device="cuda"))
+    for bad in (torch.zeros(10, 7, device="cuda"), torch.zeros(80, device="cuda"), torch.zeros(10, 8),
+                torch.zeros(10, 8, dtype=torch.float64, device="cuda")):
+        with pytest.raises(ValueError):
+            g.embedding(table, ids, grad_weight=bad)
+    into = torch.full((10, 8), 5.0, dtype=torch.bfloat16, device="cuda")
+    g.embedding(table, ids, grad_weight=into).sum().backward()
+    want = torch.zeros(10, 8, device="cuda")
+    want[[1, 7, 9]] = 1.0
+    assert torch.equal(into.float(), want)
