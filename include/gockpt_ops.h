@@ -52,8 +52,10 @@ typedef struct {
 typedef struct {
     double sumsq;     /* sum of squares of the elements as stored */
     float norm;       /* sqrt(sumsq) / scale */
-    float found_inf;  /* 1 when some element is inf or NaN, else 0 */
-    float coef;       /* min(1, max_norm / (norm + 1e-6)); 1 when found_inf */
+    float found_inf;  /* 1 when some element is inf or NaN, or times coef is rounded to inf in its dst, else 0 */
+    float coef;       /* min(1, max_norm / (norm + 1e-6)); 1 when some element is inf or NaN */
+    /* [0]: largest magnitude of the elements that go to fp16 from a wider type and
+     * are, unscaled, too large for it, [1]: of such that go to bf16 (0: none); [2]: 0 */
     float reserved_[3];
 } gockpt_grad_result;
 
@@ -85,8 +87,8 @@ int gockpt_grads_norm(gockpt_grads* list, const float* scale, double max_norm,
                       gockpt_grad_result* result, void* stream);
 
 /* dst = round(element * result->coef) for every element, one fp32 product
- * rounded once to the destination's type, to nearest even (beyond fp16's
- * range: infinity, which no found_inf of this norm tells).  In place, a
+ * rounded once to the destination's type, to nearest even; beyond that type's
+ * range: infinity, which the found_inf of this list's norm tells.  In place, a
  * coefficient of 1 leaves the memory untouched.  Errors: EINVAL, EHIP. */
 int gockpt_grads_scale(gockpt_grads* list, const gockpt_grad_result* result, void* stream);
 
@@ -95,8 +97,10 @@ int gockpt_grads_scale(gockpt_grads* list, const gockpt_grad_result* result, voi
 int gockpt_grads_clip(gockpt_grads* list, const float* scale, double max_norm,
                       gockpt_grad_result* result, void* stream);
 
-/* norm, found_inf and coef again from result->sumsq: for ranks that hold
- * different parameters and have added up their sumsq.  Errors: EINVAL, EHIP. */
+/* norm, found_inf and coef again from result->sumsq and reserved_, as a norm
+ * left them: for ranks that hold different parameters, have added up their
+ * sumsq and, where a dst is narrower than its data, taken the maximum of each
+ * of reserved_[0] and [1].  Errors: EINVAL, EHIP. */
 int gockpt_grads_result(gockpt_grad_result* result, const float* scale, double max_norm, void* stream);
 
 /* Device address of the context's loss scale (the one the next gockpt_step

@@ -2,8 +2,10 @@
 //
 //   sumsq_kernel   reads every tensor once: S = sum of squares, one fp64
 //                  partial a block; block 0 adds them in a fixed order:
-//                  norm = sqrt(S) / scale, found_inf, and the clipping
-//                  coefficient min(1, max_norm / (norm + 1e-6)).
+//                  norm = sqrt(S) / scale, the clipping coefficient
+//                  min(1, max_norm / (norm + 1e-6)), and found_inf: an inf or
+//                  NaN, or a finite element whose scaled value is rounded to
+//                  an infinity in a narrower type.
 //   scale_kernel   element * coef, rounded to the destination's type.
 //   whole_kernel   all of it in one launch for a list of at most 8 MiB.
 //
@@ -181,14 +183,82 @@ __device__ __forceinline__ double square_sum(const u32x4 (&raw)[kUnitsPerThread]
     return d;
 }
 
-__device__ __forceinline__ double block_sum(double x) {
+// The sum over the block, and whether `any` holds in one of its threads.
+__device__ __forceinline__ double block_sum(double x, bool* any = nullptr) {
     __shared__ double part[kThreads / 64];
+    __shared__ uint64_t lanes[kThreads / 64];
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
+    const uint64_t with = any != nullptr ? __ballot(*any) : 0u;
     __syncthreads();  // an earlier sum has been read
+    if ((threadIdx.x & 63) == 0) {
+        part[threadIdx.x >> 6] = x;
+        if (any != nullptr) lanes[threadIdx.x >> 6] = with;
+    }
+    __syncthreads();
+    if (any != nullptr) *any = (lanes[0] | lanes[1] | lanes[2] | lanes[3]) != 0u;
+    return (part[0] + part[1]) + (part[2] + part[3]);
+}
+
+// The least fp32 magnitudes that round to an infinity: half a step above the
+// type's largest finite value, where the tie goes to the even side, upwards.
+constexpr float kInfOfFp16 = 65520.0f;
+constexpr float kInfOfBf16 = 0x1.FFp127f;
+
+// Largest magnitudes of the elements that go to fp16 from a wider type and are
+// too large for it as they are, and of such that go to bf16 from fp32, as the
+// bits of an fp32 value, which order as the values do (0: none; an infinity or
+// NaN lies above all).  Whether one of them is still rounded to infinity is
+// known once the coefficient is (at most 1): the products with it order as the
+// elements do.
+struct Range {
+    uint32_t fp16, bf16;
+};
+
+__device__ __forceinline__ uint32_t max_bits(uint32_t a, uint32_t b) { return a > b ? a : b; }
+
+// raw, whose squares' sum is `sum`, into range.  An element of least magnitude
+// x makes the sum x^2 (1 - 2^-24) at least, so almost always the sum alone tells
+// that there is none.
+__device__ __forceinline__ void tile_range(const GradTile& t, const u32x4 (&raw)[kUnitsPerThread], double sum,
+                                           Range& range) {
+    const bool to16 = t.dst_dtype == kFP16 && t.dtype != kFP16;
+    if (!to16 && !(t.dst_dtype == kBF16 && t.dtype == kFP32)) return;
+    const float least = to16 ? kInfOfFp16 : kInfOfBf16;
+    if (!(sum >= 0.5 * least * least)) return;  // a NaN among them: found without this
+    const uint32_t mask = t.dtype == kBF16 ? 0x7FFF0000u : 0x7FFFFFFFu;
+    uint32_t m = 0u;
+#pragma unroll
+    for (int i = 0; i < kUnitsPerThread; ++i) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            m = max_bits(m, raw[i][j] & mask);
+            if (t.dtype == kBF16) m = max_bits(m, raw[i][j] << 16 & mask);
+        }
+    }
+    if (m < __float_as_uint(least)) return;
+    if (to16)
+        range.fp16 = max_bits(range.fp16, m);
+    else
+        range.bf16 = max_bits(range.bf16, m);
+}
+
+__device__ __forceinline__ Range block_range(Range x) {
+    __shared__ Range part[kThreads / 64];
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) {
+        x.fp16 = max_bits(x.fp16, __shfl_xor(x.fp16, o, 64));
+        x.bf16 = max_bits(x.bf16, __shfl_xor(x.bf16, o, 64));
+    }
+    __syncthreads();  // an earlier range has been read
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
     __syncthreads();
-    return (part[0] + part[1]) + (part[2] + part[3]);
+#pragma unroll
+    for (int k = 0; k < kThreads / 64; ++k) {
+        x.fp16 = max_bits(x.fp16, part[k].fp16);
+        x.bf16 = max_bits(x.bf16, part[k].bf16);
+    }
+    return x;
 }
 
 // raw -> the sum of its squares.
@@ -205,12 +275,16 @@ __device__ __forceinline__ double tile_sum(const GradTile& t, u32x4 (&raw)[kUnit
 // a sum of squares has no use for, the call's epoch modulo two.  Every call on
 // a list writes every slot, so a slot with the other tag is the last call's:
 // value and flag are one word, and no fence is needed, which on this chip would
-// write back an XCD's L2.  Block 0 adds the partials in a fixed order and moves
+// write back an XCD's L2.  In a list with destinations narrower than their
+// source (kRange) a block writes its range too, as two magnitudes of 31 bits and
+// a tag; the lowest bit of its partial (all partials are cut by it) says whether
+// there is one to be read, since a second read of words costs 1 us.  Block 0 adds the partials in a fixed order and moves
 // the epoch on once it has seen every one of them, that is after every block
 // has read it.  (As a launch of its own that cost 1 us more: 2^23 bf16 elements
 // 6.5 and 7.5, 2^25 14.1 and 15.2.)
 
 constexpr uint64_t kSlotTag = uint64_t{1} << 63;
+constexpr uint64_t kSlotRange = 1;
 
 __device__ __forceinline__ uint64_t slot_tag(uint32_t epoch) { return epoch & 1u ? kSlotTag : 0u; }
 
@@ -218,8 +292,20 @@ __device__ __forceinline__ uint64_t read_slot(const uint64_t* p) {
     return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-__device__ __forceinline__ void publish(uint64_t* slot, uint32_t epoch, double x) {
-    __hip_atomic_store(slot, (__builtin_bit_cast(uint64_t, x) & ~kSlotTag) | slot_tag(epoch), __ATOMIC_RELAXED,
+__device__ __forceinline__ double slot_value(uint64_t word) {
+    return __builtin_bit_cast(double, word & ~(kSlotTag | kSlotRange));
+}
+
+// A block's own partial as the others read it.
+__device__ __forceinline__ double cut(double x) { return slot_value(__builtin_bit_cast(uint64_t, x)); }
+
+__device__ __forceinline__ void publish(uint64_t* slot, uint32_t epoch, double x, bool has_range) {
+    __hip_atomic_store(slot, __builtin_bit_cast(uint64_t, cut(x)) | (has_range ? kSlotRange : 0u) | slot_tag(epoch),
+                       __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+__device__ __forceinline__ void publish(uint64_t* slot, uint32_t epoch, Range x) {
+    __hip_atomic_store(slot, uint64_t{x.fp16} << 31 | x.bf16 | slot_tag(epoch), __ATOMIC_RELAXED,
                        __HIP_MEMORY_SCOPE_AGENT);
 }
 
@@ -237,26 +323,45 @@ __device__ __forceinline__ bool read_slots(const uint64_t* slots, int blocks, ui
     return missing;
 }
 
-__device__ __forceinline__ void finish_result(double sumsq, const float* scale, double max_norm,
+// The range over all blocks, which the calling block waits for.
+template <int kPer>
+__device__ __forceinline__ Range all_ranges(const uint64_t* slots, int blocks, uint32_t epoch) {
+    uint64_t word[kPer];
+    while (read_slots(slots, blocks, epoch, word)) __builtin_amdgcn_s_sleep(2);
+    Range x = {0u, 0u};
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+        x.fp16 = max_bits(x.fp16, static_cast<uint32_t>(word[k] >> 31) & 0x7FFFFFFFu);
+        x.bf16 = max_bits(x.bf16, static_cast<uint32_t>(word[k]) & 0x7FFFFFFFu);
+    }
+    return block_range(x);
+}
+
+__device__ __forceinline__ void finish_result(double sumsq, Range range, const float* scale, double max_norm,
                                               gockpt_grad_result* out) {
     const double norm = sqrt(sumsq) / (scale != nullptr ? static_cast<double>(*scale) : 1.0);
     const bool finite = isfinite(sumsq);
     const double coef = max_norm / (norm + kClipEps);
+    const float c = finite && coef < 1.0 ? static_cast<float>(coef) : 1.0f;
+    const float fp16 = __uint_as_float(range.fp16), bf16 = __uint_as_float(range.bf16);
     out->sumsq = sumsq;
     out->norm = static_cast<float>(norm);
-    out->found_inf = finite ? 0.0f : 1.0f;
-    out->coef = finite && coef < 1.0 ? static_cast<float>(coef) : 1.0f;
-    out->reserved_[0] = out->reserved_[1] = out->reserved_[2] = 0.0f;
+    out->found_inf = finite && fp16 * c < kInfOfFp16 && bf16 * c < kInfOfBf16 ? 0.0f : 1.0f;
+    out->coef = c;
+    out->reserved_[0] = fp16;
+    out->reserved_[1] = bf16;
+    out->reserved_[2] = 0.0f;
 }
 
 // Block 0 waits for the others, none of which waits for anything.
-template <bool kNT>
+template <bool kNT, bool kRange>
 __global__ __launch_bounds__(kThreads) void sumsq_kernel(const GradTile* __restrict__ tiles, int ntiles,
-                                                         uint32_t* sync, uint64_t* slots,
+                                                         uint32_t* sync, uint64_t* slots, uint64_t* ranges,
                                                          const float* __restrict__ scale, double max_norm,
                                                          gockpt_grad_result* __restrict__ out) {
     const uint32_t epoch = *sync;
     double acc = 0.0;
+    Range range = {0u, 0u};
     u32x4 next[kUnitsPerThread];
     int i = blockIdx.x;
     GradTile t = tiles[i];
@@ -271,26 +376,40 @@ __global__ __launch_bounds__(kThreads) void sumsq_kernel(const GradTile* __restr
             t = tiles[i];
             load_tile<kNT>(t, next);
         }
-        acc += tile_sum(now, raw);
+        const double sum = tile_sum(now, raw);
+        acc += sum;
+        if constexpr (kRange) tile_range(now, raw, sum, range);
     }
-    acc = block_sum(acc);
-    if (threadIdx.x == 0) publish(slots + blockIdx.x, epoch, acc);
+    bool has_range = kRange && (range.fp16 | range.bf16) != 0u;
+    acc = block_sum(acc, kRange ? &has_range : nullptr);
+    if (has_range) range = block_range(range);
+    if (threadIdx.x == 0) {
+        publish(slots + blockIdx.x, epoch, acc, has_range);
+        if constexpr (kRange) publish(ranges + blockIdx.x, epoch, range);
+    }
     if (blockIdx.x != 0) return;
     uint64_t word[kSumBlocks / kThreads];
     while (read_slots(slots, gridDim.x, epoch, word)) __builtin_amdgcn_s_sleep(2);
     acc = 0.0;
+    has_range = false;
 #pragma unroll
-    for (int k = 0; k < kSumBlocks / kThreads; ++k) acc += __builtin_bit_cast(double, word[k] & ~kSlotTag);
-    acc = block_sum(acc);
+    for (int k = 0; k < kSumBlocks / kThreads; ++k) {
+        acc += slot_value(word[k]);
+        has_range |= kRange && (word[k] & kSlotRange) != 0u;
+    }
+    acc = block_sum(acc, kRange ? &has_range : nullptr);
+    if (has_range) range = all_ranges<kSumBlocks / kThreads>(ranges, gridDim.x, epoch);
     if (threadIdx.x == 0) {
-        finish_result(acc, scale, max_norm, out);
+        finish_result(acc, range, scale, max_norm, out);
         *sync = epoch + 1u;
     }
 }
 
-// The result of an empty list, or again from its sumsq.
+// The result of an empty list, or again from its sumsq and range.
 __global__ void result_kernel(gockpt_grad_result* out, const float* scale, double max_norm, bool empty) {
-    finish_result(empty ? 0.0 : out->sumsq, scale, max_norm, out);
+    Range range = {0u, 0u};
+    if (!empty) range = {__float_as_uint(out->reserved_[0]), __float_as_uint(out->reserved_[1])};
+    finish_result(empty ? 0.0 : out->sumsq, range, scale, max_norm, out);
 }
 
 // One element, or two, four or eight, at any address.
@@ -416,9 +535,9 @@ __global__ __launch_bounds__(kThreads) void scale_kernel(const GradTile* __restr
 // after the tile has been read, what was read is unscaled, and if it is not,
 // the slot's value is taken.
 
-template <bool kClip>
+template <bool kClip, bool kRange>
 __global__ __launch_bounds__(kThreads) void whole_kernel(const GradTile* __restrict__ tiles, uint32_t* sync,
-                                                         uint64_t* slots, int spins,
+                                                         uint64_t* slots, uint64_t* ranges, int spins,
                                                          const float* __restrict__ scale, double max_norm,
                                                          gockpt_grad_result* __restrict__ out) {
     __shared__ double all[kWholeTiles];
@@ -428,8 +547,16 @@ __global__ __launch_bounds__(kThreads) void whole_kernel(const GradTile* __restr
     const GradTile t = tiles[blockIdx.x];
     u32x4 raw[kUnitsPerThread];
     load_tile<false>(t, raw);
-    const double mine = block_sum(tile_sum(t, raw));
-    if (threadIdx.x == 0) publish(slots + blockIdx.x, epoch, mine);
+    const double sum = tile_sum(t, raw);
+    Range range = {0u, 0u};
+    if constexpr (kRange) tile_range(t, raw, sum, range);
+    bool has_range = kRange && (range.fp16 | range.bf16) != 0u;
+    const double mine = block_sum(sum, kRange ? &has_range : nullptr);
+    if (has_range) range = block_range(range);
+    if (threadIdx.x == 0) {
+        publish(slots + blockIdx.x, epoch, mine, has_range);
+        if constexpr (kRange) publish(ranges + blockIdx.x, epoch, range);
+    }
     if (!kClip && blockIdx.x != 0) return;
 
     constexpr int kPer = kWholeTiles / kThreads;
@@ -439,20 +566,22 @@ __global__ __launch_bounds__(kThreads) void whole_kernel(const GradTile* __restr
         __builtin_amdgcn_s_sleep(2);
         wait = read_slots(slots, blocks, epoch, word);
     }
+    has_range = false;
 #pragma unroll
-    for (int k = 0; k < kPer; ++k)  // -1: missing
-        all[k * kThreads + threadIdx.x] =
-            (word[k] & kSlotTag) == slot_tag(epoch) ? __builtin_bit_cast(double, word[k] & ~kSlotTag) : -1.0;
+    for (int k = 0; k < kPer; ++k) {  // -1: missing
+        all[k * kThreads + threadIdx.x] = (word[k] & kSlotTag) == slot_tag(epoch) ? slot_value(word[k]) : -1.0;
+        has_range |= kRange && (word[k] & kSlotRange) != 0u;
+    }
     if (__syncthreads_or(wait)) {
         for (int b = 0; b < blocks; ++b) {
             if (all[b] != -1.0) continue;  // the same for all threads
             const GradTile other = tiles[b];
             u32x4 again[kUnitsPerThread];
             load_tile<false>(other, again);
-            double x = block_sum(tile_sum(other, again));
+            double x = cut(block_sum(tile_sum(other, again)));
             if (threadIdx.x == 0) {
                 const uint64_t w = read_slot(slots + b);
-                if ((w & kSlotTag) == slot_tag(epoch)) x = __builtin_bit_cast(double, w & ~kSlotTag);
+                if ((w & kSlotTag) == slot_tag(epoch)) x = slot_value(w);
                 all[b] = x;
             }
             __syncthreads();
@@ -461,10 +590,12 @@ __global__ __launch_bounds__(kThreads) void whole_kernel(const GradTile* __restr
     double acc = 0.0;
 #pragma unroll
     for (int k = 0; k < kPer; ++k) acc += all[k * kThreads + threadIdx.x];
-    acc = block_sum(acc);
+    acc = block_sum(acc, kRange ? &has_range : nullptr);
+    // the coefficient does not depend on it, so only the block that writes the result needs it
+    if (has_range && blockIdx.x == 0) range = all_ranges<kPer>(ranges, blocks, epoch);
     if (threadIdx.x == 0) {
         gockpt_grad_result r;
-        finish_result(acc, scale, max_norm, &r);
+        finish_result(acc, range, scale, max_norm, &r);
         coef = r.coef;
         if (blockIdx.x == 0) {
             *out = r;
@@ -480,9 +611,10 @@ __global__ __launch_bounds__(kThreads) void whole_kernel(const GradTile* __restr
 // ---- host: the table ---------------------------------------------------------
 
 constexpr int64_t kMaxElems = int64_t{1} << 46;
-// Workspace: sync word, the blocks' partials, table.
+// Workspace: sync word, the blocks' partials, their ranges, table.
 constexpr size_t kSlotsOff = 256;
-constexpr size_t kTableOff = kSlotsOff + kSumBlocks * sizeof(uint64_t);
+constexpr size_t kRangesOff = kSlotsOff + kSumBlocks * sizeof(uint64_t);
+constexpr size_t kTableOff = kRangesOff + kSumBlocks * sizeof(uint64_t);
 static_assert(kWholeTiles <= kSumBlocks, "slots");
 
 // A tensor as the tiles see it: rows that follow one another are one row.
@@ -562,6 +694,7 @@ struct gockpt_grads {
     uint8_t* ws;
     const GradTile* tiles;
     int ntiles, spins;
+    bool range;                    // a destination has a narrower range than its source
     int64_t src_bytes, dst_bytes;  // of all tensors
 };
 
@@ -590,6 +723,7 @@ int gockpt_grads_create(const gockpt_grad_tensor* tensors, int64_t count, void* 
         return ops_fail(GOCKPT_ENOMEM, "%s: workspace of %zu bytes", name, workspace_bytes);
     std::vector<uint8_t> head;  // the workspace's contents
     int64_t src_bytes = 0, dst_bytes = 0;
+    bool range = false;
     try {
         head.resize(kTableOff + ntiles * sizeof(GradTile));
         *reinterpret_cast<uint32_t*>(head.data()) = 1u;  // the first epoch: cleared slots are not of it
@@ -602,6 +736,7 @@ int gockpt_grads_create(const gockpt_grad_tensor* tensors, int64_t count, void* 
             const int dst_dtype = in_place ? t.dtype : t.dst_dtype;
             const int64_t sb = dtype_bytes(t.dtype), db = dtype_bytes(dst_dtype);
             const int64_t dst_cols = in_place ? x.stride : x.cols;
+            range |= (dst_dtype == kFP16 && t.dtype != kFP16) || (dst_dtype == kBF16 && t.dtype == kFP32);
             uint8_t* dst = static_cast<uint8_t*>(in_place ? const_cast<void*>(t.data) : t.dst);
             const uint8_t* src = static_cast<const uint8_t*>(t.data);
             each_tile(x, t.dtype, [&](int64_t r, int64_t rows, int64_t c, int64_t cols) {
@@ -631,6 +766,7 @@ int gockpt_grads_create(const gockpt_grad_tensor* tensors, int64_t count, void* 
     list->ntiles = static_cast<int>(ntiles);
     const char* again = getenv("GOCKPT_TEST_GRADS_AGAIN");
     list->spins = again != nullptr && again[0] == '1' ? 0 : kWholeSpins;
+    list->range = range;
     list->src_bytes = src_bytes;
     list->dst_bytes = dst_bytes;
     hipStream_t s = static_cast<hipStream_t>(stream);
@@ -675,15 +811,20 @@ static int run_list(const char* name, gockpt_grads* list, const float* scale, do
     const int n = list->ntiles;
     uint32_t* sync = reinterpret_cast<uint32_t*>(list->ws);
     uint64_t* slots = reinterpret_cast<uint64_t*>(list->ws + kSlotsOff);
+    uint64_t* ranges = reinterpret_cast<uint64_t*>(list->ws + kRangesOff);
     if (n == 0) {
         hipLaunchKernelGGL(result_kernel, dim3(1), dim3(1), 0, s, result, scale, max_norm, true);
     } else if (n <= kWholeTiles) {
-        hipLaunchKernelGGL(clip ? whole_kernel<true> : whole_kernel<false>, dim3(n), dim3(kThreads), 0, s,
-                           list->tiles, sync, slots, list->spins, scale, max_norm, result);
+        const auto kernel = clip ? list->range ? whole_kernel<true, true> : whole_kernel<true, false>
+                                 : list->range ? whole_kernel<false, true> : whole_kernel<false, false>;
+        hipLaunchKernelGGL(kernel, dim3(n), dim3(kThreads), 0, s, list->tiles, sync, slots, ranges, list->spins, scale,
+                           max_norm, result);
     } else {
         const bool nt = !clip || list->src_bytes > kCachedSumBytes;
-        hipLaunchKernelGGL(nt ? sumsq_kernel<true> : sumsq_kernel<false>, dim3(n < kSumBlocks ? n : kSumBlocks),
-                           dim3(kThreads), 0, s, list->tiles, n, sync, slots, scale, max_norm, result);
+        const auto kernel = nt ? list->range ? sumsq_kernel<true, true> : sumsq_kernel<true, false>
+                               : list->range ? sumsq_kernel<false, true> : sumsq_kernel<false, false>;
+        hipLaunchKernelGGL(kernel, dim3(n < kSumBlocks ? n : kSumBlocks), dim3(kThreads), 0, s, list->tiles, n, sync,
+                           slots, ranges, scale, max_norm, result);
         if (clip) launch_scale(list, result, s);
     }
     return ops_launched(name);

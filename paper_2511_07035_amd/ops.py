@@ -125,7 +125,12 @@ class GradResult:
     """The device-resident outcome of a norm: one-element tensors ``norm``
     (of the unscaled gradients), ``found_inf`` (1.0 or 0.0; what
     ``Session(found_inf=...)`` takes), ``coef`` (the clipping coefficient) and
-    ``sumsq`` (float64, of the elements as stored: what ranks add up)."""
+    ``sumsq`` (float64, of the elements as stored: what ranks add up);
+    ``largest``: the largest magnitudes of the elements that go to float16 from
+    a wider type, and to bfloat16 from float32, and are too large for it
+    unscaled (0: none; what ranks take the maximum of).  found_inf is 1 where an
+    element is inf or NaN, and where an element times coef is rounded to inf in
+    its destination."""
 
     def __init__(self, device="cuda"):
         self.buffer = torch.zeros(8, dtype=torch.float32, device=device)
@@ -133,11 +138,12 @@ class GradResult:
         self.norm = self.buffer[2:3]
         self.found_inf = self.buffer[3:4]
         self.coef = self.buffer[4:5]
+        self.largest = self.buffer[5:7]
         self.ptr = self.buffer.data_ptr()
 
     def update(self, max_norm: float = float("inf"), scale=None, stream=None) -> "GradResult":
-        """norm, found_inf and coef again from ``sumsq``, after ranks that hold
-        different parameters have added theirs up."""
+        """norm, found_inf and coef again from ``sumsq`` and ``largest``, after
+        ranks that hold different parameters have put theirs together."""
         _here(self.buffer, "result")
         _check(_lib().gockpt_grads_result(self.ptr, _scale_ptr(scale), max_norm,
                                           _stream(stream, self.buffer.get_device())), "gockpt_grads_result", None)
@@ -227,7 +233,8 @@ class GradList:
     def clip(self, max_norm: float, *, scale=None, result=None, stream=None) -> GradResult:
         """``norm``, then every element times min(1, max_norm / (norm + 1e-6))
         in place or into ``out``.  With an inf or NaN among the gradients they
-        are left, or copied, as they are, and ``found_inf`` tells."""
+        are left, or copied, as they are, and ``found_inf`` tells, as it does
+        where a scaled element is beyond the range of its ``out``."""
         r, s = self.result if result is None else result, self._on(stream)
         _check(_lib().gockpt_grads_clip(self.handle, _scale_ptr(scale), max_norm, r.ptr, s), "gockpt_grads_clip", None)
         return r

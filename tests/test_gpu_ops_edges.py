@@ -44,3 +44,104 @@ def test_a_gradient_of_another_shape_than_the_table_is_refused(rows):
     want = torch.zeros(10, 8, device="cuda")
     want[[1, 7, 9]] = 1.0
     assert torch.equal(into.float(), want)
+
+
+# The smallest fp32 products that round to infinity: half a step above the
+# largest finite value, and ties go to even, which here is infinity.
+LEAST_INF = {torch.float16: 65520.0, torch.bfloat16: 2.0 ** 128 - 2.0 ** 119}
+NARROW = [(torch.float32, torch.float16), (torch.bfloat16, torch.float16), (torch.float32, torch.bfloat16)]
+
+
+def with_element(n, dtype, at, value):
+    t = torch.zeros(n, dtype=dtype, device="cuda")
+    t[at] = value
+    return t
+
+
+@pytest.mark.parametrize("again", ["0", "1"])
+@pytest.mark.parametrize("src,dst", NARROW)
+@pytest.mark.parametrize("n", [1, 20_001, 6_000_001])
+def test_found_inf_where_the_destination_is_too_narrow(n, src, dst, again, monkeypatch):
+    """Finite gradients whose rounding gives an infinity: the flag is set, at
+    the very value from which on the rounding gives one."""
+    monkeypatch.setenv("GOCKPT_TEST_GRADS_AGAIN", again)
+    least = LEAST_INF[dst]
+    below = float(np.nextafter(np.float32(least), np.float32(0)))
+    if src == torch.bfloat16:  # the bf16 values around it
+        least, below = 65536.0, 65280.0
+    out = torch.empty(n, dtype=dst, device="cuda")
+    for at in sorted({0, n // 2, n - 1}):
+        for value, inf in ((below, 0.0), (-below, 0.0), (least, 1.0), (-least, 1.0)):
+            t = with_element(n, src, at, value)
+            gl = g.GradList([torch.zeros(3, device="cuda"), t], [None, out])
+            r = gl.clip(float("inf"))
+            assert float(r.found_inf) == inf and float(r.coef) == 1.0
+            assert bool(torch.isinf(out).any()) == bool(inf) and math.isfinite(float(r.norm))
+            # scaled into the range: no infinity, no flag
+            r = gl.clip(1.0)
+            assert float(r.found_inf) == 0.0 and bool(torch.isfinite(out).all())
+            # the same gradients in place, or into fp32, round to nothing new
+            assert float(g.GradList([t.clone()]).clip(float("inf")).found_inf) == 0.0
+            assert float(g.GradList([t], [torch.empty(n, device="cuda")]).clip(float("inf")).found_inf) == 0.0
+
+
+def test_the_flag_of_a_narrow_destination_among_others():
+    """Each destination's own range counts, whatever lies beside it, and a NaN
+    or infinity counts as before."""
+    def flag(*pairs):
+        outs = [None if d is None else torch.empty_like(t, dtype=d) for t, d in pairs]
+        return float(g.GradList([t for t, _ in pairs], outs).clip(float("inf")).found_inf)
+
+    big = with_element(5000, torch.float32, 77, 1e30)
+    small = with_element(300, torch.float32, 3, 65504.0)
+    assert flag((big, torch.bfloat16), (small, torch.float16)) == 0.0
+    assert flag((big, torch.float16), (small, torch.bfloat16)) == 1.0
+    assert flag((big, None), (small, torch.float16)) == 0.0
+    assert flag((big, torch.float32), (small, torch.float16)) == 0.0
+    for value in (float("inf"), float("nan")):
+        assert flag((big, None), (with_element(9, torch.float32, 2, value), torch.float16)) == 1.0
+        assert flag((with_element(9, torch.float16, 2, value), torch.bfloat16)) == 1.0
+
+
+def test_ranks_put_their_ranges_together():
+    """Ranks that hold different parameters add up sumsq and take the larger
+    of their ranges: the flag is then that of all of them."""
+    a, b = with_element(100, torch.float32, 1, 70000.0), torch.ones(100, device="cuda")
+    lists = [g.GradList([t], [torch.empty(100, dtype=torch.float16, device="cuda")]) for t in (a, b)]
+    ra, rb = (gl.norm(float("inf")) for gl in lists)
+    assert float(ra.found_inf) == 1.0 and float(rb.found_inf) == 0.0
+    sumsq, largest = ra.sumsq + rb.sumsq, torch.maximum(ra.largest, rb.largest)
+    for most, inf in ((float("inf"), 1.0), (70000.0, 1.0), (65000.0, 0.0)):
+        for r in (ra, rb):
+            r.sumsq.copy_(sumsq)
+            r.largest.copy_(largest)
+            r.update(most)
+            assert float(r.found_inf) == inf
+
+
+@pytest.mark.parametrize("n", [40_000, 6_000_000])
+def test_a_step_whose_gradients_overflow_in_the_clip_is_skipped(n):
+    """fp32 sums over micro-batches clipped into the fp16 gradient of a Session
+    that takes the clip's flag: the step is skipped, the scale backs off."""
+    result = g.GradResult()
+    sess = g.Session(n, ring_bytes=1 << 20, dynamic_scale=True, init_scale=1024.0, found_inf=result.found_inf,
+                     grad_norm=False, grad_dtype="fp16")
+    try:
+        with torch.cuda.stream(sess.compute):
+            sess.master.normal_(0.0, 0.02)
+            sess.weight.copy_(sess.master)
+            sums = torch.full((n,), 0.5, device="cuda")
+            gl = g.GradList([sums], [sess.grad], stream=sess.compute)
+            before = sess.master.clone()
+            sums[n - 5] = 70000.0
+            gl.clip(1e9, scale=sess, result=result)
+            sess.step(1e-3)
+            assert torch.equal(sess.master, before) and float(result.found_inf) == 1.0
+            sums[n - 5] = 0.5
+            gl.clip(1e9, scale=sess, result=result)
+            assert float(result.norm) == float(np.float32(math.sqrt(n) * 0.5 / 512.0))
+            sess.step(1e-3)
+            assert float(result.found_inf) == 0.0
+            assert not torch.equal(sess.master, before) and bool(torch.isfinite(sess.master).all())
+    finally:
+        sess.close()
