@@ -81,7 +81,8 @@ int gockpt_grads_destroy(gockpt_grads* list);
  * coef (INFINITY: coef is 1).  Squares are summed in fp32 over at most 32
  * elements and in fp64 beyond; a group whose fp32 sum leaves [2^-100, 2^126)
  * is summed again in fp64, so no finite gradients overflow or vanish.  The
- * calls of one list use its workspace: one at a time, in stream order.
+ * calls of one list use its workspace: one at a time, in stream order (calls
+ * that overlap all the same end, with results of no meaning).
  * Errors: EINVAL, EHIP. */
 int gockpt_grads_norm(gockpt_grads* list, const float* scale, double max_norm,
                       gockpt_grad_result* result, void* stream);

@@ -47,10 +47,12 @@ constexpr int kSumBlocks = 1024;
 // and 11.4, 2^22, the limit, 11.3 and 11.4.  Above it, blocks of two or four
 // tiles that keep them in registers gained nothing (2^23 16.3 and 16.2).
 constexpr int kWholeTiles = 512;
-// Polls (about 0.5 us each) before a block computes the partials it misses;
-// none with GOCKPT_TEST_GRADS_AGAIN=1 in the environment when the list is made,
-// with which tests reach that path.
+// Polls (about 0.5 us each) before a block of whole_kernel computes the partials
+// it misses, and before block 0 does, which in a large list is a lot of work for
+// one block; none with GOCKPT_TEST_GRADS_AGAIN=1 in the environment when the list
+// is made, with which tests reach that path.
 constexpr int kWholeSpins = 64;
+constexpr int kSpins0 = 1 << 20;
 
 // Clipping up to this many source bytes: the sums leave what they read in the
 // last-level cache, and scale_kernel, last tiles first, finds part of it there
@@ -183,20 +185,20 @@ __device__ __forceinline__ double square_sum(const u32x4 (&raw)[kUnitsPerThread]
     return d;
 }
 
-// The sum over the block, and whether `any` holds in one of its threads.
-__device__ __forceinline__ double block_sum(double x, bool* any = nullptr) {
+// The sum over the block, and bits 0 and 1 of `flags` or'ed over it.
+__device__ __forceinline__ double block_sum(double x, uint32_t& flags) {
     __shared__ double part[kThreads / 64];
-    __shared__ uint64_t lanes[kThreads / 64];
+    __shared__ uint32_t bits[kThreads / 64];
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
-    const uint64_t with = any != nullptr ? __ballot(*any) : 0u;
+    const uint32_t f = (__ballot(flags & 1u) != 0u ? 1u : 0u) | (__ballot(flags & 2u) != 0u ? 2u : 0u);
     __syncthreads();  // an earlier sum has been read
     if ((threadIdx.x & 63) == 0) {
         part[threadIdx.x >> 6] = x;
-        if (any != nullptr) lanes[threadIdx.x >> 6] = with;
+        bits[threadIdx.x >> 6] = f;
     }
     __syncthreads();
-    if (any != nullptr) *any = (lanes[0] | lanes[1] | lanes[2] | lanes[3]) != 0u;
+    flags = bits[0] | bits[1] | bits[2] | bits[3];
     return (part[0] + part[1]) + (part[2] + part[3]);
 }
 
@@ -271,22 +273,35 @@ __device__ __forceinline__ double tile_sum(const GradTile& t, u32x4 (&raw)[kUnit
 
 // ---- exchange of the blocks' partials ------------------------------------------
 //
-// A partial is one 64-bit word: a double, and in the place of its sign, which
-// a sum of squares has no use for, the call's epoch modulo two.  Every call on
-// a list writes every slot, so a slot with the other tag is the last call's:
-// value and flag are one word, and no fence is needed, which on this chip would
-// write back an XCD's L2.  In a list with destinations narrower than their
-// source (kRange) a block writes its range too, as two magnitudes of 31 bits and
-// a tag; the lowest bit of its partial (all partials are cut by it) says whether
-// there is one to be read, since a second read of words costs 1 us.  Block 0 adds the partials in a fixed order and moves
-// the epoch on once it has seen every one of them, that is after every block
-// has read it.  (As a launch of its own that cost 1 us more: 2^23 bf16 elements
-// 6.5 and 7.5, 2^25 14.1 and 15.2.)
+// A partial is one 64-bit word: a double without its three lowest bits, in whose
+// place are the call's epoch modulo four, the tag, and kSlotRange.  Every call on
+// a list writes every slot, so a slot with the running call's tag is of this
+// call: value and flag are one word, and no fence is needed, which on this chip
+// would write back an XCD's L2.  In a list with destinations narrower than their
+// source (kRange) a block writes its range too, as two magnitudes of 31 bits
+// above the tag; kSlotRange says whether there is one to be read, since a second
+// read of words costs 1 us.  Block 0 adds the partials in a fixed order and
+// writes the result.  (As a launch of its own that cost 1 us more: 2^23 bf16
+// elements 6.5 and 7.5, 2^25 14.1 and 15.2.)
+//
+// A block arrives when it has read the epoch, and the epoch is the number of
+// arrivals, kGroupBlocks a call, divided by that: the next one is not reached
+// before all blocks have read this one.  The blocks count in groups, each with a
+// word and so an epoch of its own, the same in all between calls (arrivals at one
+// word took 6 us for 1024 blocks).  No wait is without end: a block that has
+// polled `spins` times computes the partials that it misses.  Calls on one list
+// whose order the caller has not seen to therefore still end, with whatever
+// results, and leave the list in order: their arrivals add up, and the tags that
+// they leave behind are not that of the next call (of up to three such calls).
 
-constexpr uint64_t kSlotTag = uint64_t{1} << 63;
-constexpr uint64_t kSlotRange = 1;
+constexpr int kGroups = 64;
+constexpr int kGroupBlocks = kSumBlocks / kGroups;  // at most
+constexpr int kGroupWords = 32;                     // from a group's word to the next
 
-__device__ __forceinline__ uint64_t slot_tag(uint32_t epoch) { return epoch & 1u ? kSlotTag : 0u; }
+constexpr uint64_t kSlotTag = 3;
+constexpr uint64_t kSlotRange = 4;
+
+__device__ __forceinline__ uint64_t slot_tag(uint32_t epoch) { return epoch & 3u; }
 
 __device__ __forceinline__ uint64_t read_slot(const uint64_t* p) {
     return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -296,17 +311,21 @@ __device__ __forceinline__ double slot_value(uint64_t word) {
     return __builtin_bit_cast(double, word & ~(kSlotTag | kSlotRange));
 }
 
-// A block's own partial as the others read it.
-__device__ __forceinline__ double cut(double x) { return slot_value(__builtin_bit_cast(uint64_t, x)); }
+__device__ __forceinline__ uint64_t sum_word(double x, bool has_range, uint32_t epoch) {
+    return (__builtin_bit_cast(uint64_t, x) & ~(kSlotTag | kSlotRange)) | (has_range ? kSlotRange : 0u) |
+           slot_tag(epoch);
+}
+
+__device__ __forceinline__ uint64_t range_word(Range x, uint32_t epoch) {
+    return uint64_t{x.fp16} << 33 | uint64_t{x.bf16} << 2 | slot_tag(epoch);
+}
 
 __device__ __forceinline__ void publish(uint64_t* slot, uint32_t epoch, double x, bool has_range) {
-    __hip_atomic_store(slot, __builtin_bit_cast(uint64_t, cut(x)) | (has_range ? kSlotRange : 0u) | slot_tag(epoch),
-                       __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(slot, sum_word(x, has_range, epoch), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
 __device__ __forceinline__ void publish(uint64_t* slot, uint32_t epoch, Range x) {
-    __hip_atomic_store(slot, uint64_t{x.fp16} << 31 | x.bf16 | slot_tag(epoch), __ATOMIC_RELAXED,
-                       __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(slot, range_word(x, epoch), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
 // This thread's slots, i, i + kThreads and so on below `blocks`; true while one
@@ -323,18 +342,129 @@ __device__ __forceinline__ bool read_slots(const uint64_t* slots, int blocks, ui
     return missing;
 }
 
-// The range over all blocks, which the calling block waits for.
+// This thread's words of all blocks, after at most `spins` polls; true while one
+// is not of this epoch.
 template <int kPer>
-__device__ __forceinline__ Range all_ranges(const uint64_t* slots, int blocks, uint32_t epoch) {
+__device__ __forceinline__ bool poll_slots(const uint64_t* slots, int blocks, uint32_t epoch, int spins,
+                                           uint64_t (&word)[kPer]) {
+    bool wait = read_slots(slots, blocks, epoch, word);
+    for (int i = 0; wait && i < spins; ++i) {
+        __builtin_amdgcn_s_sleep(2);
+        wait = read_slots(slots, blocks, epoch, word);
+    }
+    return wait;
+}
+
+// Those words that are not of this epoch are computed: again(b) is block b's, by
+// the whole block.
+template <int kPer, class Again>
+__device__ __forceinline__ void fill_words(const uint64_t* slots, int blocks, uint32_t epoch, uint64_t (&word)[kPer],
+                                           Again&& again) {
+    __shared__ uint64_t all[kPer * kThreads];
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) all[k * kThreads + threadIdx.x] = word[k];
+    __syncthreads();
+    for (int b = 0; b < blocks; ++b) {
+        if ((all[b] & kSlotTag) == slot_tag(epoch)) continue;  // the same for all threads
+        const uint64_t w = again(b);
+        if (threadIdx.x == 0) {
+            const uint64_t now = read_slot(slots + b);
+            all[b] = (now & kSlotTag) == slot_tag(epoch) ? now : w;
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) word[k] = all[k * kThreads + threadIdx.x];
+}
+
+// Block b's share of the tiles, every `step`-th from b on: the sum of their
+// squares and their range, in the order in which block b takes them.  Tiles that
+// may be scaled in place meanwhile go to their own type, so have no range.
+template <bool kRange>
+__device__ __forceinline__ double share_again(const GradTile* __restrict__ tiles, int ntiles, int b, int step,
+                                              Range& range, bool& has_range) {
+    double acc = 0.0;
+    range = {0u, 0u};
+    for (int i = b; i < ntiles; i += step) {
+        const GradTile t = tiles[i];
+        u32x4 raw[kUnitsPerThread];
+        load_tile<false>(t, raw);
+        const double sum = tile_sum(t, raw);
+        acc += sum;
+        if constexpr (kRange) tile_range(t, raw, sum, range);
+    }
+    uint32_t flags = kRange && (range.fp16 | range.bf16) != 0u;
+    acc = block_sum(acc, flags);
+    has_range = flags != 0u;
+    if (has_range) range = block_range(range);
+    return acc;
+}
+
+// The sum over all blocks' partials, in a fixed order, and whether one has a
+// range.  By a whole block.
+template <int kPer, bool kRange>
+__device__ __forceinline__ double all_sums(const GradTile* __restrict__ tiles, int ntiles, const uint64_t* slots,
+                                           uint32_t epoch, int spins, bool& has_range) {
     uint64_t word[kPer];
-    while (read_slots(slots, blocks, epoch, word)) __builtin_amdgcn_s_sleep(2);
+    const int blocks = gridDim.x;
+    // bit 0: there is a range, bit 1: a word is missing
+    uint32_t flags = poll_slots(slots, blocks, epoch, spins, word) ? 2u : 0u;
+    auto sum = [&]() {
+        double acc = 0.0;
+#pragma unroll
+        for (int k = 0; k < kPer; ++k) {
+            acc += slot_value(word[k]);
+            if (kRange && (word[k] & kSlotRange) != 0u) flags |= 1u;
+        }
+        return block_sum(acc, flags);
+    };
+    double acc = sum();
+    if (flags & 2u) {
+        fill_words(slots, blocks, epoch, word, [&](int b) {
+            Range range;
+            bool has;
+            const double x = share_again<kRange>(tiles, ntiles, b, blocks, range, has);
+            return sum_word(x, has, epoch);
+        });
+        flags = 0u;
+        acc = sum();
+    }
+    has_range = flags != 0u;
+    return acc;
+}
+
+// The range over all blocks.
+template <int kPer>
+__device__ __forceinline__ Range all_ranges(const GradTile* __restrict__ tiles, int ntiles, const uint64_t* ranges,
+                                            uint32_t epoch, int spins) {
+    uint64_t word[kPer];
+    const int blocks = gridDim.x;
+    if (__syncthreads_or(poll_slots(ranges, blocks, epoch, spins, word)))
+        fill_words(ranges, blocks, epoch, word, [&](int b) {
+            Range range;
+            bool has;
+            share_again<true>(tiles, ntiles, b, blocks, range, has);
+            return range_word(range, epoch);
+        });
     Range x = {0u, 0u};
 #pragma unroll
     for (int k = 0; k < kPer; ++k) {
-        x.fp16 = max_bits(x.fp16, static_cast<uint32_t>(word[k] >> 31) & 0x7FFFFFFFu);
-        x.bf16 = max_bits(x.bf16, static_cast<uint32_t>(word[k]) & 0x7FFFFFFFu);
+        x.fp16 = max_bits(x.fp16, static_cast<uint32_t>(word[k] >> 33));
+        x.bf16 = max_bits(x.bf16, static_cast<uint32_t>(word[k] >> 2) & 0x7FFFFFFFu);
     }
     return block_range(x);
+}
+
+__device__ __forceinline__ uint32_t* arrivals_of(uint32_t* sync) {
+    return sync + blockIdx.x % kGroups * kGroupWords;
+}
+
+// This block has read the epoch.  By the thread that has read it: the others
+// have it through LDS.  A group's first block arrives for those it lacks.
+__device__ __forceinline__ void arrive(uint32_t* sync) {
+    const uint32_t others = (gridDim.x - 1u - blockIdx.x) / kGroups;
+    __hip_atomic_fetch_add(arrivals_of(sync), blockIdx.x < kGroups ? kGroupBlocks - others : 1u, __ATOMIC_RELAXED,
+                           __HIP_MEMORY_SCOPE_AGENT);
 }
 
 __device__ __forceinline__ void finish_result(double sumsq, Range range, const float* scale, double max_norm,
@@ -357,9 +487,11 @@ __device__ __forceinline__ void finish_result(double sumsq, Range range, const f
 template <bool kNT, bool kRange>
 __global__ __launch_bounds__(kThreads) void sumsq_kernel(const GradTile* __restrict__ tiles, int ntiles,
                                                          uint32_t* sync, uint64_t* slots, uint64_t* ranges,
+                                                         int spins,
                                                          const float* __restrict__ scale, double max_norm,
                                                          gockpt_grad_result* __restrict__ out) {
-    const uint32_t epoch = *sync;
+    __shared__ uint32_t call;
+    const uint32_t arrivals = *arrivals_of(sync);  // thread 0's is the block's
     double acc = 0.0;
     Range range = {0u, 0u};
     u32x4 next[kUnitsPerThread];
@@ -380,29 +512,22 @@ __global__ __launch_bounds__(kThreads) void sumsq_kernel(const GradTile* __restr
         acc += sum;
         if constexpr (kRange) tile_range(now, raw, sum, range);
     }
-    bool has_range = kRange && (range.fp16 | range.bf16) != 0u;
-    acc = block_sum(acc, kRange ? &has_range : nullptr);
+    uint32_t flags = kRange && (range.fp16 | range.bf16) != 0u;
+    if (threadIdx.x == 0) call = arrivals / kGroupBlocks;
+    acc = block_sum(acc, flags);
+    bool has_range = flags != 0u;
+    const uint32_t epoch = call;
     if (has_range) range = block_range(range);
     if (threadIdx.x == 0) {
         publish(slots + blockIdx.x, epoch, acc, has_range);
         if constexpr (kRange) publish(ranges + blockIdx.x, epoch, range);
+        arrive(sync);
     }
     if (blockIdx.x != 0) return;
-    uint64_t word[kSumBlocks / kThreads];
-    while (read_slots(slots, gridDim.x, epoch, word)) __builtin_amdgcn_s_sleep(2);
-    acc = 0.0;
-    has_range = false;
-#pragma unroll
-    for (int k = 0; k < kSumBlocks / kThreads; ++k) {
-        acc += slot_value(word[k]);
-        has_range |= kRange && (word[k] & kSlotRange) != 0u;
-    }
-    acc = block_sum(acc, kRange ? &has_range : nullptr);
-    if (has_range) range = all_ranges<kSumBlocks / kThreads>(ranges, gridDim.x, epoch);
-    if (threadIdx.x == 0) {
-        finish_result(acc, range, scale, max_norm, out);
-        *sync = epoch + 1u;
-    }
+    constexpr int kPer = kSumBlocks / kThreads;
+    acc = all_sums<kPer, kRange>(tiles, ntiles, slots, epoch, spins, has_range);
+    if (has_range) range = all_ranges<kPer>(tiles, ntiles, ranges, epoch, spins);
+    if (threadIdx.x == 0) finish_result(acc, range, scale, max_norm, out);
 }
 
 // The result of an empty list, or again from its sumsq and range.
@@ -527,80 +652,49 @@ __global__ __launch_bounds__(kThreads) void scale_kernel(const GradTile* __restr
 // scales the tile, which it still has in registers.  For a norm only block 0
 // waits.
 //
-// No block but block 0 depends on another one running: after `spins`
-// polls it computes the missing partials itself, and block 0 thus waits only
-// for blocks that all finish on their own.  A missing partial's tile may be
-// scaled in place by its owner while it is read here, but the owner scales
-// only after it has seen its own partial published: if the slot is still empty
-// after the tile has been read, what was read is unscaled, and if it is not,
-// the slot's value is taken.
+// A block that misses a partial after its polls computes it.  That tile may be
+// scaled in place by its owner while it is read here, but the owner scales only
+// after it has seen its own partial published: if the slot is still empty after
+// the tile has been read, what was read is unscaled, and if it is not, the
+// slot's value is taken.
 
 template <bool kClip, bool kRange>
 __global__ __launch_bounds__(kThreads) void whole_kernel(const GradTile* __restrict__ tiles, uint32_t* sync,
-                                                         uint64_t* slots, uint64_t* ranges, int spins,
+                                                         uint64_t* slots, uint64_t* ranges, int spins, int spins0,
                                                          const float* __restrict__ scale, double max_norm,
                                                          gockpt_grad_result* __restrict__ out) {
-    __shared__ double all[kWholeTiles];
+    __shared__ uint32_t call;
     __shared__ float coef;
-    const int blocks = gridDim.x;
-    const uint32_t epoch = *sync;
+    const uint32_t arrivals = *arrivals_of(sync);  // thread 0's is the block's
     const GradTile t = tiles[blockIdx.x];
     u32x4 raw[kUnitsPerThread];
     load_tile<false>(t, raw);
     const double sum = tile_sum(t, raw);
     Range range = {0u, 0u};
     if constexpr (kRange) tile_range(t, raw, sum, range);
-    bool has_range = kRange && (range.fp16 | range.bf16) != 0u;
-    const double mine = block_sum(sum, kRange ? &has_range : nullptr);
+    uint32_t flags = kRange && (range.fp16 | range.bf16) != 0u;
+    if (threadIdx.x == 0) call = arrivals / kGroupBlocks;
+    const double mine = block_sum(sum, flags);
+    bool has_range = flags != 0u;
+    const uint32_t epoch = call;
     if (has_range) range = block_range(range);
     if (threadIdx.x == 0) {
         publish(slots + blockIdx.x, epoch, mine, has_range);
         if constexpr (kRange) publish(ranges + blockIdx.x, epoch, range);
+        arrive(sync);
     }
     if (!kClip && blockIdx.x != 0) return;
 
     constexpr int kPer = kWholeTiles / kThreads;
-    uint64_t word[kPer];
-    bool wait = read_slots(slots, blocks, epoch, word);
-    for (int i = 0; wait && (blockIdx.x == 0 || i < spins); ++i) {
-        __builtin_amdgcn_s_sleep(2);
-        wait = read_slots(slots, blocks, epoch, word);
-    }
-    has_range = false;
-#pragma unroll
-    for (int k = 0; k < kPer; ++k) {  // -1: missing
-        all[k * kThreads + threadIdx.x] = (word[k] & kSlotTag) == slot_tag(epoch) ? slot_value(word[k]) : -1.0;
-        has_range |= kRange && (word[k] & kSlotRange) != 0u;
-    }
-    if (__syncthreads_or(wait)) {
-        for (int b = 0; b < blocks; ++b) {
-            if (all[b] != -1.0) continue;  // the same for all threads
-            const GradTile other = tiles[b];
-            u32x4 again[kUnitsPerThread];
-            load_tile<false>(other, again);
-            double x = cut(block_sum(tile_sum(other, again)));
-            if (threadIdx.x == 0) {
-                const uint64_t w = read_slot(slots + b);
-                if ((w & kSlotTag) == slot_tag(epoch)) x = slot_value(w);
-                all[b] = x;
-            }
-            __syncthreads();
-        }
-    }
-    double acc = 0.0;
-#pragma unroll
-    for (int k = 0; k < kPer; ++k) acc += all[k * kThreads + threadIdx.x];
-    acc = block_sum(acc, kRange ? &has_range : nullptr);
+    const int polls = blockIdx.x == 0 ? spins0 : spins;
+    const double acc = all_sums<kPer, kRange>(tiles, gridDim.x, slots, epoch, polls, has_range);
     // the coefficient does not depend on it, so only the block that writes the result needs it
-    if (has_range && blockIdx.x == 0) range = all_ranges<kPer>(ranges, blocks, epoch);
+    if (has_range && blockIdx.x == 0) range = all_ranges<kPer>(tiles, gridDim.x, ranges, epoch, polls);
     if (threadIdx.x == 0) {
         gockpt_grad_result r;
         finish_result(acc, range, scale, max_norm, &r);
         coef = r.coef;
-        if (blockIdx.x == 0) {
-            *out = r;
-            *sync = epoch + 1u;
-        }
+        if (blockIdx.x == 0) *out = r;
     }
     if constexpr (kClip) {
         __syncthreads();
@@ -611,8 +705,8 @@ __global__ __launch_bounds__(kThreads) void whole_kernel(const GradTile* __restr
 // ---- host: the table ---------------------------------------------------------
 
 constexpr int64_t kMaxElems = int64_t{1} << 46;
-// Workspace: sync word, the blocks' partials, their ranges, table.
-constexpr size_t kSlotsOff = 256;
+// Workspace: arrivals, the blocks' partials, their ranges, table.
+constexpr size_t kSlotsOff = kGroups * kGroupWords * sizeof(uint32_t);
 constexpr size_t kRangesOff = kSlotsOff + kSumBlocks * sizeof(uint64_t);
 constexpr size_t kTableOff = kRangesOff + kSumBlocks * sizeof(uint64_t);
 static_assert(kWholeTiles <= kSumBlocks, "slots");
@@ -693,7 +787,7 @@ using namespace gockpt;
 struct gockpt_grads {
     uint8_t* ws;
     const GradTile* tiles;
-    int ntiles, spins;
+    int ntiles, spins, spins0;
     bool range;                    // a destination has a narrower range than its source
     int64_t src_bytes, dst_bytes;  // of all tensors
 };
@@ -726,7 +820,8 @@ int gockpt_grads_create(const gockpt_grad_tensor* tensors, int64_t count, void* 
     bool range = false;
     try {
         head.resize(kTableOff + ntiles * sizeof(GradTile));
-        *reinterpret_cast<uint32_t*>(head.data()) = 1u;  // the first epoch: cleared slots are not of it
+        for (int i = 0; i < kGroups; ++i)  // the first epoch, 1: cleared slots are not of it
+            reinterpret_cast<uint32_t*>(head.data())[i * kGroupWords] = kGroupBlocks;
         GradTile* next = reinterpret_cast<GradTile*>(head.data() + kTableOff);
         for (int64_t i = 0; i < count; ++i) {
             const gockpt_grad_tensor& t = tensors[i];
@@ -766,6 +861,7 @@ int gockpt_grads_create(const gockpt_grad_tensor* tensors, int64_t count, void* 
     list->ntiles = static_cast<int>(ntiles);
     const char* again = getenv("GOCKPT_TEST_GRADS_AGAIN");
     list->spins = again != nullptr && again[0] == '1' ? 0 : kWholeSpins;
+    list->spins0 = list->spins == 0 ? 0 : kSpins0;
     list->range = range;
     list->src_bytes = src_bytes;
     list->dst_bytes = dst_bytes;
@@ -817,14 +913,14 @@ static int run_list(const char* name, gockpt_grads* list, const float* scale, do
     } else if (n <= kWholeTiles) {
         const auto kernel = clip ? list->range ? whole_kernel<true, true> : whole_kernel<true, false>
                                  : list->range ? whole_kernel<false, true> : whole_kernel<false, false>;
-        hipLaunchKernelGGL(kernel, dim3(n), dim3(kThreads), 0, s, list->tiles, sync, slots, ranges, list->spins, scale,
-                           max_norm, result);
+        hipLaunchKernelGGL(kernel, dim3(n), dim3(kThreads), 0, s, list->tiles, sync, slots, ranges, list->spins,
+                           list->spins0, scale, max_norm, result);
     } else {
         const bool nt = !clip || list->src_bytes > kCachedSumBytes;
         const auto kernel = nt ? list->range ? sumsq_kernel<true, true> : sumsq_kernel<true, false>
                                : list->range ? sumsq_kernel<false, true> : sumsq_kernel<false, false>;
         hipLaunchKernelGGL(kernel, dim3(n < kSumBlocks ? n : kSumBlocks), dim3(kThreads), 0, s, list->tiles, n, sync,
-                           slots, ranges, scale, max_norm, result);
+                           slots, ranges, list->spins0, scale, max_norm, result);
         if (clip) launch_scale(list, result, s);
     }
     return ops_launched(name);

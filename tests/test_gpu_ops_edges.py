@@ -145,3 +145,22 @@ def test_a_step_whose_gradients_overflow_in_the_clip_is_skipped(n):
             assert not torch.equal(sess.master, before) and bool(torch.isfinite(sess.master).all())
     finally:
         sess.close()
+
+
+@pytest.mark.parametrize("n", [700, 3_000_000, 20_000_001])
+def test_no_call_depends_on_another_block(n, monkeypatch):
+    """With no polls the block that writes the result computes every partial
+    that it does not find: the same bits as with polls, call after call on one
+    list whose gradients change."""
+    t = torch.empty(n, dtype=torch.bfloat16, device="cuda")
+    polled = g.GradList([t])
+    monkeypatch.setenv("GOCKPT_TEST_GRADS_AGAIN", "1")
+    alone = g.GradList([t])
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(n)
+    for _ in range(9):
+        t.normal_(0.0, 1e-3, generator=gen)
+        want = float(t.double().square().sum())
+        a, b = polled.norm(1e-3).buffer.clone(), alone.norm(1e-3).buffer
+        assert torch.equal(a.view(torch.int32), b.view(torch.int32))
+        assert abs(float(alone.result.sumsq) - want) <= 34 * 2.0 ** -24 * want
