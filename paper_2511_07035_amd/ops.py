@@ -97,6 +97,11 @@ def _stream(stream, device: int) -> int:
     return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
 
 
+def _capturing(stream) -> bool:
+    with torch.cuda.stream(stream):
+        return torch.cuda.is_current_stream_capturing()
+
+
 def _rows(shape, stride):
     """(rows, cols, row stride) of elements in row-major order, or None where
     they are not rows of adjacent elements at one distance."""
@@ -172,7 +177,9 @@ class GradList:
     None, or None in a place: in place.  Writing in place also takes a tensor
     whose dimensions are permuted.  The handle keeps the tensors alive and
     holds their addresses: make a new one when they move.  Its calls use its
-    workspace one at a time: on several streams they have to be ordered."""
+    workspace one at a time: a call on another stream than the last one's waits
+    there for that one.  Calls recorded in a graph run whenever it is replayed:
+    the program orders the replays, and keeps the list as long as the graph."""
 
     def __init__(self, tensors, out=None, stream=None):
         self.handle = None
@@ -206,7 +213,9 @@ class GradList:
             self.workspace = torch.empty(size.value, dtype=torch.uint8, device=self.device)
             self.result = GradResult(self.device)
         handle = _P()
-        self.home, self.strayed = _stream(stream, self.device), False
+        self.last = torch.cuda.current_stream(self.device) if stream is None else stream
+        self.home = self.at = self.last.cuda_stream
+        self.strayed = False
         _check(_lib().gockpt_grads_create(table, n, self.workspace.data_ptr(), size.value, self.home,
                                           ctypes.byref(handle)), "gockpt_grads_create", None)
         self.handle = handle.value
@@ -218,9 +227,18 @@ class GradList:
         if torch.cuda.current_device() != self.device:
             raise ValueError(f"the list is on GPU {self.device}, which is not the current one")
         s = _stream(stream, self.device)
-        if s != self.home:  # not the stream that the workspace was allocated for
-            self.strayed = True
+        if s != self.at:
+            self._move(torch.cuda.current_stream(self.device) if stream is None else stream)
         return s
+
+    def _move(self, stream) -> None:
+        """To another stream than the last call's, which waits for that call."""
+        if stream.cuda_stream != self.home:  # not the one that the workspace was allocated for
+            self.strayed = True
+        if _capturing(stream) or _capturing(self.last):
+            return
+        stream.wait_stream(self.last)
+        self.last, self.at = stream, stream.cuda_stream
 
     def norm(self, max_norm: float = float("inf"), *, scale=None, result=None, stream=None) -> GradResult:
         """The norm over all tensors, divided by ``scale`` (the loss scale the

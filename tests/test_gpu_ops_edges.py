@@ -164,3 +164,22 @@ def test_no_call_depends_on_another_block(n, monkeypatch):
         a, b = polled.norm(1e-3).buffer.clone(), alone.norm(1e-3).buffer
         assert torch.equal(a.view(torch.int32), b.view(torch.int32))
         assert abs(float(alone.result.sumsq) - want) <= 34 * 2.0 ** -24 * want
+
+
+def test_calls_of_one_list_on_several_streams_run_in_order():
+    t = torch.zeros(3_000_000, device="cuda")
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    gl = g.GradList([t], stream=streams[0])
+    results = [g.GradResult() for _ in range(4)]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(streams[0]):
+        torch.cuda._sleep(20_000_000)  # the gradients are written late on the first stream
+        t.fill_(2.0)
+    for r, s in zip(results, [*streams, streams[0]]):
+        gl.norm(result=r, stream=s)
+    gl.clip(1.0)  # on the current one
+    torch.cuda.synchronize()
+    assert [float(r.sumsq) for r in results] == [12e6] * 4
+    assert float(gl.result.sumsq) == 12e6 and float(t[-1]) == float(np.float32(2.0) * np.float32(float(gl.result.coef)))
+    gl.close()

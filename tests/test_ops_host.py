@@ -215,3 +215,31 @@ def test_tensors_off_the_gpu_are_refused():
         g.embedding(torch.zeros(4, 8), torch.zeros(2, dtype=torch.int64), out=torch.zeros(2, 8))
     with pytest.raises(ValueError):
         g.embedding_grad(torch.zeros(2, 8), torch.zeros(2, dtype=torch.int64), torch.zeros(4, 8))
+
+
+class _Stream:
+    """Of a fake device: remembers what it has waited for."""
+
+    def __init__(self, number):
+        self.cuda_stream, self.waited = number, []
+
+    def wait_stream(self, other):
+        self.waited.append(other)
+
+
+def test_a_list_orders_its_calls_across_streams(monkeypatch):
+    import torch
+    a, b, c = _Stream(1), _Stream(2), _Stream(3)
+    captured = []
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "synchronize", lambda device: None)
+    monkeypatch.setattr(ops, "_capturing", lambda s: s in captured, raising=False)
+    gl = ops.GradList.__new__(ops.GradList)
+    gl.handle, gl.device, gl.last, gl.home, gl.at, gl.strayed = 7, 0, a, 1, 1, False
+    assert [gl._on(s) for s in (a, b, b, c, a)] == [1, 2, 2, 3, 1]
+    assert a.waited == [c] and b.waited == [a] and c.waited == [b] and gl.strayed
+    # a call that a graph records runs later: nothing to wait for, and nothing ran
+    captured.append(b)
+    assert gl._on(b) == 2 and b.waited == [a]
+    assert gl._on(c) == 3 and c.waited == [b, a]
+    gl.handle = None
