@@ -16,6 +16,7 @@ import functools
 import struct
 
 import torch
+from torch.autograd import forward_ad
 
 from . import GOCKPT_EINVAL, GockptError, _check, lib
 
@@ -360,10 +361,11 @@ def embedding(weight, ids, *, scale: float = 1.0, out=None, out_dtype=None, firs
     backward writes every row of grad_weight: with several lookups of one table
     in a step, clear it first and let all of them accumulate.  Tokens with
     padding_id add no gradient.  out and stream are for calls that need no
-    gradient."""
+    gradient.  The derivative along a tangent of the weight (forward mode) is the
+    tangent's lookup."""
     if accumulate and grad_weight is None:
         raise ValueError("accumulate: into a grad_weight")
-    if weight.requires_grad and torch.is_grad_enabled():
+    if (weight.requires_grad and torch.is_grad_enabled()) or _has_tangent(weight):
         if out is not None or stream is not None:
             raise ValueError("out and stream: for calls without a gradient")
         if grad_weight is not None:
@@ -406,14 +408,26 @@ def embedding_grad(grad_out, ids, grad_weight, *, scale: float = 1.0, accumulate
     return grad_weight
 
 
+def _has_tangent(t) -> bool:
+    # the level is -1 outside of a dual_level: no more than a comparison there
+    return forward_ad._current_level >= 0 and forward_ad.unpack_dual(t).tangent is not None
+
+
 class _Embedding(torch.autograd.Function):
     @staticmethod
     def forward(ctx, weight, ids, scale, out_dtype, first_id, padding_id, grad_weight, accumulate):
         ctx.save_for_backward(ids)
+        ctx.save_for_forward(ids)
+        ctx.out_dtype = out_dtype
         ctx.args = dict(scale=scale, first_id=first_id, padding_id=padding_id)
         ctx.into, ctx.accumulate = grad_weight, accumulate
         ctx.like = (weight.shape, weight.dtype, weight.device)
         return _lookup(weight.detach(), ids, scale, None, out_dtype, first_id, None)
+
+    @staticmethod
+    def jvp(ctx, tangent, *_):
+        (ids,) = ctx.saved_tensors
+        return _lookup(tangent.contiguous(), ids, ctx.args["scale"], None, ctx.out_dtype, ctx.args["first_id"], None)
 
     @staticmethod
     @torch.autograd.function.once_differentiable

@@ -183,3 +183,23 @@ def test_calls_of_one_list_on_several_streams_run_in_order():
     assert [float(r.sumsq) for r in results] == [12e6] * 4
     assert float(gl.result.sumsq) == 12e6 and float(t[-1]) == float(np.float32(2.0) * np.float32(float(gl.result.coef)))
     gl.close()
+
+
+def test_the_forward_derivative_is_the_lookup_of_the_tangent():
+    from torch.autograd import forward_ad
+    w, v = torch.randn(12, 5, device="cuda"), torch.randn(12, 5, device="cuda")
+    ids = torch.tensor([[1, 5, -1], [11, 12, 5]], device="cuda")
+    for need in (False, True):
+        with forward_ad.dual_level():
+            dual = forward_ad.make_dual(w.clone().requires_grad_(need), v)
+            y, dy = forward_ad.unpack_dual(g.embedding(dual, ids, scale=1.5, padding_id=5))
+            assert torch.equal(y, g.embedding(w, ids, scale=1.5))
+            assert dy is not None and torch.equal(dy, g.embedding(v, ids, scale=1.5))
+    with forward_ad.dual_level():  # a tangent of other strides, into another type
+        y = g.embedding(forward_ad.make_dual(w, v[:1].expand(12, 5)), ids, out_dtype=torch.bfloat16)
+        assert torch.equal(forward_ad.unpack_dual(y).tangent, g.embedding(v[:1].repeat(12, 1), ids,
+                                                                          out_dtype=torch.bfloat16))
+    with forward_ad.dual_level():  # no tangent: none comes out
+        assert forward_ad.unpack_dual(g.embedding(w, ids)).tangent is None
+        with pytest.raises(ValueError):
+            g.embedding(forward_ad.make_dual(w, v), ids, out=torch.empty(2, 3, 5, device="cuda"))
