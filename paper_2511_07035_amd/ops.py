@@ -343,6 +343,8 @@ def _lookup(weight, ids, scale, out, out_dtype, first_id, stream):
     else:
         if out.shape != shape or (out_dtype is not None and out.dtype != out_dtype):
             raise ValueError(f"out: expected shape {shape}, got {tuple(out.shape)} of {out.dtype}")
+        if out.requires_grad and torch.is_grad_enabled():
+            raise ValueError("out: requires a gradient, which the call would not give it")
         o = _matrix(out, "out", device, dim)
     _check(_lib().gockpt_embedding(w, t, scale, o, _stream(stream, device)), "gockpt_embedding", None)
     return out

@@ -203,3 +203,12 @@ def test_the_forward_derivative_is_the_lookup_of_the_tangent():
         assert forward_ad.unpack_dual(g.embedding(w, ids)).tangent is None
         with pytest.raises(ValueError):
             g.embedding(forward_ad.make_dual(w, v), ids, out=torch.empty(2, 3, 5, device="cuda"))
+
+
+def test_an_out_that_requires_a_gradient_is_refused():
+    w, ids = torch.randn(12, 5, device="cuda"), torch.tensor([1, 5], device="cuda")
+    out = torch.zeros(2, 5, device="cuda", requires_grad=True)
+    with pytest.raises(ValueError):
+        g.embedding(w, ids, out=out)
+    with torch.no_grad():
+        assert torch.equal(g.embedding(w, ids, out=out), w[ids])
