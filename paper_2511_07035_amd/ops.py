@@ -145,7 +145,7 @@ class GradResult:
         self.found_inf = self.buffer[3:4]
         self.coef = self.buffer[4:5]
         self.largest = self.buffer[5:7]
-        self.ptr = self.buffer.data_ptr()
+        self.ptr, self.device = self.buffer.data_ptr(), self.buffer.get_device()
 
     def update(self, max_norm: float = float("inf"), scale=None, stream=None) -> "GradResult":
         """norm, found_inf and coef again from ``sumsq`` and ``largest``, after
@@ -241,11 +241,19 @@ class GradList:
         stream.wait_stream(self.last)
         self.last, self.at = stream, stream.cuda_stream
 
+    def _result(self, result) -> GradResult:
+        if result is None:
+            return self.result
+        if result.device != self.device:
+            raise ValueError(f"result: on {result.buffer.device}, the list is on GPU {self.device}")
+        return result
+
     def norm(self, max_norm: float = float("inf"), *, scale=None, result=None, stream=None) -> GradResult:
         """The norm over all tensors, divided by ``scale`` (the loss scale the
         gradients carry: a device tensor or a Session), into ``result`` (the
         list's own, overwritten by its next call, if None)."""
-        r, s = self.result if result is None else result, self._on(stream)
+        s = self._on(stream)
+        r = self._result(result)
         _check(_lib().gockpt_grads_norm(self.handle, _scale_ptr(scale), max_norm, r.ptr, s), "gockpt_grads_norm", None)
         return r
 
@@ -254,13 +262,15 @@ class GradList:
         in place or into ``out``.  With an inf or NaN among the gradients they
         are left, or copied, as they are, and ``found_inf`` tells, as it does
         where a scaled element is beyond the range of its ``out``."""
-        r, s = self.result if result is None else result, self._on(stream)
+        s = self._on(stream)
+        r = self._result(result)
         _check(_lib().gockpt_grads_clip(self.handle, _scale_ptr(scale), max_norm, r.ptr, s), "gockpt_grads_clip", None)
         return r
 
     def scale(self, result=None, *, stream=None) -> None:
         """Every element times ``result.coef``: the second half of ``clip``."""
-        r, s = self.result if result is None else result, self._on(stream)
+        s = self._on(stream)
+        r = self._result(result)
         _check(_lib().gockpt_grads_scale(self.handle, r.ptr, s), "gockpt_grads_scale", None)
 
     def close(self) -> None:

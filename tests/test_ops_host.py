@@ -243,3 +243,22 @@ def test_a_list_orders_its_calls_across_streams(monkeypatch):
     assert gl._on(b) == 2 and b.waited == [a]
     assert gl._on(c) == 3 and c.waited == [b, a]
     gl.handle = None
+
+
+def test_a_result_off_the_lists_gpu_is_refused(monkeypatch):
+    import torch
+
+    class Calls:
+        def __getattr__(self, name):
+            return lambda *a: 0
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(ops, "_stream", lambda stream, device: 0)
+    monkeypatch.setattr(ops, "_lib", lambda: Calls())
+    gl = ops.GradList.__new__(ops.GradList)
+    gl.handle, gl.device, gl.home, gl.at, gl.strayed, gl.result = 7, 0, 0, 0, False, None
+    off = g.GradResult("cpu")
+    for call in (gl.norm, lambda result: gl.clip(1.0, result=result), gl.scale):
+        with pytest.raises(ValueError):
+            call(result=off)
+    gl.handle = None
