@@ -7,7 +7,8 @@
 Checks of shapes and types are made here or in the library and raise
 ValueError or GockptError; all arithmetic runs in the library's kernels.
 Calls are queued on the current torch stream, or on ``stream``; as with any
-torch operation, tensors written on another stream have to be waited for.
+torch operation, tensors written on another stream have to be waited for.  What
+a call writes counts as changed in place: a backward that has saved it raises.
 """
 from __future__ import annotations
 
@@ -17,6 +18,7 @@ import struct
 
 import torch
 from torch.autograd import forward_ad
+from torch.autograd.graph import increment_version
 
 from . import GOCKPT_EINVAL, GockptError, _check, lib
 
@@ -151,6 +153,7 @@ class GradResult:
         """norm, found_inf and coef again from ``sumsq`` and ``largest``, after
         ranks that hold different parameters have put theirs together."""
         _here(self.buffer, "result")
+        increment_version(self.buffer)
         _check(_lib().gockpt_grads_result(self.ptr, _scale_ptr(scale), max_norm,
                                           _stream(stream, self.buffer.get_device())), "gockpt_grads_result", None)
         return self
@@ -206,6 +209,10 @@ class GradList:
                     raise ValueError(f"out {i}: expected {t.numel()} contiguous elements, got {tuple(o.shape)}")
             table += GRAD_TENSOR.pack(t.data_ptr(), 0 if o is None else o.data_ptr(), *r, d,
                                       d if o is None else _dtype(o, f"out {i}"))
+        # what clip and scale write, for increment_version: a tensor for each storage's
+        # version, which views share with their base
+        written = [t if o is None else o for t, o in zip(self.tensors, self.out)]
+        self.written = list({id(b): b for b in (w if w._base is None else w._base for w in written)}.values())
         table, n, size = bytes(table), len(self.tensors), ctypes.c_size_t()
         _check(_lib().gockpt_grads_bytes(table, n, ctypes.byref(size)), "gockpt_grads_bytes", None)
         if self.device is None:
@@ -255,6 +262,7 @@ class GradList:
         s = self._on(stream)
         r = self._result(result)
         _check(_lib().gockpt_grads_norm(self.handle, _scale_ptr(scale), max_norm, r.ptr, s), "gockpt_grads_norm", None)
+        increment_version(r.buffer)
         return r
 
     def clip(self, max_norm: float, *, scale=None, result=None, stream=None) -> GradResult:
@@ -265,6 +273,7 @@ class GradList:
         s = self._on(stream)
         r = self._result(result)
         _check(_lib().gockpt_grads_clip(self.handle, _scale_ptr(scale), max_norm, r.ptr, s), "gockpt_grads_clip", None)
+        increment_version((r.buffer, *self.written))
         return r
 
     def scale(self, result=None, *, stream=None) -> None:
@@ -272,6 +281,7 @@ class GradList:
         s = self._on(stream)
         r = self._result(result)
         _check(_lib().gockpt_grads_scale(self.handle, r.ptr, s), "gockpt_grads_scale", None)
+        increment_version(self.written)
 
     def close(self) -> None:
         """Releases the handle.  Waits for the GPU if calls ran on other
@@ -343,7 +353,8 @@ def _lookup(weight, ids, scale, out, out_dtype, first_id, stream):
     w, t = _matrix(weight, "weight", device), _token_ids(ids, first_id, device)
     dim = weight.shape[1]
     shape = (*ids.shape, dim)
-    if out is None:
+    given = out is not None
+    if not given:
         dtype = weight.dtype if out_dtype is None else out_dtype
         code = _DTYPE.get(dtype)
         if code is None:
@@ -357,6 +368,8 @@ def _lookup(weight, ids, scale, out, out_dtype, first_id, stream):
             raise ValueError("out: requires a gradient, which the call would not give it")
         o = _matrix(out, "out", device, dim)
     _check(_lib().gockpt_embedding(w, t, scale, o, _stream(stream, device)), "gockpt_embedding", None)
+    if given:
+        increment_version(out)
     return out
 
 
@@ -417,6 +430,7 @@ def embedding_grad(grad_out, ids, grad_weight, *, scale: float = 1.0, accumulate
     _check(_lib().gockpt_embedding_grad(x, t, NO_PADDING if padding_id is None else padding_id, scale, accumulate, m,
                                         ptr, size, _stream(stream, device)),
            "gockpt_embedding_grad", None)
+    increment_version(grad_weight)
     return grad_weight
 
 

@@ -212,3 +212,34 @@ def test_an_out_that_requires_a_gradient_is_refused():
         g.embedding(w, ids, out=out)
     with torch.no_grad():
         assert torch.equal(g.embedding(w, ids, out=out), w[ids])
+
+
+def test_a_buffer_that_autograd_saved_cannot_change_unseen():
+    """What a call writes in place counts as a change of the tensor, of its
+    base and of its views."""
+    w, ids = torch.randn(12, 5, device="cuda"), torch.tensor([1, 5], device="cuda")
+    base = torch.ones(200, device="cuda")
+    calls = [lambda t: g.embedding(w, ids, out=t.view(2, 5)),
+             lambda t: g.embedding_grad(torch.ones(2, 5, device="cuda"), ids % 2, t.view(2, 5)),
+             lambda t: g.GradList([t]).clip(0.1),
+             lambda t: g.GradList([torch.ones(10, device="cuda")], [t]).clip(0.1),
+             lambda t: g.GradList([t]).scale(g.GradList([torch.ones(9, device="cuda")]).norm(0.1))]
+    for call in calls:
+        for buf in (torch.ones(10, device="cuda"), base[3:13]):
+            x = torch.ones(10, device="cuda", requires_grad=True)
+            loss = (x * buf).sum()
+            call(buf)
+            with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                loss.backward()
+    with torch.inference_mode():  # tensors without a version
+        t = torch.ones(10, device="cuda")
+        for call in calls:
+            call(t)
+    # a norm reads its tensors
+    x, t = torch.ones(10, device="cuda", requires_grad=True), torch.ones(10, device="cuda")
+    loss = (x * t).sum()
+    gl = g.GradList([t], [torch.empty(10, device="cuda")])
+    gl.norm(0.1)
+    gl.clip(0.1)
+    loss.backward()
+    assert torch.equal(x.grad, t)

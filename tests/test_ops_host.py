@@ -255,6 +255,7 @@ def test_a_result_off_the_lists_gpu_is_refused(monkeypatch):
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
     monkeypatch.setattr(ops, "_stream", lambda stream, device: 0)
     monkeypatch.setattr(ops, "_lib", lambda: Calls())
+    monkeypatch.setattr(ops.GradList, "__del__", lambda self: None)
     gl = ops.GradList.__new__(ops.GradList)
     gl.handle, gl.device, gl.home, gl.at, gl.strayed, gl.result = 7, 0, 0, 0, False, None
     off = g.GradResult("cpu")
