@@ -7,7 +7,11 @@
 Checks of shapes and types are made here or in the library and raise
 ValueError or GockptError; all arithmetic runs in the library's kernels.
 Calls are queued on the current torch stream, or on ``stream``; as with any
-torch operation, tensors written on another stream have to be waited for.  What
+torch operation, tensors written on another stream have to be waited for.  A
+Session's step runs on its ``compute`` stream: calls that read its weights or
+write its gradients or its found_inf go there (``with
+torch.cuda.stream(session.compute)``), or the program has each wait for the
+other.  What
 a call writes counts as changed in place: a backward that has saved it raises.
 """
 from __future__ import annotations
@@ -152,23 +156,31 @@ class GradResult:
     def update(self, max_norm: float = float("inf"), scale=None, stream=None) -> "GradResult":
         """norm, found_inf and coef again from ``sumsq`` and ``largest``, after
         ranks that hold different parameters have put theirs together."""
-        _here(self.buffer, "result")
+        device = _here(self.buffer, "result")
         increment_version(self.buffer)
-        _check(_lib().gockpt_grads_result(self.ptr, _scale_ptr(scale), max_norm,
-                                          _stream(stream, self.buffer.get_device())), "gockpt_grads_result", None)
+        s = _stream(stream, device)
+        _check(_lib().gockpt_grads_result(self.ptr, _scale_ptr(scale, device, stream, s), max_norm, s),
+               "gockpt_grads_result", None)
         return self
 
 
-def _scale_ptr(scale):
+def _scale_ptr(scale, device: int, stream, raw: int):
     """Address of a one-element float32 device tensor, or of the loss scale of
-    a Session."""
+    a Session, whose steps write it: the stream of the call (`raw` its handle)
+    waits for those queued so far."""
     if scale is None:
         return None
     if isinstance(scale, torch.Tensor):
         if scale.dtype != torch.float32 or scale.numel() != 1:
             raise ValueError("scale: expected a one-element float32 tensor or a Session")
-        _here(scale, "scale")
+        _here(scale, "scale", device)
         return scale.data_ptr()
+    if scale.compute.device_index != device:
+        raise ValueError(f"scale: the Session is on GPU {scale.compute.device_index}, the call on {device}")
+    if scale.compute.cuda_stream != raw:
+        now = torch.cuda.current_stream(device) if stream is None else stream
+        if not (_capturing(now) or _capturing(scale.compute)):
+            now.wait_stream(scale.compute)
     return gockpt_scale_ptr(scale.ctx)
 
 
@@ -257,11 +269,13 @@ class GradList:
 
     def norm(self, max_norm: float = float("inf"), *, scale=None, result=None, stream=None) -> GradResult:
         """The norm over all tensors, divided by ``scale`` (the loss scale the
-        gradients carry: a device tensor or a Session), into ``result`` (the
-        list's own, overwritten by its next call, if None)."""
+        gradients carry: a device tensor, or a Session, whose steps queued so
+        far are waited for on another stream than its own), into ``result``
+        (the list's own, overwritten by its next call, if None)."""
         s = self._on(stream)
         r = self._result(result)
-        _check(_lib().gockpt_grads_norm(self.handle, _scale_ptr(scale), max_norm, r.ptr, s), "gockpt_grads_norm", None)
+        p = _scale_ptr(scale, self.device, stream, s)
+        _check(_lib().gockpt_grads_norm(self.handle, p, max_norm, r.ptr, s), "gockpt_grads_norm", None)
         increment_version(r.buffer)
         return r
 
@@ -272,7 +286,8 @@ class GradList:
         where a scaled element is beyond the range of its ``out``."""
         s = self._on(stream)
         r = self._result(result)
-        _check(_lib().gockpt_grads_clip(self.handle, _scale_ptr(scale), max_norm, r.ptr, s), "gockpt_grads_clip", None)
+        p = _scale_ptr(scale, self.device, stream, s)
+        _check(_lib().gockpt_grads_clip(self.handle, p, max_norm, r.ptr, s), "gockpt_grads_clip", None)
         increment_version((r.buffer, *self.written))
         return r
 

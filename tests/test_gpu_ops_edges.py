@@ -243,3 +243,28 @@ def test_a_buffer_that_autograd_saved_cannot_change_unseen():
     gl.clip(0.1)
     loss.backward()
     assert torch.equal(x.grad, t)
+
+
+def test_a_call_beside_a_session_waits_for_its_steps_scale():
+    flag = torch.ones(1, device="cuda")
+    sess = g.Session(5000, ring_bytes=1 << 20, dynamic_scale=True, init_scale=1024.0, found_inf=flag, grad_norm=False)
+    try:
+        t, other = torch.full((100,), 512.0, device="cuda"), torch.cuda.Stream()
+        torch.cuda.synchronize()
+        gl = g.GradList([t])
+        torch.cuda.synchronize()
+        with torch.cuda.stream(sess.compute):
+            torch.cuda._sleep(20_000_000)  # the step that halves the scale runs late
+        sess.step(1e-3)
+        beside = gl.norm(scale=sess, result=g.GradResult())
+        updated = g.GradResult()
+        updated.sumsq.fill_(100 * 512.0 ** 2)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(sess.compute):
+            torch.cuda._sleep(20_000_000)
+        sess.step(1e-3)
+        updated.update(scale=sess, stream=other)
+        torch.cuda.synchronize()
+        assert float(beside.norm) == 10.0 and float(updated.norm) == 20.0
+    finally:
+        sess.close()

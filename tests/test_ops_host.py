@@ -263,3 +263,23 @@ def test_a_result_off_the_lists_gpu_is_refused(monkeypatch):
         with pytest.raises(ValueError):
             call(result=off)
     gl.handle = None
+
+
+def test_a_sessions_scale_is_waited_for_on_other_streams(monkeypatch):
+    import torch
+    own, other, captured = _Stream(1), _Stream(2), []
+    own.device_index = 0
+    monkeypatch.setattr(ops, "_capturing", lambda s: s in captured)
+    monkeypatch.setattr(ops, "gockpt_scale_ptr", lambda ctx: ctx + 1)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda device: other)
+
+    class Sess:
+        ctx, compute = 41, own
+
+    assert ops._scale_ptr(Sess, 0, own, 1) == 42 and own.waited == []
+    assert ops._scale_ptr(Sess, 0, other, 2) == 42 and other.waited == [own]
+    assert ops._scale_ptr(Sess, 0, None, 2) == 42 and other.waited == [own, own]  # the current one
+    captured.append(other)
+    assert ops._scale_ptr(Sess, 0, other, 2) == 42 and other.waited == [own, own]
+    with pytest.raises(ValueError):
+        ops._scale_ptr(Sess, 1, other, 2)
