@@ -22,7 +22,6 @@ import struct
 
 import torch
 from torch.autograd import forward_ad
-from torch.autograd.graph import increment_version
 
 from . import GOCKPT_EINVAL, GockptError, _check, lib
 
@@ -37,6 +36,10 @@ GRAD_TENSOR = struct.Struct("<QQqqqii")   # data, dst, rows, cols, stride, dtype
 MATRIX = struct.Struct("<Qqqqii")         # data, rows, cols, stride, dtype, reserved
 TOKEN_IDS = struct.Struct("<Qqqqqii")     # ids, batch, length, stride, first_id, bits, reserved
 GRAD_RESULT = struct.Struct("<dfff3f")    # sumsq, norm, found_inf, coef, reserved
+
+# torch.autograd.graph.increment_version, which takes a list alone, without its
+# 0.15 us of a call's 5 to 8
+_changed = torch._C._increment_version
 
 _P = ctypes.c_void_p
 _B = ctypes.c_char_p
@@ -157,7 +160,7 @@ class GradResult:
         """norm, found_inf and coef again from ``sumsq`` and ``largest``, after
         ranks that hold different parameters have put theirs together."""
         device = _here(self.buffer, "result")
-        increment_version(self.buffer)
+        _changed((self.buffer,))
         s = _stream(stream, device)
         _check(_lib().gockpt_grads_result(self.ptr, _scale_ptr(scale, device, stream, s), max_norm, s),
                "gockpt_grads_result", None)
@@ -221,7 +224,7 @@ class GradList:
                     raise ValueError(f"out {i}: expected {t.numel()} contiguous elements, got {tuple(o.shape)}")
             table += GRAD_TENSOR.pack(t.data_ptr(), 0 if o is None else o.data_ptr(), *r, d,
                                       d if o is None else _dtype(o, f"out {i}"))
-        # what clip and scale write, for increment_version: a tensor for each storage's
+        # what clip and scale write, for _changed: a tensor for each storage's
         # version, which views share with their base
         written = [t if o is None else o for t, o in zip(self.tensors, self.out)]
         self.written = list({id(b): b for b in (w if w._base is None else w._base for w in written)}.values())
@@ -276,7 +279,7 @@ class GradList:
         r = self._result(result)
         p = _scale_ptr(scale, self.device, stream, s)
         _check(_lib().gockpt_grads_norm(self.handle, p, max_norm, r.ptr, s), "gockpt_grads_norm", None)
-        increment_version(r.buffer)
+        _changed((r.buffer,))
         return r
 
     def clip(self, max_norm: float, *, scale=None, result=None, stream=None) -> GradResult:
@@ -288,7 +291,7 @@ class GradList:
         r = self._result(result)
         p = _scale_ptr(scale, self.device, stream, s)
         _check(_lib().gockpt_grads_clip(self.handle, p, max_norm, r.ptr, s), "gockpt_grads_clip", None)
-        increment_version((r.buffer, *self.written))
+        _changed((r.buffer, *self.written))
         return r
 
     def scale(self, result=None, *, stream=None) -> None:
@@ -296,7 +299,7 @@ class GradList:
         s = self._on(stream)
         r = self._result(result)
         _check(_lib().gockpt_grads_scale(self.handle, r.ptr, s), "gockpt_grads_scale", None)
-        increment_version(self.written)
+        _changed(self.written)
 
     def close(self) -> None:
         """Releases the handle.  Waits for the GPU if calls ran on other
@@ -315,9 +318,11 @@ class GradList:
             pass
 
 
-def _matrix(t, what: str, device: int, cols=None) -> bytes:
-    """A 2-D tensor, or with cols the rows of that many elements of any."""
-    _here(t, what, device)
+def _matrix(t, what: str, device: int | None, cols=None) -> bytes:
+    """A 2-D tensor, or with cols the rows of that many elements of any; on GPU
+    `device` (None: checked by the caller)."""
+    if device is not None:
+        _here(t, what, device)
     d = _dtype(t, what)
     shape = t.shape
     if cols is not None and len(shape) > 0 and shape[-1] == cols and t.is_contiguous():
@@ -365,7 +370,7 @@ def _empty(like, shape, dtype, stream):
 
 def _lookup(weight, ids, scale, out, out_dtype, first_id, stream):
     device = _here(weight, "weight")
-    w, t = _matrix(weight, "weight", device), _token_ids(ids, first_id, device)
+    w, t = _matrix(weight, "weight", None), _token_ids(ids, first_id, device)
     dim = weight.shape[1]
     shape = (*ids.shape, dim)
     given = out is not None
@@ -384,7 +389,7 @@ def _lookup(weight, ids, scale, out, out_dtype, first_id, stream):
         o = _matrix(out, "out", device, dim)
     _check(_lib().gockpt_embedding(w, t, scale, o, _stream(stream, device)), "gockpt_embedding", None)
     if given:
-        increment_version(out)
+        _changed((out,))
     return out
 
 
@@ -405,7 +410,9 @@ def embedding(weight, ids, *, scale: float = 1.0, out=None, out_dtype=None, firs
     tangent's lookup."""
     if accumulate and grad_weight is None:
         raise ValueError("accumulate: into a grad_weight")
-    if (weight.requires_grad and torch.is_grad_enabled()) or _has_tangent(weight):
+    # the level is -1 outside of a dual_level
+    if (weight.requires_grad and torch.is_grad_enabled()) or (
+            forward_ad._current_level >= 0 and forward_ad.unpack_dual(weight).tangent is not None):
         if out is not None or stream is not None:
             raise ValueError("out and stream: for calls without a gradient")
         if grad_weight is not None:
@@ -426,7 +433,7 @@ def embedding_grad(grad_out, ids, grad_weight, *, scale: float = 1.0, accumulate
     token are left alone.  workspace: a uint8 tensor of at least
     gockpt_embedding_grad_bytes(tokens, rows, dim) (None: allocated)."""
     device = _here(grad_weight, "grad_weight")
-    m = _matrix(grad_weight, "grad_weight", device)
+    m = _matrix(grad_weight, "grad_weight", None)
     if grad_out.shape[:-1] != ids.shape:
         raise ValueError(f"grad_out of shape {tuple(grad_out.shape)} for ids of shape {tuple(ids.shape)}")
     rows, cols = grad_weight.shape
@@ -445,13 +452,8 @@ def embedding_grad(grad_out, ids, grad_weight, *, scale: float = 1.0, accumulate
     _check(_lib().gockpt_embedding_grad(x, t, NO_PADDING if padding_id is None else padding_id, scale, accumulate, m,
                                         ptr, size, _stream(stream, device)),
            "gockpt_embedding_grad", None)
-    increment_version(grad_weight)
+    _changed((grad_weight,))
     return grad_weight
-
-
-def _has_tangent(t) -> bool:
-    # the level is -1 outside of a dual_level: no more than a comparison there
-    return forward_ad._current_level >= 0 and forward_ad.unpack_dual(t).tangent is not None
 
 
 class _Embedding(torch.autograd.Function):
