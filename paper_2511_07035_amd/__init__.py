@@ -561,5 +561,6 @@ def __getattr__(name: str):
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
 
 
+# without _OPS: a star import takes every name here, and must not need torch
 __all__ = [n for n in dir() if n.startswith(("gockpt_", "GOCKPT_"))] + ["Session", "StateSlab", "GockptError", "lib",
-                                                           "RECORD_DTYPE", *_OPS]
+                                                           "RECORD_DTYPE"]

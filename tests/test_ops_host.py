@@ -283,3 +283,11 @@ def test_a_sessions_scale_is_waited_for_on_other_streams(monkeypatch):
     assert ops._scale_ptr(Sess, 0, other, 2) == 42 and other.waited == [own, own]
     with pytest.raises(ValueError):
         ops._scale_ptr(Sess, 1, other, 2)
+
+
+def test_a_star_import_needs_no_torch():
+    import sys
+    code = ("import sys; sys.modules['torch'] = None\nfrom paper_2511_07035_amd import *\n"
+            "print(gockpt_workspace_bytes(1000) > 0, Session.__name__)")
+    r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True)
+    assert r.stdout.split() == ["True", "Session"], r.stderr
