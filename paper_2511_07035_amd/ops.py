@@ -18,6 +18,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import math
 import struct
 
 import torch
@@ -326,7 +327,7 @@ def _matrix(t, what: str, device: int | None, cols=None) -> bytes:
     d = _dtype(t, what)
     shape = t.shape
     if cols is not None and len(shape) > 0 and shape[-1] == cols and t.is_contiguous():
-        return MATRIX.pack(t.data_ptr(), t.numel() // cols if cols else 0, cols, cols, d, 0)
+        return MATRIX.pack(t.data_ptr(), t.numel() // cols if cols else math.prod(shape[:-1]), cols, cols, d, 0)
     if len(shape) == 2:
         (rows, n), (stride, step) = shape, t.stride()
     elif cols is not None and len(shape) > 0:

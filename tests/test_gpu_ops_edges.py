@@ -268,3 +268,14 @@ def test_a_call_beside_a_session_waits_for_its_steps_scale():
         assert float(beside.norm) == 10.0 and float(updated.norm) == 20.0
     finally:
         sess.close()
+
+
+def test_a_table_without_columns():
+    w, ids = torch.zeros(10, 0, device="cuda"), torch.tensor([[1, 5, 11]], device="cuda")
+    assert g.embedding(w, ids).shape == (1, 3, 0)
+    assert g.embedding(w, ids, out=torch.zeros(1, 3, 0, device="cuda")).shape == (1, 3, 0)
+    into = torch.zeros(10, 0, device="cuda")
+    assert g.embedding_grad(torch.zeros(1, 3, 0, device="cuda"), ids, into) is into
+    w.requires_grad_()
+    g.embedding(w, ids).sum().backward()
+    assert w.grad.shape == (10, 0)
