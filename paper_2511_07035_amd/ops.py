@@ -179,6 +179,8 @@ def _scale_ptr(scale, device: int, stream, raw: int):
             raise ValueError("scale: expected a one-element float32 tensor or a Session")
         _here(scale, "scale", device)
         return scale.data_ptr()
+    if not hasattr(scale, "ctx"):
+        raise ValueError(f"scale: expected a one-element float32 tensor or a Session, got {type(scale).__name__}")
     if scale.compute.device_index != device:
         raise ValueError(f"scale: the Session is on GPU {scale.compute.device_index}, the call on {device}")
     if scale.compute.cuda_stream != raw:

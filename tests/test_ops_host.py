@@ -291,3 +291,9 @@ def test_a_star_import_needs_no_torch():
             "print(gockpt_workspace_bytes(1000) > 0, Session.__name__)")
     r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True)
     assert r.stdout.split() == ["True", "Session"], r.stderr
+
+
+@pytest.mark.parametrize("scale", [2.0, 65536, "1"])
+def test_a_scale_of_another_kind_is_refused(scale):
+    with pytest.raises(ValueError, match="scale"):
+        ops._scale_ptr(scale, 0, None, 0)
