@@ -89,12 +89,4 @@ __device__ __forceinline__ void store_elem(uint8_t* p, float x) {
         *reinterpret_cast<uint16_t*>(p) = static_cast<uint16_t>(pack2<kT>(x, x));
 }
 
-template <int kT>
-__device__ __forceinline__ float load_elem(const uint8_t* p) {
-    if constexpr (kT == kFP32)
-        return *reinterpret_cast<const float*>(p);
-    else
-        return elem_to_f32<kT>(*reinterpret_cast<const uint16_t*>(p));
-}
-
 }  // namespace gockpt
