@@ -15,9 +15,10 @@
 //
 //   Memory bounds it: grad_out read once, every row of the table written.
 //   131072 tokens x 4096 fp16 into 32000 rows, a tenth masked (0.97 GB + 0.26
-//   GB): 272 us, of which the sort 42 (half of the table is cleared meanwhile),
-//   the sums 215 at 5.6 TB/s, the join 16.  16384 x 2048 bf16 into 50304 rows
-//   (67 + 206 MB): 62 us.  A copy moves the same bytes in 260 and 58.
+//   GB): 271 us, of which the sort 32 (half of the table is cleared meanwhile),
+//   the sums 223 at 5.4 TB/s, the join 16.  16384 x 2048 bf16 into 50304 rows
+//   (67 + 206 MB): 62 us; accumulated, with no zeros to write, 58.  A copy moves
+//   the bytes of the first two in 260 and 58.
 #include <limits.h>
 
 #include "gockpt_ops_internal.h"
@@ -155,7 +156,8 @@ __device__ __forceinline__ void store_cols(uint8_t* p, int64_t c, int64_t cols, 
 // in the last-level cache 250 (1.34 GB written: 195 us at the rate of a fill,
 // 312 at a copy's over all 1.48 GB); 131072 x 4096 bf16 287, 16384 x 2048 bf16
 // 19.  us with 2, 3, 4 and 8 pieces: 396, 338, 345, 355; 310, 302, 287, 325;
-// 18.8, 19.0, 19.3, 21.9.  Slower: the same column block of several rows in a
+// 18.8, 19.0, 19.3, 21.9: with 4 each is within 3% of its best, with the others
+// one is 5% off or more.  Slower: the same column block of several rows in a
 // block (357, 310); a row's column blocks on one XCD each, so that its L2 holds
 // parts of more rows; contiguous tokens on each XCD; loads past the caches
 // (389); stores written through the L2.
@@ -774,7 +776,9 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(GradArgs a) {
 }
 
 // Rows that go on from one chunk into others: by the group of the chunk in
-// which the row begins, the partials in order.
+// which the row begins, the partials in order.  A row that has many chunks is
+// one group's, kJoinAhead loads at a time: 131072 x 4096 fp16, by text's law 284
+// us in all, with half of the tokens on one id 314.
 constexpr int kJoinCols = 4;
 constexpr int kJoinAhead = 16;
 

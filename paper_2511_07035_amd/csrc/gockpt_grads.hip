@@ -7,7 +7,7 @@
 //                  NaN, or a finite element whose scaled value is rounded to
 //                  an infinity in a narrower type.
 //   scale_kernel   element * coef, rounded to the destination's type.
-//   whole_kernel   all of it in one launch for a list of at most 8 MiB.
+//   whole_kernel   all of it in one launch for a list of at most 512 tiles.
 //
 // The host cuts the tensors into tiles of at most 1024 units of 16 source
 // bytes (16 KiB) once, when the list is made; a tensor of any size, type,
@@ -17,8 +17,9 @@
 // the 1.31e9 bf16 gradients of GPT 1.3B (2.62 GB in 195 tensors) the norm takes
 // 374 us, 7.0 TB/s, which is what a read-only probe reaches.  Clipping reads
 // twice, since no element can be scaled before the last one is squared: 5.2 GB
-// of fp32 gradients rounded into bf16 take 1992 us, 6.6 TB/s over the 13.1 GB
-// moved.  Up to 8 MiB a launch costs more than the data, hence whole_kernel.
+// of fp32 gradients rounded into bf16 take 1995 us, 6.6 TB/s over the 13.1 GB
+// moved; 2.6 GB of bf16 in place 1235, 6.4 TB/s over 7.9 GB.  In a small list a
+// launch costs more than the data, hence whole_kernel.
 #include <math.h>
 #include <stdlib.h>
 
@@ -42,10 +43,11 @@ constexpr int kTileUnits = kThreads * kUnitsPerThread;
 // fewer partials are left to add (GPT 1.3B in bf16 376 us, with 2048 390).
 constexpr int kSumBlocks = 1024;
 
-// Lists of up to this many tiles (8 MiB) take one launch, a tile a block.  us
-// a clip in one launch and in three: 2^17 bf16 elements 6.0 and 11.1, 2^21 8.6
-// and 11.4, 2^22, the limit, 11.3 and 11.4.  Above it, blocks of two or four
-// tiles that keep them in registers gained nothing (2^23 16.3 and 16.2).
+// Lists of up to this many tiles (8 MiB where the tensors fill theirs; 512
+// tensors of any size below) take one launch, a tile a block.  us a clip in one
+// launch and in two: 2^17 bf16 elements 5.6 and 8.8, 2^21 7.1 and 9.7, 2^22, the
+// limit, 10.1 and 11.0.  Above it, blocks of two or four tiles that keep them in
+// registers gained nothing (2^23 16.3 and 16.2).
 constexpr int kWholeTiles = 512;
 // Polls (about 0.5 us each) before a block of whole_kernel computes the partials
 // it misses, and before block 0 does, which in a large list is a lot of work for
@@ -281,8 +283,8 @@ __device__ __forceinline__ double tile_sum(const GradTile& t, u32x4 (&raw)[kUnit
 // source (kRange) a block writes its range too, as two magnitudes of 31 bits
 // above the tag; kSlotRange says whether there is one to be read, since a second
 // read of words costs 1 us.  Block 0 adds the partials in a fixed order and
-// writes the result.  (As a launch of its own that cost 1 us more: 2^23 bf16
-// elements 6.5 and 7.5, 2^25 14.1 and 15.2.)
+// writes the result.  (As a launch of its own that cost 1 us more, with 2^23 and
+// with 2^25 bf16 elements.)
 //
 // A block arrives when it has read the epoch, and the epoch is the number of
 // arrivals, kGroupBlocks a call, divided by that: the next one is not reached
