@@ -461,8 +461,13 @@ __device__ __forceinline__ uint32_t* arrivals_of(uint32_t* sync) {
     return sync + blockIdx.x % kGroups * kGroupWords;
 }
 
-// This block has read the epoch.  By the thread that has read it: the others
-// have it through LDS.  A group's first block arrives for those it lacks.
+// By thread 0 alone: the others have the epoch through LDS, where it is by the
+// time that the block arrives.
+__device__ __forceinline__ uint32_t read_arrivals(uint32_t* sync) {
+    return __hip_atomic_load(arrivals_of(sync), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// This block has read the epoch.  A group's first block arrives for those it lacks.
 __device__ __forceinline__ void arrive(uint32_t* sync) {
     const uint32_t others = (gridDim.x - 1u - blockIdx.x) / kGroups;
     __hip_atomic_fetch_add(arrivals_of(sync), blockIdx.x < kGroups ? kGroupBlocks - others : 1u, __ATOMIC_RELAXED,
@@ -493,7 +498,7 @@ __global__ __launch_bounds__(kThreads) void sumsq_kernel(const GradTile* __restr
                                                          const float* __restrict__ scale, double max_norm,
                                                          gockpt_grad_result* __restrict__ out) {
     __shared__ uint32_t call;
-    const uint32_t arrivals = *arrivals_of(sync);  // thread 0's is the block's
+    const uint32_t arrivals = threadIdx.x == 0 ? read_arrivals(sync) : 0u;
     double acc = 0.0;
     Range range = {0u, 0u};
     u32x4 next[kUnitsPerThread];
@@ -667,7 +672,7 @@ __global__ __launch_bounds__(kThreads) void whole_kernel(const GradTile* __restr
                                                          gockpt_grad_result* __restrict__ out) {
     __shared__ uint32_t call;
     __shared__ float coef;
-    const uint32_t arrivals = *arrivals_of(sync);  // thread 0's is the block's
+    const uint32_t arrivals = threadIdx.x == 0 ? read_arrivals(sync) : 0u;
     const GradTile t = tiles[blockIdx.x];
     u32x4 raw[kUnitsPerThread];
     load_tile<false>(t, raw);
