@@ -240,9 +240,9 @@ class GradList:
             self.result = GradResult(self.device)
         handle = _P()
         self.last = torch.cuda.current_stream(self.device) if stream is None else stream
-        self.home = self.at = self.last.cuda_stream
-        self.strayed = False
-        _check(_lib().gockpt_grads_create(table, n, self.workspace.data_ptr(), size.value, self.home,
+        self.at = self.last.cuda_stream
+        self.streams = {self.at}
+        _check(_lib().gockpt_grads_create(table, n, self.workspace.data_ptr(), size.value, self.at,
                                           ctypes.byref(handle)), "gockpt_grads_create", None)
         self.handle = handle.value
 
@@ -259,8 +259,11 @@ class GradList:
 
     def _move(self, stream) -> None:
         """To another stream than the last call's, which waits for that call."""
-        if stream.cuda_stream != self.home:  # not the one that the workspace was allocated for
-            self.strayed = True
+        if stream.cuda_stream not in self.streams:
+            # the allocator gives no memory of the list away before its work there is done
+            for t in (self.workspace, self.result.buffer, *self.tensors, *(o for o in self.out if o is not None)):
+                t.record_stream(stream)
+            self.streams.add(stream.cuda_stream)
         if _capturing(stream) or _capturing(self.last):
             return
         stream.wait_stream(self.last)
@@ -305,12 +308,9 @@ class GradList:
         _changed(self.written)
 
     def close(self) -> None:
-        """Releases the handle.  Waits for the GPU if calls ran on other
-        streams than the one the list was made on, which torch's allocator
-        does not know of."""
+        """Releases the handle.  Waits for nothing: work that calls have queued,
+        on whichever stream, still runs."""
         if self.handle is not None:
-            if self.strayed:
-                torch.cuda.synchronize(self.device)
             _lib().gockpt_grads_destroy(self.handle)
             self.handle = None
 

@@ -279,3 +279,24 @@ def test_a_table_without_columns():
     w.requires_grad_()
     g.embedding(w, ids).sum().backward()
     assert w.grad.shape == (10, 0)
+
+
+def test_a_list_that_ends_while_a_graph_records():
+    """Closing a list whose calls ran on another stream waits for nothing that
+    a recording forbids."""
+    t, x, other = torch.ones(5000, device="cuda"), torch.zeros(4, device="cuda"), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    lists = [g.GradList([t]) for _ in range(2)]
+    for gl in lists:
+        gl.norm(stream=other)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        x.add_(1.0)
+        lists.pop().close()
+        lists.clear()
+        x.add_(1.0)
+    for k in range(3):
+        graph.replay()
+        torch.cuda.synchronize()
+        assert float(x[0]) == 2.0 * (k + 1)

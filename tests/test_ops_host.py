@@ -232,12 +232,21 @@ def test_a_list_orders_its_calls_across_streams(monkeypatch):
     a, b, c = _Stream(1), _Stream(2), _Stream(3)
     captured = []
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
-    monkeypatch.setattr(torch.cuda, "synchronize", lambda device: None)
     monkeypatch.setattr(ops, "_capturing", lambda s: s in captured, raising=False)
+
+    class Memory:
+        recorded = []
+
+        def record_stream(self, stream):
+            self.recorded.append(stream)
+
     gl = ops.GradList.__new__(ops.GradList)
-    gl.handle, gl.device, gl.last, gl.home, gl.at, gl.strayed = 7, 0, a, 1, 1, False
+    gl.handle, gl.device, gl.last, gl.at, gl.streams = 7, 0, a, 1, {1}
+    gl.workspace, gl.tensors, gl.out, gl.result = Memory(), [Memory()], [None], ops.GradResult("cpu")
+    gl.result.buffer = Memory()
     assert [gl._on(s) for s in (a, b, b, c, a)] == [1, 2, 2, 3, 1]
-    assert a.waited == [c] and b.waited == [a] and c.waited == [b] and gl.strayed
+    assert a.waited == [c] and b.waited == [a] and c.waited == [b]
+    assert Memory.recorded == [b] * 3 + [c] * 3  # once for each stream but the list's own
     # a call that a graph records runs later: nothing to wait for, and nothing ran
     captured.append(b)
     assert gl._on(b) == 2 and b.waited == [a]
@@ -257,7 +266,7 @@ def test_a_result_off_the_lists_gpu_is_refused(monkeypatch):
     monkeypatch.setattr(ops, "_lib", lambda: Calls())
     monkeypatch.setattr(ops.GradList, "__del__", lambda self: None)
     gl = ops.GradList.__new__(ops.GradList)
-    gl.handle, gl.device, gl.home, gl.at, gl.strayed, gl.result = 7, 0, 0, 0, False, None
+    gl.handle, gl.device, gl.at, gl.result = 7, 0, 0, None
     off = g.GradResult("cpu")
     for call in (gl.norm, lambda result: gl.clip(1.0, result=result), gl.scale):
         with pytest.raises(ValueError):
