@@ -11,8 +11,8 @@ torch operation, tensors written on another stream have to be waited for.  A
 Session's step runs on its ``compute`` stream: calls that read its weights or
 write its gradients or its found_inf go there (``with
 torch.cuda.stream(session.compute)``), or the program has each wait for the
-other.  What
-a call writes counts as changed in place: a backward that has saved it raises.
+other.  What a call writes counts as changed in place: a backward that has
+saved it raises.
 """
 from __future__ import annotations
 
