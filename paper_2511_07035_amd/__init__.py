@@ -547,10 +547,13 @@ def gockpt_load(ctx, path: str, host_ptr: int, host_bytes: int, nthreads: int = 
 
 from .session import Session, StateSlab  # noqa: E402  (torch-backed buffers around the C-ABI)
 
-# Operators around the step (torch tensors in and out): loaded at their first
-# use, since this module itself is imported without torch.
+# Operators around the step and of the model (torch tensors in and out): loaded
+# at their first use, since this module itself is imported without torch.
 _OPS = ("GradList", "GradResult", "embedding", "embedding_grad", "gockpt_embedding_grad_bytes", "gockpt_scale_ptr",
         "GOCKPT_BF16", "GOCKPT_FP16", "GOCKPT_FP32")
+_MODEL = ("linear_cross_entropy", "head_stats", "head_grad", "Act8", "act8_pack", "linear8", "linear8_grad_weight",
+          "gate8", "GOCKPT_EACH", "GOCKPT_SUM", "GOCKPT_MEAN", "GOCKPT_SILU", "GOCKPT_GELU", "GOCKPT_GELU_TANH",
+          "GOCKPT_ACT8_BLOCK")
 
 
 def __getattr__(name: str):
@@ -558,9 +561,13 @@ def __getattr__(name: str):
         from . import ops
         globals().update({n: getattr(ops, n) for n in _OPS})
         return globals()[name]
+    if name in _MODEL:
+        from . import model
+        globals().update({n: getattr(model, n) for n in _MODEL})
+        return globals()[name]
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
 
 
-# without _OPS: a star import takes every name here, and must not need torch
+# without _OPS and _MODEL: a star import takes every name here, and must not need torch
 __all__ = [n for n in dir() if n.startswith(("gockpt_", "GOCKPT_"))] + ["Session", "StateSlab", "GockptError", "lib",
                                                            "RECORD_DTYPE"]

@@ -3,8 +3,8 @@
     python -m paper_2511_07035_amd.build
 
 Produces ``paper_2511_07035_amd/libgockpt.so`` (the C-ABI declared in
-``include/gockpt.h`` and ``include/gockpt_ops.h``) and ``paper_2511_07035_amd/libgockpt_bench.so`` (device
-helpers of the benchmark harness and tests: the forward/backward stand-in,
+``include/gockpt.h``, ``include/gockpt_ops.h`` and ``include/gockpt_model.h``) and
+``paper_2511_07035_amd/libgockpt_bench.so`` (device helpers of the benchmark harness and tests: the forward/backward stand-in,
 HBM probes, a kernel that holds every wave slot, and a device division and
 square root for bitwise checks).
 Cross-compiles without a GPU.
@@ -15,6 +15,7 @@ import os
 import subprocess
 import sys
 import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -39,7 +40,8 @@ HIP_FLAGS = [
 HOST_FLAGS = ["-O3", "-std=c++17", "-fPIC", "-ffp-contract=off", "-fno-math-errno", "-mavx2", "-msse4.2", "-Wall",
               f"-I{INCLUDE}"]
 
-LIB_HIP = ["gockpt_kernels.hip", "gockpt_cast.hip", "gockpt_runtime.hip", "gockpt_grads.hip", "gockpt_embed.hip"]
+LIB_HIP = ["gockpt_kernels.hip", "gockpt_cast.hip", "gockpt_runtime.hip", "gockpt_grads.hip", "gockpt_embed.hip",
+           "gockpt_products.hip", "gockpt_linear8.hip", "gockpt_act8.hip", "gockpt_head.hip"]
 LIB_HOST = ["gockpt_plan.cpp", "gockpt_planner.cpp", "gockpt_restore.cpp", "gockpt_persist.cpp"]
 BENCH_HIP = ["bench_kernels.hip"]
 
@@ -64,22 +66,17 @@ def _link(out, objs, tmp):
 
 def build(verbose: bool = False) -> None:
     with tempfile.TemporaryDirectory(prefix="gockpt_build_") as tmp:
-        objs = []
-        for src in LIB_HIP:
+        def compile_(src):
             o = os.path.join(tmp, src + ".o")
-            _run([HIPCC, *HIP_FLAGS, "-c", os.path.join(CSRC, src), "-o", o])
-            objs.append(o)
-        for src in LIB_HOST:
-            o = os.path.join(tmp, src + ".o")
-            _run([CLANGXX, *HOST_FLAGS, "-c", os.path.join(CSRC, src), "-o", o])
-            objs.append(o)
-        _link(LIB, objs, tmp)
-        bobjs = []
-        for src in BENCH_HIP:
-            o = os.path.join(tmp, src + ".o")
-            _run([HIPCC, *HIP_FLAGS, "-c", os.path.join(CSRC, src), "-o", o])
-            bobjs.append(o)
-        _link(BENCH_LIB, bobjs, tmp)
+            tool = [CLANGXX, *HOST_FLAGS] if src in LIB_HOST else [HIPCC, *HIP_FLAGS]
+            _run([*tool, "-c", os.path.join(CSRC, src), "-o", o])
+            return o
+
+        with ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
+            objs = list(pool.map(compile_, LIB_HIP + LIB_HOST + BENCH_HIP))
+        n = len(LIB_HIP + LIB_HOST)
+        _link(LIB, objs[:n], tmp)
+        _link(BENCH_LIB, objs[n:], tmp)
     if verbose:
         print("built", LIB, BENCH_LIB)
 

@@ -1,0 +1,771 @@
+// gockpt_head.hip -- cross entropy of the head's logits over the whole
+// vocabulary and its gradients, without keeping the logits.
+//
+//   l[t][v] = scale <x_t, w_v>,  lse_t = log sum_v exp l[t][v],  loss_t = lse_t - l[t][y_t]
+//   z[t][v] = g_t (exp(l[t][v] - lse_t) - [v = y_t]),  dX = scale Z W,  dW = scale Z^T X
+//
+// Exponentials are taken to the base 2: with l2 = l log2(e), a tile of logits
+// leaves each of its tokens the tile's largest l2 and sum of 2^(l2 - largest);
+// one wavefront a token joins them.  The gradients compute the logits again in
+// pieces of the vocabulary whose Z fits the workspace; a piece's Z is read by two
+// products, dW's rows of the piece, which is done, and dX, which is summed in
+// fp32 over the pieces.  Tokens that are masked are left out at the start: the
+// others' numbers are put together, and every kernel works on so many.
+//
+// Z is rounded to the inputs' 16-bit type, as the matrix cores take it: each
+// term of dX and dW is off by half a step of that type, which the sums average.
+// Not so a token's largest term, its target's: what rounding took from that is
+// kept, and its product with the target's row of the table is added to dX in fp32
+// (root mean square error of dX at 16384 tokens of 2048 columns against float64:
+// 0.0029 of its own without, 0.0019 with; its rounding to bf16 alone makes 0.0017).
+// Z is scaled by a power of two, 2^13 / 2^q where 2^q <= max |g| < 2^(q + 1), so
+// that fp16 has probabilities down to 2^-37 and nothing overflows; the products
+// are scaled back in fp32.
+#include "gockpt_mma.h"
+#include "gockpt_model_internal.h"
+
+namespace gockpt {
+
+namespace {
+
+constexpr double kLog2e = 1.4426950408889634074;
+constexpr float kLn2 = 0.69314718055994530942f;
+
+// ---- the tokens that count --------------------------------------------------------
+
+struct TokenArgs {
+    const void* ids;
+    int64_t stride, first, low, high, ignore;  // counts: low <= id < high, not ignore
+    int32_t tokens, length, rows, wide;
+    int32_t reduction;
+    int32_t* count;
+    int32_t* of_kept;   // token of the k-th that counts
+    int32_t* target;    // and its row of the table, -1 where that is another rank's
+    // the loss: zeros for masked tokens (null: not wanted)
+    float *lse, *logit, *loss;
+    uint32_t* ticket;
+    // the gradients (null: not)
+    const float *lse_in, *grad;
+    int32_t* of_token;  // number among those that count, or -1
+    float* base;        // log2(e) lse of the k-th
+    float* factor;      // g 2^(13 - q)
+    float* unscale;     // 2^(q - 13)
+};
+
+constexpr int kTokenThreads = 1024, kTokenWaves = kTokenThreads / 64;
+
+__device__ __forceinline__ int64_t target_of(const TokenArgs& a, int32_t t) {
+    const int64_t at = a.length == a.stride ? t : static_cast<int64_t>(t / a.length) * a.stride + t % a.length;
+    return a.wide ? static_cast<const int64_t*>(a.ids)[at] : static_cast<const int32_t*>(a.ids)[at];
+}
+
+__device__ __forceinline__ bool counts(const TokenArgs& a, int64_t id) {
+    return id >= a.low && id < a.high && id != a.ignore;
+}
+
+// One block: each wavefront counts its stretch of tokens, then numbers it from
+// the sum of those before.  16384 tokens take 9 us beside 11 ms of products.
+__global__ __launch_bounds__(kTokenThreads) void token_kernel(TokenArgs a) {
+    __shared__ int32_t counted[kTokenWaves];
+    __shared__ float largest[kTokenWaves];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int32_t each = (a.tokens + kTokenThreads - 1) / kTokenThreads * 64;
+    const int64_t from = static_cast<int64_t>(wave) * each;
+    const int64_t to = min(from + each, static_cast<int64_t>(a.tokens));
+    const bool weighted = a.grad != nullptr && a.reduction == GOCKPT_EACH;
+    int32_t mine = 0;
+    float most = 0.0f;
+#pragma unroll 4
+    for (int64_t t = from + lane; t < to; t += 64) {
+        if (!counts(a, target_of(a, static_cast<int32_t>(t)))) continue;
+        ++mine;
+        if (weighted) most = fmaxf(most, fabsf(a.grad[t]));
+    }
+    for (int d = 32; d > 0; d >>= 1) {
+        mine += __shfl_xor(mine, d);
+        most = fmaxf(most, __shfl_xor(most, d));
+    }
+    if (lane == 0) {
+        counted[wave] = mine;
+        largest[wave] = most;
+    }
+    __syncthreads();
+    int32_t before = 0, all = 0;
+    for (int w = 0; w < kTokenWaves; ++w) {
+        if (w < wave) before += counted[w];
+        all += counted[w];
+        most = fmaxf(most, largest[w]);
+    }
+    float g = 0.0f, up_by = 1.0f;
+    if (a.grad != nullptr) {
+        if (!weighted) {
+            g = a.grad[0];
+            if (a.reduction == GOCKPT_MEAN) g = g / static_cast<float>(max(all, 1));
+            most = fabsf(g);
+        }
+        // no power of two makes infinities or NaN finite: they go through
+        int q = 0;
+        if (most > 0.0f && most <= 3.402823466e38f) q = max(ilogbf(most), -100);
+        up_by = ldexpf(1.0f, 13 - q);
+        if (threadIdx.x == 0) *a.unscale = ldexpf(1.0f, q - 13);
+    }
+    if (threadIdx.x == 0) {
+        *a.count = all;
+        if (a.ticket != nullptr) *a.ticket = 0;
+    }
+    for (int64_t at = from; at < to; at += 64) {
+        const int64_t t = at + lane;
+        const int64_t id = t < to ? target_of(a, static_cast<int32_t>(t)) : 0;
+        const bool there = t < to && counts(a, id);
+        const uint64_t votes = __ballot(there);
+        const int32_t k = before + __popcll(votes & ((uint64_t{1} << lane) - 1));
+        before += __popcll(votes);
+        if (there) {
+            const int64_t row = id - a.first;
+            a.of_kept[k] = static_cast<int32_t>(t);
+            a.target[k] = row >= 0 && row < a.rows ? static_cast<int32_t>(row) : -1;
+            if (a.grad != nullptr) {
+                a.base[k] = a.lse_in[t] * static_cast<float>(kLog2e);
+                a.factor[k] = (weighted ? a.grad[t] : g) * up_by;
+            }
+        } else if (t < to) {
+            if (a.lse != nullptr) a.lse[t] = 0.0f;
+            if (a.logit != nullptr) a.logit[t] = 0.0f;
+            if (a.loss != nullptr && a.reduction == GOCKPT_EACH) a.loss[t] = 0.0f;
+        }
+        if (t < to && a.of_token != nullptr) a.of_token[t] = there ? k : -1;
+    }
+}
+
+// ---- the loss ---------------------------------------------------------------------
+
+struct LossArgs {
+    MmaArgs a;       // R: the table, C: the hidden rows that count
+    float log2_scale;  // scale log2(e)
+    const int32_t* target;
+    float2* part;    // token k's largest l2 and sum in tile r at k * tiles_r + r
+    float* logit;    // l2 of its target
+};
+
+template <class M>
+__global__ __launch_bounds__(M::kThreads) void logits_kernel(LossArgs g) {
+    GOCKPT_MMA_LDS(M)
+    const MmaPlace p = mma_place(g.a, M::kBR, M::kBC);
+    const int cn = *g.a.cn_dev;
+    if (p.c0 >= cn) return;
+    typename M::Acc acc;
+    GOCKPT_MMA_RUN(M, g.a, p, cn, g.a.k, acc);
+    __syncthreads();  // the buffers are free
+    float2(*waves)[M::kBC] = reinterpret_cast<float2(*)[M::kBC]>(lr0);
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+#pragma unroll
+    for (int j = 0; j < M::kFC; ++j) {
+        const int c = M::c_of(p, j);
+        const int want = c < cn ? g.target[c] : -1;
+        float most = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < M::kFR; ++i) {
+            const int r = M::r_of(p, i), left = g.a.rn - r, at = want - r;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int to = 8 * (e / 4) + e % 4;
+                const float l = acc[i][j][e] * g.log2_scale;
+                acc[i][j][e] = to < left ? l : -INFINITY;
+                most = fmaxf(most, acc[i][j][e]);
+                if (at == to && c < cn) g.logit[c] = l;
+            }
+        }
+        most = fmaxf(most, __shfl_xor(most, 32));
+        // a row of nothing but -inf keeps a sum of 0
+        const float from = most == -INFINITY ? 0.0f : most;
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < M::kFR; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f(acc[i][j][e] - from);
+        sum += __shfl_xor(sum, 32);
+        if (lane < 32) waves[wave / M::kWC][(wave % M::kWC * M::kFC + j) * 32 + lane] = float2{most, sum};
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < M::kBC; i += M::kThreads) {
+        if (p.c0 + i >= cn) break;
+        float most = -INFINITY, sum = 0.0f;
+#pragma unroll
+        for (int w = 0; w < M::kWR; ++w) most = fmaxf(most, waves[w][i].x);
+        const float from = most == -INFINITY ? 0.0f : most;
+#pragma unroll
+        for (int w = 0; w < M::kWR; ++w) sum += waves[w][i].y * __builtin_amdgcn_exp2f(waves[w][i].x - from);
+        g.part[static_cast<int64_t>(p.c0 + i) * g.a.tiles_r + p.tile_r] = float2{most, sum};
+    }
+}
+
+struct JoinArgs {
+    const float2* part;
+    const int32_t *count, *of_kept, *target;
+    const float* logit2;
+    uint32_t tiles_r;
+    int32_t reduction;
+    float *lse, *logit, *loss;
+    float* each;  // the tokens' losses, for their sum
+    uint32_t* ticket;
+};
+
+// A wavefront a token.  For a sum, the block that ends last adds up the tokens'
+// losses, in an order that is the same on every call.
+__global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
+    const int lane = threadIdx.x & 63;
+    const int32_t count = *a.count;
+    const bool single = a.reduction == GOCKPT_EACH;
+    for (int32_t k = blockIdx.x * 4 + (threadIdx.x >> 6); k < count; k += gridDim.x * 4) {
+        const float2* p = a.part + static_cast<int64_t>(k) * a.tiles_r;
+        float most = -INFINITY, sum = 0.0f;
+        for (uint32_t i = lane; i < a.tiles_r; i += 64) {
+            const float2 x = p[i];
+            const float top = fmaxf(most, x.x), from = top == -INFINITY ? 0.0f : top;
+            sum = sum * __builtin_amdgcn_exp2f(most - from) + x.y * __builtin_amdgcn_exp2f(x.x - from);
+            most = top;
+        }
+        float top = most;
+        for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+        const float from = top == -INFINITY ? 0.0f : top;
+        sum *= __builtin_amdgcn_exp2f(most - from);
+        for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+        if (lane == 0) {
+            const int32_t t = a.of_kept[k];
+            const float log2_sum = __builtin_amdgcn_logf(sum);
+            const float logit2 = a.target[k] >= 0 ? a.logit2[k] : 0.0f;
+            if (a.lse != nullptr) a.lse[t] = (from + log2_sum) * kLn2;
+            if (a.logit != nullptr) a.logit[t] = logit2 * kLn2;
+            const float loss = (from - logit2 + log2_sum) * kLn2;
+            if (a.loss != nullptr) {
+                if (single)
+                    a.loss[t] = loss;
+                else
+                    a.each[k] = loss;
+            }
+        }
+    }
+    if (single || a.loss == nullptr) return;
+    __shared__ uint32_t last;
+    __shared__ double sums[4];
+    __syncthreads();
+    if (threadIdx.x == 0)
+        last = __hip_atomic_fetch_add(a.ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
+    __syncthreads();
+    if (!last) return;
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+    double total = 0.0;
+    for (int32_t k = threadIdx.x; k < count; k += 256) total += static_cast<double>(a.each[k]);
+    for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d);
+    if (lane == 0) sums[threadIdx.x >> 6] = total;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    total = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+    *a.loss = static_cast<float>(a.reduction == GOCKPT_MEAN ? total / max(count, 1) : total);
+}
+
+// ---- the gradients ------------------------------------------------------------------
+
+struct GradArgs {
+    MmaArgs a;       // R: the piece's rows of the table, C: the hidden rows that count
+    float log2_scale;
+    const int32_t* target;
+    int32_t first;   // the piece's first row
+    const float *base, *factor;
+    uint8_t* z;      // token k's row at z + k * z_stride
+    int64_t z_stride;
+    float* lost;     // what rounding took from the target's z
+};
+
+template <class M>
+__global__ __launch_bounds__(M::kThreads) void z_kernel(GradArgs g) {
+    GOCKPT_MMA_LDS(M)
+    const MmaPlace p = mma_place(g.a, M::kBR, M::kBC);
+    const int cn = *g.a.cn_dev;
+    if (p.c0 >= cn) return;
+    typename M::Acc acc;
+    GOCKPT_MMA_RUN(M, g.a, p, cn, g.a.k, acc);
+    const int wide = (g.a.rn + 7) / 8 * 8;  // the products read whole pieces of 8: zeros behind the last row
+#pragma unroll
+    for (int j = 0; j < M::kFC; ++j) {
+        const int c = M::c_of(p, j);
+        if (c >= cn) continue;
+        const float base = g.base[c], factor = g.factor[c];
+        const int want = g.target[c] - g.first;
+        uint8_t* row = g.z + c * g.z_stride;
+#pragma unroll
+        for (int i = 0; i < M::kFR; ++i) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int r = M::r_of(p, i) + 8 * q;
+                if (r >= wide) continue;
+                float z[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    z[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][4 * q + e], g.log2_scale, -base));
+                    if (want == r + e) {
+                        z[e] = (z[e] - 1.0f) * factor;
+                        g.lost[c] = z[e] - elem_to_f32<M::kT>(pack2<M::kT>(z[e], z[e]) & 0xffff);
+                    } else {
+                        z[e] = r + e < g.a.rn ? z[e] * factor : 0.0f;
+                    }
+                }
+                *reinterpret_cast<u32x2*>(row + r * 2) = u32x2{pack2<M::kT>(z[0], z[1]), pack2<M::kT>(z[2], z[3])};
+            }
+        }
+    }
+}
+
+// ---- host ---------------------------------------------------------------------------
+
+constexpr int64_t kPieceBytes = int64_t{256} << 20;  // of Z: what the last-level cache holds
+constexpr int64_t kSliceBytes = int64_t{256} << 20;  // of dX's fp32 sums, where one slice is less
+
+template <int kT>
+void start_logits(int shape, const LossArgs& g, hipStream_t s) {
+    const dim3 grid(g.a.tiles_r * g.a.tiles_c);
+    using W = Mma<kT, kAlongK, kAlongK, 256, 256, 2, 4>;
+    using D = Mma<kT, kAlongK, kAlongK, 128, 128, 2, 2>;
+    using T = Mma<kT, kAlongK, kAlongK, 128, 32, 4, 1>;
+    if (shape == kWide)
+        hipLaunchKernelGGL(logits_kernel<W>, grid, dim3(W::kThreads), 0, s, g);
+    else if (shape == kMid)
+        hipLaunchKernelGGL(logits_kernel<D>, grid, dim3(D::kThreads), 0, s, g);
+    else
+        hipLaunchKernelGGL(logits_kernel<T>, grid, dim3(T::kThreads), 0, s, g);
+}
+
+template <int kT>
+void start_z(int shape, const GradArgs& g, hipStream_t s) {
+    const dim3 grid(g.a.tiles_r * g.a.tiles_c);
+    using W = Mma<kT, kAlongK, kAlongK, 256, 256, 2, 4>;
+    using D = Mma<kT, kAlongK, kAlongK, 128, 128, 2, 2>;
+    using T = Mma<kT, kAlongK, kAlongK, 128, 32, 4, 1>;
+    if (shape == kWide)
+        hipLaunchKernelGGL(z_kernel<W>, grid, dim3(W::kThreads), 0, s, g);
+    else if (shape == kMid)
+        hipLaunchKernelGGL(z_kernel<D>, grid, dim3(D::kThreads), 0, s, g);
+    else
+        hipLaunchKernelGGL(z_kernel<T>, grid, dim3(T::kThreads), 0, s, g);
+}
+
+void place_tiles(MmaArgs& a, const ProductPlan& p) {
+    a.tiles_r = p.tiles_r;
+    a.tiles_c = p.tiles_c;
+    a.splits = 1;
+    a.split_k = p.split_k;
+}
+
+int check_head(const char* name, const gockpt_head* h, TokenArgs* t) {
+    if (h == nullptr) return ops_fail(GOCKPT_EINVAL, "%s: null head", name);
+    int rc = check_model_matrix(name, "hidden", &h->hidden, kHalfTypes);
+    if (rc == GOCKPT_OK) rc = check_model_matrix(name, "table", &h->table, kHalfTypes);
+    if (rc != GOCKPT_OK) return rc;
+    if (h->hidden.dtype != h->table.dtype)
+        return ops_fail(GOCKPT_EINVAL, "%s: hidden of dtype %d, table of %d", name, h->hidden.dtype, h->table.dtype);
+    if (h->hidden.cols != h->table.cols)
+        return ops_fail(GOCKPT_EINVAL, "%s: hidden of %lld columns, table of %lld", name,
+                        static_cast<long long>(h->hidden.cols), static_cast<long long>(h->table.cols));
+    const gockpt_token_ids& y = h->targets;
+    if (y.batch < 0 || y.length < 0 || y.batch > kMaxExtent || y.length > kMaxExtent ||
+        y.batch * y.length > kMaxExtent)
+        return ops_fail(GOCKPT_EINVAL, "%s: %lld x %lld targets", name, static_cast<long long>(y.batch),
+                        static_cast<long long>(y.length));
+    const int64_t n = y.batch * y.length;
+    if (n != h->hidden.rows)
+        return ops_fail(GOCKPT_EINVAL, "%s: %lld targets, %lld rows of hidden", name, static_cast<long long>(n),
+                        static_cast<long long>(h->hidden.rows));
+    if (y.batch > 1 && (y.stride < y.length || y.stride > int64_t{1} << 31))
+        return ops_fail(GOCKPT_EINVAL, "%s: targets stride %lld for sequences of %lld", name,
+                        static_cast<long long>(y.stride), static_cast<long long>(y.length));
+    if (y.bits != 32 && y.bits != 64) return ops_fail(GOCKPT_EINVAL, "%s: targets of %d bits", name, y.bits);
+    if (n > 0 && (y.ids == nullptr || reinterpret_cast<uintptr_t>(y.ids) % (y.bits / 8) != 0))
+        return ops_fail(GOCKPT_EINVAL, "%s: targets are null or not aligned", name);
+    if (h->classes < 0 || (h->classes > 0 && (y.first_id < 0 || y.first_id > h->classes - h->table.rows)))
+        return ops_fail(GOCKPT_EINVAL, "%s: rows %lld to %lld of %lld classes", name,
+                        static_cast<long long>(y.first_id), static_cast<long long>(y.first_id + h->table.rows),
+                        static_cast<long long>(h->classes));
+    if (y.first_id > INT64_MAX - kMaxExtent)
+        return ops_fail(GOCKPT_EINVAL, "%s: first_id %lld", name, static_cast<long long>(y.first_id));
+    if (t != nullptr) {
+        t->ids = y.ids;
+        t->length = static_cast<int32_t>(y.length);
+        t->stride = y.batch > 1 ? y.stride : y.length;
+        t->first = y.first_id;
+        t->low = h->classes > 0 ? 0 : y.first_id;
+        t->high = h->classes > 0 ? h->classes : y.first_id + h->table.rows;
+        t->ignore = h->ignore_id;
+        t->tokens = static_cast<int32_t>(n);
+        t->rows = static_cast<int32_t>(h->table.rows);
+        t->wide = y.bits == 64;
+    }
+    return GOCKPT_OK;
+}
+
+int check_reduction(const char* name, int r) {
+    if (r < GOCKPT_EACH || r > GOCKPT_MEAN) return ops_fail(GOCKPT_EINVAL, "%s: reduction %d", name, r);
+    return GOCKPT_OK;
+}
+
+// Rows that count are taken by their numbers where offsets from the first one
+// stay within 32 bits.
+bool hidden_in_place(const gockpt_matrix& x) {
+    return in_place(x) && (x.rows <= 1 || x.rows * x.stride * 2 < (int64_t{1} << 32));
+}
+
+struct LossPlan {
+    ProductPlan logits;
+    size_t count, of_kept, target, part, logit2, each, hidden, table, bytes;
+};
+
+LossPlan plan_loss(const gockpt_head& h) {
+    LossPlan p{};
+    Parts parts;
+    const int64_t n = h.hidden.rows;
+    p.logits = plan_product(kAlongAlong, h.table.rows, n, h.table.cols, 1);
+    p.count = parts.take(8);  // and the ticket
+    p.of_kept = parts.take(n * 4);
+    p.target = parts.take(n * 4);
+    p.part = parts.take(n * p.logits.tiles_r * 8);
+    p.logit2 = parts.take(n * 4);
+    p.each = parts.take(n * 4);
+    p.hidden = parts.take(hidden_in_place(h.hidden) ? 0 : n * up(h.hidden.cols, 8) * 2);
+    p.table = parts.take(copy_bytes(h.table));
+    p.bytes = parts.bytes;
+    return p;
+}
+
+// One piece of the vocabulary: Z, dX and dW of so many rows.
+struct Piece {
+    ProductPlan z, by_hidden, by_table;
+};
+
+struct GradPlan {
+    int64_t piece;   // rows of the table in a piece
+    Piece full, rest;
+    size_t count, unscale, of_kept, target, of_token, base, factor, lost, hidden, table, z, slices_hidden, slices_table, bytes;
+    int64_t z_stride;
+};
+
+Piece plan_piece(int64_t tokens, int64_t rows, int64_t cols, bool by_hidden, bool by_table, int most_hidden) {
+    Piece p{};
+    p.z = plan_product(kAlongAlong, rows, tokens, cols, 1);
+    if (by_hidden) p.by_hidden = plan_product(kAcrossAlong, cols, tokens, rows, most_hidden);
+    if (by_table) p.by_table = plan_product(kAcrossAcross, cols, rows, tokens, 64);
+    return p;
+}
+
+GradPlan plan_grad(const gockpt_head& h, bool by_hidden, bool by_table) {
+    GradPlan p{};
+    Parts parts;
+    const int64_t n = h.hidden.rows, rows = h.table.rows, cols = h.table.cols;
+    const int most_hidden = static_cast<int>(
+        std::max<int64_t>(1, std::min<int64_t>(64, kSliceBytes / std::max<int64_t>(1, n * cols * 4))));
+    const auto cost = [&](int64_t r) {
+        const Piece x = plan_piece(n, r, cols, by_hidden, by_table, most_hidden);
+        // dX's sums are read and written once a piece
+        return x.z.us + x.by_hidden.us + x.by_table.us +
+               (by_hidden ? static_cast<double>(n) * static_cast<double>(cols) * 8.0 / 4.5e6 : 0.0);
+    };
+    const int64_t most = std::max<int64_t>(256, kPieceBytes / std::max<int64_t>(1, n * 2) / 256 * 256);
+    p.piece = std::max<int64_t>(rows, 1);
+    if (rows > most) {
+        // tiles run in rounds: pieces whose tiles fill them, the rest's too
+        const int64_t step = std::max<int64_t>(256, most / 32 / 256 * 256);
+        double least = -1.0;
+        for (int64_t r = most; r >= 256 && r >= most / 2; r -= step) {
+            const int64_t whole = rows / r, rest = rows % r;
+            const double us = static_cast<double>(whole) * cost(r) + (rest > 0 ? cost(rest) : 0.0);
+            if (least < 0.0 || us < least) {
+                least = us;
+                p.piece = r;
+            }
+        }
+    }
+    const int64_t rest = rows % p.piece;
+    p.full = plan_piece(n, std::min(p.piece, rows), cols, by_hidden, by_table, most_hidden);
+    p.rest = rest > 0 ? plan_piece(n, rest, cols, by_hidden, by_table, p.full.by_hidden.splits) : p.full;
+    p.z_stride = up(p.piece, 64) * 2;
+    p.count = parts.take(4);
+    p.unscale = parts.take(4);
+    p.of_kept = parts.take(n * 4);
+    p.target = parts.take(n * 4);
+    p.of_token = parts.take(n * 4);
+    p.base = parts.take(n * 4);
+    p.factor = parts.take(n * 4);
+    p.lost = parts.take(n * 4);
+    p.hidden = parts.take(n * up(cols, 8) * 2);
+    p.table = parts.take(copy_bytes(h.table));
+    p.z = parts.take(n * p.z_stride);
+    if (by_hidden) p.slices_hidden = parts.take(p.full.by_hidden.splits * n * cols * 4);
+    if (by_table) {
+        const auto bytes = [&](const ProductPlan& x, int64_t r) { return x.splits > 1 ? x.splits * r * cols * 4 : 0; };
+        p.slices_table = parts.take(std::max(bytes(p.full.by_table, std::min(p.piece, rows)), bytes(p.rest.by_table, rest)));
+    }
+    p.bytes = parts.bytes;
+    return p;
+}
+
+int check_grads(const char* name, const gockpt_head* h, const gockpt_matrix* gx, const gockpt_matrix* gw) {
+    if (gx != nullptr) {
+        const int rc = check_model_matrix(name, "grad_hidden", gx, kAnyType);
+        if (rc != GOCKPT_OK) return rc;
+        if (gx->rows != h->hidden.rows || gx->cols != h->hidden.cols)
+            return ops_fail(GOCKPT_EINVAL, "%s: grad_hidden of %lld x %lld", name, static_cast<long long>(gx->rows),
+                            static_cast<long long>(gx->cols));
+    }
+    if (gw != nullptr) {
+        const int rc = check_model_matrix(name, "grad_table", gw, kAnyType);
+        if (rc != GOCKPT_OK) return rc;
+        if (gw->rows != h->table.rows || gw->cols != h->table.cols)
+            return ops_fail(GOCKPT_EINVAL, "%s: grad_table of %lld x %lld", name, static_cast<long long>(gw->rows),
+                            static_cast<long long>(gw->cols));
+    }
+    return GOCKPT_OK;
+}
+
+}  // namespace
+
+}  // namespace gockpt
+
+using namespace gockpt;
+
+extern "C" {
+
+int gockpt_head_loss_bytes(const gockpt_head* head, size_t* bytes) {
+    const char* name = "gockpt_head_loss_bytes";
+    if (bytes == nullptr) return ops_fail(GOCKPT_EINVAL, "%s: null argument", name);
+    *bytes = 0;
+    const int rc = check_head(name, head, nullptr);
+    if (rc == GOCKPT_OK) *bytes = plan_loss(*head).bytes;
+    return rc;
+}
+
+int gockpt_head_loss(const gockpt_head* head, int reduction, float* loss, float* lse, float* logit, void* workspace,
+                     size_t workspace_bytes, void* stream) {
+    const char* name = "gockpt_head_loss";
+    TokenArgs t{};
+    int rc = check_head(name, head, &t);
+    if (rc == GOCKPT_OK) rc = check_reduction(name, reduction);
+    if (rc == GOCKPT_OK && loss != nullptr && head->classes > 0)
+        rc = ops_fail(GOCKPT_EINVAL, "%s: the loss of a range of the classes", name);
+    for (const float* p : {loss, lse, logit})
+        if (rc == GOCKPT_OK && reinterpret_cast<uintptr_t>(p) % 4 != 0)
+            rc = ops_fail(GOCKPT_EINVAL, "%s: an output is not aligned", name);
+    if (rc != GOCKPT_OK) return rc;
+    const LossPlan p = plan_loss(*head);
+    rc = check_workspace(name, workspace, workspace_bytes, p.bytes);
+    if (rc != GOCKPT_OK) return rc;
+    if (loss == nullptr && lse == nullptr && logit == nullptr) return GOCKPT_OK;
+    if (t.tokens == 0 && (loss == nullptr || reduction == GOCKPT_EACH)) return GOCKPT_OK;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    t.reduction = reduction;
+    t.count = reinterpret_cast<int32_t*>(ws + p.count);
+    t.ticket = reinterpret_cast<uint32_t*>(ws + p.count + 4);
+    t.of_kept = reinterpret_cast<int32_t*>(ws + p.of_kept);
+    t.target = reinterpret_cast<int32_t*>(ws + p.target);
+    t.lse = lse;
+    t.logit = logit;
+    t.loss = loss;
+    hipLaunchKernelGGL(token_kernel, dim3(1), dim3(kTokenThreads), 0, s, t);
+    LossArgs g{};
+    const Source table = source_of(head->table, ws + p.table, s);
+    g.a.r = table.data;
+    g.a.r_stride = table.stride;
+    if (hidden_in_place(head->hidden)) {
+        g.a.c = static_cast<const uint8_t*>(head->hidden.data);
+        g.a.c_stride = (head->hidden.rows > 1 ? head->hidden.stride : head->hidden.cols) * 2;
+        g.a.c_rows = t.of_kept;
+    } else {
+        launch_rows(head->hidden, t.of_kept, t.count, head->hidden.rows, ws + p.hidden, s);
+        g.a.c = ws + p.hidden;
+        g.a.c_stride = up(head->hidden.cols, 8) * 2;
+    }
+    g.a.rn = t.rows;
+    g.a.cn = t.tokens;
+    g.a.cn_dev = t.count;
+    g.a.k = static_cast<int32_t>(head->table.cols);
+    place_tiles(g.a, p.logits);
+    g.log2_scale = static_cast<float>(static_cast<double>(head->scale) * kLog2e);
+    g.target = t.target;
+    g.part = reinterpret_cast<float2*>(ws + p.part);
+    g.logit = reinterpret_cast<float*>(ws + p.logit2);
+    if (g.a.tiles_r > 0 && g.a.tiles_c > 0) {
+        if (head->table.dtype == kBF16)
+            start_logits<kBF16>(p.logits.shape, g, s);
+        else
+            start_logits<kFP16>(p.logits.shape, g, s);
+    }
+    JoinArgs j{};
+    j.part = g.part;
+    j.count = t.count;
+    j.of_kept = t.of_kept;
+    j.target = t.target;
+    j.logit2 = g.logit;
+    j.tiles_r = g.a.tiles_r;
+    j.reduction = reduction;
+    j.lse = lse;
+    j.logit = logit;
+    j.loss = loss;
+    j.each = reinterpret_cast<float*>(ws + p.each);
+    j.ticket = t.ticket;
+    hipLaunchKernelGGL(join_kernel, dim3(std::max(1, std::min((t.tokens + 3) / 4, kUnits * 4))), dim3(256), 0, s, j);
+    return ops_launched(name);
+}
+
+int gockpt_head_grad_bytes(const gockpt_head* head, const gockpt_matrix* grad_hidden,
+                           const gockpt_matrix* grad_table, size_t* bytes) {
+    const char* name = "gockpt_head_grad_bytes";
+    if (bytes == nullptr) return ops_fail(GOCKPT_EINVAL, "%s: null argument", name);
+    *bytes = 0;
+    int rc = check_head(name, head, nullptr);
+    if (rc == GOCKPT_OK) rc = check_grads(name, head, grad_hidden, grad_table);
+    if (rc == GOCKPT_OK) *bytes = plan_grad(*head, grad_hidden != nullptr, grad_table != nullptr).bytes;
+    return rc;
+}
+
+int gockpt_head_grad(const gockpt_head* head, const float* lse, int reduction, const float* grad,
+                     const gockpt_matrix* grad_hidden, const gockpt_matrix* grad_table, int accumulate,
+                     void* workspace, size_t workspace_bytes, void* stream) {
+    const char* name = "gockpt_head_grad";
+    TokenArgs t{};
+    int rc = check_head(name, head, &t);
+    if (rc == GOCKPT_OK) rc = check_grads(name, head, grad_hidden, grad_table);
+    if (rc == GOCKPT_OK) rc = check_reduction(name, reduction);
+    if (rc == GOCKPT_OK && t.tokens > 0 && (lse == nullptr || grad == nullptr))
+        rc = ops_fail(GOCKPT_EINVAL, "%s: null lse or grad", name);
+    for (const float* p : {lse, grad})
+        if (rc == GOCKPT_OK && reinterpret_cast<uintptr_t>(p) % 4 != 0)
+            rc = ops_fail(GOCKPT_EINVAL, "%s: lse or grad is not aligned", name);
+    if (rc != GOCKPT_OK) return rc;
+    const GradPlan p = plan_grad(*head, grad_hidden != nullptr, grad_table != nullptr);
+    rc = check_workspace(name, workspace, workspace_bytes, p.bytes);
+    if (rc != GOCKPT_OK) return rc;
+    const int64_t rows = head->table.rows, cols = head->table.cols;
+    const bool by_hidden = grad_hidden != nullptr && t.tokens > 0 && cols > 0;
+    const bool by_table = grad_table != nullptr && rows > 0 && cols > 0 && !(accumulate && t.tokens == 0);
+    if (!by_hidden && !by_table) return GOCKPT_OK;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    t.reduction = reduction;
+    t.count = reinterpret_cast<int32_t*>(ws + p.count);
+    t.of_kept = reinterpret_cast<int32_t*>(ws + p.of_kept);
+    t.target = reinterpret_cast<int32_t*>(ws + p.target);
+    t.of_token = reinterpret_cast<int32_t*>(ws + p.of_token);
+    t.lse_in = lse;
+    t.grad = t.tokens > 0 ? grad : nullptr;
+    t.base = reinterpret_cast<float*>(ws + p.base);
+    t.factor = reinterpret_cast<float*>(ws + p.factor);
+    t.unscale = reinterpret_cast<float*>(ws + p.unscale);
+    hipLaunchKernelGGL(token_kernel, dim3(1), dim3(kTokenThreads), 0, s, t);
+    launch_rows(head->hidden, t.of_kept, t.count, t.tokens, ws + p.hidden, s);
+    const Source table = source_of(head->table, ws + p.table, s);
+    const int64_t hidden_stride = up(cols, 8) * 2;
+    const int dtype = head->table.dtype;
+    float* slices = reinterpret_cast<float*>(ws + p.slices_hidden);
+    for (int64_t first = 0; first < rows; first += p.piece) {
+        const int64_t here = std::min(p.piece, rows - first);
+        const Piece& plan = here == p.piece ? p.full : p.rest;
+        if (t.tokens > 0) {
+            GradArgs g{};
+            g.a.r = table.data + first * table.stride;
+            g.a.r_stride = table.stride;
+            g.a.c = ws + p.hidden;
+            g.a.c_stride = hidden_stride;
+            g.a.rn = static_cast<int32_t>(here);
+            g.a.cn = t.tokens;
+            g.a.cn_dev = t.count;
+            g.a.k = static_cast<int32_t>(cols);
+            place_tiles(g.a, plan.z);
+            g.log2_scale = static_cast<float>(static_cast<double>(head->scale) * kLog2e);
+            g.target = t.target;
+            g.first = static_cast<int32_t>(first);
+            g.base = t.base;
+            g.factor = t.factor;
+            g.z = ws + p.z;
+            g.z_stride = p.z_stride;
+            g.lost = reinterpret_cast<float*>(ws + p.lost);
+            if (dtype == kBF16)
+                start_z<kBF16>(plan.z.shape, g, s);
+            else
+                start_z<kFP16>(plan.z.shape, g, s);
+        }
+        if (by_hidden) {
+            MmaArgs a{};
+            a.r = table.data + first * table.stride;
+            a.r_stride = table.stride;
+            a.c = ws + p.z;
+            a.c_stride = p.z_stride;
+            a.rn = static_cast<int32_t>(cols);
+            a.cn = t.tokens;
+            a.cn_dev = t.count;
+            a.k = static_cast<int32_t>(here);
+            StoreArgs o{};
+            o.slices = slices;
+            o.add = first > 0;
+            launch_product(kAcrossAlong, dtype, plan.by_hidden, a, o, s);
+        }
+        if (by_table) {
+            MmaArgs a{};
+            a.r = ws + p.hidden;
+            a.r_stride = hidden_stride;
+            a.c = ws + p.z;
+            a.c_stride = p.z_stride;
+            a.rn = static_cast<int32_t>(cols);
+            a.cn = static_cast<int32_t>(here);
+            a.k = t.tokens;
+            a.k_dev = t.count;
+            const int64_t stride = (rows > 1 ? grad_table->stride : cols) * dtype_bytes(grad_table->dtype);
+            FinishArgs f{};
+            f.out = static_cast<uint8_t*>(const_cast<void*>(grad_table->data)) + first * stride;
+            f.stride = stride;
+            f.dtype = grad_table->dtype;
+            f.accumulate = accumulate != 0;
+            f.alpha = head->scale;
+            f.beta = t.unscale;
+            StoreArgs o{};
+            if (plan.by_table.splits > 1) {
+                o.slices = reinterpret_cast<float*>(ws + p.slices_table);
+                launch_product(kAcrossAcross, dtype, plan.by_table, a, o, s);
+                f.slices = o.slices;
+                f.slice_step = here * cols;
+                f.count = plan.by_table.splits;
+                f.rows = static_cast<int32_t>(here);
+                f.cols = static_cast<int32_t>(cols);
+                launch_finish(f, s);
+            } else {
+                o.out = f.out;
+                o.stride = f.stride;
+                o.dtype = f.dtype;
+                o.accumulate = f.accumulate;
+                o.alpha = f.alpha;
+                o.beta = f.beta;
+                launch_product(kAcrossAcross, dtype, plan.by_table, a, o, s);
+            }
+        }
+    }
+    if (by_hidden) {
+        FinishArgs f{};
+        f.slices = slices;
+        f.slice_step = int64_t{t.tokens} * cols;
+        f.count = rows > 0 ? p.full.by_hidden.splits : 0;
+        f.rows = t.tokens;
+        f.cols = static_cast<int32_t>(cols);
+        f.of_row = t.of_token;
+        f.out = static_cast<uint8_t*>(const_cast<void*>(grad_hidden->data));
+        f.stride = (t.tokens > 1 ? grad_hidden->stride : cols) * dtype_bytes(grad_hidden->dtype);
+        f.dtype = grad_hidden->dtype;
+        f.alpha = head->scale;
+        f.beta = t.unscale;
+        f.fix = reinterpret_cast<const float*>(ws + p.lost);
+        f.fix_row = t.target;
+        f.fix_from = table.data;
+        f.fix_stride = table.stride;
+        f.fix_dtype = dtype;
+        launch_finish(f, s);
+    }
+    return ops_launched(name);
+}
+
+}  // extern "C"

@@ -1,0 +1,505 @@
+// gockpt_mma.h -- the matrix product that the head's loss and the 8-bit linear
+// layers share, on gfx950's matrix cores.
+//
+//   out[c][r] = sum over k of R(r, k) * C(c, k)
+//
+// R's index r runs along the output's rows (its contiguous direction), C's
+// index c counts them.  Each operand is 16 bits wide and lies either with k
+// contiguous (kAlongK: element (i, k) at data + i * stride + k) or with i
+// contiguous (kAcrossK: at data + k * stride + i); kCodes8 is kAcrossK in 8-bit
+// codes with a power-of-two scale for every 32 of them, widened to 16 bits
+// (exactly) on the way into shared memory.
+//
+// One block computes a tile of kBR x kBC over steps of 64 k.  Tiles go from
+// global memory straight into LDS, 16 bytes a lane, into one of two buffers
+// while the other is multiplied.  The copy writes lanes one after another, so
+// the order that keeps LDS reads free of bank conflicts is made by permuting
+// which 16 bytes a lane fetches, and undone by the reads:
+//   kAlongK   rows of 128 bytes, 16-byte piece p of row i at p ^ (i & 7); a
+//             fragment is one 16-byte read a lane.
+//   kAcrossK  rows of k, 32-byte unit u of row k at u ^ f(k & 3), f = 0, 3, 5, 6:
+//             the four rows that a transposing read takes together then lie in
+//             different banks, also where two units are read at once.
+// A fragment of step s + 1 is read while step s is multiplied, across the
+// barrier between two tiles as well: a wave holds the last step's fragments
+// in registers when it passes it.
+#pragma once
+
+#include "gockpt_ops_internal.h"
+
+namespace gockpt {
+
+typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef f32x4 f32x4_any __attribute__((aligned(2)));
+
+enum Lay : int { kAlongK = 0, kAcrossK = 1, kCodes8 = 2 };
+
+constexpr int kStepK = 64;  // k of one LDS tile
+
+#define GOCKPT_LDS __attribute__((address_space(3)))
+
+// What every product is given.  Strides are in bytes.
+struct MmaArgs {
+    const uint8_t* r;
+    const uint8_t* c;
+    int64_t r_stride, c_stride;
+    const uint8_t* scales;   // of kCodes8: one byte for 32 columns of a row of k
+    int64_t scale_stride;
+    int32_t rn, cn;          // extents of r and c
+    int32_t k;               // of k; a multiple of 8 for kAlongK
+    const int32_t* cn_dev;   // the extent of c, or of k, on the device (null: as above);
+    const int32_t* k_dev;    // at most what the field above says
+    const int32_t* c_rows;   // kAlongK: row of C that stands at c (null: c itself)
+    uint32_t tiles_r, tiles_c;
+    int32_t splits, split_k;  // slices of k and their length, a multiple of 64
+};
+
+template <int kT>
+__device__ __forceinline__ f32x16 mma(u32x4 a, u32x4 b, f32x16 c) {
+    if constexpr (kT == kBF16)
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c,
+                                                       0, 0, 0);
+    else
+        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0,
+                                                      0, 0);
+}
+
+__device__ __forceinline__ int unit_swizzle(int k) { return ((k & 3) << 1) | ((k ^ (k >> 1)) & 1); }
+
+template <class T>
+__device__ __forceinline__ T* uniform(T* p) {
+    const uint64_t v = reinterpret_cast<uint64_t>(p);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v));
+    const uint32_t hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(v >> 32));
+    return reinterpret_cast<T*>(static_cast<uint64_t>(hi) << 32 | lo);
+}
+
+// This wave's copies into LDS have landed.
+__device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// The tile of one operand: kB indexes by 64 k, filled by kWaves wavefronts.
+template <int kLay, int kB, int kWaves>
+struct Filler {
+    static constexpr int kPieces = kB / 8 / kWaves;  // copies of 1 KiB a wave makes for a tile
+    static constexpr int kRowLanes = kB / 8;         // kAcrossK: lanes that copy a row of k
+    static_assert(kPieces >= 1, "each wave copies");
+
+    const uint8_t* base;  // of the tile's first index, at k = 0
+    int64_t step;         // bytes from one tile of k to the next
+    uint32_t off[kPieces];
+    uint32_t back[kPieces];  // from off to a place that is there in every tile of k
+    int k_of[kPieces];       // first k of the lane's piece within the tile
+
+    // Tile at index i0 < n of the operand; rows: see MmaArgs.c_rows.
+    __device__ __forceinline__ void init(const uint8_t* data, int64_t stride, int i0, int n, const int32_t* rows,
+                                         int lane, int wave) {
+        if constexpr (kLay == kAlongK) {
+            base = uniform(rows != nullptr ? data : data + static_cast<int64_t>(i0) * stride);
+            step = 2 * kStepK;
+            const int piece = (lane & 7) ^ (lane >> 3);
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) {
+                const int i = min((j * kWaves + wave) * 8 + (lane >> 3), n - 1 - i0);
+                const uint32_t row = rows != nullptr ? static_cast<uint32_t>(rows[i0 + i]) : static_cast<uint32_t>(i);
+                off[j] = row * static_cast<uint32_t>(stride) + piece * 16;
+                back[j] = piece * 16;
+                k_of[j] = piece * 8;
+            }
+        } else {
+            base = uniform(data + static_cast<int64_t>(i0) * 2);
+            step = stride * kStepK;
+            constexpr int kRows = 64 / kRowLanes;  // rows of k in one copy
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) {
+                const int k = (j * kWaves + wave) * kRows + lane / kRowLanes;
+                const int at = lane % kRowLanes;
+                int piece = ((at >> 1) ^ (unit_swizzle(k) & (kRowLanes / 2 - 1))) * 2 + (at & 1);
+                if (i0 + piece * 8 >= n) piece = 0;
+                back[j] = static_cast<uint32_t>(k) * static_cast<uint32_t>(stride);
+                off[j] = back[j] + piece * 16;
+                k_of[j] = k;
+            }
+        }
+    }
+
+    // Starts the copies of the tile of k that begins at tile * 64; `left` k
+    // are there (64 or more: all).
+    __device__ __forceinline__ void fill(GOCKPT_LDS uint8_t* lds, int tile, int left, int wave) {
+        __amdgpu_buffer_rsrc_t res = __builtin_amdgcn_make_buffer_rsrc(
+            const_cast<uint8_t*>(base + static_cast<int64_t>(tile) * step), 0, 0xffffffff, 0x00027000);
+        if (left >= kStepK) {
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(res, (GOCKPT_LDS void*)(lds + (j * kWaves + wave) * 1024), 16,
+                                                         off[j], 0, 0, 0);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(res, (GOCKPT_LDS void*)(lds + (j * kWaves + wave) * 1024), 16,
+                                                         k_of[j] < left ? off[j] : off[j] - back[j], 0, 0, 0);
+        }
+    }
+
+    // Zeros in place of what the wave copied beyond the last k, once landed.
+    __device__ __forceinline__ void clear(GOCKPT_LDS uint8_t* lds, int left, int lane, int wave) {
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j)
+            if (k_of[j] >= left)
+                *reinterpret_cast<GOCKPT_LDS u32x4*>(lds + (j * kWaves + wave) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
+    }
+
+    __device__ __forceinline__ void land(GOCKPT_LDS uint8_t* lds, int left, int lane, int wave) {
+        if (left < kStepK) clear(lds, left, lane, wave);
+    }
+};
+
+// 8-bit codes pass through registers: each thread takes the 32 codes of one
+// scale, and writes them widened when the tile is to land.
+template <int kT, int kB, int kWaves>
+struct Filler8 {
+    static constexpr int kBlocks = kB / 32;  // scales in a row of the tile
+    static_assert(kBlocks * kStepK == kWaves * 64, "a scale a thread");
+
+    const uint8_t* codes;
+    const uint8_t* scales;
+    int64_t step, scale_step;
+    int k, block;
+    u32x4 held[2];
+    uint32_t scale;
+
+    __device__ __forceinline__ void init(const MmaArgs& a, int i0, int thread) {
+        k = thread / kBlocks;
+        block = thread % kBlocks;
+        const int from = i0 + block * 32 < a.rn ? i0 + block * 32 : i0;
+        codes = a.r + k * a.r_stride + from;
+        scales = a.scales + k * a.scale_stride + from / 32;
+        step = a.r_stride * kStepK;
+        scale_step = a.scale_stride * kStepK;
+    }
+
+    __device__ __forceinline__ void fill(int tile, int left) {
+        if (k < left) {
+            const u32x4* p = reinterpret_cast<const u32x4*>(codes + tile * step);
+            held[0] = p[0];
+            held[1] = p[1];
+            scale = scales[tile * scale_step];
+        } else {
+            held[0] = held[1] = u32x4{0, 0, 0, 0};
+            scale = 1;
+        }
+    }
+
+    __device__ __forceinline__ void land(GOCKPT_LDS uint8_t* lds) {
+        // a scale of 255 stands for what is no number
+        const float s = __uint_as_float(scale << 23 | (scale == 255 ? 0x400000u : 0u));
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint32_t w[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t x = held[h][i];
+                const float f0 = static_cast<float>(static_cast<int8_t>(x)) * s;
+                const float f1 = static_cast<float>(static_cast<int8_t>(x >> 8)) * s;
+                const float f2 = static_cast<float>(static_cast<int8_t>(x >> 16)) * s;
+                const float f3 = static_cast<float>(static_cast<int8_t>(x >> 24)) * s;
+                w[2 * i] = pack2<kT>(f0, f1);
+                w[2 * i + 1] = pack2<kT>(f2, f3);
+            }
+            const int unit = (block * 2 + h) ^ (unit_swizzle(k) & (kB / 16 - 1));
+            GOCKPT_LDS u32x4* to = reinterpret_cast<GOCKPT_LDS u32x4*>(lds + k * (2 * kB) + unit * 32);
+            to[0] = u32x4{w[0], w[1], w[2], w[3]};
+            to[1] = u32x4{w[4], w[5], w[6], w[7]};
+        }
+    }
+};
+
+// Fragments of 32 indexes by 16 k: lane l holds index l & 31, k 8 * (l >> 5) on.
+template <int kLay, int kB>
+struct Reader {
+    uint32_t at[4];  // kAlongK: of each step's piece; kAcrossK: of index blocks 0 to 3
+
+    __device__ __forceinline__ void init(int first, int lane) {
+        if constexpr (kLay == kAlongK) {
+#pragma unroll
+            for (int s = 0; s < 4; ++s)
+                at[s] = (first + (lane & 31)) * 128 + (((2 * s + (lane >> 5)) ^ (lane & 7)) << 4);
+        } else {
+            const int t = lane & 15, k = (lane >> 5) * 8 + (t >> 2);
+            const int f = unit_swizzle(t >> 2) & (kB / 16 - 1);
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+                at[b] = k * (2 * kB) + (((first + 32 * b) / 16 + ((lane >> 4) & 1)) ^ f) * 32 + (t & 3) * 8;
+        }
+    }
+
+    // Index block b (32 indexes from first on), k step s.
+    __device__ __forceinline__ u32x4 read(const GOCKPT_LDS uint8_t* lds, int b, int s) const {
+        if constexpr (kLay == kAlongK) {
+            return *reinterpret_cast<const GOCKPT_LDS u32x4*>(lds + at[s] + b * 32 * 128);
+        } else {
+            GOCKPT_LDS s16x4* p = (GOCKPT_LDS s16x4*)(lds + at[b] + s * 16 * (2 * kB));
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(p);
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(p + 4 * (2 * kB) / 8);
+            const u32x2 a = __builtin_bit_cast(u32x2, lo), c = __builtin_bit_cast(u32x2, hi);
+            return u32x4{a.x, a.y, c.x, c.y};
+        }
+    }
+};
+
+// Tile of r0.. x c0.. that a block computes, and its slice of k.
+struct MmaPlace {
+    int r0, c0, split;
+    uint32_t tile_r;
+};
+
+// Blocks go to the 8 XCDs in turn; each XCD takes one run of tiles, in groups
+// of 8 tiles of c, so that the blocks that run on it together read few
+// different tiles and find the others' in its L2.
+__device__ __forceinline__ MmaPlace mma_place(const MmaArgs& a, int br, int bc) {
+    const uint32_t n = a.tiles_r * a.tiles_c, all = n * a.splits;
+    uint32_t id = blockIdx.x;
+    const uint32_t each = all / 8, over = all % 8, xcd = id % 8, at = id / 8;
+    id = xcd * each + min(xcd, over) + at;
+    const uint32_t split = id / n;
+    id -= split * n;
+    const uint32_t group = id / (8 * a.tiles_r), first = group * 8;
+    const uint32_t wide = min(a.tiles_c - first, 8u);
+    id -= group * 8 * a.tiles_r;
+    MmaPlace p;
+    p.tile_r = id / wide;
+    p.r0 = static_cast<int>(p.tile_r) * br;
+    p.c0 = static_cast<int>(first + id % wide) * bc;
+    p.split = static_cast<int>(split);
+    return p;
+}
+
+template <int kT_, int kRLay, int kCLay, int kBR_, int kBC_, int kWR_, int kWC_>
+struct Mma {
+    static constexpr int kT = kT_, kBR = kBR_, kBC = kBC_, kWR = kWR_, kWC = kWC_;
+    static constexpr int kWaves = kWR * kWC, kThreads = kWaves * 64;
+    static constexpr int kFR = kBR / kWR / 32, kFC = kBC / kWC / 32;  // fragments of a wave
+    static constexpr int kRBytes = kBR * kStepK * 2, kCBytes = kBC * kStepK * 2;
+    static_assert(kFR >= 1 && kFC >= 1 && kFR <= 4 && kFC <= 4, "fragments of a wave");
+
+    using Acc = f32x16[kFR][kFC];
+
+    struct State {
+        Filler<kRLay == kCodes8 ? kAcrossK : kRLay, kBR, kWaves> fr;
+        Filler8<kT, kRLay == kCodes8 ? kBR : kWaves * 32, kWaves> fr8;
+        Filler<kCLay, kBC, kWaves> fc;
+        Reader<kRLay == kCodes8 ? kAcrossK : kRLay, kBR> rr;
+        Reader<kCLay, kBC> rc;
+        int lane, wave, k;
+    };
+
+    static __device__ __forceinline__ void fill(State& st, GOCKPT_LDS uint8_t* r, GOCKPT_LDS uint8_t* c, int tile) {
+        const int left = st.k - tile * kStepK;
+        if constexpr (kRLay == kCodes8)
+            st.fr8.fill(tile, left);
+        else
+            st.fr.fill(r, tile, left, st.wave);
+        st.fc.fill(c, tile, left, st.wave);
+    }
+
+    // The tile's copies have landed for all waves; nobody reads the other buffer any more.
+    static __device__ __forceinline__ void land(State& st, GOCKPT_LDS uint8_t* r, GOCKPT_LDS uint8_t* c, int tile) {
+        const int left = st.k - tile * kStepK;
+        wait_copies();
+        if constexpr (kRLay == kCodes8)
+            st.fr8.land(r);
+        else
+            st.fr.land(r, left, st.lane, st.wave);
+        st.fc.land(c, left, st.lane, st.wave);
+        __syncthreads();
+    }
+
+    struct Frags {
+        u32x4 r[kFR], c[kFC];
+    };
+
+    static __device__ __forceinline__ void read(const State& st, Frags& f, const GOCKPT_LDS uint8_t* r,
+                                                const GOCKPT_LDS uint8_t* c, int s) {
+#pragma unroll
+        for (int j = 0; j < kFC; ++j) f.c[j] = st.rc.read(c, j, s);
+#pragma unroll
+        for (int i = 0; i < kFR; ++i) f.r[i] = st.rr.read(r, i, s);
+    }
+
+    static __device__ __forceinline__ void multiply(const Frags& f, Acc& acc) {
+#pragma unroll
+        for (int i = 0; i < kFR; ++i)
+#pragma unroll
+            for (int j = 0; j < kFC; ++j) acc[i][j] = mma<kT>(f.r[i], f.c[j], acc[i][j]);
+    }
+
+    // One tile of k: reads the rest of `r`, `c`, starts reading the next ones.
+    static __device__ __forceinline__ void tile(State& st, Frags& f0, Acc& acc, GOCKPT_LDS uint8_t* r,
+                                                GOCKPT_LDS uint8_t* c, GOCKPT_LDS uint8_t* nr, GOCKPT_LDS uint8_t* nc,
+                                                int t, int tiles) {
+        Frags f1;
+        read(st, f1, r, c, 1);
+        multiply(f0, acc);
+        read(st, f0, r, c, 2);
+        multiply(f1, acc);
+        read(st, f1, r, c, 3);
+        multiply(f0, acc);
+        if (t + 1 < tiles) {
+            land(st, nr, nc, t + 1);
+            read(st, f0, nr, nc, 0);
+            if (t + 2 < tiles) fill(st, r, c, t + 2);
+        }
+        multiply(f1, acc);
+    }
+
+    // acc = the block's tile of the product over its slice of k.  The LDS
+    // buffers are separate objects so that the compiler knows a copy into one
+    // from a read of the other.
+    static __device__ __forceinline__ void run(const MmaArgs& a, const MmaPlace& p, int cn, int k_all,
+                                               GOCKPT_LDS uint8_t* r0, GOCKPT_LDS uint8_t* c0,
+                                               GOCKPT_LDS uint8_t* r1, GOCKPT_LDS uint8_t* c1, Acc& acc) {
+#pragma unroll
+        for (int i = 0; i < kFR; ++i)
+#pragma unroll
+            for (int j = 0; j < kFC; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+        State st;
+        const int thread = threadIdx.x;
+        st.lane = thread & 63;
+        st.wave = __builtin_amdgcn_readfirstlane(thread >> 6);
+        const int64_t k0 = static_cast<int64_t>(p.split) * a.split_k;
+        st.k = static_cast<int>(min(static_cast<int64_t>(a.split_k), k_all - k0));
+        if (st.k <= 0) return;
+        const int tiles = (st.k + kStepK - 1) / kStepK;
+        if constexpr (kRLay == kCodes8) {
+            MmaArgs b = a;
+            b.r += k0 * a.r_stride;
+            b.scales += k0 * a.scale_stride;
+            st.fr8.init(b, p.r0, thread);
+        } else {
+            st.fr.init(a.r + k0 * (kRLay == kAlongK ? 2 : a.r_stride), a.r_stride, p.r0, a.rn, nullptr, st.lane,
+                       st.wave);
+        }
+        st.fc.init(a.c + k0 * (kCLay == kAlongK ? 2 : a.c_stride), a.c_stride, p.c0, cn,
+                   kCLay == kAlongK ? a.c_rows : nullptr, st.lane, st.wave);
+        st.rr.init(st.wave / kWC * (kFR * 32), st.lane);
+        st.rc.init(st.wave % kWC * (kFC * 32), st.lane);
+        fill(st, r0, c0, 0);
+        land(st, r0, c0, 0);
+        Frags f;
+        read(st, f, r0, c0, 0);
+        if (tiles > 1) fill(st, r1, c1, 1);
+        int t = 0;
+        for (; t + 1 < tiles; t += 2) {
+            tile(st, f, acc, r0, c0, r1, c1, t, tiles);
+            tile(st, f, acc, r1, c1, r0, c0, t + 1, tiles);
+        }
+        if (t < tiles) tile(st, f, acc, r0, c0, r1, c1, t, tiles);
+    }
+
+    // First r and the c of this lane's element 0 of fragment (i, j); element e
+    // lies 8 * (e / 4) + e % 4 further in r.
+    static __device__ __forceinline__ int r_of(const MmaPlace& p, int i) {
+        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+        return p.r0 + (wave / kWC * kFR + i) * 32 + 4 * (lane >> 5);
+    }
+    static __device__ __forceinline__ int c_of(const MmaPlace& p, int j) {
+        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+        return p.c0 + (wave % kWC * kFC + j) * 32 + (lane & 31);
+    }
+};
+
+// Where a product's values go.
+struct StoreArgs {
+    uint8_t* out;       // row c at out + c * stride bytes
+    int64_t stride;
+    int32_t dtype, accumulate;
+    float alpha;        // factor of every value,
+    const float* beta;  // and one on the device (null: 1)
+    float* slices;      // not null: fp32 sums instead, slice s at s * cn * rn, unscaled;
+    int32_t add;        // added to what is there
+};
+
+// Four values along r.  x is rounded once; with accumulate the sum is.
+__device__ __forceinline__ void store4(uint8_t* p, int dtype, bool accumulate, f32x4 x, int n) {
+    if (dtype == kFP32) {
+        if (n >= 4) {
+            f32x4_any* q = reinterpret_cast<f32x4_any*>(p);
+            *q = accumulate ? *q + x : x;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+                if (i < n) {
+                    float* q = reinterpret_cast<float*>(p) + i;
+                    *q = accumulate ? *q + x[i] : x[i];
+                }
+        }
+        return;
+    }
+    if (accumulate) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (i < n) {
+                const uint16_t old = reinterpret_cast<const uint16_t*>(p)[i];
+                x[i] += dtype == kBF16 ? elem_to_f32<kBF16>(old) : elem_to_f32<kFP16>(old);
+            }
+    }
+    u32x2 w;
+    if (dtype == kBF16)
+        w = u32x2{pack2<kBF16>(x[0], x[1]), pack2<kBF16>(x[2], x[3])};
+    else
+        w = u32x2{pack2<kFP16>(x[0], x[1]), pack2<kFP16>(x[2], x[3])};
+    if (n >= 4) {
+        *reinterpret_cast<u32x2_any*>(p) = w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (i < n) reinterpret_cast<uint16_t*>(p)[i] = static_cast<uint16_t>(w[i / 2] >> (16 * (i & 1)));
+    }
+}
+
+template <class M>
+__device__ __forceinline__ void store_tile(const MmaArgs& a, const StoreArgs& o, const MmaPlace& p, int cn,
+                                           const typename M::Acc& acc) {
+    const float alpha = o.alpha * (o.beta != nullptr ? *o.beta : 1.0f);
+#pragma unroll
+    for (int j = 0; j < M::kFC; ++j) {
+        const int c = M::c_of(p, j);
+        if (c >= cn) continue;
+#pragma unroll
+        for (int i = 0; i < M::kFR; ++i) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int r = M::r_of(p, i) + 8 * q, n = a.rn - r;
+                if (n <= 0) continue;
+                const f32x16& v = acc[i][j];
+                f32x4 x = {v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+                if (o.slices != nullptr) {
+                    float* to = o.slices + (static_cast<int64_t>(p.split) * a.cn + c) * a.rn + r;
+                    store4(reinterpret_cast<uint8_t*>(to), kFP32, o.add != 0, x, n);
+                } else {
+                    x *= alpha;
+                    store4(o.out + c * o.stride + static_cast<int64_t>(r) * dtype_bytes(o.dtype), o.dtype,
+                           o.accumulate != 0, x, n);
+                }
+            }
+        }
+    }
+}
+
+#define GOCKPT_MMA_LDS(M)                                              \
+    __shared__ __attribute__((aligned(1024))) uint8_t lr0[M::kRBytes]; \
+    __shared__ __attribute__((aligned(1024))) uint8_t lc0[M::kCBytes]; \
+    __shared__ __attribute__((aligned(1024))) uint8_t lr1[M::kRBytes]; \
+    __shared__ __attribute__((aligned(1024))) uint8_t lc1[M::kCBytes];
+
+#define GOCKPT_MMA_RUN(M, a, p, cn, k, acc)                                                     \
+    M::run(a, p, cn, k, (GOCKPT_LDS uint8_t*)lr0, (GOCKPT_LDS uint8_t*)lc0,                     \
+           (GOCKPT_LDS uint8_t*)lr1, (GOCKPT_LDS uint8_t*)lc1, acc)
+
+}  // namespace gockpt

@@ -1,0 +1,228 @@
+// gockpt_products.hip -- the matrix products of the head's gradients and the
+// linear layers: which tile and how many slices of k, the launches, the join of
+// slices, and copies of matrices that products cannot read in place.
+#include "gockpt_mma.h"
+#include "gockpt_model_internal.h"
+
+namespace gockpt {
+
+namespace {
+
+template <class M>
+__global__ __launch_bounds__(M::kThreads) void product_kernel(MmaArgs a, StoreArgs o) {
+    GOCKPT_MMA_LDS(M)
+    const MmaPlace p = mma_place(a, M::kBR, M::kBC);
+    const int cn = a.cn_dev != nullptr ? *a.cn_dev : a.cn;
+    if (p.c0 >= cn) return;
+    const int k = a.k_dev != nullptr ? *a.k_dev : a.k;
+    typename M::Acc acc;
+    GOCKPT_MMA_RUN(M, a, p, cn, k, acc);
+    store_tile<M>(a, o, p, cn, acc);
+}
+
+template <class M>
+void start(const MmaArgs& a, const StoreArgs& o, hipStream_t s) {
+    hipLaunchKernelGGL(product_kernel<M>, dim3(a.tiles_r * a.tiles_c * a.splits), dim3(M::kThreads), 0, s, a, o);
+}
+
+template <int kT, int kR, int kC>
+void start_shape(int shape, const MmaArgs& a, const StoreArgs& o, hipStream_t s) {
+    if (shape == kWide) return start<Mma<kT, kR, kC, 256, 256, 2, 4>>(a, o, s);
+    if (shape == kMid) return start<Mma<kT, kR, kC, 128, 128, 2, 2>>(a, o, s);
+    if constexpr (kC == kAlongK) start<Mma<kT, kR, kC, 128, 32, 4, 1>>(a, o, s);
+}
+
+template <int kT>
+void start_kind(int kind, int shape, const MmaArgs& a, const StoreArgs& o, hipStream_t s) {
+    if (kind == kAlongAlong) return start_shape<kT, kAlongK, kAlongK>(shape, a, o, s);
+    if (kind == kAcrossAlong) return start_shape<kT, kAcrossK, kAlongK>(shape, a, o, s);
+    if (kind == kAcrossAcross) return start_shape<kT, kAcrossK, kAcrossK>(shape, a, o, s);
+    start_shape<kT, kCodes8, kAcrossK>(shape, a, o, s);
+}
+
+// ---- the join of slices ---------------------------------------------------------
+
+__global__ __launch_bounds__(256) void finish_kernel(FinishArgs f) {
+    const int64_t groups = (f.cols + 3) / 4, all = groups * f.rows;
+    const float alpha = f.alpha * (f.beta != nullptr ? *f.beta : 1.0f);
+    for (int64_t at = blockIdx.x * int64_t{256} + threadIdx.x; at < all; at += gridDim.x * int64_t{256}) {
+        const int64_t row = at / groups;
+        const int col = static_cast<int>(at - row * groups) * 4, n = min(4, f.cols - col);
+        const int64_t c = f.of_row != nullptr ? f.of_row[row] : row;
+        f32x4 sum = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (c >= 0) {
+            const float* p = f.slices + c * f.cols + col;
+            for (int k = 0; k < f.count; ++k, p += f.slice_step) {
+                if (n == 4) {
+                    sum += *reinterpret_cast<const f32x4_any*>(p);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 3; ++i)
+                        if (i < n) sum[i] += p[i];
+                }
+            }
+            if (f.fix != nullptr && f.fix_row[c] >= 0) {
+                const float x = f.fix[c];
+                const u32x2 w =
+                    *reinterpret_cast<const u32x2*>(f.fix_from + f.fix_row[c] * f.fix_stride + int64_t{col} * 2);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t b = w[i / 2] >> (16 * (i & 1)) & 0xffff;
+                    sum[i] += x * (f.fix_dtype == kBF16 ? elem_to_f32<kBF16>(b) : elem_to_f32<kFP16>(b));
+                }
+            }
+            sum *= alpha;
+        }
+        store4(f.out + row * f.stride + static_cast<int64_t>(col) * dtype_bytes(f.dtype), f.dtype, f.accumulate != 0,
+               sum, n);
+    }
+}
+
+// ---- copies ---------------------------------------------------------------------
+
+// 8 columns a thread: rows that start anywhere become rows of whole 16-byte
+// pieces.  An index past the source's columns is never read.
+__global__ __launch_bounds__(256) void rows_kernel(const uint8_t* src, int64_t stride, int32_t cols,
+                                                   const int32_t* rows, const int32_t* count, int32_t n,
+                                                   uint8_t* dst) {
+    const int64_t groups = (cols + 7) / 8;
+    const int64_t all = groups * (count != nullptr ? *count : n);
+    for (int64_t at = blockIdx.x * int64_t{256} + threadIdx.x; at < all; at += gridDim.x * int64_t{256}) {
+        const int64_t row = at / groups;
+        const int col = static_cast<int>(at - row * groups) * 8;
+        const int64_t from = rows != nullptr ? rows[row] : row;
+        const uint8_t* p = src + from * stride + static_cast<int64_t>(col) * 2;
+        u32x4 w = {0, 0, 0, 0};
+        if (col + 8 <= cols) {
+            w = *reinterpret_cast<const u32x4_any*>(p);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 7; ++i)
+                if (col + i < cols)
+                    w[i / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(p)[i]) << (16 * (i & 1));
+        }
+        *reinterpret_cast<u32x4*>(dst + at * 16) = w;
+    }
+}
+
+uint32_t copy_grid(int64_t items) {
+    return static_cast<uint32_t>(std::min<int64_t>((items + 255) / 256, kUnits * 16));
+}
+
+}  // namespace
+
+void launch_finish(const FinishArgs& f, hipStream_t s) {
+    const int64_t items = (int64_t{f.cols} + 3) / 4 * f.rows;
+    if (items > 0) hipLaunchKernelGGL(finish_kernel, dim3(copy_grid(items)), dim3(256), 0, s, f);
+}
+
+void launch_rows(const gockpt_matrix& src, const int32_t* rows, const int32_t* count, int64_t n, uint8_t* dst,
+                 hipStream_t s) {
+    const int64_t items = (src.cols + 7) / 8 * n;
+    if (items > 0)
+        hipLaunchKernelGGL(rows_kernel, dim3(copy_grid(items)), dim3(256), 0, s,
+                           static_cast<const uint8_t*>(src.data), src.stride * 2, static_cast<int32_t>(src.cols), rows,
+                           count, static_cast<int32_t>(n), dst);
+}
+
+Source source_of(const gockpt_matrix& m, uint8_t* copy, hipStream_t s) {
+    if (in_place(m)) return {static_cast<const uint8_t*>(m.data), (m.rows > 1 ? m.stride : m.cols) * 2};
+    launch_rows(m, nullptr, nullptr, m.rows, copy, s);
+    return {copy, up(m.cols, 8) * 2};
+}
+
+// A tile's time is a fixed part (its first copies, its stores) and a part for
+// each k; tiles run in rounds of as many as fit the device.  us: 8192 x 16384 x
+// 2048 (r x c x k) 621 in wide tiles, 598 in mid ones, 2048 x 16384 x 8192 507
+// and 557, 2048 x 8192 x 16384 455 and 569; 32000 x 1 x 4096 in thin ones 44.
+ProductPlan plan_product(int kind, int64_t rn, int64_t cn, int64_t k, int most_splits) {
+    struct Cost {
+        int br, bc, each;
+        double fixed, per_k;
+    };
+    static constexpr Cost kCosts[3] = {{256, 256, 1, 5.0, 0.0275}, {128, 128, 2, 4.0, 0.0165}, {128, 32, 4, 3.0, 0.012}};
+    const bool along = kind == kAlongAlong || kind == kAcrossAlong;
+    const double least = 2.0 * static_cast<double>(rn + cn) * static_cast<double>(k) / 5.5e6;  // us to read both
+    ProductPlan best{};
+    best.us = -1.0;
+    for (int shape = kWide; shape <= kThin; ++shape) {
+        if (shape == kThin && (!along || cn > 32)) continue;
+        const Cost& t = kCosts[shape];
+        const int64_t tr = (rn + t.br - 1) / t.br, tc = (cn + t.bc - 1) / t.bc, tiles = tr * tc;
+        const int64_t slots = int64_t{kUnits} * t.each;
+        for (int want = 1; want <= most_splits; want *= 2) {
+            // of two roundings, slices that fill the slots best
+            for (int extra = 0; extra < (want > 1 ? 2 : 1); ++extra) {
+                int64_t splits = want;
+                if (extra == 1) splits = std::min<int64_t>(most_splits, std::max<int64_t>(1, slots / std::max<int64_t>(1, tiles)));
+                const int64_t split_k = up((k + splits - 1) / splits, 64);
+                splits = split_k > 0 ? std::max<int64_t>(1, (k + split_k - 1) / split_k) : 1;
+                const int64_t rounds = (tiles * splits + slots - 1) / slots;
+                double us = static_cast<double>(rounds) * (t.fixed + t.per_k * static_cast<double>(std::min(split_k, k)));
+                us = std::max(us, least);
+                if (splits > 1)
+                    us += 4.0 + 8.0 * static_cast<double>(splits) * static_cast<double>(rn) * static_cast<double>(cn) / 4.5e6;
+                if (best.us < 0.0 || us < best.us) {
+                    best.shape = shape;
+                    best.splits = static_cast<int>(splits);
+                    best.split_k = static_cast<int32_t>(std::max<int64_t>(split_k, 64));
+                    best.tiles_r = static_cast<uint32_t>(tr);
+                    best.tiles_c = static_cast<uint32_t>(tc);
+                    best.us = us;
+                }
+            }
+        }
+    }
+    return best;
+}
+
+void launch_product(int kind, int dtype, const ProductPlan& p, MmaArgs& a, const StoreArgs& o, hipStream_t s) {
+    a.tiles_r = p.tiles_r;
+    a.tiles_c = p.tiles_c;
+    a.splits = p.splits;
+    a.split_k = p.split_k;
+    if (a.tiles_r == 0 || a.tiles_c == 0) return;
+    if (dtype == kBF16)
+        start_kind<kBF16>(kind, p.shape, a, o, s);
+    else
+        start_kind<kFP16>(kind, p.shape, a, o, s);
+}
+
+// ---- checks -----------------------------------------------------------------------
+
+int check_model_matrix(const char* name, const char* what, const gockpt_matrix* m, int types) {
+    if (m == nullptr) return ops_fail(GOCKPT_EINVAL, "%s: null %s", name, what);
+    if (!dtype_ok(m->dtype) || (types >> m->dtype & 1) == 0)
+        return ops_fail(GOCKPT_EINVAL, "%s: %s dtype %d", name, what, m->dtype);
+    if (m->rows < 0 || m->cols < 0 || m->rows > kMaxExtent || m->cols > kMaxWidth)
+        return ops_fail(GOCKPT_EINVAL, "%s: %s of %lld x %lld", name, what, static_cast<long long>(m->rows),
+                        static_cast<long long>(m->cols));
+    if (m->rows > 1 && (m->stride < m->cols || m->stride > (int64_t{1} << 46) / m->rows))
+        return ops_fail(GOCKPT_EINVAL, "%s: %s stride %lld for rows of %lld", name, what,
+                        static_cast<long long>(m->stride), static_cast<long long>(m->cols));
+    if (m->rows > 0 && m->cols > 0 && (m->data == nullptr || !elem_aligned(m->data, m->dtype)))
+        return ops_fail(GOCKPT_EINVAL, "%s: %s is null or not aligned to its element", name, what);
+    return GOCKPT_OK;
+}
+
+int check_act8(const char* name, const char* what, const gockpt_act8* a, int64_t rows, int64_t cols) {
+    if (a == nullptr) return ops_fail(GOCKPT_EINVAL, "%s: null %s", name, what);
+    if (a->rows != rows || a->cols != cols)
+        return ops_fail(GOCKPT_EINVAL, "%s: %s of %lld x %lld, expected %lld x %lld", name, what,
+                        static_cast<long long>(a->rows), static_cast<long long>(a->cols), static_cast<long long>(rows),
+                        static_cast<long long>(cols));
+    if (rows > 0 && cols > 0 &&
+        (a->codes == nullptr || a->scales == nullptr || reinterpret_cast<uintptr_t>(a->codes) % 16 != 0))
+        return ops_fail(GOCKPT_EINVAL, "%s: %s is null or its codes are not aligned to 16 bytes", name, what);
+    return GOCKPT_OK;
+}
+
+int check_workspace(const char* name, const void* workspace, size_t have, size_t need) {
+    if (need == 0) return GOCKPT_OK;
+    if (workspace == nullptr || reinterpret_cast<uintptr_t>(workspace) % 256 != 0)
+        return ops_fail(GOCKPT_EINVAL, "%s: the workspace must be 256-byte aligned", name);
+    if (have < need) return ops_fail(GOCKPT_ENOMEM, "%s: workspace of %zu bytes, %zu needed", name, have, need);
+    return GOCKPT_OK;
+}
+
+}  // namespace gockpt
