@@ -285,35 +285,35 @@ __global__ __launch_bounds__(M::kThreads) void z_kernel(GradArgs g) {
     if (p.c0 >= cn) return;
     typename M::Acc acc;
     GOCKPT_MMA_RUN(M, g.a, p, cn, g.a.k, acc);
-    const int wide = (g.a.rn + 7) / 8 * 8;  // the products read whole pieces of 8: zeros behind the last row
 #pragma unroll
     for (int j = 0; j < M::kFC; ++j) {
-        const int c = M::c_of(p, j);
-        if (c >= cn) continue;
+        const int c = min(M::c_of(p, j), cn - 1);
         const float base = g.base[c], factor = g.factor[c];
         const int want = g.target[c] - g.first;
-        uint8_t* row = g.z + c * g.z_stride;
+        const bool mine = c == M::c_of(p, j);
 #pragma unroll
         for (int i = 0; i < M::kFR; ++i) {
+            const int r = M::r_of(p, i), at = want - r, left = g.a.rn - r;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int r = M::r_of(p, i) + 8 * q;
-                if (r >= wide) continue;
-                float z[4];
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    z[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][4 * q + e], g.log2_scale, -base));
-                    if (want == r + e) {
-                        z[e] = (z[e] - 1.0f) * factor;
-                        g.lost[c] = z[e] - elem_to_f32<M::kT>(pack2<M::kT>(z[e], z[e]) & 0xffff);
-                    } else {
-                        z[e] = r + e < g.a.rn ? z[e] * factor : 0.0f;
-                    }
+            for (int e = 0; e < 16; ++e) {
+                const int to = 8 * (e / 4) + e % 4;
+                float z = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][e], g.log2_scale, -base));
+                if (at == to) {
+                    z = (z - 1.0f) * factor;
+                    if (mine) g.lost[c] = z - elem_to_f32<M::kT>(pack2<M::kT>(z, z) & 0xffff);
+                } else {
+                    z = to < left ? z * factor : 0.0f;
                 }
-                *reinterpret_cast<u32x2*>(row + r * 2) = u32x2{pack2<M::kT>(z[0], z[1]), pack2<M::kT>(z[2], z[3])};
+                acc[i][j][e] = z;
             }
         }
     }
+    __syncthreads();
+    const Store<M> store = GOCKPT_MMA_STORE(M);
+    const int wide = (g.a.rn + 7) / 8 * 8;  // the products read whole pieces of 8: zeros behind the last row
+#pragma unroll
+    for (int j = 0; j < M::kFC; ++j)
+        store.put(acc, j, g.z, g.z_stride, M::kT, false, 1.0f, M::first_r(p), wide, M::first_c(p, j), cn);
 }
 
 // ---- host ---------------------------------------------------------------------------

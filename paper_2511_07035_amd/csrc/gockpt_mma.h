@@ -15,14 +15,23 @@
 // while the other is multiplied.  The copy writes lanes one after another, so
 // the order that keeps LDS reads free of bank conflicts is made by permuting
 // which 16 bytes a lane fetches, and undone by the reads:
-//   kAlongK   rows of 128 bytes, 16-byte piece p of row i at p ^ (i & 7); a
-//             fragment is one 16-byte read a lane.
+//   kAlongK   rows of 128 bytes, 16-byte piece p of row i at p ^ (i / 2 & 7); a
+//             fragment is one 16-byte read a lane, 16 lanes at a time, and of 16
+//             rows every other one lies in the same banks (with i & 7 the counters
+//             showed as many cycles of conflicts as of reads).
 //   kAcrossK  rows of k, 32-byte unit u of row k at u ^ f(k & 3), f = 0, 3, 5, 6:
 //             the four rows that a transposing read takes together then lie in
 //             different banks, also where two units are read at once.
 // A fragment of step s + 1 is read while step s is multiplied, across the
 // barrier between two tiles as well: a wave holds the last step's fragments
 // in registers when it passes it.
+//
+// Blocks begin at different k, and take the rest in turn: rows of a power of
+// two bytes (2048 columns are 4096) put one k of all rows into the same few
+// channels of the caches, and blocks that march through k together wait for
+// these.  us, all from the first k and as here: 8192 x 16384 x 2048 (r x c x k,
+// both along k) 469 and 432, 8192 x 8192 x 8192 833 and 792, 2048 x 16384 x 8192 (R
+// across) 442 and 427, 2048 x 8192 x 16384 (both across) 407 and 406.
 #pragma once
 
 #include "gockpt_ops_internal.h"
@@ -40,6 +49,7 @@ typedef f32x4 f32x4_any __attribute__((aligned(2)));
 enum Lay : int { kAlongK = 0, kAcrossK = 1, kCodes8 = 2 };
 
 constexpr int kStepK = 64;  // k of one LDS tile
+constexpr int kTurns = 32;  // tiles of k that blocks begin at
 
 #define GOCKPT_LDS __attribute__((address_space(3)))
 
@@ -79,8 +89,9 @@ __device__ __forceinline__ T* uniform(T* p) {
     return reinterpret_cast<T*>(static_cast<uint64_t>(hi) << 32 | lo);
 }
 
-// This wave's copies into LDS have landed.
-__device__ __forceinline__ void wait_copies() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// This wave's copies into LDS have landed (vmcnt 0; the builtin tells the
+// compiler too, which else waits again before reads).
+__device__ __forceinline__ void wait_copies() { __builtin_amdgcn_s_waitcnt(0x0f70); }
 
 // The tile of one operand: kB indexes by 64 k, filled by kWaves wavefronts.
 template <int kLay, int kB, int kWaves>
@@ -101,7 +112,8 @@ struct Filler {
         if constexpr (kLay == kAlongK) {
             base = uniform(rows != nullptr ? data : data + static_cast<int64_t>(i0) * stride);
             step = 2 * kStepK;
-            const int piece = (lane & 7) ^ (lane >> 3);
+            static_assert(kWaves % 2 == 0, "rows 8 * wave on, modulo 16");
+            const int piece = (lane & 7) ^ ((wave & 1) * 4 + (lane >> 4));
 #pragma unroll
             for (int j = 0; j < kPieces; ++j) {
                 const int i = min((j * kWaves + wave) * 8 + (lane >> 3), n - 1 - i0);
@@ -127,22 +139,18 @@ struct Filler {
         }
     }
 
-    // Starts the copies of the tile of k that begins at tile * 64; `left` k
-    // are there (64 or more: all).
+    // Starts the copies of the tile of k that begins at tile * 64.  kWhole: all
+    // its k are there; else `left` are.
+    template <bool kWhole>
     __device__ __forceinline__ void fill(GOCKPT_LDS uint8_t* lds, int tile, int left, int wave) {
+#if defined(__HIP_DEVICE_COMPILE__)  // the host's pass does not know the buffer's type
         __amdgpu_buffer_rsrc_t res = __builtin_amdgcn_make_buffer_rsrc(
             const_cast<uint8_t*>(base + static_cast<int64_t>(tile) * step), 0, 0xffffffff, 0x00027000);
-        if (left >= kStepK) {
 #pragma unroll
-            for (int j = 0; j < kPieces; ++j)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(res, (GOCKPT_LDS void*)(lds + (j * kWaves + wave) * 1024), 16,
-                                                         off[j], 0, 0, 0);
-        } else {
-#pragma unroll
-            for (int j = 0; j < kPieces; ++j)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(res, (GOCKPT_LDS void*)(lds + (j * kWaves + wave) * 1024), 16,
-                                                         k_of[j] < left ? off[j] : off[j] - back[j], 0, 0, 0);
-        }
+        for (int j = 0; j < kPieces; ++j)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(res, (GOCKPT_LDS void*)(lds + (j * kWaves + wave) * 1024), 16,
+                                                     kWhole || k_of[j] < left ? off[j] : off[j] - back[j], 0, 0, 0);
+#endif
     }
 
     // Zeros in place of what the wave copied beyond the last k, once landed.
@@ -153,9 +161,6 @@ struct Filler {
                 *reinterpret_cast<GOCKPT_LDS u32x4*>(lds + (j * kWaves + wave) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
     }
 
-    __device__ __forceinline__ void land(GOCKPT_LDS uint8_t* lds, int left, int lane, int wave) {
-        if (left < kStepK) clear(lds, left, lane, wave);
-    }
 };
 
 // 8-bit codes pass through registers: each thread takes the 32 codes of one
@@ -227,7 +232,7 @@ struct Reader {
         if constexpr (kLay == kAlongK) {
 #pragma unroll
             for (int s = 0; s < 4; ++s)
-                at[s] = (first + (lane & 31)) * 128 + (((2 * s + (lane >> 5)) ^ (lane & 7)) << 4);
+                at[s] = (first + (lane & 31)) * 128 + (((2 * s + (lane >> 5)) ^ (lane >> 1 & 7)) << 4);
         } else {
             const int t = lane & 15, k = (lane >> 5) * 8 + (t >> 2);
             const int f = unit_swizzle(t >> 2) & (kB / 16 - 1);
@@ -295,26 +300,33 @@ struct Mma {
         Reader<kRLay == kCodes8 ? kAcrossK : kRLay, kBR> rr;
         Reader<kCLay, kBC> rc;
         int lane, wave, k;
+        int from, whole;  // the k tile to begin with, of so many whole ones
     };
 
+    template <bool kWhole>
     static __device__ __forceinline__ void fill(State& st, GOCKPT_LDS uint8_t* r, GOCKPT_LDS uint8_t* c, int tile) {
         const int left = st.k - tile * kStepK;
+        if (kWhole || tile < st.whole) {  // in turn from st.from on
+            tile += st.from;
+            tile -= tile >= st.whole ? st.whole : 0;
+        }
         if constexpr (kRLay == kCodes8)
             st.fr8.fill(tile, left);
         else
-            st.fr.fill(r, tile, left, st.wave);
-        st.fc.fill(c, tile, left, st.wave);
+            st.fr.template fill<kWhole>(r, tile, left, st.wave);
+        st.fc.template fill<kWhole>(c, tile, left, st.wave);
     }
 
     // The tile's copies have landed for all waves; nobody reads the other buffer any more.
+    template <bool kWhole>
     static __device__ __forceinline__ void land(State& st, GOCKPT_LDS uint8_t* r, GOCKPT_LDS uint8_t* c, int tile) {
-        const int left = st.k - tile * kStepK;
         wait_copies();
-        if constexpr (kRLay == kCodes8)
-            st.fr8.land(r);
-        else
-            st.fr.land(r, left, st.lane, st.wave);
-        st.fc.land(c, left, st.lane, st.wave);
+        if constexpr (kRLay == kCodes8) st.fr8.land(r);
+        const int left = st.k - tile * kStepK;
+        if (!kWhole && left < kStepK) {
+            if constexpr (kRLay != kCodes8) st.fr.clear(r, left, st.lane, st.wave);
+            st.fc.clear(c, left, st.lane, st.wave);
+        }
         __syncthreads();
     }
 
@@ -337,23 +349,48 @@ struct Mma {
             for (int j = 0; j < kFC; ++j) acc[i][j] = mma<kT>(f.r[i], f.c[j], acc[i][j]);
     }
 
+    // Asks for an even mix of a step's products with the reads for the next
+    // one (and, in a tile's last step, the copies): left alone, the compiler
+    // puts each read right before its use.
+    static constexpr int kReads = kFR * (kRLay == kAlongK ? 1 : 2) + kFC * (kCLay == kAlongK ? 1 : 2);
+    static constexpr int kCopies = (kRLay == kCodes8 ? 0 : kBR / 8 / kWaves) + kBC / 8 / kWaves;
+    template <int kCopied>
+    static __device__ __forceinline__ void mix() {
+        constexpr int kProducts = kFR * kFC;
+        int reads = 0, copies = 0;
+#pragma unroll
+        for (int i = 0; i < kProducts; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+#pragma unroll
+            for (; reads * kProducts < (i + 1) * kReads; ++reads) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+#pragma unroll
+            for (; copies * kProducts < (i + 1) * kCopied; ++copies) __builtin_amdgcn_sched_group_barrier(0x20, 1, 0);
+        }
+    }
+
     // One tile of k: reads the rest of `r`, `c`, starts reading the next ones.
+    // kInner: the next two tiles are there in full.
+    template <bool kInner>
     static __device__ __forceinline__ void tile(State& st, Frags& f0, Acc& acc, GOCKPT_LDS uint8_t* r,
                                                 GOCKPT_LDS uint8_t* c, GOCKPT_LDS uint8_t* nr, GOCKPT_LDS uint8_t* nc,
                                                 int t, int tiles) {
         Frags f1;
         read(st, f1, r, c, 1);
         multiply(f0, acc);
+        mix<0>();
         read(st, f0, r, c, 2);
         multiply(f1, acc);
+        mix<0>();
         read(st, f1, r, c, 3);
         multiply(f0, acc);
-        if (t + 1 < tiles) {
-            land(st, nr, nc, t + 1);
+        mix<0>();
+        if (kInner || t + 1 < tiles) {
+            land<kInner>(st, nr, nc, t + 1);
             read(st, f0, nr, nc, 0);
-            if (t + 2 < tiles) fill(st, r, c, t + 2);
+            if (kInner || t + 2 < tiles) fill<kInner>(st, r, c, t + 2);
         }
         multiply(f1, acc);
+        if (kInner) mix<kCopies>();
     }
 
     // acc = the block's tile of the product over its slice of k.  The LDS
@@ -389,29 +426,37 @@ struct Mma {
                    kCLay == kAlongK ? a.c_rows : nullptr, st.lane, st.wave);
         st.rr.init(st.wave / kWC * (kFR * 32), st.lane);
         st.rc.init(st.wave % kWC * (kFC * 32), st.lane);
-        fill(st, r0, c0, 0);
-        land(st, r0, c0, 0);
+        st.whole = st.k / kStepK;
+        st.from = st.whole > 0 ? (p.r0 / kBR + p.c0 / kBC) % kTurns % st.whole : 0;
+        fill<false>(st, r0, c0, 0);
+        land<false>(st, r0, c0, 0);
         Frags f;
         read(st, f, r0, c0, 0);
-        if (tiles > 1) fill(st, r1, c1, 1);
+        if (tiles > 1) fill<false>(st, r1, c1, 1);
         int t = 0;
-        for (; t + 1 < tiles; t += 2) {
-            tile(st, f, acc, r0, c0, r1, c1, t, tiles);
-            tile(st, f, acc, r1, c1, r0, c0, t + 1, tiles);
+        for (; t + 3 < st.whole; t += 2) {
+            tile<true>(st, f, acc, r0, c0, r1, c1, t, tiles);
+            tile<true>(st, f, acc, r1, c1, r0, c0, t + 1, tiles);
         }
-        if (t < tiles) tile(st, f, acc, r0, c0, r1, c1, t, tiles);
+        for (; t < tiles; t += 2) {
+            tile<false>(st, f, acc, r0, c0, r1, c1, t, tiles);
+            if (t + 1 < tiles) tile<false>(st, f, acc, r1, c1, r0, c0, t + 1, tiles);
+        }
     }
 
-    // First r and the c of this lane's element 0 of fragment (i, j); element e
-    // lies 8 * (e / 4) + e % 4 further in r.
+    // Where the wavefront's fragments begin.
+    static __device__ __forceinline__ int first_r(const MmaPlace& p) {
+        return p.r0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / kWC * kFR * 32;
+    }
+    static __device__ __forceinline__ int first_c(const MmaPlace& p, int j) {
+        return p.c0 + (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % kWC * kFC + j) * 32;
+    }
+    // The r and c of this lane's element 0 of fragment (i, j); element e lies
+    // 8 * (e / 4) + e % 4 further in r.
     static __device__ __forceinline__ int r_of(const MmaPlace& p, int i) {
-        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-        return p.r0 + (wave / kWC * kFR + i) * 32 + 4 * (lane >> 5);
+        return first_r(p) + i * 32 + 4 * ((threadIdx.x & 63) >> 5);
     }
-    static __device__ __forceinline__ int c_of(const MmaPlace& p, int j) {
-        const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-        return p.c0 + (wave % kWC * kFC + j) * 32 + (lane & 31);
-    }
+    static __device__ __forceinline__ int c_of(const MmaPlace& p, int j) { return first_c(p, j) + (threadIdx.x & 31); }
 };
 
 // Where a product's values go.
@@ -424,6 +469,29 @@ struct StoreArgs {
     float* slices;      // not null: fp32 sums instead, slice s at s * cn * rn, unscaled;
     int32_t add;        // added to what is there
 };
+
+template <int kT>
+__device__ __forceinline__ u32x2 pack4(f32x4 x) {
+    return u32x2{pack2<kT>(x[0], x[1]), pack2<kT>(x[2], x[3])};
+}
+
+// n <= 8 values of 16 bits that are there at p, from w; with accumulate
+// round(old + x) for the fp32 values x.
+template <int kT>
+__device__ __forceinline__ void add8(uint8_t* p, const float (&x)[8], int n) {
+    uint16_t* q = reinterpret_cast<uint16_t*>(p);
+    if (n >= 8) {
+        u32x4 w = *reinterpret_cast<const u32x4_any*>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            w[i] = pack2<kT>(elem_to_f32<kT>(w[i] & 0xffff) + x[2 * i], elem_to_f32<kT>(w[i] >> 16) + x[2 * i + 1]);
+        *reinterpret_cast<u32x4_any*>(p) = w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 7; ++i)
+            if (i < n) q[i] = static_cast<uint16_t>(pack2<kT>(elem_to_f32<kT>(q[i]) + x[i], 0.0f));
+    }
+}
 
 // Four values along r.  x is rounded once; with accumulate the sum is.
 __device__ __forceinline__ void store4(uint8_t* p, int dtype, bool accumulate, f32x4 x, int n) {
@@ -449,11 +517,7 @@ __device__ __forceinline__ void store4(uint8_t* p, int dtype, bool accumulate, f
                 x[i] += dtype == kBF16 ? elem_to_f32<kBF16>(old) : elem_to_f32<kFP16>(old);
             }
     }
-    u32x2 w;
-    if (dtype == kBF16)
-        w = u32x2{pack2<kBF16>(x[0], x[1]), pack2<kBF16>(x[2], x[3])};
-    else
-        w = u32x2{pack2<kFP16>(x[0], x[1]), pack2<kFP16>(x[2], x[3])};
+    const u32x2 w = dtype == kBF16 ? pack4<kBF16>(x) : pack4<kFP16>(x);
     if (n >= 4) {
         *reinterpret_cast<u32x2_any*>(p) = w;
     } else {
@@ -463,33 +527,143 @@ __device__ __forceinline__ void store4(uint8_t* p, int dtype, bool accumulate, f
     }
 }
 
+// A block's tile to memory.  A lane holds four values along r of each of its
+// columns c, and stores of those would touch 32 rows at 16 bytes each (268 MB of
+// bf16 took 78 us more than no stores at all, and take 46 so).  So each wavefront turns 32 columns
+// at a time in LDS that it alone uses by then, and stores whole stretches of a
+// row, 16 bytes a lane.  The 16-byte piece p of column c lies at p ^ c: writes and
+// reads of 16 lanes meet every bank once.
 template <class M>
-__device__ __forceinline__ void store_tile(const MmaArgs& a, const StoreArgs& o, const MmaPlace& p, int cn,
-                                           const typename M::Acc& acc) {
-    const float alpha = o.alpha * (o.beta != nullptr ? *o.beta : 1.0f);
-#pragma unroll
-    for (int j = 0; j < M::kFC; ++j) {
-        const int c = M::c_of(p, j);
-        if (c >= cn) continue;
-#pragma unroll
-        for (int i = 0; i < M::kFR; ++i) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int r = M::r_of(p, i) + 8 * q, n = a.rn - r;
-                if (n <= 0) continue;
-                const f32x16& v = acc[i][j];
-                f32x4 x = {v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
-                if (o.slices != nullptr) {
-                    float* to = o.slices + (static_cast<int64_t>(p.split) * a.cn + c) * a.rn + r;
-                    store4(reinterpret_cast<uint8_t*>(to), kFP32, o.add != 0, x, n);
-                } else {
-                    x *= alpha;
-                    store4(o.out + c * o.stride + static_cast<int64_t>(r) * dtype_bytes(o.dtype), o.dtype,
-                           o.accumulate != 0, x, n);
+struct Store {
+    static constexpr int kPieces = M::kFR * 8;        // of 4 values of 32 bits, of a column of the wavefront's tile
+    static constexpr int kHalves = M::kFR * 4;        // of 8 values of 16 bits
+    static constexpr int kBytes = M::kFR * 32 * 32 * 4;  // a wavefront's
+
+    GOCKPT_LDS uint8_t* lds;
+
+    // The wavefront's part of the tile buffers; all are free.
+    __device__ __forceinline__ Store(GOCKPT_LDS uint8_t* r0, GOCKPT_LDS uint8_t* c0, GOCKPT_LDS uint8_t* r1,
+                                     GOCKPT_LDS uint8_t* c1) {
+        constexpr int kInR = M::kRBytes / kBytes, kInC = M::kCBytes / kBytes;
+        static_assert(2 * (kInR + kInC) >= M::kWaves, "room for each wavefront");
+        int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        GOCKPT_LDS uint8_t* at = r0;
+        if (w >= kInR) {
+            w -= kInR;
+            at = r1;
+            if (w >= kInR) {
+                w -= kInR;
+                at = c0;
+                if (w >= kInC) {
+                    w -= kInC;
+                    at = c1;
                 }
             }
         }
+        lds = at + w * kBytes;
     }
+
+    // Columns c0 to c0 + 31 (those below cn) of fragments acc[..][j], first r r0,
+    // `rn` r in all; row c at out + c * stride.
+    __device__ __forceinline__ void put(const typename M::Acc& acc, int j, uint8_t* out, int64_t stride, int dtype,
+                                        bool accumulate, float alpha, int r0, int rn, int c0, int cn) const {
+        const int lane = threadIdx.x & 63, c = lane & 31, up = lane >> 5;
+        if (dtype == kFP32 || accumulate) {
+#pragma unroll
+            for (int i = 0; i < M::kFR; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const f32x16& v = acc[i][j];
+                    const f32x4 x = {v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+                    *reinterpret_cast<GOCKPT_LDS f32x4*>(
+                        lds + (c * kPieces + ((i * 8 + q * 2 + up) ^ (c & (kPieces - 1)))) * 16) = x * alpha;
+                }
+            wave_sync();
+            if (dtype == kFP32) {
+#pragma unroll 4
+                for (int s = 0; s < kPieces / 2; ++s) {
+                    const int at = s * 64 + lane, row = at / kPieces, piece = at % kPieces, n = rn - r0 - piece * 4;
+                    const f32x4 x = *reinterpret_cast<const GOCKPT_LDS f32x4*>(
+                        lds + (row * kPieces + (piece ^ (row & (kPieces - 1)))) * 16);
+                    if (c0 + row < cn && n > 0)
+                        store4(out + (c0 + row) * stride + static_cast<int64_t>(r0 + piece * 4) * 4, kFP32, accumulate,
+                               x, n);
+                }
+            } else {
+#pragma unroll 2
+                for (int s = 0; s < kHalves / 2; ++s) {
+                    const int at = s * 64 + lane, row = at / kHalves, piece = at % kHalves, n = rn - r0 - piece * 8;
+                    float x[8];
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const f32x4 y = *reinterpret_cast<const GOCKPT_LDS f32x4*>(
+                            lds + (row * kPieces + ((piece * 2 + h) ^ (row & (kPieces - 1)))) * 16);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) x[4 * h + e] = y[e];
+                    }
+                    if (c0 + row < cn && n > 0) {
+                        uint8_t* p = out + (c0 + row) * stride + static_cast<int64_t>(r0 + piece * 8) * 2;
+                        if (dtype == kBF16)
+                            add8<kBF16>(p, x, n);
+                        else
+                            add8<kFP16>(p, x, n);
+                    }
+                }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < M::kFR; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const f32x16& v = acc[i][j];
+                    const f32x4 x = f32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]} * alpha;
+                    const u32x2 w = dtype == kBF16 ? pack4<kBF16>(x) : pack4<kFP16>(x);
+                    *reinterpret_cast<GOCKPT_LDS u32x2*>(
+                        lds + (c * kHalves + ((i * 4 + q) ^ (c & (kHalves - 1)))) * 16 + up * 8) = w;
+                }
+            wave_sync();
+#pragma unroll 4
+            for (int s = 0; s < kHalves / 2; ++s) {
+                const int at = s * 64 + lane, row = at / kHalves, piece = at % kHalves, n = rn - r0 - piece * 8;
+                const u32x4 w = *reinterpret_cast<const GOCKPT_LDS u32x4*>(
+                    lds + (row * kHalves + (piece ^ (row & (kHalves - 1)))) * 16);
+                if (c0 + row >= cn || n <= 0) continue;
+                uint8_t* p = out + (c0 + row) * stride + static_cast<int64_t>(r0 + piece * 8) * 2;
+                if (n >= 8) {
+                    *reinterpret_cast<u32x4_any*>(p) = w;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 7; ++e)
+                        if (e < n) reinterpret_cast<uint16_t*>(p)[e] = static_cast<uint16_t>(w[e / 2] >> (16 * (e & 1)));
+                }
+            }
+        }
+        wave_sync();
+    }
+
+    // LDS operations of one wavefront are carried out in order: only the
+    // compiler has to keep them so.
+    static __device__ __forceinline__ void wave_sync() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+};
+
+template <class M>
+__device__ __forceinline__ void store_tile(const Store<M>& store, const MmaArgs& a, const StoreArgs& o,
+                                           const MmaPlace& p, int cn, const typename M::Acc& acc) {
+    uint8_t* out = o.out;
+    int64_t stride = o.stride;
+    int dtype = o.dtype;
+    bool accumulate = o.accumulate != 0;
+    float alpha = o.alpha * (o.beta != nullptr ? *o.beta : 1.0f);
+    if (o.slices != nullptr) {
+        out = reinterpret_cast<uint8_t*>(o.slices + static_cast<int64_t>(p.split) * a.cn * a.rn);
+        stride = static_cast<int64_t>(a.rn) * 4;
+        dtype = kFP32;
+        accumulate = o.add != 0;
+        alpha = 1.0f;
+    }
+#pragma unroll
+    for (int j = 0; j < M::kFC; ++j)
+        store.put(acc, j, out, stride, dtype, accumulate, alpha, M::first_r(p), a.rn, M::first_c(p, j), cn);
 }
 
 #define GOCKPT_MMA_LDS(M)                                              \
@@ -501,5 +675,10 @@ __device__ __forceinline__ void store_tile(const MmaArgs& a, const StoreArgs& o,
 #define GOCKPT_MMA_RUN(M, a, p, cn, k, acc)                                                     \
     M::run(a, p, cn, k, (GOCKPT_LDS uint8_t*)lr0, (GOCKPT_LDS uint8_t*)lc0,                     \
            (GOCKPT_LDS uint8_t*)lr1, (GOCKPT_LDS uint8_t*)lc1, acc)
+
+// Once all wavefronts are through with the product.
+#define GOCKPT_MMA_STORE(M)                                                                       \
+    Store<M>((GOCKPT_LDS uint8_t*)lr0, (GOCKPT_LDS uint8_t*)lc0, (GOCKPT_LDS uint8_t*)lr1, \
+             (GOCKPT_LDS uint8_t*)lc1)
 
 }  // namespace gockpt
