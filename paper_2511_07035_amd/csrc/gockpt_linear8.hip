@@ -1,4 +1,11 @@
 // gockpt_linear8.hip -- the linear layer that keeps its input in 8 bits.
+//
+// The weight's gradient restores the input to its 16-bit type (which holds it
+// exactly) in the workspace and multiplies that: 20 and 400 us for 16384 x 2048
+// values by 8192.  A product that took the codes themselves, widened between
+// global memory and LDS, needed 673 us with the conversion before each tile's
+// barrier and 539 with it between the matrix instructions: each of the 32 tiles
+// along the outputs converts all codes again.
 #include "gockpt_mma.h"
 #include "gockpt_model_internal.h"
 
@@ -62,7 +69,7 @@ ForwardPlan plan_forward(const gockpt_matrix& x, const gockpt_matrix& w) {
 
 struct BackwardPlan {
     ProductPlan by_x, by_weight;
-    size_t grad, weight, slices_x, slices_weight, bytes;
+    size_t grad, weight, slices_x, input, slices_weight, bytes;
 };
 
 BackwardPlan plan_backward(const gockpt_matrix& g, const gockpt_matrix* w, const gockpt_act8* keep, bool by_x,
@@ -76,7 +83,8 @@ BackwardPlan plan_backward(const gockpt_matrix& g, const gockpt_matrix* w, const
         p.slices_x = parts.take(slice_bytes(p.by_x, w->cols, g.rows));
     }
     if (by_weight) {
-        p.by_weight = plan_product(kCodesAcross, keep->cols, g.cols, g.rows, kMostSplits);
+        p.by_weight = plan_product(kAcrossAcross, keep->cols, g.cols, g.rows, kMostSplits);
+        p.input = parts.take(g.rows * up(keep->cols, 8) * 2);
         p.slices_weight = parts.take(slice_bytes(p.by_weight, keep->cols, g.cols));
     }
     p.bytes = parts.bytes;
@@ -211,18 +219,18 @@ int gockpt_linear8_grad(const gockpt_matrix* grad_out, const gockpt_matrix* weig
         product_into(kAcrossAlong, grad_out->dtype, p.by_x, a, *grad_x, 0, ws + p.slices_x, s);
     }
     if (by_weight) {
+        const gockpt_matrix input{ws + p.input, keep->rows, keep->cols, up(keep->cols, 8), grad_out->dtype, 0};
+        rc = gockpt_act8_unpack(keep, &input, stream);
+        if (rc != GOCKPT_OK) return rc;
         MmaArgs a{};
-        const int64_t blocks = up(keep->cols, GOCKPT_ACT8_BLOCK) / GOCKPT_ACT8_BLOCK;
-        a.r = static_cast<const uint8_t*>(keep->codes);
-        a.r_stride = blocks * GOCKPT_ACT8_BLOCK;
-        a.scales = static_cast<const uint8_t*>(keep->scales);
-        a.scale_stride = blocks;
+        a.r = ws + p.input;
+        a.r_stride = input.stride * 2;
         a.c = sg.data;
         a.c_stride = sg.stride;
         a.rn = static_cast<int32_t>(keep->cols);
         a.cn = static_cast<int32_t>(grad_out->cols);
         a.k = static_cast<int32_t>(grad_out->rows);
-        product_into(kCodesAcross, grad_out->dtype, p.by_weight, a, *grad_weight, accumulate, ws + p.slices_weight, s);
+        product_into(kAcrossAcross, grad_out->dtype, p.by_weight, a, *grad_weight, accumulate, ws + p.slices_weight, s);
     }
     return ops_launched(name);
 }

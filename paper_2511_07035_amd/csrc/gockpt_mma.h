@@ -6,9 +6,7 @@
 // R's index r runs along the output's rows (its contiguous direction), C's
 // index c counts them.  Each operand is 16 bits wide and lies either with k
 // contiguous (kAlongK: element (i, k) at data + i * stride + k) or with i
-// contiguous (kAcrossK: at data + k * stride + i); kCodes8 is kAcrossK in 8-bit
-// codes with a power-of-two scale for every 32 of them, widened to 16 bits
-// (exactly) on the way into shared memory.
+// contiguous (kAcrossK: at data + k * stride + i).
 //
 // One block computes a tile of kBR x kBC over steps of 64 k.  Tiles go from
 // global memory straight into LDS, 16 bytes a lane, into one of two buffers
@@ -46,7 +44,7 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef f32x4 f32x4_any __attribute__((aligned(2)));
 
-enum Lay : int { kAlongK = 0, kAcrossK = 1, kCodes8 = 2 };
+enum Lay : int { kAlongK = 0, kAcrossK = 1 };
 
 constexpr int kStepK = 64;  // k of one LDS tile
 constexpr int kTurns = 32;  // tiles of k that blocks begin at
@@ -58,8 +56,6 @@ struct MmaArgs {
     const uint8_t* r;
     const uint8_t* c;
     int64_t r_stride, c_stride;
-    const uint8_t* scales;   // of kCodes8: one byte for 32 columns of a row of k
-    int64_t scale_stride;
     int32_t rn, cn;          // extents of r and c
     int32_t k;               // of k; a multiple of 8 for kAlongK
     const int32_t* cn_dev;   // the extent of c, or of k, on the device (null: as above);
@@ -163,66 +159,6 @@ struct Filler {
 
 };
 
-// 8-bit codes pass through registers: each thread takes the 32 codes of one
-// scale, and writes them widened when the tile is to land.
-template <int kT, int kB, int kWaves>
-struct Filler8 {
-    static constexpr int kBlocks = kB / 32;  // scales in a row of the tile
-    static_assert(kBlocks * kStepK == kWaves * 64, "a scale a thread");
-
-    const uint8_t* codes;
-    const uint8_t* scales;
-    int64_t step, scale_step;
-    int k, block;
-    u32x4 held[2];
-    uint32_t scale;
-
-    __device__ __forceinline__ void init(const MmaArgs& a, int i0, int thread) {
-        k = thread / kBlocks;
-        block = thread % kBlocks;
-        const int from = i0 + block * 32 < a.rn ? i0 + block * 32 : i0;
-        codes = a.r + k * a.r_stride + from;
-        scales = a.scales + k * a.scale_stride + from / 32;
-        step = a.r_stride * kStepK;
-        scale_step = a.scale_stride * kStepK;
-    }
-
-    __device__ __forceinline__ void fill(int tile, int left) {
-        if (k < left) {
-            const u32x4* p = reinterpret_cast<const u32x4*>(codes + tile * step);
-            held[0] = p[0];
-            held[1] = p[1];
-            scale = scales[tile * scale_step];
-        } else {
-            held[0] = held[1] = u32x4{0, 0, 0, 0};
-            scale = 1;
-        }
-    }
-
-    __device__ __forceinline__ void land(GOCKPT_LDS uint8_t* lds) {
-        // a scale of 255 stands for what is no number
-        const float s = __uint_as_float(scale << 23 | (scale == 255 ? 0x400000u : 0u));
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            uint32_t w[8];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t x = held[h][i];
-                const float f0 = static_cast<float>(static_cast<int8_t>(x)) * s;
-                const float f1 = static_cast<float>(static_cast<int8_t>(x >> 8)) * s;
-                const float f2 = static_cast<float>(static_cast<int8_t>(x >> 16)) * s;
-                const float f3 = static_cast<float>(static_cast<int8_t>(x >> 24)) * s;
-                w[2 * i] = pack2<kT>(f0, f1);
-                w[2 * i + 1] = pack2<kT>(f2, f3);
-            }
-            const int unit = (block * 2 + h) ^ (unit_swizzle(k) & (kB / 16 - 1));
-            GOCKPT_LDS u32x4* to = reinterpret_cast<GOCKPT_LDS u32x4*>(lds + k * (2 * kB) + unit * 32);
-            to[0] = u32x4{w[0], w[1], w[2], w[3]};
-            to[1] = u32x4{w[4], w[5], w[6], w[7]};
-        }
-    }
-};
-
 // Fragments of 32 indexes by 16 k: lane l holds index l & 31, k 8 * (l >> 5) on.
 template <int kLay, int kB>
 struct Reader {
@@ -294,26 +230,29 @@ struct Mma {
     using Acc = f32x16[kFR][kFC];
 
     struct State {
-        Filler<kRLay == kCodes8 ? kAcrossK : kRLay, kBR, kWaves> fr;
-        Filler8<kT, kRLay == kCodes8 ? kBR : kWaves * 32, kWaves> fr8;
+        Filler<kRLay, kBR, kWaves> fr;
         Filler<kCLay, kBC, kWaves> fc;
-        Reader<kRLay == kCodes8 ? kAcrossK : kRLay, kBR> rr;
+        Reader<kRLay, kBR> rr;
         Reader<kCLay, kBC> rc;
         int lane, wave, k;
         int from, whole;  // the k tile to begin with, of so many whole ones
     };
 
+    // Which tile of k comes as the tile-th: the whole ones in turn from st.from on.
     template <bool kWhole>
-    static __device__ __forceinline__ void fill(State& st, GOCKPT_LDS uint8_t* r, GOCKPT_LDS uint8_t* c, int tile) {
-        const int left = st.k - tile * kStepK;
-        if (kWhole || tile < st.whole) {  // in turn from st.from on
+    static __device__ __forceinline__ int turned(const State& st, int tile) {
+        if (kWhole || tile < st.whole) {
             tile += st.from;
             tile -= tile >= st.whole ? st.whole : 0;
         }
-        if constexpr (kRLay == kCodes8)
-            st.fr8.fill(tile, left);
-        else
-            st.fr.template fill<kWhole>(r, tile, left, st.wave);
+        return tile;
+    }
+
+    template <bool kWhole>
+    static __device__ __forceinline__ void fill(State& st, GOCKPT_LDS uint8_t* r, GOCKPT_LDS uint8_t* c, int tile) {
+        const int left = st.k - tile * kStepK;
+        tile = turned<kWhole>(st, tile);
+        st.fr.template fill<kWhole>(r, tile, left, st.wave);
         st.fc.template fill<kWhole>(c, tile, left, st.wave);
     }
 
@@ -321,10 +260,9 @@ struct Mma {
     template <bool kWhole>
     static __device__ __forceinline__ void land(State& st, GOCKPT_LDS uint8_t* r, GOCKPT_LDS uint8_t* c, int tile) {
         wait_copies();
-        if constexpr (kRLay == kCodes8) st.fr8.land(r);
         const int left = st.k - tile * kStepK;
         if (!kWhole && left < kStepK) {
-            if constexpr (kRLay != kCodes8) st.fr.clear(r, left, st.lane, st.wave);
+            st.fr.clear(r, left, st.lane, st.wave);
             st.fc.clear(c, left, st.lane, st.wave);
         }
         __syncthreads();
@@ -353,7 +291,7 @@ struct Mma {
     // one (and, in a tile's last step, the copies): left alone, the compiler
     // puts each read right before its use.
     static constexpr int kReads = kFR * (kRLay == kAlongK ? 1 : 2) + kFC * (kCLay == kAlongK ? 1 : 2);
-    static constexpr int kCopies = (kRLay == kCodes8 ? 0 : kBR / 8 / kWaves) + kBC / 8 / kWaves;
+    static constexpr int kCopies = (kBR + kBC) / 8 / kWaves;
     template <int kCopied>
     static __device__ __forceinline__ void mix() {
         constexpr int kProducts = kFR * kFC;
@@ -413,15 +351,7 @@ struct Mma {
         st.k = static_cast<int>(min(static_cast<int64_t>(a.split_k), k_all - k0));
         if (st.k <= 0) return;
         const int tiles = (st.k + kStepK - 1) / kStepK;
-        if constexpr (kRLay == kCodes8) {
-            MmaArgs b = a;
-            b.r += k0 * a.r_stride;
-            b.scales += k0 * a.scale_stride;
-            st.fr8.init(b, p.r0, thread);
-        } else {
-            st.fr.init(a.r + k0 * (kRLay == kAlongK ? 2 : a.r_stride), a.r_stride, p.r0, a.rn, nullptr, st.lane,
-                       st.wave);
-        }
+        st.fr.init(a.r + k0 * (kRLay == kAlongK ? 2 : a.r_stride), a.r_stride, p.r0, a.rn, nullptr, st.lane, st.wave);
         st.fc.init(a.c + k0 * (kCLay == kAlongK ? 2 : a.c_stride), a.c_stride, p.c0, cn,
                    kCLay == kAlongK ? a.c_rows : nullptr, st.lane, st.wave);
         st.rr.init(st.wave / kWC * (kFR * 32), st.lane);

@@ -37,8 +37,7 @@ template <int kT>
 void start_kind(int kind, int shape, const MmaArgs& a, const StoreArgs& o, hipStream_t s) {
     if (kind == kAlongAlong) return start_shape<kT, kAlongK, kAlongK>(shape, a, o, s);
     if (kind == kAcrossAlong) return start_shape<kT, kAcrossK, kAlongK>(shape, a, o, s);
-    if (kind == kAcrossAcross) return start_shape<kT, kAcrossK, kAcrossK>(shape, a, o, s);
-    start_shape<kT, kCodes8, kAcrossK>(shape, a, o, s);
+    start_shape<kT, kAcrossK, kAcrossK>(shape, a, o, s);
 }
 
 // ---- the join of slices ---------------------------------------------------------
