@@ -36,6 +36,7 @@ GOCKPT_EACH, GOCKPT_SUM, GOCKPT_MEAN = 0, 1, 2
 GOCKPT_SILU, GOCKPT_GELU, GOCKPT_GELU_TANH = 0, 1, 2
 GOCKPT_ACT8_BLOCK = 32
 
+_TYPES = (torch.bfloat16, torch.float16, torch.float32)
 _REDUCTION = {"none": GOCKPT_EACH, "sum": GOCKPT_SUM, "mean": GOCKPT_MEAN}
 _KIND = {"silu": GOCKPT_SILU, "gelu": GOCKPT_GELU, "gelu_tanh": GOCKPT_GELU_TANH}
 
@@ -74,28 +75,34 @@ def _lib():
 def _workspace(like, name: str, args, stream):
     """(tensor or None, address, bytes) of a call's workspace."""
     n = ctypes.c_size_t()
-    _check(getattr(_lib(), name)(*args, ctypes.byref(n)), name, None)
-    if n.value == 0:
+    rc = getattr(_lib(), name)(*args, ctypes.byref(n))
+    if rc < 0:
+        _check(rc, name, None)
+    n = n.value
+    if n == 0:
         return None, None, 0
-    t = _empty(like, (n.value,), torch.uint8, stream)
-    return t, t.data_ptr(), n.value
+    t = _empty(like, (n,), torch.uint8, stream)
+    return t, t.data_ptr(), n
 
 
-def _differentiable(stream, *tensors) -> bool:
+def _differentiable(stream, a, b=None) -> bool:
     """Whether a call has to be recorded; refuses what it would answer without
     the derivative that is asked for."""
     if forward_ad._current_level >= 0 and any(t is not None and forward_ad.unpack_dual(t).tangent is not None
-                                              for t in tensors):
+                                              for t in (a, b)):
         raise NotImplementedError("no forward-mode derivative")
-    needed = torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors)
-    if needed and stream is not None:
+    if not (a.requires_grad or (b is not None and b.requires_grad)) or not torch.is_grad_enabled():
+        return False
+    if stream is not None:
         raise ValueError("stream: for calls without a gradient")
-    return needed
+    return True
 
 
 def _own_rows(t, cols: int):
     """t, or a copy where its rows do not lie at one distance (an expanded or
     transposed gradient)."""
+    if t.is_contiguous():
+        return t
     try:
         _matrix(t, "", None, cols)
     except ValueError:
@@ -224,7 +231,7 @@ def head_grad(hidden, table, targets, lse, grad, *, scale: float = 1.0, first_id
 class _LinearCrossEntropy(torch.autograd.Function):
     @staticmethod
     def forward(ctx, hidden, table, targets, args, reduction, grad_weight, accumulate):
-        loss, lse, _ = _loss(hidden.detach(), table.detach(), targets, args, reduction, True, False, True, None)
+        loss, lse, _ = _loss(hidden, table, targets, args, reduction, True, False, True, None)
         ctx.save_for_backward(hidden, table, targets, lse)
         ctx.args, ctx.reduction, ctx.into, ctx.accumulate = args, reduction, grad_weight, accumulate
         return loss
@@ -253,23 +260,34 @@ class Act8:
     exponent + 127; 255: a block with an inf or NaN, which stands for NaN).  What
     it stands for, bfloat16, float16 and float32 hold exactly."""
 
-    __slots__ = ("codes", "scales", "shape", "dtype", "rows", "cols", "buffer")
+    __slots__ = ("shape", "dtype", "rows", "cols", "blocks", "buffer", "packed")
 
     def __init__(self, shape, dtype, device="cuda", stream=None):
         if len(shape) == 0:
             raise ValueError("a tensor without dimensions has no blocks")
-        if dtype not in (torch.bfloat16, torch.float16, torch.float32):
+        if dtype not in _TYPES:
             raise ValueError(f"expected bfloat16, float16 or float32, got {dtype}")
         self.shape, self.dtype = torch.Size(shape), dtype
-        self.cols = self.shape[-1]
-        self.rows = math.prod(self.shape[:-1])
-        blocks = -(-self.cols // GOCKPT_ACT8_BLOCK)
-        n = self.rows * blocks
-        with torch.cuda.stream(stream):
+        self.cols = cols = self.shape[-1]
+        self.rows = rows = math.prod(self.shape[:-1])
+        self.blocks = blocks = -(-cols // GOCKPT_ACT8_BLOCK)
+        n = rows * blocks
+        if stream is None:
             self.buffer = torch.empty(n * (GOCKPT_ACT8_BLOCK + 1), dtype=torch.uint8, device=device)
-        wide = n * GOCKPT_ACT8_BLOCK
-        self.codes = self.buffer[:wide].view(torch.int8).view(self.rows, blocks * GOCKPT_ACT8_BLOCK)
-        self.scales = self.buffer[wide:].view(self.rows, blocks)
+        else:
+            with torch.cuda.stream(stream):
+                self.buffer = torch.empty(n * (GOCKPT_ACT8_BLOCK + 1), dtype=torch.uint8, device=device)
+        at = self.buffer.data_ptr()
+        self.packed = ACT8.pack(at, at + n * GOCKPT_ACT8_BLOCK, rows, cols)
+
+    @property
+    def codes(self):
+        n = self.rows * self.blocks * GOCKPT_ACT8_BLOCK
+        return self.buffer[:n].view(torch.int8).view(self.rows, self.blocks * GOCKPT_ACT8_BLOCK)
+
+    @property
+    def scales(self):
+        return self.buffer[self.rows * self.blocks * GOCKPT_ACT8_BLOCK:].view(self.rows, self.blocks)
 
     @property
     def nbytes(self) -> int:
@@ -277,7 +295,7 @@ class Act8:
 
     def _pack(self, device: int) -> bytes:
         _here(self.buffer, "Act8", device)
-        return ACT8.pack(self.codes.data_ptr(), self.scales.data_ptr(), self.rows, self.cols)
+        return self.packed
 
     def unpack(self, *, out=None, dtype=None, stream=None):
         """What it stands for, in dtype (default: the packed tensor's), or in out."""
@@ -327,7 +345,7 @@ def _linear8(x, weight, keep: bool, stream):
     ws, ptr, size = _workspace(weight, "gockpt_linear8_bytes", (mx, mw), stream)
     out = _empty(x, (*x.shape[:-1], rows), x.dtype, stream)
     kept = Act8(x.shape, x.dtype, x.device, stream) if keep else None
-    _check(_lib().gockpt_linear8(mx, mw, _matrix(out, "out", None, rows), None if kept is None else kept._pack(device),
+    _check(_lib().gockpt_linear8(mx, mw, _matrix(out, "out", None, rows), None if kept is None else kept.packed,
                                  ptr, size, _stream(stream, device)), "gockpt_linear8", None)
     return out, kept
 
@@ -374,7 +392,7 @@ def linear8_grad_weight(grad_out, kept: Act8, grad_weight, *, accumulate: bool =
 class _Linear8(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, grad_weight, accumulate):
-        out, kept = _linear8(x.detach(), weight.detach(), ctx.needs_input_grad[1], None)
+        out, kept = _linear8(x, weight, ctx.needs_input_grad[1], None)
         # the weight is read again for x's gradient alone
         ctx.save_for_backward(weight if ctx.needs_input_grad[0] else None, None if kept is None else kept.buffer)
         ctx.kept, ctx.into, ctx.accumulate = kept, grad_weight, accumulate
@@ -423,7 +441,7 @@ def _gate8(x, factor, kind: int, keep: bool, stream):
     out = _empty(x, x.shape, x.dtype, stream)
     kept = [Act8(x.shape, x.dtype, x.device, stream) if keep and t is not None else None for t in (x, factor)]
     _check(_lib().gockpt_gate8(kind, mx, mf, _matrix(out, "out", None, cols),
-                               *(None if k is None else k._pack(device) for k in kept), _stream(stream, device)),
+                               *(None if k is None else k.packed for k in kept), _stream(stream, device)),
            "gockpt_gate8", None)
     return out, kept
 
@@ -442,7 +460,7 @@ def gate8(x, factor=None, *, kind: str = "silu", stream=None):
 class _Gate8(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, factor, kind):
-        out, kept = _gate8(x.detach(), None if factor is None else factor.detach(), kind, True, None)
+        out, kept = _gate8(x, factor, kind, True, None)
         ctx.save_for_backward(*(None if k is None else k.buffer for k in kept))
         ctx.kept, ctx.kind = kept, kind
         return out
