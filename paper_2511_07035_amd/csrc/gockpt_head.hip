@@ -43,7 +43,6 @@ struct TokenArgs {
     int32_t* target;    // and its row of the table, -1 where that is another rank's
     // the loss: zeros for masked tokens (null: not wanted)
     float *lse, *logit, *loss;
-    uint32_t* ticket;
     // the gradients (null: not)
     const float *lse_in, *grad;
     int32_t* of_token;  // number among those that count, or -1
@@ -75,9 +74,12 @@ __global__ __launch_bounds__(kTokenThreads) void token_kernel(TokenArgs a) {
     const bool weighted = a.grad != nullptr && a.reduction == GOCKPT_EACH;
     int32_t mine = 0;
     float most = 0.0f;
+    int64_t first_id = 0;  // of a lane's first token, which may be its only one
 #pragma unroll 4
     for (int64_t t = from + lane; t < to; t += 64) {
-        if (!counts(a, target_of(a, static_cast<int32_t>(t)))) continue;
+        const int64_t id = target_of(a, static_cast<int32_t>(t));
+        if (t == from + lane) first_id = id;
+        if (!counts(a, id)) continue;
         ++mine;
         if (weighted) most = fmaxf(most, fabsf(a.grad[t]));
     }
@@ -109,13 +111,10 @@ __global__ __launch_bounds__(kTokenThreads) void token_kernel(TokenArgs a) {
         up_by = ldexpf(1.0f, 13 - q);
         if (threadIdx.x == 0) *a.unscale = ldexpf(1.0f, q - 13);
     }
-    if (threadIdx.x == 0) {
-        *a.count = all;
-        if (a.ticket != nullptr) *a.ticket = 0;
-    }
+    if (threadIdx.x == 0) *a.count = all;
     for (int64_t at = from; at < to; at += 64) {
         const int64_t t = at + lane;
-        const int64_t id = t < to ? target_of(a, static_cast<int32_t>(t)) : 0;
+        const int64_t id = at == from ? first_id : t < to ? target_of(a, static_cast<int32_t>(t)) : 0;
         const bool there = t < to && counts(a, id);
         const uint64_t votes = __ballot(there);
         const int32_t k = before + __popcll(votes & ((uint64_t{1} << lane) - 1));
@@ -148,6 +147,14 @@ struct LossArgs {
 };
 
 template <class M>
+__device__ __forceinline__ void negate(typename M::Acc& acc) {
+#pragma unroll
+    for (int i = 0; i < M::kFR; ++i)
+#pragma unroll
+        for (int j = 0; j < M::kFC; ++j) acc[i][j] = -acc[i][j];
+}
+
+template <class M>
 __global__ __launch_bounds__(M::kThreads) void logits_kernel(LossArgs g) {
     GOCKPT_MMA_LDS(M)
     const MmaPlace p = mma_place(g.a, M::kBR, M::kBC);
@@ -155,38 +162,63 @@ __global__ __launch_bounds__(M::kThreads) void logits_kernel(LossArgs g) {
     if (p.c0 >= cn) return;
     typename M::Acc acc;
     GOCKPT_MMA_RUN(M, g.a, p, cn, g.a.k, acc);
-    __syncthreads();  // the buffers are free
+    M::sync();  // the buffers are free
     float2(*waves)[M::kBC] = reinterpret_cast<float2(*)[M::kBC]>(lr0);
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    if (g.log2_scale < 0.0f) negate<M>(acc);
+    const float scale = fabsf(g.log2_scale);  // >= 0: the largest product with it is the largest logit
+    const bool edge = M::first_r(p) + M::kFR * 32 > g.a.rn;
 #pragma unroll
     for (int j = 0; j < M::kFC; ++j) {
         const int c = M::c_of(p, j);
         const int want = c < cn ? g.target[c] : -1;
-        float most = -INFINITY;
+        // most tiles hold the targets of none of their tokens
+        if (__any(want >= M::first_r(p) && want < M::first_r(p) + M::kFR * 32)) {
+            float l = 0.0f;
+            bool here = false;
 #pragma unroll
-        for (int i = 0; i < M::kFR; ++i) {
-            const int r = M::r_of(p, i), left = g.a.rn - r, at = want - r;
+            for (int i = 0; i < M::kFR; ++i) {
+                const int at = want - M::r_of(p, i);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int to = 8 * (e / 4) + e % 4;
-                const float l = acc[i][j][e] * g.log2_scale;
-                acc[i][j][e] = to < left ? l : -INFINITY;
-                most = fmaxf(most, acc[i][j][e]);
-                if (at == to && c < cn) g.logit[c] = l;
+                for (int e = 0; e < 16; ++e)
+                    if (at == 8 * (e / 4) + e % 4) {
+                        l = acc[i][j][e];
+                        here = true;
+                    }
+            }
+            if (here) g.logit[c] = l * scale;
+        }
+        if (edge) {
+#pragma unroll
+            for (int i = 0; i < M::kFR; ++i) {
+                const int left = g.a.rn - M::r_of(p, i);
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (8 * (e / 4) + e % 4 >= left) acc[i][j][e] = -INFINITY;
             }
         }
+        float most = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < M::kFR; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) most = fmaxf(most, acc[i][j][e]);
         most = fmaxf(most, __shfl_xor(most, 32));
+        // beyond the last row there is nothing, whatever the scale
+        most = most == -INFINITY ? most : most * scale;
         // a row of nothing but -inf keeps a sum of 0
         const float from = most == -INFINITY ? 0.0f : most;
         float sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < M::kFR; ++i)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) sum += __builtin_amdgcn_exp2f(acc[i][j][e] - from);
+            for (int e = 0; e < 16; ++e) {
+                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][e], scale, -from));
+                sum += edge && acc[i][j][e] == -INFINITY ? 0.0f : x;
+            }
         sum += __shfl_xor(sum, 32);
         if (lane < 32) waves[wave / M::kWC][(wave % M::kWC * M::kFC + j) * 32 + lane] = float2{most, sum};
     }
-    __syncthreads();
+    M::sync();
     for (int i = threadIdx.x; i < M::kBC; i += M::kThreads) {
         if (p.c0 + i >= cn) break;
         float most = -INFINITY, sum = 0.0f;
@@ -207,23 +239,45 @@ struct JoinArgs {
     int32_t reduction;
     float *lse, *logit, *loss;
     float* each;  // the tokens' losses, for their sum
-    uint32_t* ticket;
 };
 
-// A wavefront a token.  For a sum, the block that ends last adds up the tokens'
-// losses, in an order that is the same on every call.
-__global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
+// Up to so many tokens one block joins and adds up.
+constexpr int kJoinWaves = 16, kJoinAlone = 4 * kJoinWaves;
+
+// The sum of all tokens' losses, in an order that is the same on every call.
+__device__ __forceinline__ void sum_losses(const JoinArgs& a, int32_t count) {
+    __shared__ double sums[kJoinWaves];
+    double total = 0.0;
+    for (int32_t k = threadIdx.x; k < count; k += kJoinWaves * 64) total += static_cast<double>(a.each[k]);
+    for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d);
+    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = total;
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    total = 0.0;
+    for (int w = 0; w < kJoinWaves; ++w) total += sums[w];
+    *a.loss = static_cast<float>(a.reduction == GOCKPT_MEAN ? total / max(count, 1) : total);
+}
+
+// A wavefront a token.
+template <bool kAlone>
+__global__ __launch_bounds__(kAlone ? kJoinWaves * 64 : 256) void join_kernel(JoinArgs a) {
+    constexpr int kWaves = kAlone ? kJoinWaves : 4;
     const int lane = threadIdx.x & 63;
     const int32_t count = *a.count;
     const bool single = a.reduction == GOCKPT_EACH;
-    for (int32_t k = blockIdx.x * 4 + (threadIdx.x >> 6); k < count; k += gridDim.x * 4) {
+    for (int32_t k = blockIdx.x * kWaves + (threadIdx.x >> 6); k < count; k += gridDim.x * kWaves) {
         const float2* p = a.part + static_cast<int64_t>(k) * a.tiles_r;
         float most = -INFINITY, sum = 0.0f;
-        for (uint32_t i = lane; i < a.tiles_r; i += 64) {
-            const float2 x = p[i];
-            const float top = fmaxf(most, x.x), from = top == -INFINITY ? 0.0f : top;
-            sum = sum * __builtin_amdgcn_exp2f(most - from) + x.y * __builtin_amdgcn_exp2f(x.x - from);
-            most = top;
+        for (uint32_t i = lane; i < a.tiles_r; i += 256) {
+            float2 x[4];  // on their way together
+#pragma unroll
+            for (int u = 0; u < 4; ++u) x[u] = i + 64 * u < a.tiles_r ? p[i + 64 * u] : float2{-INFINITY, 0.0f};
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const float top = fmaxf(most, x[u].x), from = top == -INFINITY ? 0.0f : top;
+                sum = sum * __builtin_amdgcn_exp2f(most - from) + x[u].y * __builtin_amdgcn_exp2f(x[u].x - from);
+                most = top;
+            }
         }
         float top = most;
         for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
@@ -245,24 +299,15 @@ __global__ __launch_bounds__(256) void join_kernel(JoinArgs a) {
             }
         }
     }
-    if (single || a.loss == nullptr) return;
-    __shared__ uint32_t last;
-    __shared__ double sums[4];
-    __syncthreads();
-    if (threadIdx.x == 0)
-        last = __hip_atomic_fetch_add(a.ticket, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == gridDim.x - 1;
-    __syncthreads();
-    if (!last) return;
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-    double total = 0.0;
-    for (int32_t k = threadIdx.x; k < count; k += 256) total += static_cast<double>(a.each[k]);
-    for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d);
-    if (lane == 0) sums[threadIdx.x >> 6] = total;
-    __syncthreads();
-    if (threadIdx.x != 0) return;
-    total = (sums[0] + sums[1]) + (sums[2] + sums[3]);
-    *a.loss = static_cast<float>(a.reduction == GOCKPT_MEAN ? total / max(count, 1) : total);
+    if constexpr (kAlone) {
+        if (single || a.loss == nullptr) return;
+        __threadfence_block();
+        __syncthreads();
+        sum_losses(a, count);
+    }
 }
+
+__global__ __launch_bounds__(kJoinWaves * 64) void sum_kernel(JoinArgs a) { sum_losses(a, *a.count); }
 
 // ---- the gradients ------------------------------------------------------------------
 
@@ -285,30 +330,47 @@ __global__ __launch_bounds__(M::kThreads) void z_kernel(GradArgs g) {
     if (p.c0 >= cn) return;
     typename M::Acc acc;
     GOCKPT_MMA_RUN(M, g.a, p, cn, g.a.k, acc);
+    const bool edge = M::first_r(p) + M::kFR * 32 > g.a.rn;
 #pragma unroll
     for (int j = 0; j < M::kFC; ++j) {
         const int c = min(M::c_of(p, j), cn - 1);
         const float base = g.base[c], factor = g.factor[c];
-        const int want = g.target[c] - g.first;
-        const bool mine = c == M::c_of(p, j);
+        const int want = M::c_of(p, j) < cn ? g.target[c] - g.first : -1;
 #pragma unroll
-        for (int i = 0; i < M::kFR; ++i) {
-            const int r = M::r_of(p, i), at = want - r, left = g.a.rn - r;
+        for (int i = 0; i < M::kFR; ++i)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int to = 8 * (e / 4) + e % 4;
-                float z = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][e], g.log2_scale, -base));
-                if (at == to) {
-                    z = (z - 1.0f) * factor;
-                    if (mine) g.lost[c] = z - elem_to_f32<M::kT>(pack2<M::kT>(z, z) & 0xffff);
-                } else {
-                    z = to < left ? z * factor : 0.0f;
-                }
-                acc[i][j][e] = z;
+            for (int e = 0; e < 16; ++e)
+                acc[i][j][e] =
+                    __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][e], g.log2_scale, -base)) * factor;
+        // most tiles hold the targets of none of their tokens
+        if (__any(want >= M::first_r(p) && want < M::first_r(p) + M::kFR * 32)) {
+            float lost = 0.0f;
+            bool here = false;
+#pragma unroll
+            for (int i = 0; i < M::kFR; ++i) {
+                const int at = want - M::r_of(p, i);
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (at == 8 * (e / 4) + e % 4) {
+                        const float z = acc[i][j][e] - factor;
+                        acc[i][j][e] = z;
+                        lost = z - elem_to_f32<M::kT>(pack2<M::kT>(z, z) & 0xffff);
+                        here = true;
+                    }
+            }
+            if (here) g.lost[c] = lost;
+        }
+        if (edge) {
+#pragma unroll
+            for (int i = 0; i < M::kFR; ++i) {
+                const int left = g.a.rn - M::r_of(p, i);
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (8 * (e / 4) + e % 4 >= left) acc[i][j][e] = 0.0f;
             }
         }
     }
-    __syncthreads();
+    M::sync();
     const Store<M> store = GOCKPT_MMA_STORE(M);
     const int wide = (g.a.rn + 7) / 8 * 8;  // the products read whole pieces of 8: zeros behind the last row
 #pragma unroll
@@ -326,7 +388,7 @@ void start_logits(int shape, const LossArgs& g, hipStream_t s) {
     const dim3 grid(g.a.tiles_r * g.a.tiles_c);
     using W = Mma<kT, kAlongK, kAlongK, 256, 256, 2, 4>;
     using D = Mma<kT, kAlongK, kAlongK, 128, 128, 2, 2>;
-    using T = Mma<kT, kAlongK, kAlongK, 128, 32, 4, 1>;
+    using T = Stream<kT>;
     if (shape == kWide)
         hipLaunchKernelGGL(logits_kernel<W>, grid, dim3(W::kThreads), 0, s, g);
     else if (shape == kMid)
@@ -340,7 +402,7 @@ void start_z(int shape, const GradArgs& g, hipStream_t s) {
     const dim3 grid(g.a.tiles_r * g.a.tiles_c);
     using W = Mma<kT, kAlongK, kAlongK, 256, 256, 2, 4>;
     using D = Mma<kT, kAlongK, kAlongK, 128, 128, 2, 2>;
-    using T = Mma<kT, kAlongK, kAlongK, 128, 32, 4, 1>;
+    using T = Stream<kT>;
     if (shape == kWide)
         hipLaunchKernelGGL(z_kernel<W>, grid, dim3(W::kThreads), 0, s, g);
     else if (shape == kMid)
@@ -423,7 +485,7 @@ LossPlan plan_loss(const gockpt_head& h) {
     Parts parts;
     const int64_t n = h.hidden.rows;
     p.logits = plan_product(kAlongAlong, h.table.rows, n, h.table.cols, 1);
-    p.count = parts.take(8);  // and the ticket
+    p.count = parts.take(4);
     p.of_kept = parts.take(n * 4);
     p.target = parts.take(n * 4);
     p.part = parts.take(n * p.logits.tiles_r * 8);
@@ -562,7 +624,6 @@ int gockpt_head_loss(const gockpt_head* head, int reduction, float* loss, float*
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     t.reduction = reduction;
     t.count = reinterpret_cast<int32_t*>(ws + p.count);
-    t.ticket = reinterpret_cast<uint32_t*>(ws + p.count + 4);
     t.of_kept = reinterpret_cast<int32_t*>(ws + p.of_kept);
     t.target = reinterpret_cast<int32_t*>(ws + p.target);
     t.lse = lse;
@@ -609,8 +670,13 @@ int gockpt_head_loss(const gockpt_head* head, int reduction, float* loss, float*
     j.logit = logit;
     j.loss = loss;
     j.each = reinterpret_cast<float*>(ws + p.each);
-    j.ticket = t.ticket;
-    hipLaunchKernelGGL(join_kernel, dim3(std::max(1, std::min((t.tokens + 3) / 4, kUnits * 4))), dim3(256), 0, s, j);
+    if (t.tokens <= kJoinAlone) {
+        hipLaunchKernelGGL(join_kernel<true>, dim3(1), dim3(kJoinWaves * 64), 0, s, j);
+    } else {
+        hipLaunchKernelGGL(join_kernel<false>, dim3(std::min((t.tokens + 3) / 4, kUnits * 8)), dim3(256), 0, s, j);
+        if (loss != nullptr && reduction != GOCKPT_EACH)
+            hipLaunchKernelGGL(sum_kernel, dim3(1), dim3(kJoinWaves * 64), 0, s, j);
+    }
     return ops_launched(name);
 }
 

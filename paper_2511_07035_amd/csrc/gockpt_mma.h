@@ -108,10 +108,9 @@ struct Filler {
         if constexpr (kLay == kAlongK) {
             base = uniform(rows != nullptr ? data : data + static_cast<int64_t>(i0) * stride);
             step = 2 * kStepK;
-            static_assert(kWaves % 2 == 0, "rows 8 * wave on, modulo 16");
-            const int piece = (lane & 7) ^ ((wave & 1) * 4 + (lane >> 4));
 #pragma unroll
             for (int j = 0; j < kPieces; ++j) {
+                const int piece = (lane & 7) ^ (((j * kWaves + wave) & 1) * 4 + (lane >> 4));
                 const int i = min((j * kWaves + wave) * 8 + (lane >> 3), n - 1 - i0);
                 const uint32_t row = rows != nullptr ? static_cast<uint32_t>(rows[i0 + i]) : static_cast<uint32_t>(i);
                 off[j] = row * static_cast<uint32_t>(stride) + piece * 16;
@@ -225,6 +224,7 @@ struct Mma {
     static constexpr int kWaves = kWR * kWC, kThreads = kWaves * 64;
     static constexpr int kFR = kBR / kWR / 32, kFC = kBC / kWC / 32;  // fragments of a wave
     static constexpr int kRBytes = kBR * kStepK * 2, kCBytes = kBC * kStepK * 2;
+    static constexpr bool kOneWave = false;
     static_assert(kFR >= 1 && kFC >= 1 && kFR <= 4 && kFC <= 4, "fragments of a wave");
 
     using Acc = f32x16[kFR][kFC];
@@ -374,6 +374,9 @@ struct Mma {
         }
     }
 
+    // All wavefronts are through with the product.
+    static __device__ __forceinline__ void sync() { __syncthreads(); }
+
     // Where the wavefront's fragments begin.
     static __device__ __forceinline__ int first_r(const MmaPlace& p) {
         return p.r0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / kWC * kFR * 32;
@@ -387,6 +390,158 @@ struct Mma {
         return first_r(p) + i * 32 + 4 * ((threadIdx.x & 63) >> 5);
     }
     static __device__ __forceinline__ int c_of(const MmaPlace& p, int j) { return first_c(p, j) + (threadIdx.x & 31); }
+};
+
+// The product of at most 32 c, both operands along k: R is read once, and that is
+// the time it takes.  A block takes 32 r, each of its wavefronts every fourth tile
+// of k: R's through buffers of its own, kAhead of them on their way, C's straight
+// into registers, with no barrier before the sums of the four are put together.
+// 32000 x 1 x 4096, 262 MB not read before: 46 us; R's fragments loaded into
+// registers, whose every load takes a quarter of 32 lines, 53; tiles of 128 r, of
+// which a compute unit has one with 16 KiB on their way, 58.
+template <int kT_>
+struct Stream {
+    static constexpr int kT = kT_, kBR = 32, kBC = 32, kWR = 1, kWC = 1, kFR = 1, kFC = 1;
+    static constexpr int kWaves = 4, kThreads = 256, kAhead = 4;
+    static constexpr int kTile = 32 * kStepK * 2;
+    static constexpr int kRBytes = kWaves * kTile, kCBytes = kWaves * kTile;
+    static constexpr bool kOneWave = true;  // the first wavefront has the sum
+    using Acc = f32x16[1][1];
+
+    struct State {
+        Filler<kAlongK, 32, 1> fill;
+        Reader<kAlongK, 32> reader;
+        const uint8_t* c;  // this lane's index of C at the first k, its half's piece
+        int lane, wave, k, from, whole;
+
+        // The wavefront's t-th tile of k: the whole ones in turn (see above).
+        __device__ __forceinline__ int turned(int t) const {
+            if (t < whole) {
+                t += from;
+                t -= t >= whole ? whole : 0;
+            }
+            return t * kWaves + wave;
+        }
+
+        template <bool kWhole>
+        __device__ __forceinline__ void load(GOCKPT_LDS uint8_t* r, u32x4 (&f)[4], int t) {
+            const int tile = turned(t), left = k - tile * kStepK;
+            fill.template fill<kWhole>(r, tile, left, 0);
+            const uint8_t* p = c + static_cast<int64_t>(tile) * (2 * kStepK);
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const bool there = kWhole || (2 * s + (lane >> 5)) * 8 < left;
+                // the tile's first piece is there
+                const u32x4 x = *reinterpret_cast<const u32x4*>(there ? p + s * 32 : p - (lane >> 5) * 16);
+                f[s] = there ? x : u32x4{0, 0, 0, 0};
+            }
+        }
+
+        template <bool kWhole>
+        __device__ __forceinline__ void multiply(GOCKPT_LDS uint8_t* r, const u32x4 (&f)[4], int t, Acc& acc) {
+            if (!kWhole) {
+                const int left = k - turned(t) * kStepK;
+                wait_copies();
+                if (left < kStepK) fill.clear(r, left, lane, 0);
+            }
+#pragma unroll
+            for (int s = 0; s < 4; ++s) acc[0][0] = mma<kT>(reader.read(r, 0, s), f[s], acc[0][0]);
+        }
+    };
+
+    static __device__ __forceinline__ void run(const MmaArgs& a, const MmaPlace& p, int cn, int k_all,
+                                               GOCKPT_LDS uint8_t* b0, GOCKPT_LDS uint8_t* b1, GOCKPT_LDS uint8_t* b2,
+                                               GOCKPT_LDS uint8_t* b3, Acc& acc) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[0][0][e] = 0.0f;
+        State st;
+        st.lane = threadIdx.x & 63;
+        st.wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        const int64_t k0 = static_cast<int64_t>(p.split) * a.split_k;
+        st.k = static_cast<int>(min(static_cast<int64_t>(a.split_k), k_all - k0));
+        GOCKPT_LDS uint8_t* const first = b0;
+        b0 += st.wave * kTile;
+        b1 += st.wave * kTile;
+        b2 += st.wave * kTile;
+        b3 += st.wave * kTile;
+        if (st.k > 0) {
+            st.fill.init(a.r + k0 * 2, a.r_stride, p.r0, a.rn, nullptr, st.lane, 0);
+            st.reader.init(0, st.lane);
+            const int at = min(p.c0 + (st.lane & 31), cn - 1);
+            st.c = a.c + k0 * 2 + (a.c_rows != nullptr ? a.c_rows[at] : at) * a.c_stride + (st.lane >> 5) * 16;
+            const int tiles = ((st.k + kStepK - 1) / kStepK - st.wave + kWaves - 1) / kWaves;  // wave, wave + 4, ...
+            st.whole = (st.k / kStepK - st.wave + kWaves - 1) / kWaves;
+            st.from = st.whole > 0 ? static_cast<int>(p.tile_r % st.whole) : 0;
+            u32x4 f[kAhead][4];
+            int t = 0;
+            const auto next = [&](GOCKPT_LDS uint8_t* b, u32x4 (&g)[4], int u) {
+                st.template multiply<true>(b, g, u, acc);
+                st.template load<true>(b, g, u + kAhead);
+                // else the compiler waits once for all four tiles
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            if (2 * kAhead <= st.whole) {
+                // the loop's loads in the loop's order: waits then count them
+                st.template load<true>(b0, f[0], 0);
+                __builtin_amdgcn_sched_barrier(0);
+                st.template load<true>(b1, f[1], 1);
+                __builtin_amdgcn_sched_barrier(0);
+                st.template load<true>(b2, f[2], 2);
+                __builtin_amdgcn_sched_barrier(0);
+                st.template load<true>(b3, f[3], 3);
+                __builtin_amdgcn_sched_barrier(0);
+                do {
+                    next(b0, f[0], t);
+                    next(b1, f[1], t + 1);
+                    next(b2, f[2], t + 2);
+                    next(b3, f[3], t + 3);
+                    t += kAhead;
+                } while (t + 2 * kAhead <= st.whole);
+            } else {
+                if (0 < tiles) st.template load<false>(b0, f[0], 0);
+                if (1 < tiles) st.template load<false>(b1, f[1], 1);
+                if (2 < tiles) st.template load<false>(b2, f[2], 2);
+                if (3 < tiles) st.template load<false>(b3, f[3], 3);
+            }
+            const auto last = [&](GOCKPT_LDS uint8_t* b, u32x4 (&g)[4], int u) {
+                if (u < tiles) {
+                    st.template multiply<false>(b, g, u, acc);
+                    if (u + kAhead < tiles) st.template load<false>(b, g, u + kAhead);
+                }
+            };
+            for (; t < tiles; t += kAhead) {
+                last(b0, f[0], t);
+                last(b1, f[1], t + 1);
+                last(b2, f[2], t + 2);
+                last(b3, f[3], t + 3);
+            }
+        }
+        if (st.wave > 0) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *reinterpret_cast<GOCKPT_LDS f32x4*>(b0 + (q * 64 + st.lane) * 16) = f32x4{
+                    acc[0][0][4 * q], acc[0][0][4 * q + 1], acc[0][0][4 * q + 2], acc[0][0][4 * q + 3]};
+        }
+        __syncthreads();
+        if (st.wave > 0) return;
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const f32x4 x =
+                    *reinterpret_cast<const GOCKPT_LDS f32x4*>(first + w * kTile + (q * 64 + st.lane) * 16);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[0][0][4 * q + e] += x[e];
+            }
+        }
+    }
+
+    // One wavefront is left.
+    static __device__ __forceinline__ void sync() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+    static __device__ __forceinline__ int first_r(const MmaPlace& p) { return p.r0; }
+    static __device__ __forceinline__ int first_c(const MmaPlace& p, int) { return p.c0; }
+    static __device__ __forceinline__ int r_of(const MmaPlace& p, int) { return p.r0 + 4 * ((threadIdx.x & 63) >> 5); }
+    static __device__ __forceinline__ int c_of(const MmaPlace& p, int) { return p.c0 + (threadIdx.x & 31); }
 };
 
 // Where a product's values go.
@@ -604,7 +759,8 @@ __device__ __forceinline__ void store_tile(const Store<M>& store, const MmaArgs&
 
 #define GOCKPT_MMA_RUN(M, a, p, cn, k, acc)                                                     \
     M::run(a, p, cn, k, (GOCKPT_LDS uint8_t*)lr0, (GOCKPT_LDS uint8_t*)lc0,                     \
-           (GOCKPT_LDS uint8_t*)lr1, (GOCKPT_LDS uint8_t*)lc1, acc)
+           (GOCKPT_LDS uint8_t*)lr1, (GOCKPT_LDS uint8_t*)lc1, acc);                            \
+    if (M::kOneWave && threadIdx.x >= 64) return
 
 // Once all wavefronts are through with the product.
 #define GOCKPT_MMA_STORE(M)                                                                       \

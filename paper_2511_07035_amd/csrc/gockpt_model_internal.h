@@ -57,7 +57,8 @@ void launch_rows(const gockpt_matrix& src, const int32_t* rows, const int32_t* c
 
 // The products by how their operands lie (R, C).
 enum ProductKind : int { kAlongAlong = 0, kAcrossAlong = 1, kAcrossAcross = 2 };
-enum Shape : int { kWide = 0, kMid = 1, kThin = 2 };  // 256 x 256, 128 x 128, 128 x 32 tiles of r x c
+// 256 x 256, 128 x 128 and 128 x 32 tiles of r x c, the last one 32 x 32 where both lie along k
+enum Shape : int { kWide = 0, kMid = 1, kThin = 2 };
 
 struct ProductPlan {
     int shape;

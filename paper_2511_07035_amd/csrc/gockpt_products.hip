@@ -17,7 +17,7 @@ __global__ __launch_bounds__(M::kThreads) void product_kernel(MmaArgs a, StoreAr
     const int k = a.k_dev != nullptr ? *a.k_dev : a.k;
     typename M::Acc acc;
     GOCKPT_MMA_RUN(M, a, p, cn, k, acc);
-    __syncthreads();
+    M::sync();
     store_tile<M>(GOCKPT_MMA_STORE(M), a, o, p, cn, acc);
 }
 
@@ -30,7 +30,10 @@ template <int kT, int kR, int kC>
 void start_shape(int shape, const MmaArgs& a, const StoreArgs& o, hipStream_t s) {
     if (shape == kWide) return start<Mma<kT, kR, kC, 256, 256, 2, 4>>(a, o, s);
     if (shape == kMid) return start<Mma<kT, kR, kC, 128, 128, 2, 2>>(a, o, s);
-    if constexpr (kC == kAlongK) start<Mma<kT, kR, kC, 128, 32, 4, 1>>(a, o, s);
+    if constexpr (kR == kAlongK)
+        start<Stream<kT>>(a, o, s);
+    else if constexpr (kC == kAlongK)
+        start<Mma<kT, kR, kC, 128, 32, 4, 1>>(a, o, s);
 }
 
 template <int kT>
@@ -140,14 +143,15 @@ ProductPlan plan_product(int kind, int64_t rn, int64_t cn, int64_t k, int most_s
         int br, bc, each;
         double fixed, per_k;
     };
-    static constexpr Cost kCosts[3] = {{256, 256, 1, 5.0, 0.0275}, {128, 128, 2, 4.0, 0.0165}, {128, 32, 4, 3.0, 0.012}};
+    static constexpr Cost kWideTile = {256, 256, 1, 5.0, 0.0275}, kMidTile = {128, 128, 2, 4.0, 0.0165},
+                          kThinTile = {128, 32, 4, 3.0, 0.012}, kStream = {32, 32, 4, 2.0, 0.003};
     const bool along = kind == kAlongAlong || kind == kAcrossAlong;
     const double least = 2.0 * static_cast<double>(rn + cn) * static_cast<double>(k) / 5.5e6;  // us to read both
     ProductPlan best{};
     best.us = -1.0;
     for (int shape = kWide; shape <= kThin; ++shape) {
         if (shape == kThin && (!along || cn > 32)) continue;
-        const Cost& t = kCosts[shape];
+        const Cost& t = shape == kWide ? kWideTile : shape == kMid ? kMidTile : kind == kAlongAlong ? kStream : kThinTile;
         const int64_t tr = (rn + t.br - 1) / t.br, tc = (cn + t.bc - 1) / t.bc, tiles = tr * tc;
         const int64_t slots = int64_t{kUnits} * t.each;
         for (int want = 1; want <= most_splits; want *= 2) {
