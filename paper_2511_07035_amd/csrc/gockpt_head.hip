@@ -167,21 +167,21 @@ __global__ __launch_bounds__(M::kThreads) void logits_kernel(LossArgs g) {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     if (g.log2_scale < 0.0f) negate<M>(acc);
     const float scale = fabsf(g.log2_scale);  // >= 0: the largest product with it is the largest logit
-    const bool edge = M::first_r(p) + M::kFR * 32 > g.a.rn;
+    const bool edge = M::first_r(p) + M::kFR * 16 > g.a.rn;
 #pragma unroll
     for (int j = 0; j < M::kFC; ++j) {
         const int c = M::c_of(p, j);
         const int want = c < cn ? g.target[c] : -1;
         // most tiles hold the targets of none of their tokens
-        if (__any(want >= M::first_r(p) && want < M::first_r(p) + M::kFR * 32)) {
+        if (__any(want >= M::first_r(p) && want < M::first_r(p) + M::kFR * 16)) {
             float l = 0.0f;
             bool here = false;
 #pragma unroll
             for (int i = 0; i < M::kFR; ++i) {
                 const int at = want - M::r_of(p, i);
 #pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (at == 8 * (e / 4) + e % 4) {
+                for (int e = 0; e < 4; ++e)
+                    if (at == e) {
                         l = acc[i][j][e];
                         here = true;
                     }
@@ -193,15 +193,16 @@ __global__ __launch_bounds__(M::kThreads) void logits_kernel(LossArgs g) {
             for (int i = 0; i < M::kFR; ++i) {
                 const int left = g.a.rn - M::r_of(p, i);
 #pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (8 * (e / 4) + e % 4 >= left) acc[i][j][e] = -INFINITY;
+                for (int e = 0; e < 4; ++e)
+                    if (e >= left) acc[i][j][e] = -INFINITY;
             }
         }
         float most = -INFINITY;
 #pragma unroll
         for (int i = 0; i < M::kFR; ++i)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) most = fmaxf(most, acc[i][j][e]);
+            for (int e = 0; e < 4; ++e) most = fmaxf(most, acc[i][j][e]);
+        most = fmaxf(most, __shfl_xor(most, 16));
         most = fmaxf(most, __shfl_xor(most, 32));
         // beyond the last row there is nothing, whatever the scale
         most = most == -INFINITY ? most : most * scale;
@@ -211,12 +212,13 @@ __global__ __launch_bounds__(M::kThreads) void logits_kernel(LossArgs g) {
 #pragma unroll
         for (int i = 0; i < M::kFR; ++i)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
+            for (int e = 0; e < 4; ++e) {
                 const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][e], scale, -from));
                 sum += edge && acc[i][j][e] == -INFINITY ? 0.0f : x;
             }
+        sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
-        if (lane < 32) waves[wave / M::kWC][(wave % M::kWC * M::kFC + j) * 32 + lane] = float2{most, sum};
+        if (lane < 16) waves[wave / M::kWC][(wave % M::kWC * M::kFC + j) * 16 + lane] = float2{most, sum};
     }
     M::sync();
     for (int i = threadIdx.x; i < M::kBC; i += M::kThreads) {
@@ -330,7 +332,7 @@ __global__ __launch_bounds__(M::kThreads) void z_kernel(GradArgs g) {
     if (p.c0 >= cn) return;
     typename M::Acc acc;
     GOCKPT_MMA_RUN(M, g.a, p, cn, g.a.k, acc);
-    const bool edge = M::first_r(p) + M::kFR * 32 > g.a.rn;
+    const bool edge = M::first_r(p) + M::kFR * 16 > g.a.rn;
 #pragma unroll
     for (int j = 0; j < M::kFC; ++j) {
         const int c = min(M::c_of(p, j), cn - 1);
@@ -339,19 +341,19 @@ __global__ __launch_bounds__(M::kThreads) void z_kernel(GradArgs g) {
 #pragma unroll
         for (int i = 0; i < M::kFR; ++i)
 #pragma unroll
-            for (int e = 0; e < 16; ++e)
+            for (int e = 0; e < 4; ++e)
                 acc[i][j][e] =
                     __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][e], g.log2_scale, -base)) * factor;
         // most tiles hold the targets of none of their tokens
-        if (__any(want >= M::first_r(p) && want < M::first_r(p) + M::kFR * 32)) {
+        if (__any(want >= M::first_r(p) && want < M::first_r(p) + M::kFR * 16)) {
             float lost = 0.0f;
             bool here = false;
 #pragma unroll
             for (int i = 0; i < M::kFR; ++i) {
                 const int at = want - M::r_of(p, i);
 #pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (at == 8 * (e / 4) + e % 4) {
+                for (int e = 0; e < 4; ++e)
+                    if (at == e) {
                         const float z = acc[i][j][e] - factor;
                         acc[i][j][e] = z;
                         lost = z - elem_to_f32<M::kT>(pack2<M::kT>(z, z) & 0xffff);
@@ -365,8 +367,8 @@ __global__ __launch_bounds__(M::kThreads) void z_kernel(GradArgs g) {
             for (int i = 0; i < M::kFR; ++i) {
                 const int left = g.a.rn - M::r_of(p, i);
 #pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    if (8 * (e / 4) + e % 4 >= left) acc[i][j][e] = 0.0f;
+                for (int e = 0; e < 4; ++e)
+                    if (e >= left) acc[i][j][e] = 0.0f;
             }
         }
     }

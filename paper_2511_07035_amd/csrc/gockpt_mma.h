@@ -17,9 +17,9 @@
 //             fragment is one 16-byte read a lane, 16 lanes at a time, and of 16
 //             rows every other one lies in the same banks (with i & 7 the counters
 //             showed as many cycles of conflicts as of reads).
-//   kAcrossK  rows of k, 32-byte unit u of row k at u ^ f(k & 3), f = 0, 3, 5, 6:
-//             the four rows that a transposing read takes together then lie in
-//             different banks, also where two units are read at once.
+//   kAcrossK  rows of k, 32-byte unit u of row k at u ^ f(k), f = 0, 3, 5, 6 for k &
+//             3, and the lowest bit of that turned where k & 8: the eight rows that
+//             32 lanes of a transposing read take then lie in different banks.
 // A fragment of step s + 1 is read while step s is multiplied, across the
 // barrier between two tiles as well: a wave holds the last step's fragments
 // in registers when it passes it.
@@ -41,7 +41,6 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef f32x4 f32x4_any __attribute__((aligned(2)));
 
 enum Lay : int { kAlongK = 0, kAcrossK = 1 };
@@ -65,17 +64,19 @@ struct MmaArgs {
     int32_t splits, split_k;  // slices of k and their length, a multiple of 64
 };
 
+// 16 r by 16 c by 32 k.  (32 by 32 by 16 needs as many cycles and registers, and
+// was slower: 8192 x 8192 x 8192 817 us against 744.)
 template <int kT>
-__device__ __forceinline__ f32x16 mma(u32x4 a, u32x4 b, f32x16 c) {
+__device__ __forceinline__ f32x4 mma(u32x4 a, u32x4 b, f32x4 c) {
     if constexpr (kT == kBF16)
-        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c,
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c,
                                                        0, 0, 0);
     else
-        return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0,
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0,
                                                       0, 0);
 }
 
-__device__ __forceinline__ int unit_swizzle(int k) { return ((k & 3) << 1) | ((k ^ (k >> 1)) & 1); }
+__device__ __forceinline__ int unit_swizzle(int k) { return (((k & 3) << 1) | ((k ^ (k >> 1)) & 1)) ^ (k >> 3 & 1); }
 
 template <class T>
 __device__ __forceinline__ T* uniform(T* p) {
@@ -96,11 +97,16 @@ struct Filler {
     static constexpr int kRowLanes = kB / 8;         // kAcrossK: lanes that copy a row of k
     static_assert(kPieces >= 1, "each wave copies");
 
+    // kAcrossK: a wave's copies lie 16 rows of k apart, at the same piece each
+    static_assert(kLay == kAlongK || 64 / kRowLanes * kWaves == 16, "rows of k alike in the swizzle");
+    static constexpr int kOffs = kLay == kAlongK ? kPieces : 1;
+
     const uint8_t* base;  // of the tile's first index, at k = 0
     int64_t step;         // bytes from one tile of k to the next
-    uint32_t off[kPieces];
-    uint32_t back[kPieces];  // from off to a place that is there in every tile of k
-    int k_of[kPieces];       // first k of the lane's piece within the tile
+    uint32_t apart;       // kAcrossK: from one copy to the next
+    uint32_t off[kOffs];
+    uint32_t back[kOffs];  // from off to a place that is there in every tile of k
+    int k_of[kOffs];       // first k of the lane's piece within the tile
 
     // Tile at index i0 < n of the operand; rows: see MmaArgs.c_rows.
     __device__ __forceinline__ void init(const uint8_t* data, int64_t stride, int i0, int n, const int32_t* rows,
@@ -120,17 +126,13 @@ struct Filler {
         } else {
             base = uniform(data + static_cast<int64_t>(i0) * 2);
             step = stride * kStepK;
-            constexpr int kRows = 64 / kRowLanes;  // rows of k in one copy
-#pragma unroll
-            for (int j = 0; j < kPieces; ++j) {
-                const int k = (j * kWaves + wave) * kRows + lane / kRowLanes;
-                const int at = lane % kRowLanes;
-                int piece = ((at >> 1) ^ (unit_swizzle(k) & (kRowLanes / 2 - 1))) * 2 + (at & 1);
-                if (i0 + piece * 8 >= n) piece = 0;
-                back[j] = static_cast<uint32_t>(k) * static_cast<uint32_t>(stride);
-                off[j] = back[j] + piece * 16;
-                k_of[j] = k;
-            }
+            apart = 16 * static_cast<uint32_t>(stride);
+            const int k = wave * (64 / kRowLanes) + lane / kRowLanes, at = lane % kRowLanes;
+            int piece = ((at >> 1) ^ (unit_swizzle(k) & (kRowLanes / 2 - 1))) * 2 + (at & 1);
+            if (i0 + piece * 8 >= n) piece = 0;
+            back[0] = static_cast<uint32_t>(k) * static_cast<uint32_t>(stride);
+            off[0] = back[0] + piece * 16;
+            k_of[0] = k;
         }
     }
 
@@ -142,9 +144,18 @@ struct Filler {
         __amdgpu_buffer_rsrc_t res = __builtin_amdgcn_make_buffer_rsrc(
             const_cast<uint8_t*>(base + static_cast<int64_t>(tile) * step), 0, 0xffffffff, 0x00027000);
 #pragma unroll
-        for (int j = 0; j < kPieces; ++j)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(res, (GOCKPT_LDS void*)(lds + (j * kWaves + wave) * 1024), 16,
-                                                     kWhole || k_of[j] < left ? off[j] : off[j] - back[j], 0, 0, 0);
+        for (int j = 0; j < kPieces; ++j) {
+            GOCKPT_LDS void* const to = (GOCKPT_LDS void*)(lds + (j * kWaves + wave) * 1024);
+            if constexpr (kLay == kAlongK) {
+                const uint32_t at = kWhole || k_of[j] < left ? off[j] : off[j] - back[j];
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(res, to, 16, at, 0, 0, 0);
+            } else if constexpr (kWhole) {
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(res, to, 16, off[0], j * apart, 0, 0);
+            } else {  // in place of a row that is not there, the tile's first
+                const uint32_t at = k_of[0] + j * 16 < left ? off[0] + j * apart : off[0] - back[0];
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(res, to, 16, at, 0, 0, 0);
+            }
+        }
 #endif
     }
 
@@ -152,37 +163,35 @@ struct Filler {
     __device__ __forceinline__ void clear(GOCKPT_LDS uint8_t* lds, int left, int lane, int wave) {
 #pragma unroll
         for (int j = 0; j < kPieces; ++j)
-            if (k_of[j] >= left)
+            if ((kLay == kAlongK ? k_of[j % kOffs] : k_of[0] + j * 16) >= left)
                 *reinterpret_cast<GOCKPT_LDS u32x4*>(lds + (j * kWaves + wave) * 1024 + lane * 16) = u32x4{0, 0, 0, 0};
     }
 
 };
 
-// Fragments of 32 indexes by 16 k: lane l holds index l & 31, k 8 * (l >> 5) on.
-template <int kLay, int kB>
+// Fragments of 16 indexes by 32 k: lane l holds index l & 15, k 8 * (l >> 4) on.
+template <int kLay, int kB, int kBlocks>
 struct Reader {
-    uint32_t at[4];  // kAlongK: of each step's piece; kAcrossK: of index blocks 0 to 3
+    uint32_t at[kLay == kAlongK ? 2 : kBlocks];  // of each step's piece, or of each block of indexes
 
     __device__ __forceinline__ void init(int first, int lane) {
+        const int t = lane & 15, up = lane >> 4;
         if constexpr (kLay == kAlongK) {
 #pragma unroll
-            for (int s = 0; s < 4; ++s)
-                at[s] = (first + (lane & 31)) * 128 + (((2 * s + (lane >> 5)) ^ (lane >> 1 & 7)) << 4);
+            for (int s = 0; s < 2; ++s) at[s] = (first + t) * 128 + (((4 * s + up) ^ (lane >> 1 & 7)) << 4);
         } else {
-            const int t = lane & 15, k = (lane >> 5) * 8 + (t >> 2);
-            const int f = unit_swizzle(t >> 2) & (kB / 16 - 1);
+            const int k = up * 8 + (t >> 2), f = unit_swizzle(k) & (kB / 16 - 1);
 #pragma unroll
-            for (int b = 0; b < 4; ++b)
-                at[b] = k * (2 * kB) + (((first + 32 * b) / 16 + ((lane >> 4) & 1)) ^ f) * 32 + (t & 3) * 8;
+            for (int b = 0; b < kBlocks; ++b) at[b] = k * (2 * kB) + ((first / 16 + b) ^ f) * 32 + (t & 3) * 8;
         }
     }
 
-    // Index block b (32 indexes from first on), k step s.
+    // Block b (16 indexes from first on), step s of the tile's two.
     __device__ __forceinline__ u32x4 read(const GOCKPT_LDS uint8_t* lds, int b, int s) const {
         if constexpr (kLay == kAlongK) {
-            return *reinterpret_cast<const GOCKPT_LDS u32x4*>(lds + at[s] + b * 32 * 128);
+            return *reinterpret_cast<const GOCKPT_LDS u32x4*>(lds + at[s] + b * 16 * 128);
         } else {
-            GOCKPT_LDS s16x4* p = (GOCKPT_LDS s16x4*)(lds + at[b] + s * 16 * (2 * kB));
+            GOCKPT_LDS s16x4* p = (GOCKPT_LDS s16x4*)(lds + at[b] + s * 32 * (2 * kB));
             const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(p);
             const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(p + 4 * (2 * kB) / 8);
             const u32x2 a = __builtin_bit_cast(u32x2, lo), c = __builtin_bit_cast(u32x2, hi);
@@ -222,18 +231,18 @@ template <int kT_, int kRLay, int kCLay, int kBR_, int kBC_, int kWR_, int kWC_>
 struct Mma {
     static constexpr int kT = kT_, kBR = kBR_, kBC = kBC_, kWR = kWR_, kWC = kWC_;
     static constexpr int kWaves = kWR * kWC, kThreads = kWaves * 64;
-    static constexpr int kFR = kBR / kWR / 32, kFC = kBC / kWC / 32;  // fragments of a wave
+    static constexpr int kFR = kBR / kWR / 16, kFC = kBC / kWC / 16;  // fragments of a wave
     static constexpr int kRBytes = kBR * kStepK * 2, kCBytes = kBC * kStepK * 2;
     static constexpr bool kOneWave = false;
-    static_assert(kFR >= 1 && kFC >= 1 && kFR <= 4 && kFC <= 4, "fragments of a wave");
+    static_assert(kFR % 2 == 0 && kFC >= 1, "fragments of a wave");
 
-    using Acc = f32x16[kFR][kFC];
+    using Acc = f32x4[kFR][kFC];
 
     struct State {
         Filler<kRLay, kBR, kWaves> fr;
         Filler<kCLay, kBC, kWaves> fc;
-        Reader<kRLay, kBR> rr;
-        Reader<kCLay, kBC> rc;
+        Reader<kRLay, kBR, kFR> rr;
+        Reader<kCLay, kBC, kFC> rc;
         int lane, wave, k;
         int from, whole;  // the k tile to begin with, of so many whole ones
     };
@@ -268,33 +277,41 @@ struct Mma {
         __syncthreads();
     }
 
-    struct Frags {
-        u32x4 r[kFR], c[kFC];
+    // A step's fragments of C, and one half of R's.
+    struct Cols {
+        u32x4 f[kFC];
+    };
+    struct Half {
+        u32x4 f[kFR / 2];
     };
 
-    static __device__ __forceinline__ void read(const State& st, Frags& f, const GOCKPT_LDS uint8_t* r,
-                                                const GOCKPT_LDS uint8_t* c, int s) {
+    static __device__ __forceinline__ void read(const State& st, Cols& x, const GOCKPT_LDS uint8_t* c, int s) {
 #pragma unroll
-        for (int j = 0; j < kFC; ++j) f.c[j] = st.rc.read(c, j, s);
-#pragma unroll
-        for (int i = 0; i < kFR; ++i) f.r[i] = st.rr.read(r, i, s);
+        for (int j = 0; j < kFC; ++j) x.f[j] = st.rc.read(c, j, s);
     }
 
-    static __device__ __forceinline__ void multiply(const Frags& f, Acc& acc) {
+    static __device__ __forceinline__ void read(const State& st, Half& x, const GOCKPT_LDS uint8_t* r, int s, int h) {
 #pragma unroll
-        for (int i = 0; i < kFR; ++i)
-#pragma unroll
-            for (int j = 0; j < kFC; ++j) acc[i][j] = mma<kT>(f.r[i], f.c[j], acc[i][j]);
+        for (int i = 0; i < kFR / 2; ++i) x.f[i] = st.rr.read(r, h * (kFR / 2) + i, s);
     }
 
-    // Asks for an even mix of a step's products with the reads for the next
-    // one (and, in a tile's last step, the copies): left alone, the compiler
-    // puts each read right before its use.
-    static constexpr int kReads = kFR * (kRLay == kAlongK ? 1 : 2) + kFC * (kCLay == kAlongK ? 1 : 2);
+    static __device__ __forceinline__ void multiply(const Half& r, const Cols& c, int h, Acc& acc) {
+#pragma unroll
+        for (int i = 0; i < kFR / 2; ++i)
+#pragma unroll
+            for (int j = 0; j < kFC; ++j)
+                acc[h * (kFR / 2) + i][j] = mma<kT>(r.f[i], c.f[j], acc[h * (kFR / 2) + i][j]);
+    }
+
+    // Asks for an even mix of half a step's products with the reads for the next
+    // half (and, in a tile's last one, the copies): left alone, the compiler puts
+    // each read right before its use.
+    static constexpr int kHalfReads = kFR / 2 * (kRLay == kAlongK ? 1 : 2);
+    static constexpr int kColReads = kFC * (kCLay == kAlongK ? 1 : 2);
     static constexpr int kCopies = (kBR + kBC) / 8 / kWaves;
-    template <int kCopied>
+    template <int kReads, int kCopied>
     static __device__ __forceinline__ void mix() {
-        constexpr int kProducts = kFR * kFC;
+        constexpr int kProducts = kFR / 2 * kFC;
         int reads = 0, copies = 0;
 #pragma unroll
         for (int i = 0; i < kProducts; ++i) {
@@ -309,26 +326,29 @@ struct Mma {
     // One tile of k: reads the rest of `r`, `c`, starts reading the next ones.
     // kInner: the next two tiles are there in full.
     template <bool kInner>
-    static __device__ __forceinline__ void tile(State& st, Frags& f0, Acc& acc, GOCKPT_LDS uint8_t* r,
+    static __device__ __forceinline__ void tile(State& st, Half& r0, Cols& c0, Acc& acc, GOCKPT_LDS uint8_t* r,
                                                 GOCKPT_LDS uint8_t* c, GOCKPT_LDS uint8_t* nr, GOCKPT_LDS uint8_t* nc,
                                                 int t, int tiles) {
-        Frags f1;
-        read(st, f1, r, c, 1);
-        multiply(f0, acc);
-        mix<0>();
-        read(st, f0, r, c, 2);
-        multiply(f1, acc);
-        mix<0>();
-        read(st, f1, r, c, 3);
-        multiply(f0, acc);
-        mix<0>();
+        Half r1;
+        Cols c1;
+        read(st, r1, r, 0, 1);
+        multiply(r0, c0, 0, acc);
+        mix<kHalfReads, 0>();
+        read(st, r0, r, 1, 0);
+        read(st, c1, c, 1);
+        multiply(r1, c0, 1, acc);
+        mix<kHalfReads + kColReads, 0>();
+        read(st, r1, r, 1, 1);
+        multiply(r0, c1, 0, acc);
+        mix<kHalfReads, 0>();
         if (kInner || t + 1 < tiles) {
             land<kInner>(st, nr, nc, t + 1);
-            read(st, f0, nr, nc, 0);
+            read(st, r0, nr, 0, 0);
+            read(st, c0, nc, 0);
             if (kInner || t + 2 < tiles) fill<kInner>(st, r, c, t + 2);
         }
-        multiply(f1, acc);
-        if (kInner) mix<kCopies>();
+        multiply(r1, c1, 1, acc);
+        if (kInner) mix<kHalfReads + kColReads, kCopies>();
     }
 
     // acc = the block's tile of the product over its slice of k.  The LDS
@@ -340,9 +360,7 @@ struct Mma {
 #pragma unroll
         for (int i = 0; i < kFR; ++i)
 #pragma unroll
-            for (int j = 0; j < kFC; ++j)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+            for (int j = 0; j < kFC; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         State st;
         const int thread = threadIdx.x;
         st.lane = thread & 63;
@@ -354,23 +372,25 @@ struct Mma {
         st.fr.init(a.r + k0 * (kRLay == kAlongK ? 2 : a.r_stride), a.r_stride, p.r0, a.rn, nullptr, st.lane, st.wave);
         st.fc.init(a.c + k0 * (kCLay == kAlongK ? 2 : a.c_stride), a.c_stride, p.c0, cn,
                    kCLay == kAlongK ? a.c_rows : nullptr, st.lane, st.wave);
-        st.rr.init(st.wave / kWC * (kFR * 32), st.lane);
-        st.rc.init(st.wave % kWC * (kFC * 32), st.lane);
+        st.rr.init(st.wave / kWC * (kFR * 16), st.lane);
+        st.rc.init(st.wave % kWC * (kFC * 16), st.lane);
         st.whole = st.k / kStepK;
         st.from = st.whole > 0 ? (p.r0 / kBR + p.c0 / kBC) % kTurns % st.whole : 0;
         fill<false>(st, r0, c0, 0);
         land<false>(st, r0, c0, 0);
-        Frags f;
-        read(st, f, r0, c0, 0);
+        Half fr;
+        Cols fc;
+        read(st, fr, r0, 0, 0);
+        read(st, fc, c0, 0);
         if (tiles > 1) fill<false>(st, r1, c1, 1);
         int t = 0;
         for (; t + 3 < st.whole; t += 2) {
-            tile<true>(st, f, acc, r0, c0, r1, c1, t, tiles);
-            tile<true>(st, f, acc, r1, c1, r0, c0, t + 1, tiles);
+            tile<true>(st, fr, fc, acc, r0, c0, r1, c1, t, tiles);
+            tile<true>(st, fr, fc, acc, r1, c1, r0, c0, t + 1, tiles);
         }
         for (; t < tiles; t += 2) {
-            tile<false>(st, f, acc, r0, c0, r1, c1, t, tiles);
-            if (t + 1 < tiles) tile<false>(st, f, acc, r1, c1, r0, c0, t + 1, tiles);
+            tile<false>(st, fr, fc, acc, r0, c0, r1, c1, t, tiles);
+            if (t + 1 < tiles) tile<false>(st, fr, fc, acc, r1, c1, r0, c0, t + 1, tiles);
         }
     }
 
@@ -379,17 +399,17 @@ struct Mma {
 
     // Where the wavefront's fragments begin.
     static __device__ __forceinline__ int first_r(const MmaPlace& p) {
-        return p.r0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / kWC * kFR * 32;
+        return p.r0 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / kWC * kFR * 16;
     }
     static __device__ __forceinline__ int first_c(const MmaPlace& p, int j) {
-        return p.c0 + (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % kWC * kFC + j) * 32;
+        return p.c0 + (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % kWC * kFC + j) * 16;
     }
-    // The r and c of this lane's element 0 of fragment (i, j); element e lies
-    // 8 * (e / 4) + e % 4 further in r.
+    // The r of this lane's four elements of fragments (i, ..), from the first on,
+    // and the c of those of fragments (.., j).
     static __device__ __forceinline__ int r_of(const MmaPlace& p, int i) {
-        return first_r(p) + i * 32 + 4 * ((threadIdx.x & 63) >> 5);
+        return first_r(p) + i * 16 + 4 * ((threadIdx.x & 63) >> 4);
     }
-    static __device__ __forceinline__ int c_of(const MmaPlace& p, int j) { return first_c(p, j) + (threadIdx.x & 31); }
+    static __device__ __forceinline__ int c_of(const MmaPlace& p, int j) { return first_c(p, j) + (threadIdx.x & 15); }
 };
 
 // The product of at most 32 c, both operands along k: R is read once, and that is
@@ -401,17 +421,17 @@ struct Mma {
 // which a compute unit has one with 16 KiB on their way, 58.
 template <int kT_>
 struct Stream {
-    static constexpr int kT = kT_, kBR = 32, kBC = 32, kWR = 1, kWC = 1, kFR = 1, kFC = 1;
+    static constexpr int kT = kT_, kBR = 32, kBC = 32, kWR = 1, kWC = 1, kFR = 2, kFC = 2;
     static constexpr int kWaves = 4, kThreads = 256, kAhead = 4;
     static constexpr int kTile = 32 * kStepK * 2;
     static constexpr int kRBytes = kWaves * kTile, kCBytes = kWaves * kTile;
     static constexpr bool kOneWave = true;  // the first wavefront has the sum
-    using Acc = f32x16[1][1];
+    using Acc = f32x4[2][2];
 
     struct State {
         Filler<kAlongK, 32, 1> fill;
-        Reader<kAlongK, 32> reader;
-        const uint8_t* c;  // this lane's index of C at the first k, its half's piece
+        Reader<kAlongK, 32, 2> reader;
+        const uint8_t* c[2];  // this lane's index of each block of C at the first k, its quarter's piece
         int lane, wave, k, from, whole;
 
         // The wavefront's t-th tile of k: the whole ones in turn (see above).
@@ -427,13 +447,13 @@ struct Stream {
         __device__ __forceinline__ void load(GOCKPT_LDS uint8_t* r, u32x4 (&f)[4], int t) {
             const int tile = turned(t), left = k - tile * kStepK;
             fill.template fill<kWhole>(r, tile, left, 0);
-            const uint8_t* p = c + static_cast<int64_t>(tile) * (2 * kStepK);
 #pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                const bool there = kWhole || (2 * s + (lane >> 5)) * 8 < left;
+            for (int i = 0; i < 4; ++i) {  // step i / 2, block i % 2
+                const uint8_t* p = c[i % 2] + static_cast<int64_t>(tile) * (2 * kStepK);
+                const bool there = kWhole || (4 * (i / 2) + (lane >> 4)) * 8 < left;
                 // the tile's first piece is there
-                const u32x4 x = *reinterpret_cast<const u32x4*>(there ? p + s * 32 : p - (lane >> 5) * 16);
-                f[s] = there ? x : u32x4{0, 0, 0, 0};
+                const u32x4 x = *reinterpret_cast<const u32x4*>(there ? p + i / 2 * 64 : p - (lane >> 4) * 16);
+                f[i] = there ? x : u32x4{0, 0, 0, 0};
             }
         }
 
@@ -445,15 +465,18 @@ struct Stream {
                 if (left < kStepK) fill.clear(r, left, lane, 0);
             }
 #pragma unroll
-            for (int s = 0; s < 4; ++s) acc[0][0] = mma<kT>(reader.read(r, 0, s), f[s], acc[0][0]);
+            for (int i = 0; i < 4; ++i) {  // step i / 2, block i % 2 of r
+                const u32x4 x = reader.read(r, i % 2, i / 2);
+#pragma unroll
+                for (int j = 0; j < 2; ++j) acc[i % 2][j] = mma<kT>(x, f[i / 2 * 2 + j], acc[i % 2][j]);
+            }
         }
     };
 
     static __device__ __forceinline__ void run(const MmaArgs& a, const MmaPlace& p, int cn, int k_all,
                                                GOCKPT_LDS uint8_t* b0, GOCKPT_LDS uint8_t* b1, GOCKPT_LDS uint8_t* b2,
                                                GOCKPT_LDS uint8_t* b3, Acc& acc) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) acc[0][0][e] = 0.0f;
+        acc[0][0] = acc[0][1] = acc[1][0] = acc[1][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         State st;
         st.lane = threadIdx.x & 63;
         st.wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -467,8 +490,11 @@ struct Stream {
         if (st.k > 0) {
             st.fill.init(a.r + k0 * 2, a.r_stride, p.r0, a.rn, nullptr, st.lane, 0);
             st.reader.init(0, st.lane);
-            const int at = min(p.c0 + (st.lane & 31), cn - 1);
-            st.c = a.c + k0 * 2 + (a.c_rows != nullptr ? a.c_rows[at] : at) * a.c_stride + (st.lane >> 5) * 16;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int at = min(p.c0 + j * 16 + (st.lane & 15), cn - 1);
+                st.c[j] = a.c + k0 * 2 + (a.c_rows != nullptr ? a.c_rows[at] : at) * a.c_stride + (st.lane >> 4) * 16;
+            }
             const int tiles = ((st.k + kStepK - 1) / kStepK - st.wave + kWaves - 1) / kWaves;  // wave, wave + 4, ...
             st.whole = (st.k / kStepK - st.wave + kWaves - 1) / kWaves;
             st.from = st.whole > 0 ? static_cast<int>(p.tile_r % st.whole) : 0;
@@ -519,29 +545,27 @@ struct Stream {
         if (st.wave > 0) {
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-                *reinterpret_cast<GOCKPT_LDS f32x4*>(b0 + (q * 64 + st.lane) * 16) = f32x4{
-                    acc[0][0][4 * q], acc[0][0][4 * q + 1], acc[0][0][4 * q + 2], acc[0][0][4 * q + 3]};
+                *reinterpret_cast<GOCKPT_LDS f32x4*>(b0 + (q * 64 + st.lane) * 16) = acc[q / 2][q % 2];
         }
         __syncthreads();
         if (st.wave > 0) return;
 #pragma unroll
         for (int w = 1; w < kWaves; ++w) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const f32x4 x =
+            for (int q = 0; q < 4; ++q)
+                acc[q / 2][q % 2] +=
                     *reinterpret_cast<const GOCKPT_LDS f32x4*>(first + w * kTile + (q * 64 + st.lane) * 16);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[0][0][4 * q + e] += x[e];
-            }
         }
     }
 
     // One wavefront is left.
     static __device__ __forceinline__ void sync() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
     static __device__ __forceinline__ int first_r(const MmaPlace& p) { return p.r0; }
-    static __device__ __forceinline__ int first_c(const MmaPlace& p, int) { return p.c0; }
-    static __device__ __forceinline__ int r_of(const MmaPlace& p, int) { return p.r0 + 4 * ((threadIdx.x & 63) >> 5); }
-    static __device__ __forceinline__ int c_of(const MmaPlace& p, int) { return p.c0 + (threadIdx.x & 31); }
+    static __device__ __forceinline__ int first_c(const MmaPlace& p, int j) { return p.c0 + j * 16; }
+    static __device__ __forceinline__ int r_of(const MmaPlace& p, int i) {
+        return p.r0 + i * 16 + 4 * ((threadIdx.x & 63) >> 4);
+    }
+    static __device__ __forceinline__ int c_of(const MmaPlace& p, int j) { return p.c0 + j * 16 + (threadIdx.x & 15); }
 };
 
 // Where a product's values go.
@@ -613,16 +637,16 @@ __device__ __forceinline__ void store4(uint8_t* p, int dtype, bool accumulate, f
 }
 
 // A block's tile to memory.  A lane holds four values along r of each of its
-// columns c, and stores of those would touch 32 rows at 16 bytes each (268 MB of
-// bf16 took 78 us more than no stores at all, and take 46 so).  So each wavefront turns 32 columns
-// at a time in LDS that it alone uses by then, and stores whole stretches of a
-// row, 16 bytes a lane.  The 16-byte piece p of column c lies at p ^ c: writes and
-// reads of 16 lanes meet every bank once.
+// columns c, and stores of those would touch 16 rows at 32 bytes each (268 MB of
+// bf16 took 78 us more than no stores at all, and take 46 so).  So each wavefront
+// turns 16 columns at a time in LDS that it alone uses by then, and stores whole
+// stretches of a row, 16 bytes a lane.  The 16-byte piece p of column c lies at p ^
+// c: writes and reads of 16 lanes meet every bank once.
 template <class M>
 struct Store {
-    static constexpr int kPieces = M::kFR * 8;        // of 4 values of 32 bits, of a column of the wavefront's tile
-    static constexpr int kHalves = M::kFR * 4;        // of 8 values of 16 bits
-    static constexpr int kBytes = M::kFR * 32 * 32 * 4;  // a wavefront's
+    static constexpr int kPieces = M::kFR * 4;    // of 4 values of 32 bits, of a column of the wavefront's tile
+    static constexpr int kHalves = M::kFR * 2;    // of 8 values of 16 bits
+    static constexpr int kBytes = 16 * kPieces * 16;  // a wavefront's
 
     GOCKPT_LDS uint8_t* lds;
 
@@ -648,25 +672,20 @@ struct Store {
         lds = at + w * kBytes;
     }
 
-    // Columns c0 to c0 + 31 (those below cn) of fragments acc[..][j], first r r0,
+    // Columns c0 to c0 + 15 (those below cn) of fragments acc[..][j], first r r0,
     // `rn` r in all; row c at out + c * stride.
     __device__ __forceinline__ void put(const typename M::Acc& acc, int j, uint8_t* out, int64_t stride, int dtype,
                                         bool accumulate, float alpha, int r0, int rn, int c0, int cn) const {
-        const int lane = threadIdx.x & 63, c = lane & 31, up = lane >> 5;
+        const int lane = threadIdx.x & 63, c = lane & 15, up = lane >> 4;
         if (dtype == kFP32 || accumulate) {
 #pragma unroll
             for (int i = 0; i < M::kFR; ++i)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const f32x16& v = acc[i][j];
-                    const f32x4 x = {v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
-                    *reinterpret_cast<GOCKPT_LDS f32x4*>(
-                        lds + (c * kPieces + ((i * 8 + q * 2 + up) ^ (c & (kPieces - 1)))) * 16) = x * alpha;
-                }
+                *reinterpret_cast<GOCKPT_LDS f32x4*>(
+                    lds + (c * kPieces + ((i * 4 + up) ^ (c & (kPieces - 1)))) * 16) = acc[i][j] * alpha;
             wave_sync();
             if (dtype == kFP32) {
 #pragma unroll 4
-                for (int s = 0; s < kPieces / 2; ++s) {
+                for (int s = 0; s < kPieces / 4; ++s) {
                     const int at = s * 64 + lane, row = at / kPieces, piece = at % kPieces, n = rn - r0 - piece * 4;
                     const f32x4 x = *reinterpret_cast<const GOCKPT_LDS f32x4*>(
                         lds + (row * kPieces + (piece ^ (row & (kPieces - 1)))) * 16);
@@ -676,7 +695,7 @@ struct Store {
                 }
             } else {
 #pragma unroll 2
-                for (int s = 0; s < kHalves / 2; ++s) {
+                for (int s = 0; s < kHalves / 4; ++s) {
                     const int at = s * 64 + lane, row = at / kHalves, piece = at % kHalves, n = rn - r0 - piece * 8;
                     float x[8];
 #pragma unroll
@@ -697,18 +716,15 @@ struct Store {
             }
         } else {
 #pragma unroll
-            for (int i = 0; i < M::kFR; ++i)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const f32x16& v = acc[i][j];
-                    const f32x4 x = f32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]} * alpha;
-                    const u32x2 w = dtype == kBF16 ? pack4<kBF16>(x) : pack4<kFP16>(x);
-                    *reinterpret_cast<GOCKPT_LDS u32x2*>(
-                        lds + (c * kHalves + ((i * 4 + q) ^ (c & (kHalves - 1)))) * 16 + up * 8) = w;
-                }
+            for (int i = 0; i < M::kFR; ++i) {
+                const f32x4 x = acc[i][j] * alpha;
+                const u32x2 w = dtype == kBF16 ? pack4<kBF16>(x) : pack4<kFP16>(x);
+                *reinterpret_cast<GOCKPT_LDS u32x2*>(
+                    lds + (c * kHalves + ((i * 2 + up / 2) ^ (c & (kHalves - 1)))) * 16 + up % 2 * 8) = w;
+            }
             wave_sync();
 #pragma unroll 4
-            for (int s = 0; s < kHalves / 2; ++s) {
+            for (int s = 0; s < kHalves / 4; ++s) {
                 const int at = s * 64 + lane, row = at / kHalves, piece = at % kHalves, n = rn - r0 - piece * 8;
                 const u32x4 w = *reinterpret_cast<const GOCKPT_LDS u32x4*>(
                     lds + (row * kHalves + (piece ^ (row & (kHalves - 1)))) * 16);
