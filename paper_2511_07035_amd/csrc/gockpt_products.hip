@@ -134,42 +134,61 @@ Source source_of(const gockpt_matrix& m, uint8_t* copy, hipStream_t s) {
     return {copy, up(m.cols, 8) * 2};
 }
 
-// A tile's time is a fixed part (its first copies, its stores) and a part for
-// each k; tiles run in rounds of as many as fit the device.  us: 8192 x 16384 x
-// 2048 (r x c x k) 621 in wide tiles, 598 in mid ones, 2048 x 16384 x 8192 507
-// and 557, 2048 x 8192 x 16384 455 and 569; 32000 x 1 x 4096 in thin ones 44.
+namespace {
+
+// Microseconds of so many blocks that take k each.  They run in rounds of as many
+// as fit the device; a tile's time has a fixed part (its first copies, its stores)
+// and a part for each k, which is less where a unit has one block instead of two,
+// or the last round leaves units idle and the others their clock.  Measured
+// (wide, mid): 8192 x 8192 x 8192 (r x c x k, both along k) 728, 958; 8192 x 16384 x
+// 2048 412, 510; 4096 x 2048 x 4096 80, 68; 4096 x 1024 x 4096 76, 46; 256 x 128 x
+// 4096 67, 31; 3088 x 3000 x 1160 36, 45; 2048 x 8192 x 16384 (across) 389, 497; 1160 x
+// 3088 x 3000 (across) 62, 40.  Streamed, 32000 x 1 x 4096: 46.
+double blocks_us(int shape, bool streamed, int64_t blocks, double k) {
+    const auto over = [](int64_t n, int64_t slots) { return static_cast<double>(n) / static_cast<double>(slots); };
+    if (shape == kWide) {
+        const int64_t rounds = blocks / kUnits, rest = blocks % kUnits;
+        return static_cast<double>(rounds) * (4.5 + 0.0222 * k) +
+               (rest > 0 ? 4.0 + (0.0165 + 0.0057 * over(rest, kUnits)) * k : 0.0);
+    }
+    if (shape == kMid) {
+        const int64_t rounds = blocks / (2 * kUnits), rest = blocks % (2 * kUnits);
+        return static_cast<double>(rounds) * (4.0 + 0.0166 * k) +
+               (rest > kUnits ? 4.0 + 0.0166 * k : rest > 0 ? 3.0 + (0.0075 + 0.003 * over(rest, kUnits)) * k : 0.0);
+    }
+    const double rounds = static_cast<double>((blocks + 4 * kUnits - 1) / (4 * kUnits));
+    return rounds * (streamed ? 2.0 + 0.003 * k : 3.0 + 0.012 * k);
+}
+
+}  // namespace
+
 ProductPlan plan_product(int kind, int64_t rn, int64_t cn, int64_t k, int most_splits) {
-    struct Cost {
-        int br, bc, each;
-        double fixed, per_k;
-    };
-    static constexpr Cost kWideTile = {256, 256, 1, 5.0, 0.0275}, kMidTile = {128, 128, 2, 4.0, 0.0165},
-                          kThinTile = {128, 32, 4, 3.0, 0.012}, kStream = {32, 32, 4, 2.0, 0.003};
     const bool along = kind == kAlongAlong || kind == kAcrossAlong;
-    const double least = 2.0 * static_cast<double>(rn + cn) * static_cast<double>(k) / 5.5e6;  // us to read both
+    const double least = 2.0 * static_cast<double>(rn + cn) * static_cast<double>(k) / 5.5e6;  // to read both
     ProductPlan best{};
     best.us = -1.0;
     for (int shape = kWide; shape <= kThin; ++shape) {
-        if (shape == kThin && (!along || cn > 32)) continue;
-        const Cost& t = shape == kWide ? kWideTile : shape == kMid ? kMidTile : kind == kAlongAlong ? kStream : kThinTile;
-        const int64_t tr = (rn + t.br - 1) / t.br, tc = (cn + t.bc - 1) / t.bc, tiles = tr * tc;
-        const int64_t slots = int64_t{kUnits} * t.each;
+        if ((shape == kThin) != (along && cn <= 32)) continue;  // few c: memory's time, which wider tiles do not reach
+        const bool streamed = shape == kThin && kind == kAlongAlong;
+        const int64_t br = shape == kWide ? 256 : streamed ? 32 : 128, bc = shape == kWide ? 256 : shape == kMid ? 128 : 32;
+        const int64_t tr = (rn + br - 1) / br, tc = (cn + bc - 1) / bc, tiles = tr * tc;
+        const int64_t slots = int64_t{kUnits} * (shape == kWide ? 1 : shape == kMid ? 2 : 4);
         for (int want = 1; want <= most_splits; want *= 2) {
-            // of two roundings, slices that fill the slots best
-            for (int extra = 0; extra < (want > 1 ? 2 : 1); ++extra) {
+            // a power of two, and as many as fill the slots
+            for (int fill = 0; fill < (want > 1 ? 2 : 1); ++fill) {
                 int64_t splits = want;
-                if (extra == 1) splits = std::min<int64_t>(most_splits, std::max<int64_t>(1, slots / std::max<int64_t>(1, tiles)));
-                const int64_t split_k = up((k + splits - 1) / splits, 64);
-                splits = split_k > 0 ? std::max<int64_t>(1, (k + split_k - 1) / split_k) : 1;
-                const int64_t rounds = (tiles * splits + slots - 1) / slots;
-                double us = static_cast<double>(rounds) * (t.fixed + t.per_k * static_cast<double>(std::min(split_k, k)));
-                us = std::max(us, least);
-                if (splits > 1)
+                if (fill == 1)
+                    splits = std::min<int64_t>(most_splits, std::max<int64_t>(1, slots / std::max<int64_t>(1, tiles)));
+                const int64_t split_k = std::max<int64_t>(64, up((k + splits - 1) / splits, 64));
+                splits = std::max<int64_t>(1, (k + split_k - 1) / split_k);
+                double us = std::max(
+                    blocks_us(shape, streamed, tiles * splits, static_cast<double>(std::min(split_k, k))), least);
+                if (splits > 1)  // the slices' sums, written and read
                     us += 4.0 + 8.0 * static_cast<double>(splits) * static_cast<double>(rn) * static_cast<double>(cn) / 4.5e6;
                 if (best.us < 0.0 || us < best.us) {
                     best.shape = shape;
                     best.splits = static_cast<int>(splits);
-                    best.split_k = static_cast<int32_t>(std::max<int64_t>(split_k, 64));
+                    best.split_k = static_cast<int32_t>(split_k);
                     best.tiles_r = static_cast<uint32_t>(tr);
                     best.tiles_c = static_cast<uint32_t>(tc);
                     best.us = us;
