@@ -110,6 +110,8 @@ __global__ __launch_bounds__(kTokenThreads) void token_kernel(TokenArgs a) {
         if (most > 0.0f && most <= 3.402823466e38f) q = max(ilogbf(most), -100);
         up_by = ldexpf(1.0f, 13 - q);
         if (threadIdx.x == 0) *a.unscale = ldexpf(1.0f, q - 13);
+    } else if (a.unscale != nullptr && threadIdx.x == 0) {
+        *a.unscale = 1.0f;  // no tokens: the gradients are sums of nothing, times this
     }
     if (threadIdx.x == 0) *a.count = all;
     for (int64_t at = from; at < to; at += 64) {
@@ -244,7 +246,7 @@ struct JoinArgs {
 };
 
 // Up to so many tokens one block joins and adds up.
-constexpr int kJoinWaves = 16, kJoinAlone = 4 * kJoinWaves;
+constexpr int kJoinWaves = 16, kJoinAlone = 8 * kJoinWaves;
 
 // The sum of all tokens' losses, in an order that is the same on every call.
 __device__ __forceinline__ void sum_losses(const JoinArgs& a, int32_t count) {
@@ -466,6 +468,12 @@ int check_head(const char* name, const gockpt_head* h, TokenArgs* t) {
     return GOCKPT_OK;
 }
 
+int check_blocks(const char* name, const ProductPlan& p) {
+    if (too_many_blocks(p))
+        return ops_fail(GOCKPT_EINVAL, "%s: a product of %u x %u tiles", name, p.tiles_r, p.tiles_c);
+    return GOCKPT_OK;
+}
+
 int check_reduction(const char* name, int r) {
     if (r < GOCKPT_EACH || r > GOCKPT_MEAN) return ops_fail(GOCKPT_EINVAL, "%s: reduction %d", name, r);
     return GOCKPT_OK;
@@ -570,6 +578,13 @@ GradPlan plan_grad(const gockpt_head& h, bool by_hidden, bool by_table) {
     return p;
 }
 
+int check_blocks(const char* name, const GradPlan& p) {
+    int rc = GOCKPT_OK;
+    for (const ProductPlan& x : {p.full.z, p.full.by_hidden, p.full.by_table, p.rest.z, p.rest.by_hidden, p.rest.by_table})
+        if (rc == GOCKPT_OK) rc = check_blocks(name, x);
+    return rc;
+}
+
 int check_grads(const char* name, const gockpt_head* h, const gockpt_matrix* gx, const gockpt_matrix* gw) {
     if (gx != nullptr) {
         const int rc = check_model_matrix(name, "grad_hidden", gx, kAnyType);
@@ -600,8 +615,11 @@ int gockpt_head_loss_bytes(const gockpt_head* head, size_t* bytes) {
     const char* name = "gockpt_head_loss_bytes";
     if (bytes == nullptr) return ops_fail(GOCKPT_EINVAL, "%s: null argument", name);
     *bytes = 0;
-    const int rc = check_head(name, head, nullptr);
-    if (rc == GOCKPT_OK) *bytes = plan_loss(*head).bytes;
+    int rc = check_head(name, head, nullptr);
+    if (rc != GOCKPT_OK) return rc;
+    const LossPlan p = plan_loss(*head);
+    rc = check_blocks(name, p.logits);
+    if (rc == GOCKPT_OK) *bytes = p.bytes;
     return rc;
 }
 
@@ -618,7 +636,8 @@ int gockpt_head_loss(const gockpt_head* head, int reduction, float* loss, float*
             rc = ops_fail(GOCKPT_EINVAL, "%s: an output is not aligned", name);
     if (rc != GOCKPT_OK) return rc;
     const LossPlan p = plan_loss(*head);
-    rc = check_workspace(name, workspace, workspace_bytes, p.bytes);
+    rc = check_blocks(name, p.logits);
+    if (rc == GOCKPT_OK) rc = check_workspace(name, workspace, workspace_bytes, p.bytes);
     if (rc != GOCKPT_OK) return rc;
     if (loss == nullptr && lse == nullptr && logit == nullptr) return GOCKPT_OK;
     if (t.tokens == 0 && (loss == nullptr || reduction == GOCKPT_EACH)) return GOCKPT_OK;
@@ -689,7 +708,10 @@ int gockpt_head_grad_bytes(const gockpt_head* head, const gockpt_matrix* grad_hi
     *bytes = 0;
     int rc = check_head(name, head, nullptr);
     if (rc == GOCKPT_OK) rc = check_grads(name, head, grad_hidden, grad_table);
-    if (rc == GOCKPT_OK) *bytes = plan_grad(*head, grad_hidden != nullptr, grad_table != nullptr).bytes;
+    if (rc != GOCKPT_OK) return rc;
+    const GradPlan p = plan_grad(*head, grad_hidden != nullptr, grad_table != nullptr);
+    rc = check_blocks(name, p);
+    if (rc == GOCKPT_OK) *bytes = p.bytes;
     return rc;
 }
 
@@ -708,7 +730,8 @@ int gockpt_head_grad(const gockpt_head* head, const float* lse, int reduction, c
             rc = ops_fail(GOCKPT_EINVAL, "%s: lse or grad is not aligned", name);
     if (rc != GOCKPT_OK) return rc;
     const GradPlan p = plan_grad(*head, grad_hidden != nullptr, grad_table != nullptr);
-    rc = check_workspace(name, workspace, workspace_bytes, p.bytes);
+    rc = check_blocks(name, p);
+    if (rc == GOCKPT_OK) rc = check_workspace(name, workspace, workspace_bytes, p.bytes);
     if (rc != GOCKPT_OK) return rc;
     const int64_t rows = head->table.rows, cols = head->table.cols;
     const bool by_hidden = grad_hidden != nullptr && t.tokens > 0 && cols > 0;

@@ -105,6 +105,12 @@ int check_forward(const char* name, const gockpt_matrix* x, const gockpt_matrix*
     return GOCKPT_OK;
 }
 
+int check_blocks(const char* name, const ProductPlan& p) {
+    if (too_many_blocks(p))
+        return ops_fail(GOCKPT_EINVAL, "%s: a product of %u x %u tiles", name, p.tiles_r, p.tiles_c);
+    return GOCKPT_OK;
+}
+
 int check_backward(const char* name, const gockpt_matrix* g, const gockpt_matrix* w, const gockpt_act8* keep,
                    const gockpt_matrix* gx, const gockpt_matrix* gw) {
     int rc = check_model_matrix(name, "grad_out", g, kHalfTypes);
@@ -141,8 +147,11 @@ int gockpt_linear8_bytes(const gockpt_matrix* x, const gockpt_matrix* weight, si
     const char* name = "gockpt_linear8_bytes";
     if (bytes == nullptr) return ops_fail(GOCKPT_EINVAL, "%s: null argument", name);
     *bytes = 0;
-    const int rc = check_forward(name, x, weight);
-    if (rc == GOCKPT_OK) *bytes = plan_forward(*x, *weight).bytes;
+    int rc = check_forward(name, x, weight);
+    if (rc != GOCKPT_OK) return rc;
+    const ForwardPlan p = plan_forward(*x, *weight);
+    rc = check_blocks(name, p.product);
+    if (rc == GOCKPT_OK) *bytes = p.bytes;
     return rc;
 }
 
@@ -158,7 +167,8 @@ int gockpt_linear8(const gockpt_matrix* x, const gockpt_matrix* weight, const go
     if (rc == GOCKPT_OK && keep != nullptr) rc = check_act8(name, "keep", keep, x->rows, x->cols);
     if (rc != GOCKPT_OK) return rc;
     const ForwardPlan p = plan_forward(*x, *weight);
-    rc = check_workspace(name, workspace, workspace_bytes, p.bytes);
+    rc = check_blocks(name, p.product);
+    if (rc == GOCKPT_OK) rc = check_workspace(name, workspace, workspace_bytes, p.bytes);
     if (rc != GOCKPT_OK) return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (keep != nullptr) {
@@ -185,9 +195,12 @@ int gockpt_linear8_grad_bytes(const gockpt_matrix* grad_out, const gockpt_matrix
     const char* name = "gockpt_linear8_grad_bytes";
     if (bytes == nullptr) return ops_fail(GOCKPT_EINVAL, "%s: null argument", name);
     *bytes = 0;
-    const int rc = check_backward(name, grad_out, weight, keep, grad_x, grad_weight);
-    if (rc == GOCKPT_OK)
-        *bytes = plan_backward(*grad_out, weight, keep, grad_x != nullptr, grad_weight != nullptr).bytes;
+    int rc = check_backward(name, grad_out, weight, keep, grad_x, grad_weight);
+    if (rc != GOCKPT_OK) return rc;
+    const BackwardPlan p = plan_backward(*grad_out, weight, keep, grad_x != nullptr, grad_weight != nullptr);
+    rc = check_blocks(name, p.by_x);
+    if (rc == GOCKPT_OK) rc = check_blocks(name, p.by_weight);
+    if (rc == GOCKPT_OK) *bytes = p.bytes;
     return rc;
 }
 
@@ -198,7 +211,9 @@ int gockpt_linear8_grad(const gockpt_matrix* grad_out, const gockpt_matrix* weig
     int rc = check_backward(name, grad_out, weight, keep, grad_x, grad_weight);
     if (rc != GOCKPT_OK) return rc;
     const BackwardPlan p = plan_backward(*grad_out, weight, keep, grad_x != nullptr, grad_weight != nullptr);
-    rc = check_workspace(name, workspace, workspace_bytes, p.bytes);
+    rc = check_blocks(name, p.by_x);
+    if (rc == GOCKPT_OK) rc = check_blocks(name, p.by_weight);
+    if (rc == GOCKPT_OK) rc = check_workspace(name, workspace, workspace_bytes, p.bytes);
     if (rc != GOCKPT_OK) return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);
     uint8_t* ws = static_cast<uint8_t*>(workspace);

@@ -70,6 +70,11 @@ struct ProductPlan {
 // most_splits 1: not split.
 ProductPlan plan_product(int kind, int64_t rn, int64_t cn, int64_t k, int most_splits);
 
+// A grid of that many blocks there is not.
+inline bool too_many_blocks(const ProductPlan& p) {
+    return p.splits > 0 && uint64_t{p.tiles_r} * p.tiles_c > uint64_t{INT32_MAX} / static_cast<uint64_t>(p.splits);
+}
+
 // Starts the product of the operands in `a`, which the plan completes.
 void launch_product(int kind, int dtype, const ProductPlan& p, MmaArgs& a, const StoreArgs& o, hipStream_t s);
 

@@ -16,7 +16,10 @@ the current torch stream, or on ``stream`` where no gradient is needed, and what
 a call writes counts as changed in place.  With ``grad_weight`` (of the weight's
 shape: its part of ``Session.grad``, or an fp32 sum) the backward writes the
 weight's gradient there, or adds to it with ``accumulate``, and returns none for
-it; where the weight requires no gradient, nothing is written.
+it; where the weight requires no gradient, nothing is written.  Each backward
+without ``accumulate`` writes every element: of several calls on one weight in a
+step all but the one whose backward runs first (the last one made) accumulate, or
+the program clears the sum first and all of them do.
 """
 from __future__ import annotations
 
@@ -98,15 +101,16 @@ def _differentiable(stream, a, b=None) -> bool:
     return True
 
 
-def _own_rows(t, cols: int):
-    """t, or a copy where its rows do not lie at one distance (an expanded or
-    transposed gradient)."""
+def _own_rows(t, cols: int, stream):
+    """t, or a copy, made on the call's stream, where its rows do not lie at one
+    distance (an expanded or transposed gradient)."""
     if t.is_contiguous():
         return t
     try:
         _matrix(t, "", None, cols)
     except ValueError:
-        return t.contiguous()
+        with torch.cuda.stream(stream):
+            return t.contiguous()
     return t
 
 
@@ -148,7 +152,7 @@ def _reduction(reduction: str) -> int:
 
 def _loss(hidden, table, targets, args, reduction: int, lse: bool, logit: bool, loss: bool, stream):
     """The outputs asked for, as float32 tensors (None where not)."""
-    hidden = _own_rows(hidden, table.shape[-1])
+    hidden = _own_rows(hidden, table.shape[-1], stream)
     device, head = _head(hidden, table, targets, *args)
     out = [_empty(table, targets.shape if each else (), torch.float32, stream) if wanted else None
            for wanted, each in ((loss, reduction == GOCKPT_EACH), (lse, True), (logit, True))]
@@ -203,7 +207,7 @@ def head_grad(hidden, table, targets, lse, grad, *, scale: float = 1.0, first_id
     r = _reduction(reduction)
     if accumulate and grad_weight is None:
         raise ValueError("accumulate: into a grad_weight")
-    hidden, table = _own_rows(hidden.detach(), table.shape[-1]), table.detach()
+    hidden, table = _own_rows(hidden.detach(), table.shape[-1], stream), table.detach()
     device, head = _head(hidden, table, targets, scale, first_id, ignore_id, classes or 0)
     dim = table.shape[1]
     n = 1 if r != GOCKPT_EACH else targets.numel()
@@ -323,7 +327,7 @@ def act8_pack(x, *, out: Act8 | None = None, stream=None) -> Act8:
         out = Act8(x.shape, x.dtype, x.device, stream)
     elif out.shape != x.shape or out.dtype != x.dtype:
         raise ValueError(f"out: of shape {tuple(out.shape)} and {out.dtype} for x of {tuple(x.shape)} and {x.dtype}")
-    x = _own_rows(x.detach(), out.cols)
+    x = _own_rows(x.detach(), out.cols, stream)
     _check(_lib().gockpt_act8_pack(_matrix(x, "x", None, out.cols), out._pack(device), _stream(stream, device)),
            "gockpt_act8_pack", None)
     _changed((out.buffer,))
@@ -340,7 +344,7 @@ def _linear8(x, weight, keep: bool, stream):
     rows, cols = weight.shape
     if x.dim() == 0 or x.shape[-1] != cols:
         raise ValueError(f"x of shape {tuple(x.shape)} for a weight of shape {tuple(weight.shape)}")
-    x = _own_rows(x, cols)
+    x = _own_rows(x, cols, stream)
     mx, mw = _matrix(x, "x", device, cols), _matrix(weight, "weight", None)
     ws, ptr, size = _workspace(weight, "gockpt_linear8_bytes", (mx, mw), stream)
     out = _empty(x, (*x.shape[:-1], rows), x.dtype, stream)
@@ -353,7 +357,7 @@ def _linear8(x, weight, keep: bool, stream):
 def _linear8_grad(grad_out, weight, kept, grad_x, grad_weight, accumulate, stream):
     device = _here(grad_out, "grad_out")
     rows = grad_out.shape[-1]
-    grad_out = _own_rows(grad_out, rows)
+    grad_out = _own_rows(grad_out, rows, stream)
     args = (_matrix(grad_out, "grad_out", None, rows), None if weight is None else _matrix(weight, "weight", device),
             None if kept is None else kept._pack(device),
             None if grad_x is None else _matrix(grad_x, "grad_x", device, grad_x.shape[-1]),
@@ -433,10 +437,10 @@ def _gate8(x, factor, kind: int, keep: bool, stream):
         raise ValueError(f"factor of shape {tuple(factor.shape)} and {factor.dtype} for x of {tuple(x.shape)} and "
                          f"{x.dtype}")
     cols = x.shape[-1]
-    x = _own_rows(x, cols)
+    x = _own_rows(x, cols, stream)
     mx, mf = _matrix(x, "x", None, cols), None
     if factor is not None:
-        factor = _own_rows(factor, cols)
+        factor = _own_rows(factor, cols, stream)
         mf = _matrix(factor, "factor", device, cols)
     out = _empty(x, x.shape, x.dtype, stream)
     kept = [Act8(x.shape, x.dtype, x.device, stream) if keep and t is not None else None for t in (x, factor)]
@@ -471,7 +475,7 @@ class _Gate8(torch.autograd.Function):
         ctx.saved_tensors  # raises where the graph's buffers have been freed
         device = _here(grad_out, "grad_out")
         cols = grad_out.shape[-1]
-        grad_out = _own_rows(grad_out, cols)
+        grad_out = _own_rows(grad_out, cols, None)
         grads = [torch.empty(grad_out.shape, dtype=grad_out.dtype, device=grad_out.device) if needed else None
                  for needed in ctx.needs_input_grad[:2]]
         _check(_lib().gockpt_gate8_grad(ctx.kind, _matrix(grad_out, "grad_out", None, cols),

@@ -820,6 +820,29 @@ def test_head_empty():
     assert float(loss.detach()) == 0.0 and bool((x.grad == 0).all()) and w.grad.shape == (0, 8)
 
 
+def test_head_without_tokens_over_memory_that_held_nan():
+    """What a workspace held before does not reach the gradients of no tokens."""
+    for _ in range(3):
+        junk = [torch.full((1 << k,), float("nan"), device="cuda") for k in range(6, 16)]
+        del junk
+        table = randn((10, 8), torch.bfloat16, 1).requires_grad_()
+        x = torch.zeros(0, 8, dtype=torch.bfloat16, device="cuda", requires_grad=True)
+        g.linear_cross_entropy(x, table, torch.zeros(0, dtype=torch.int64, device="cuda")).backward()
+        assert bool((table.grad == 0).all())
+
+
+def test_transposed_inputs_on_a_stream():
+    x, w = randn((64, 600), torch.bfloat16, 1), randn((200, 600), torch.bfloat16, 2)
+    want = g.linear8(x, w)
+    s = torch.cuda.Stream()
+    for _ in range(3):
+        turned = x.t().contiguous().t()
+        s.wait_stream(torch.cuda.current_stream())
+        got = g.linear8(turned, w, stream=s)
+        s.synchronize()
+        assert torch.equal(got, want)
+
+
 def test_head_gradients_that_are_not_wanted():
     hidden, table, targets = head_inputs(50, 300, 64, "bf16")
     both = hidden.detach().requires_grad_(), table.detach().requires_grad_()

@@ -251,3 +251,38 @@ def test_8_bits_take_33_bytes_for_32():
         g.Act8((), torch.bfloat16, "cpu")
     with pytest.raises(ValueError):
         g.Act8((3,), torch.int8, "cpu")
+
+
+def test_products_of_more_blocks_than_a_grid_are_refused():
+    L = model._lib()
+    # 2^30 tokens and 2^22 classes of 8 columns: 2^22 x 2^14 tiles of 256 x 256
+    n = 1 << 30
+    h = head(M(n, 8), M(1 << 22, 8), ids=(P, 1, n, n, 0, 64, 0))
+    rc, need = size("gockpt_head_loss_bytes", h)
+    assert rc == g.GOCKPT_EINVAL and need == 0 and "tiles" in said()
+    assert L.gockpt_head_loss(h, 0, P, P, P, P, 1 << 62, None) == g.GOCKPT_EINVAL
+    x, w = M(n, 8), M(1 << 22, 8)
+    assert size("gockpt_linear8_bytes", x, w)[0] == g.GOCKPT_EINVAL and "tiles" in said()
+    assert L.gockpt_linear8(x, w, M(n, 1 << 22), None, P, 1 << 62, None) == g.GOCKPT_EINVAL
+
+
+def test_copies_are_made_on_the_calls_stream(monkeypatch):
+    import torch
+    seen = []
+
+    class Now:
+        def __init__(self, stream):
+            self.stream = stream
+
+        def __enter__(self):
+            seen.append(self.stream)
+
+        def __exit__(self, *a):
+            seen.append("out")
+
+    monkeypatch.setattr(torch.cuda, "stream", Now)
+    t = torch.zeros(6, 4).t()
+    own = model._own_rows(t, 6, "s")
+    assert own.is_contiguous() and seen == ["s", "out"]
+    rows = torch.zeros(4, 8)[:, :6]
+    assert model._own_rows(rows, 6, "s") is rows and len(seen) == 2
