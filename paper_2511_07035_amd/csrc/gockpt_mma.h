@@ -24,12 +24,13 @@
 // barrier between two tiles as well: a wave holds the last step's fragments
 // in registers when it passes it.
 //
-// Blocks begin at different k, and take the rest in turn: rows of a power of
-// two bytes (2048 columns are 4096) put one k of all rows into the same few
-// channels of the caches, and blocks that march through k together wait for
-// these.  us, all from the first k and as here: 8192 x 16384 x 2048 (r x c x k,
-// both along k) 469 and 432, 8192 x 8192 x 8192 833 and 792, 2048 x 16384 x 8192 (R
-// across) 442 and 427, 2048 x 8192 x 16384 (both across) 407 and 406.
+// Over many tiles of k blocks begin at different ones, and take the rest in turn:
+// blocks that march through k together wait for the same few channels of the
+// caches, which hold one k of all rows.  us, all from the first k and in turn (r x c
+// x k): both along k, 8192 x 8192 x 8192 749 and 724, 16384 x 4096 x 5120 501 and 488;
+// R across, 2048 x 16384 x 8192 393 and 384.  With fewer tiles, and where no operand
+// lies along k, blocks in step share more of the L2: 8192 x 16384 x 2048 398 and 407,
+// 4096 x 16384 x 4096 (R across) 366 and 374, 2048 x 8192 x 16384 (both) 367 and 374.
 #pragma once
 
 #include "gockpt_ops_internal.h"
@@ -46,7 +47,8 @@ typedef f32x4 f32x4_any __attribute__((aligned(2)));
 enum Lay : int { kAlongK = 0, kAcrossK = 1 };
 
 constexpr int kStepK = 64;  // k of one LDS tile
-constexpr int kTurns = 32;  // tiles of k that blocks begin at
+constexpr int kTurns = 32;        // tiles of k that blocks begin at,
+constexpr int kTurnsFrom = 64;    // with more of them than this
 
 #define GOCKPT_LDS __attribute__((address_space(3)))
 
@@ -207,8 +209,8 @@ struct MmaPlace {
 };
 
 // Blocks go to the 8 XCDs in turn; each XCD takes one run of tiles, in groups
-// of 4 tiles of c (16 and 8 were slower by up to 4%), so that the blocks that run on it together read few
-// different tiles and find the others' in its L2.
+// of 4 tiles of c (2, 8 and 16 were slower by up to 4%), so that the blocks that
+// run on it together read few different tiles and find the others' in its L2.
 __device__ __forceinline__ MmaPlace mma_place(const MmaArgs& a, int br, int bc) {
     const uint32_t n = a.tiles_r * a.tiles_c, all = n * a.splits;
     uint32_t id = blockIdx.x;
@@ -375,7 +377,7 @@ struct Mma {
         st.rr.init(st.wave / kWC * (kFR * 16), st.lane);
         st.rc.init(st.wave % kWC * (kFC * 16), st.lane);
         st.whole = st.k / kStepK;
-        st.from = st.whole > 0 ? (p.r0 / kBR + p.c0 / kBC) % kTurns % st.whole : 0;
+        st.from = kCLay == kAlongK && st.whole > kTurnsFrom ? (p.r0 / kBR + p.c0 / kBC) % kTurns : 0;
         fill<false>(st, r0, c0, 0);
         land<false>(st, r0, c0, 0);
         Half fr;
@@ -432,20 +434,11 @@ struct Stream {
         Filler<kAlongK, 32, 1> fill;
         Reader<kAlongK, 32, 2> reader;
         const uint8_t* c[2];  // this lane's index of each block of C at the first k, its quarter's piece
-        int lane, wave, k, from, whole;
-
-        // The wavefront's t-th tile of k: the whole ones in turn (see above).
-        __device__ __forceinline__ int turned(int t) const {
-            if (t < whole) {
-                t += from;
-                t -= t >= whole ? whole : 0;
-            }
-            return t * kWaves + wave;
-        }
+        int lane, wave, k, whole;
 
         template <bool kWhole>
         __device__ __forceinline__ void load(GOCKPT_LDS uint8_t* r, u32x4 (&f)[4], int t) {
-            const int tile = turned(t), left = k - tile * kStepK;
+            const int tile = t * kWaves + wave, left = k - tile * kStepK;  // the wavefront's t-th
             fill.template fill<kWhole>(r, tile, left, 0);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {  // step i / 2, block i % 2
@@ -460,7 +453,7 @@ struct Stream {
         template <bool kWhole>
         __device__ __forceinline__ void multiply(GOCKPT_LDS uint8_t* r, const u32x4 (&f)[4], int t, Acc& acc) {
             if (!kWhole) {
-                const int left = k - turned(t) * kStepK;
+                const int left = k - (t * kWaves + wave) * kStepK;
                 wait_copies();
                 if (left < kStepK) fill.clear(r, left, lane, 0);
             }
@@ -497,7 +490,6 @@ struct Stream {
             }
             const int tiles = ((st.k + kStepK - 1) / kStepK - st.wave + kWaves - 1) / kWaves;  // wave, wave + 4, ...
             st.whole = (st.k / kStepK - st.wave + kWaves - 1) / kWaves;
-            st.from = st.whole > 0 ? static_cast<int>(p.tile_r % st.whole) : 0;
             u32x4 f[kAhead][4];
             int t = 0;
             const auto next = [&](GOCKPT_LDS uint8_t* b, u32x4 (&g)[4], int u) {
