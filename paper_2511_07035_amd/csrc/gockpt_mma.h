@@ -434,11 +434,21 @@ struct Stream {
         Filler<kAlongK, 32, 1> fill;
         Reader<kAlongK, 32, 2> reader;
         const uint8_t* c[2];  // this lane's index of each block of C at the first k, its quarter's piece
-        int lane, wave, k, whole;
+        int lane, wave, k, from, whole;
+
+        // The wavefront's t-th tile of k: the whole ones in turn, from another one
+        // in each block (49 us from the first one in all).
+        __device__ __forceinline__ int turned(int t) const {
+            if (t < whole) {
+                t += from;
+                t -= t >= whole ? whole : 0;
+            }
+            return t * kWaves + wave;
+        }
 
         template <bool kWhole>
         __device__ __forceinline__ void load(GOCKPT_LDS uint8_t* r, u32x4 (&f)[4], int t) {
-            const int tile = t * kWaves + wave, left = k - tile * kStepK;  // the wavefront's t-th
+            const int tile = turned(t), left = k - tile * kStepK;
             fill.template fill<kWhole>(r, tile, left, 0);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {  // step i / 2, block i % 2
@@ -453,7 +463,7 @@ struct Stream {
         template <bool kWhole>
         __device__ __forceinline__ void multiply(GOCKPT_LDS uint8_t* r, const u32x4 (&f)[4], int t, Acc& acc) {
             if (!kWhole) {
-                const int left = k - (t * kWaves + wave) * kStepK;
+                const int left = k - turned(t) * kStepK;
                 wait_copies();
                 if (left < kStepK) fill.clear(r, left, lane, 0);
             }
@@ -490,6 +500,7 @@ struct Stream {
             }
             const int tiles = ((st.k + kStepK - 1) / kStepK - st.wave + kWaves - 1) / kWaves;  // wave, wave + 4, ...
             st.whole = (st.k / kStepK - st.wave + kWaves - 1) / kWaves;
+            st.from = st.whole > 0 ? static_cast<int>(p.tile_r % st.whole) : 0;
             u32x4 f[kAhead][4];
             int t = 0;
             const auto next = [&](GOCKPT_LDS uint8_t* b, u32x4 (&g)[4], int u) {
