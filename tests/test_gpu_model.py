@@ -219,6 +219,29 @@ def test_linear8(tokens, rows, cols, dtype):
     assert torch.equal(other, y.detach())
 
 
+@pytest.mark.parametrize("dtype,tokens,rows,cols", [("bf16", 4100, 4104, 4200), ("fp16", 3999, 4133, 4331),
+                                                    ("bf16", 2111, 3090, 1160), ("fp16", 20_001, 130, 72)])
+def test_linear8_of_many_tiles(dtype, tokens, rows, cols):
+    """Large tiles, with edges in every direction, and sums long enough that
+    blocks take them in turn; into fp32 as well."""
+    t = DT[dtype]
+    x, w = randn((tokens, cols), t, 1).requires_grad_(), randn((rows, cols), t, 2, 0.05).requires_grad_()
+    dy = randn((tokens, rows), t, 3)
+    into = randn((rows, cols), torch.float32, 4)
+    old = into.double().clone()
+    y = g.linear8(x, w, grad_weight=into, accumulate=True)
+    y.backward(dy)
+    X, W, D = x.detach().double(), w.detach().double(), dy.double()
+    want = X @ W.t()
+    assert_close(y.detach(), want, product_error(X, W.t(), want, t), "y")
+    want = D @ W
+    assert_close(x.grad, want, product_error(D, W, want, t), "dx")
+    K = kept64(x)
+    want = D.t() @ K + old
+    extra = 2 * U * (want.abs() + old.abs())
+    assert_close(into, want, product_error(D.t(), K, want, torch.float32, extra), "dw")
+
+
 @pytest.mark.parametrize("grad", ["bf16", "fp16", "fp32"])
 @pytest.mark.parametrize("accumulate", [False, True])
 @pytest.mark.parametrize("tokens,rows,cols", [(1, 8, 8), (70, 33, 50), (300, 520, 264), (3000, 64, 48)])
@@ -570,6 +593,15 @@ def test_head(tokens, vocab, dim, dtype):
     targets[::3] = -1
     head_check(hidden, table, targets, reduction="sum", up=0.5)
     head_check(hidden, table, targets.int(), reduction="none", scale=0.5, grad="fp32", accumulate=True)
+
+
+@pytest.mark.parametrize("dtype,dim", [("bf16", 520), ("fp16", 523)])
+def test_head_of_many_tiles(dtype, dim):
+    hidden, table, targets = head_inputs(1500, 9001, dim, dtype)
+    targets[7::11] = -1
+    targets[0], targets[1] = 0, 9000
+    head_check(hidden, table, targets, up=1024.0)
+    head_check(hidden, table, targets, reduction="none", scale=-0.25, grad="fp32", accumulate=True)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
