@@ -59,8 +59,13 @@ __device__ __forceinline__ void store16(uint8_t* p, u32x4 x, bool far) {
         *q = x;
 }
 
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+
+// A lane's 8 values (zeros for missing ones), and the bits, as fp32's, of the
+// largest magnitude: infinity and NaN above all others.
 template <int kT>
-__device__ __forceinline__ void load8(const uint8_t* p, int n, bool far, float (&x)[8]) {
+__device__ __forceinline__ void load8(const uint8_t* p, int n, bool far, float (&x)[8], uint32_t& top) {
+    top = 0;
     if (n == kLaneCols) {
         if constexpr (kT == kFP32) {
             const u32x4 a = load16(p, far), b = load16(p + 16, far);
@@ -68,14 +73,18 @@ __device__ __forceinline__ void load8(const uint8_t* p, int n, bool far, float (
             for (int i = 0; i < 4; ++i) {
                 x[i] = __uint_as_float(a[i]);
                 x[4 + i] = __uint_as_float(b[i]);
+                top = max(top, max(a[i] & 0x7fffffffu, b[i] & 0x7fffffffu));
             }
         } else {
             const u32x4 a = load16(p, far);
+            u16x2 most = {0, 0};  // magnitudes of 16 bits compare as their bits do, two at a time
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 x[2 * i] = elem_to_f32<kT>(a[i] & 0xffff);
                 x[2 * i + 1] = elem_to_f32<kT>(a[i] >> 16);
+                most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, a[i] & 0x7fff7fffu));
             }
+            top = __float_as_uint(elem_to_f32<kT>(max(most.x, most.y)));
         }
         return;
     }
@@ -88,6 +97,7 @@ __device__ __forceinline__ void load8(const uint8_t* p, int n, bool far, float (
             else
                 x[i] = elem_to_f32<kT>(reinterpret_cast<const uint16_t*>(p)[i]);
         }
+        top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
     }
 }
 
@@ -122,33 +132,36 @@ __device__ __forceinline__ uint32_t max_of_4(uint32_t x) {
     return max(x, static_cast<uint32_t>(__builtin_amdgcn_mov_dpp(static_cast<int>(x), 0x4E, 0xf, 0xf, true)));  // 2 3 0 1
 }
 
+// Four codes: the lowest byte of each number in turn.
+__device__ __forceinline__ uint32_t bytes_of(const uint32_t (&b)[8], int i) {
+    return __builtin_amdgcn_perm(b[i + 1], b[i], 0x0c0c0400) | __builtin_amdgcn_perm(b[i + 3], b[i + 2], 0x04000c0c);
+}
+
 // Codes and the scale's byte of a block that four lanes hold.  The largest
 // magnitude m * 2^q, 1 <= m < 2, is at most 127 * 2^(q - 6) where m is at most
-// 127 / 64, that is where its fraction's bits are at most 0x7e0000.  Magnitudes
-// compare as their bits do, infinity and NaN above all others.
+// 127 / 64, that is where its fraction's bits are at most 0x7e0000.  x / 2^e is
+// exact, so its sum with 1.5 * 2^23 rounds it to the nearest whole number, ties to
+// even, and leaves that in two's complement in the lowest bits.
 template <int kT>
-__device__ __forceinline__ uint32_t encode8(const float (&x)[8], u32x2& codes) {
-    uint32_t most = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(x[i]) & 0x7fffffffu);
-    most = max_of_4(most);
-    if (most >= 0x7f800000u) {
-        codes = u32x2{0, 0};
-        return 255;
-    }
+__device__ __forceinline__ uint32_t encode8(const float (&x)[8], uint32_t top, u32x2& codes) {
+    const uint32_t most = max_of_4(top);
     const int scale = max(1, static_cast<int>(most >> 23) - ((most & 0x7fffffu) <= 0x7e0000u ? 6 : 5));
     // up to here 64 times the scale is within the type's range
     constexpr int kTop = kT == kFP16 ? 127 + 9 : 127 + 121;
     const float down = __uint_as_float(static_cast<uint32_t>(254 - scale) << 23);
-    uint32_t w[2] = {0, 0};
+    uint32_t b[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        int c = static_cast<int>(__builtin_rintf(x[i] * down));
-        if (scale > kTop) c = max(-63, min(63, c));
-        w[i / 4] |= (static_cast<uint32_t>(c) & 0xff) << (8 * (i & 3));
+    for (int i = 0; i < 8; ++i) b[i] = __float_as_uint(__builtin_fmaf(x[i], down, 12582912.0f));
+    if (scale > kTop) {  // at the end of the type's range, or beyond it
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int c = max(-63, min(63, static_cast<int>(b[i] << 24) >> 24));
+            b[i] = static_cast<uint32_t>(c);
+        }
     }
-    codes = u32x2{w[0], w[1]};
-    return static_cast<uint32_t>(scale);
+    codes = u32x2{bytes_of(b, 0), bytes_of(b, 4)};
+    if (most >= 0x7f800000u) codes = u32x2{0, 0};
+    return most >= 0x7f800000u ? 255 : static_cast<uint32_t>(scale);
 }
 
 __device__ __forceinline__ void keep8(const Kept& k, int64_t group, bool far, u32x2 codes, uint32_t scale) {
@@ -160,6 +173,7 @@ __device__ __forceinline__ void keep8(const Kept& k, int64_t group, bool far, u3
     if ((group & 3) == 0) k.scales[group >> 2] = static_cast<uint8_t>(scale);
 }
 
+// (128 s, which would save an instruction, need not be finite.)
 __device__ __forceinline__ void decode8(u32x2 codes, uint32_t scale, float (&x)[8]) {
     const float s = __uint_as_float(scale << 23 | (scale == 255 ? 0x400000u : 0u));
 #pragma unroll
@@ -249,9 +263,10 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(PackArgs a) {
     for (int64_t g = blockIdx.x * int64_t{kThreads} + threadIdx.x; g < a.groups; g += gridDim.x * int64_t{kThreads}) {
         const Place p = place_of(g, a.blocks, a.cols);
         float x[8];
-        load8<kT>(a.x.p + p.row * a.x.stride + int64_t{p.col} * dtype_bytes(kT), p.n, false, x);
+        uint32_t top;
+        load8<kT>(a.x.p + p.row * a.x.stride + int64_t{p.col} * dtype_bytes(kT), p.n, false, x, top);
         u32x2 codes;
-        const uint32_t scale = encode8<kT>(x, codes);
+        const uint32_t scale = encode8<kT>(x, top, codes);
         keep8(a.kept, g, false, codes, scale);
     }
 }
@@ -282,8 +297,9 @@ __global__ __launch_bounds__(kThreads) void gate_kernel(GateArgs a) {
         const Place p = place_of(g, a.blocks, a.cols);
         const int64_t at = int64_t{p.col} * dtype_bytes(kT);
         float x[8], f[8], y[8], unused;
-        load8<kT>(a.x.p + p.row * a.x.stride + at, p.n, far, x);
-        if (kGated) load8<kT>(a.factor.p + p.row * a.factor.stride + at, p.n, far, f);
+        uint32_t top_x, top_f;
+        load8<kT>(a.x.p + p.row * a.x.stride + at, p.n, far, x, top_x);
+        if (kGated) load8<kT>(a.factor.p + p.row * a.factor.stride + at, p.n, far, f, top_f);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             activate<kT, kKind, false>(x[i], y[i], unused);
@@ -292,10 +308,10 @@ __global__ __launch_bounds__(kThreads) void gate_kernel(GateArgs a) {
         if (p.n > 0) store8<kT>(a.out.p + p.row * a.out.stride + at, p.n, far, y);
         if (a.keep_x.codes != nullptr) {
             u32x2 codes;
-            uint32_t scale = encode8<kT>(x, codes);
+            uint32_t scale = encode8<kT>(x, top_x, codes);
             keep8(a.keep_x, g, far, codes, scale);
             if (kGated) {
-                scale = encode8<kT>(f, codes);
+                scale = encode8<kT>(f, top_f, codes);
                 keep8(a.keep_factor, g, far, codes, scale);
             }
         }
@@ -310,7 +326,8 @@ __global__ __launch_bounds__(kThreads) void gate_grad_kernel(GateArgs a) {
         if (p.n <= 0) continue;
         const int64_t at = int64_t{p.col} * dtype_bytes(kT);
         float dy[8], x[8], f[8], dx[8], df[8];
-        load8<kT>(a.out.p + p.row * a.out.stride + at, p.n, far, dy);
+        uint32_t unused;
+        load8<kT>(a.out.p + p.row * a.out.stride + at, p.n, far, dy, unused);
         restore8(a.keep_x, g, x);
         if (kGated) restore8(a.keep_factor, g, f);
 #pragma unroll
