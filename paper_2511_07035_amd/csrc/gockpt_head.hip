@@ -62,24 +62,44 @@ __device__ __forceinline__ bool counts(const TokenArgs& a, int64_t id) {
     return id >= a.low && id < a.high && id != a.ignore;
 }
 
+// What a lane keeps of a token: its row of the table, or
+constexpr int32_t kElsewhere = -1, kMasked = -2;
+
+__device__ __forceinline__ int32_t row_of(const TokenArgs& a, int64_t t) {
+    const int64_t id = target_of(a, static_cast<int32_t>(t));
+    if (!counts(a, id)) return kMasked;
+    const int64_t row = id - a.first;
+    return row >= 0 && row < a.rows ? static_cast<int32_t>(row) : kElsewhere;
+}
+
 // One block: each wavefront counts its stretch of tokens, then numbers it from
-// the sum of those before.  16384 tokens take 9 us beside 11 ms of products.
+// the sum of those before.  A lane holds its first tokens from one pass to the
+// other, all 16384 of a block's.
 __global__ __launch_bounds__(kTokenThreads) void token_kernel(TokenArgs a) {
     __shared__ int32_t counted[kTokenWaves];
     __shared__ float largest[kTokenWaves];
+    constexpr int kHeld = 16;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int32_t each = (a.tokens + kTokenThreads - 1) / kTokenThreads * 64;
     const int64_t from = static_cast<int64_t>(wave) * each;
     const int64_t to = min(from + each, static_cast<int64_t>(a.tokens));
     const bool weighted = a.grad != nullptr && a.reduction == GOCKPT_EACH;
+    int32_t held[kHeld];
+#pragma unroll
+    for (int u = 0; u < kHeld; ++u) {
+        const int64_t t = from + 64 * u + lane;
+        held[u] = t < to ? row_of(a, t) : kMasked;
+    }
     int32_t mine = 0;
     float most = 0.0f;
-    int64_t first_id = 0;  // of a lane's first token, which may be its only one
+#pragma unroll
+    for (int u = 0; u < kHeld; ++u) {
+        mine += held[u] != kMasked;
+        if (weighted && held[u] != kMasked) most = fmaxf(most, fabsf(a.grad[from + 64 * u + lane]));
+    }
 #pragma unroll 4
-    for (int64_t t = from + lane; t < to; t += 64) {
-        const int64_t id = target_of(a, static_cast<int32_t>(t));
-        if (t == from + lane) first_id = id;
-        if (!counts(a, id)) continue;
+    for (int64_t t = from + 64 * kHeld + lane; t < to; t += 64) {
+        if (row_of(a, t) == kMasked) continue;
         ++mine;
         if (weighted) most = fmaxf(most, fabsf(a.grad[t]));
     }
@@ -114,28 +134,31 @@ __global__ __launch_bounds__(kTokenThreads) void token_kernel(TokenArgs a) {
         *a.unscale = 1.0f;  // no tokens: the gradients are sums of nothing, times this
     }
     if (threadIdx.x == 0) *a.count = all;
-    for (int64_t at = from; at < to; at += 64) {
-        const int64_t t = at + lane;
-        const int64_t id = at == from ? first_id : t < to ? target_of(a, static_cast<int32_t>(t)) : 0;
-        const bool there = t < to && counts(a, id);
+    const auto number = [&](int64_t t, int32_t row) {
+        const bool there = row != kMasked;
         const uint64_t votes = __ballot(there);
         const int32_t k = before + __popcll(votes & ((uint64_t{1} << lane) - 1));
         before += __popcll(votes);
+        if (t >= to) return;
         if (there) {
-            const int64_t row = id - a.first;
             a.of_kept[k] = static_cast<int32_t>(t);
-            a.target[k] = row >= 0 && row < a.rows ? static_cast<int32_t>(row) : -1;
+            a.target[k] = row;
             if (a.grad != nullptr) {
                 a.base[k] = a.lse_in[t] * static_cast<float>(kLog2e);
                 a.factor[k] = (weighted ? a.grad[t] : g) * up_by;
             }
-        } else if (t < to) {
+        } else {
             if (a.lse != nullptr) a.lse[t] = 0.0f;
             if (a.logit != nullptr) a.logit[t] = 0.0f;
             if (a.loss != nullptr && a.reduction == GOCKPT_EACH) a.loss[t] = 0.0f;
         }
-        if (t < to && a.of_token != nullptr) a.of_token[t] = there ? k : -1;
-    }
+        if (a.of_token != nullptr) a.of_token[t] = there ? k : -1;
+    };
+#pragma unroll
+    for (int u = 0; u < kHeld; ++u)
+        if (from + 64 * u < to) number(from + 64 * u + lane, held[u]);
+    for (int64_t at = from + 64 * kHeld; at < to; at += 64)
+        number(at + lane, at + lane < to ? row_of(a, at + lane) : kMasked);
 }
 
 // ---- the loss ---------------------------------------------------------------------
@@ -246,7 +269,8 @@ struct JoinArgs {
 };
 
 // Up to so many tokens one block joins and adds up.
-constexpr int kJoinWaves = 16, kJoinAlone = 8 * kJoinWaves;
+constexpr int kJoinWaves = 16, kJoinAlone = 64;
+constexpr uint32_t kJoinFew = 64;  // partials that 16 lanes take at once
 
 // The sum of all tokens' losses, in an order that is the same on every call.
 __device__ __forceinline__ void sum_losses(const JoinArgs& a, int32_t count) {
@@ -262,20 +286,21 @@ __device__ __forceinline__ void sum_losses(const JoinArgs& a, int32_t count) {
     *a.loss = static_cast<float>(a.reduction == GOCKPT_MEAN ? total / max(count, 1) : total);
 }
 
-// A wavefront a token.
-template <bool kAlone>
+// A wavefront a token, or 16 lanes where it has few partials.
+template <bool kAlone, int kLanes>
 __global__ __launch_bounds__(kAlone ? kJoinWaves * 64 : 256) void join_kernel(JoinArgs a) {
-    constexpr int kWaves = kAlone ? kJoinWaves : 4;
-    const int lane = threadIdx.x & 63;
+    constexpr int kTokens = (kAlone ? kJoinWaves * 64 : 256) / kLanes;  // of a block at once
+    const int lane = threadIdx.x % kLanes;
     const int32_t count = *a.count;
     const bool single = a.reduction == GOCKPT_EACH;
-    for (int32_t k = blockIdx.x * kWaves + (threadIdx.x >> 6); k < count; k += gridDim.x * kWaves) {
+    for (int32_t k = blockIdx.x * kTokens + threadIdx.x / kLanes; k < count; k += gridDim.x * kTokens) {
         const float2* p = a.part + static_cast<int64_t>(k) * a.tiles_r;
         float most = -INFINITY, sum = 0.0f;
-        for (uint32_t i = lane; i < a.tiles_r; i += 256) {
+        for (uint32_t i = lane; i < a.tiles_r; i += 4 * kLanes) {
             float2 x[4];  // on their way together
 #pragma unroll
-            for (int u = 0; u < 4; ++u) x[u] = i + 64 * u < a.tiles_r ? p[i + 64 * u] : float2{-INFINITY, 0.0f};
+            for (int u = 0; u < 4; ++u)
+                x[u] = i + kLanes * u < a.tiles_r ? p[i + kLanes * u] : float2{-INFINITY, 0.0f};
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const float top = fmaxf(most, x[u].x), from = top == -INFINITY ? 0.0f : top;
@@ -284,10 +309,10 @@ __global__ __launch_bounds__(kAlone ? kJoinWaves * 64 : 256) void join_kernel(Jo
             }
         }
         float top = most;
-        for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+        for (int d = kLanes / 2; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
         const float from = top == -INFINITY ? 0.0f : top;
         sum *= __builtin_amdgcn_exp2f(most - from);
-        for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
+        for (int d = kLanes / 2; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
         if (lane == 0) {
             const int32_t t = a.of_kept[k];
             const float log2_sum = __builtin_amdgcn_logf(sum);
@@ -691,10 +716,13 @@ int gockpt_head_loss(const gockpt_head* head, int reduction, float* loss, float*
     j.logit = logit;
     j.loss = loss;
     j.each = reinterpret_cast<float*>(ws + p.each);
+    const bool few = g.a.tiles_r <= kJoinFew;
     if (t.tokens <= kJoinAlone) {
-        hipLaunchKernelGGL(join_kernel<true>, dim3(1), dim3(kJoinWaves * 64), 0, s, j);
+        hipLaunchKernelGGL((few ? join_kernel<true, 16> : join_kernel<true, 64>), dim3(1), dim3(kJoinWaves * 64), 0, s, j);
     } else {
-        hipLaunchKernelGGL(join_kernel<false>, dim3(std::min((t.tokens + 3) / 4, kUnits * 8)), dim3(256), 0, s, j);
+        const int tokens = few ? 16 : 4;
+        hipLaunchKernelGGL((few ? join_kernel<false, 16> : join_kernel<false, 64>),
+                           dim3(std::min((t.tokens + tokens - 1) / tokens, kUnits * 8)), dim3(256), 0, s, j);
         if (loss != nullptr && reduction != GOCKPT_EACH)
             hipLaunchKernelGGL(sum_kernel, dim3(1), dim3(kJoinWaves * 64), 0, s, j);
     }
