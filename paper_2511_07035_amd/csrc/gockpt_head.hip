@@ -182,9 +182,9 @@ __device__ __forceinline__ void negate(typename M::Acc& acc) {
 template <class M>
 __global__ __launch_bounds__(M::kThreads) void logits_kernel(LossArgs g) {
     GOCKPT_MMA_LDS(M)
-    const MmaPlace p = mma_place(g.a, M::kBR, M::kBC);
     const int cn = *g.a.cn_dev;
-    if (p.c0 >= cn) return;
+    MmaPlace p;
+    if (!mma_place(g.a, cn, M::kBR, M::kBC, p)) return;
     typename M::Acc acc;
     GOCKPT_MMA_RUN(M, g.a, p, cn, g.a.k, acc);
     M::sync();  // the buffers are free
@@ -354,9 +354,9 @@ struct GradArgs {
 template <class M>
 __global__ __launch_bounds__(M::kThreads) void z_kernel(GradArgs g) {
     GOCKPT_MMA_LDS(M)
-    const MmaPlace p = mma_place(g.a, M::kBR, M::kBC);
     const int cn = *g.a.cn_dev;
-    if (p.c0 >= cn) return;
+    MmaPlace p;
+    if (!mma_place(g.a, cn, M::kBR, M::kBC, p)) return;
     typename M::Acc acc;
     GOCKPT_MMA_RUN(M, g.a, p, cn, g.a.k, acc);
     const bool edge = M::first_r(p) + M::kFR * 16 > g.a.rn;

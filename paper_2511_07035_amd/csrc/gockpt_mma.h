@@ -211,22 +211,25 @@ struct MmaPlace {
 // Blocks go to the 8 XCDs in turn; each XCD takes one run of tiles, in groups
 // of 4 tiles of c (2, 8 and 16 were slower by up to 4%), so that the blocks that
 // run on it together read few different tiles and find the others' in its L2.
-__device__ __forceinline__ MmaPlace mma_place(const MmaArgs& a, int br, int bc) {
-    const uint32_t n = a.tiles_r * a.tiles_c, all = n * a.splits;
+// Only the tiles below cn are shared out: were the others' blocks to end at
+// once, the last XCDs' would, and the others work as long as ever.
+__device__ __forceinline__ bool mma_place(const MmaArgs& a, int cn, int br, int bc, MmaPlace& p) {
+    const uint32_t tiles_c = static_cast<uint32_t>((cn + bc - 1) / bc);
+    const uint32_t n = a.tiles_r * tiles_c, all = n * a.splits;
     uint32_t id = blockIdx.x;
+    if (id >= all) return false;
     const uint32_t each = all / 8, over = all % 8, xcd = id % 8, at = id / 8;
     id = xcd * each + min(xcd, over) + at;
     const uint32_t split = id / n;
     id -= split * n;
     const uint32_t group = id / (4 * a.tiles_r), first = group * 4;
-    const uint32_t wide = min(a.tiles_c - first, 4u);
+    const uint32_t wide = min(tiles_c - first, 4u);
     id -= group * 4 * a.tiles_r;
-    MmaPlace p;
     p.tile_r = id / wide;
     p.r0 = static_cast<int>(p.tile_r) * br;
     p.c0 = static_cast<int>(first + id % wide) * bc;
     p.split = static_cast<int>(split);
-    return p;
+    return true;
 }
 
 template <int kT_, int kRLay, int kCLay, int kBR_, int kBC_, int kWR_, int kWC_>

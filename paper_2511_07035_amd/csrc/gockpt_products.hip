@@ -11,9 +11,9 @@ namespace {
 template <class M>
 __global__ __launch_bounds__(M::kThreads) void product_kernel(MmaArgs a, StoreArgs o) {
     GOCKPT_MMA_LDS(M)
-    const MmaPlace p = mma_place(a, M::kBR, M::kBC);
     const int cn = a.cn_dev != nullptr ? *a.cn_dev : a.cn;
-    if (p.c0 >= cn) return;
+    MmaPlace p;
+    if (!mma_place(a, cn, M::kBR, M::kBC, p)) return;
     const int k = a.k_dev != nullptr ? *a.k_dev : a.k;
     typename M::Acc acc;
     GOCKPT_MMA_RUN(M, a, p, cn, k, acc);
