@@ -17,7 +17,9 @@
 // Not so a token's largest term, its target's: what rounding took from that is
 // kept, and its product with the target's row of the table is added to dX in fp32
 // (root mean square error of dX at 16384 tokens of 2048 columns against float64:
-// 0.0029 of its own without, 0.0019 with; its rounding to bf16 alone makes 0.0017).
+// 0.0029 of its own without, 0.0018 with; its rounding to bf16 alone makes 0.0017),
+// and for the first two tokens of each class its product with the hidden row to
+// dW, where a class that few tokens have has few terms to average.
 // Z is scaled by a power of two, 2^13 / 2^q where 2^q <= max |g| < 2^(q + 1), so
 // that fp16 has probabilities down to 2^-37 and nothing overflows; the products
 // are scaled back in fp32.
@@ -46,6 +48,7 @@ struct TokenArgs {
     // the gradients (null: not)
     const float *lse_in, *grad;
     int32_t* of_token;  // number among those that count, or -1
+    int32_t* seen;      // the first of them that have each row of the table, the second (null: not wanted)
     float* base;        // log2(e) lse of the k-th
     float* factor;      // g 2^(13 - q)
     float* unscale;     // 2^(q - 13)
@@ -70,6 +73,28 @@ __device__ __forceinline__ int32_t row_of(const TokenArgs& a, int64_t t) {
     if (!counts(a, id)) return kMasked;
     const int64_t row = id - a.first;
     return row >= 0 && row < a.rows ? static_cast<int32_t>(row) : kElsewhere;
+}
+
+// Up to so many tokens the block that numbers them also fills `seen` (of 16384 it
+// took 87 us for that, the three launches take 5, 14 and 14: atomics on 16384
+// places of a table that no L2 owns).
+constexpr int32_t kSeenAlone = 1024;
+
+// Token k's part in filling `seen`: its row's entries reset; then, for each entry,
+// the least number above the entry before, which is the same whatever the order.
+// Rows that no token has keep what the memory held: a reader asks target whether
+// an entry is true.
+__device__ __forceinline__ void see(const TokenArgs& a, int32_t k, int stage) {
+    const int32_t row = a.target[k];
+    if (row < 0) return;
+    if (stage == 0) {
+        for (int u = 0; u < kSeen; ++u) a.seen[u * static_cast<int64_t>(a.rows) + row] = INT32_MAX;
+        return;
+    }
+    int32_t* const entry = a.seen + (stage - 1) * static_cast<int64_t>(a.rows) + row;
+    const int32_t above =
+        stage > 1 ? __hip_atomic_load(entry - a.rows, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : -1;
+    if (k > above) __hip_atomic_fetch_min(entry, k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
 // One block: each wavefront counts its stretch of tokens, then numbers it from
@@ -159,6 +184,18 @@ __global__ __launch_bounds__(kTokenThreads) void token_kernel(TokenArgs a) {
         if (from + 64 * u < to) number(from + 64 * u + lane, held[u]);
     for (int64_t at = from + 64 * kHeld; at < to; at += 64)
         number(at + lane, at + lane < to ? row_of(a, at + lane) : kMasked);
+    if (a.seen == nullptr || a.tokens > kSeenAlone) return;
+    for (int stage = 0; stage <= kSeen; ++stage) {
+        __threadfence();
+        __syncthreads();
+        for (int32_t k = threadIdx.x; k < all; k += kTokenThreads) see(a, k, stage);
+    }
+}
+
+// Of more tokens, a launch for each stage.
+__global__ __launch_bounds__(256) void seen_kernel(TokenArgs a, int stage) {
+    const int32_t k = blockIdx.x * 256 + threadIdx.x;
+    if (k < *a.count) see(a, k, stage);
 }
 
 // ---- the loss ---------------------------------------------------------------------
@@ -540,7 +577,7 @@ struct Piece {
 struct GradPlan {
     int64_t piece;   // rows of the table in a piece
     Piece full, rest;
-    size_t count, unscale, of_kept, target, of_token, base, factor, lost, hidden, table, z, slices_hidden, slices_table, bytes;
+    size_t count, unscale, of_kept, target, of_token, seen, base, factor, lost, hidden, table, z, slices_hidden, slices_table, bytes;
     int64_t z_stride;
 };
 
@@ -591,6 +628,7 @@ GradPlan plan_grad(const gockpt_head& h, bool by_hidden, bool by_table) {
     p.base = parts.take(n * 4);
     p.factor = parts.take(n * 4);
     p.lost = parts.take(n * 4);
+    if (by_table) p.seen = parts.take(kSeen * rows * 4);
     p.hidden = parts.take(n * up(cols, 8) * 2);
     p.table = parts.take(copy_bytes(h.table));
     p.z = parts.take(n * p.z_stride);
@@ -774,10 +812,14 @@ int gockpt_head_grad(const gockpt_head* head, const float* lse, int reduction, c
     t.of_token = reinterpret_cast<int32_t*>(ws + p.of_token);
     t.lse_in = lse;
     t.grad = t.tokens > 0 ? grad : nullptr;
+    if (by_table) t.seen = reinterpret_cast<int32_t*>(ws + p.seen);
     t.base = reinterpret_cast<float*>(ws + p.base);
     t.factor = reinterpret_cast<float*>(ws + p.factor);
     t.unscale = reinterpret_cast<float*>(ws + p.unscale);
     hipLaunchKernelGGL(token_kernel, dim3(1), dim3(kTokenThreads), 0, s, t);
+    if (t.seen != nullptr && t.tokens > kSeenAlone)
+        for (int stage = 0; stage <= kSeen; ++stage)
+            hipLaunchKernelGGL(seen_kernel, dim3((t.tokens + 255) / 256), dim3(256), 0, s, t, stage);
     launch_rows(head->hidden, t.of_kept, t.count, t.tokens, ws + p.hidden, s);
     const Source table = source_of(head->table, ws + p.table, s);
     const int64_t hidden_stride = up(cols, 8) * 2;
@@ -844,6 +886,11 @@ int gockpt_head_grad(const gockpt_head* head, const float* lse, int reduction, c
             f.alpha = head->scale;
             f.beta = t.unscale;
             StoreArgs o{};
+            o.seen = t.seen;
+            o.seen_step = rows;
+            o.owner = t.target;
+            o.fix = reinterpret_cast<const float*>(ws + p.lost);
+            o.first = static_cast<int32_t>(first);
             if (plan.by_table.splits > 1) {
                 o.slices = reinterpret_cast<float*>(ws + p.slices_table);
                 launch_product(kAcrossAcross, dtype, plan.by_table, a, o, s);

@@ -235,6 +235,7 @@ __device__ __forceinline__ bool mma_place(const MmaArgs& a, int cn, int br, int 
 template <int kT_, int kRLay, int kCLay, int kBR_, int kBC_, int kWR_, int kWC_>
 struct Mma {
     static constexpr int kT = kT_, kBR = kBR_, kBC = kBC_, kWR = kWR_, kWC = kWC_;
+    static constexpr bool kBothAcross = kRLay == kAcrossK && kCLay == kAcrossK;
     static constexpr int kWaves = kWR * kWC, kThreads = kWaves * 64;
     static constexpr int kFR = kBR / kWR / 16, kFC = kBC / kWC / 16;  // fragments of a wave
     static constexpr int kRBytes = kBR * kStepK * 2, kCBytes = kBC * kStepK * 2;
@@ -431,6 +432,7 @@ struct Stream {
     static constexpr int kTile = 32 * kStepK * 2;
     static constexpr int kRBytes = kWaves * kTile, kCBytes = kWaves * kTile;
     static constexpr bool kOneWave = true;  // the first wavefront has the sum
+    static constexpr bool kBothAcross = false;
     using Acc = f32x4[2][2];
 
     struct State {
@@ -583,7 +585,42 @@ struct StoreArgs {
     const float* beta;  // and one on the device (null: 1)
     float* slices;      // not null: fp32 sums instead, slice s at s * cn * rn, unscaled;
     int32_t add;        // added to what is there
+    // not null: fix[k] R(r, k) is added to c's sum, for the k that `seen` names for c
+    // (entry u of c at seen[u * seen_step + first + c], kSeen of them) and whose
+    // owner[k] is first + c; other entries may hold anything.  R lies across k.
+    const int32_t* seen;
+    int64_t seen_step;
+    const int32_t* owner;
+    const float* fix;
+    int32_t first;
 };
+constexpr int kSeen = 2;
+
+template <class M>
+__device__ __forceinline__ void add_fixes(const MmaArgs& a, const StoreArgs& o, const MmaPlace& p, int cn, int k_all,
+                                          typename M::Acc& acc) {
+#pragma unroll
+    for (int j = 0; j < M::kFC; ++j) {
+        const int c = M::c_of(p, j);
+#pragma unroll
+        for (int u = 0; u < kSeen; ++u) {
+            const int k = c < cn ? o.seen[u * o.seen_step + o.first + c] : -1;
+            const bool there = k >= 0 && k < k_all && o.owner[k] == o.first + c;
+            if (!__any(there)) continue;
+            const float x = there ? o.fix[k] : 0.0f;
+            const uint8_t* row = a.r + (there ? k : 0) * a.r_stride;
+#pragma unroll
+            for (int i = 0; i < M::kFR; ++i) {
+                const int r = M::r_of(p, i);
+                if (!there || r >= a.rn) continue;
+                const u32x2 w = *reinterpret_cast<const u32x2*>(row + r * 2);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    acc[i][j][e] += x * elem_to_f32<M::kT>(w[e / 2] >> (16 * (e & 1)) & 0xffff);
+            }
+        }
+    }
+}
 
 template <int kT>
 __device__ __forceinline__ u32x2 pack4(f32x4 x) {

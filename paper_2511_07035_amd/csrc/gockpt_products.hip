@@ -17,6 +17,8 @@ __global__ __launch_bounds__(M::kThreads) void product_kernel(MmaArgs a, StoreAr
     const int k = a.k_dev != nullptr ? *a.k_dev : a.k;
     typename M::Acc acc;
     GOCKPT_MMA_RUN(M, a, p, cn, k, acc);
+    if constexpr (M::kBothAcross)
+        if (o.seen != nullptr && p.split == 0) add_fixes<M>(a, o, p, cn, k, acc);
     M::sync();
     store_tile<M>(GOCKPT_MMA_STORE(M), a, o, p, cn, acc);
 }
