@@ -204,6 +204,7 @@ struct LossArgs {
     MmaArgs a;       // R: the table, C: the hidden rows that count
     float log2_scale;  // scale log2(e)
     const int32_t* target;
+    TokenArgs few;   // the streaming kernel's: c is the token itself, whether it counts or not
     float2* part;    // token k's largest l2 and sum in tile r at k * tiles_r + r
     float* logit;    // l2 of its target
 };
@@ -219,9 +220,14 @@ __device__ __forceinline__ void negate(typename M::Acc& acc) {
 template <class M>
 __global__ __launch_bounds__(M::kThreads) void logits_kernel(LossArgs g) {
     GOCKPT_MMA_LDS(M)
-    const int cn = *g.a.cn_dev;
+    const int cn = M::kOneWave ? g.few.tokens : *g.a.cn_dev;
     MmaPlace p;
     if (!mma_place(g.a, cn, M::kBR, M::kBC, p)) return;
+    int wants[M::kFC];
+    if constexpr (M::kOneWave) {  // on their way while the table is read
+#pragma unroll
+        for (int j = 0; j < M::kFC; ++j) wants[j] = M::c_of(p, j) < cn ? row_of(g.few, M::c_of(p, j)) : kMasked;
+    }
     typename M::Acc acc;
     GOCKPT_MMA_RUN(M, g.a, p, cn, g.a.k, acc);
     M::sync();  // the buffers are free
@@ -233,7 +239,7 @@ __global__ __launch_bounds__(M::kThreads) void logits_kernel(LossArgs g) {
 #pragma unroll
     for (int j = 0; j < M::kFC; ++j) {
         const int c = M::c_of(p, j);
-        const int want = c < cn ? g.target[c] : -1;
+        const int want = M::kOneWave ? wants[j] : c < cn ? g.target[c] : -1;
         // most tiles hold the targets of none of their tokens
         if (__any(want >= M::first_r(p) && want < M::first_r(p) + M::kFR * 16)) {
             float l = 0.0f;
@@ -298,6 +304,7 @@ __global__ __launch_bounds__(M::kThreads) void logits_kernel(LossArgs g) {
 struct JoinArgs {
     const float2* part;
     const int32_t *count, *of_kept, *target;
+    TokenArgs few;  // kAlone, with tokens: the k-th is token k itself, whether it counts or not
     const float* logit2;
     uint32_t tiles_r;
     int32_t reduction;
@@ -309,8 +316,9 @@ struct JoinArgs {
 constexpr int kJoinWaves = 16, kJoinAlone = 64;
 constexpr uint32_t kJoinFew = 64;  // partials that 16 lanes take at once
 
-// The sum of all tokens' losses, in an order that is the same on every call.
-__device__ __forceinline__ void sum_losses(const JoinArgs& a, int32_t count) {
+// The sum of all tokens' losses, in an order that is the same on every call, of
+// which `kept` count.
+__device__ __forceinline__ void sum_losses(const JoinArgs& a, int32_t count, int32_t kept) {
     __shared__ double sums[kJoinWaves];
     double total = 0.0;
     for (int32_t k = threadIdx.x; k < count; k += kJoinWaves * 64) total += static_cast<double>(a.each[k]);
@@ -320,7 +328,7 @@ __device__ __forceinline__ void sum_losses(const JoinArgs& a, int32_t count) {
     if (threadIdx.x != 0) return;
     total = 0.0;
     for (int w = 0; w < kJoinWaves; ++w) total += sums[w];
-    *a.loss = static_cast<float>(a.reduction == GOCKPT_MEAN ? total / max(count, 1) : total);
+    *a.loss = static_cast<float>(a.reduction == GOCKPT_MEAN ? total / max(kept, 1) : total);
 }
 
 // A wavefront a token, or 16 lanes where it has few partials.
@@ -328,10 +336,12 @@ template <bool kAlone, int kLanes>
 __global__ __launch_bounds__(kAlone ? kJoinWaves * 64 : 256) void join_kernel(JoinArgs a) {
     constexpr int kTokens = (kAlone ? kJoinWaves * 64 : 256) / kLanes;  // of a block at once
     const int lane = threadIdx.x % kLanes;
-    const int32_t count = *a.count;
+    const bool few = kAlone && a.few.tokens > 0;
+    const int32_t count = few ? a.few.tokens : *a.count;
     const bool single = a.reduction == GOCKPT_EACH;
     for (int32_t k = blockIdx.x * kTokens + threadIdx.x / kLanes; k < count; k += gridDim.x * kTokens) {
         const float2* p = a.part + static_cast<int64_t>(k) * a.tiles_r;
+        const int32_t row = few ? row_of(a.few, k) : a.target[k];
         float most = -INFINITY, sum = 0.0f;
         for (uint32_t i = lane; i < a.tiles_r; i += 4 * kLanes) {
             float2 x[4];  // on their way together
@@ -351,12 +361,13 @@ __global__ __launch_bounds__(kAlone ? kJoinWaves * 64 : 256) void join_kernel(Jo
         sum *= __builtin_amdgcn_exp2f(most - from);
         for (int d = kLanes / 2; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
         if (lane == 0) {
-            const int32_t t = a.of_kept[k];
+            const int32_t t = few ? k : a.of_kept[k];
+            const bool there = row != kMasked;
             const float log2_sum = __builtin_amdgcn_logf(sum);
-            const float logit2 = a.target[k] >= 0 ? a.logit2[k] : 0.0f;
-            if (a.lse != nullptr) a.lse[t] = (from + log2_sum) * kLn2;
+            const float logit2 = row >= 0 ? a.logit2[k] : 0.0f;
+            if (a.lse != nullptr) a.lse[t] = there ? (from + log2_sum) * kLn2 : 0.0f;
             if (a.logit != nullptr) a.logit[t] = logit2 * kLn2;
-            const float loss = (from - logit2 + log2_sum) * kLn2;
+            const float loss = there ? (from - logit2 + log2_sum) * kLn2 : 0.0f;
             if (a.loss != nullptr) {
                 if (single)
                     a.loss[t] = loss;
@@ -368,12 +379,16 @@ __global__ __launch_bounds__(kAlone ? kJoinWaves * 64 : 256) void join_kernel(Jo
     if constexpr (kAlone) {
         if (single || a.loss == nullptr) return;
         __threadfence_block();
-        __syncthreads();
-        sum_losses(a, count);
+        int32_t kept = count;
+        if (few)
+            kept = __syncthreads_count(static_cast<int32_t>(threadIdx.x) < count && row_of(a.few, threadIdx.x) != kMasked);
+        else
+            __syncthreads();
+        sum_losses(a, count, kept);
     }
 }
 
-__global__ __launch_bounds__(kJoinWaves * 64) void sum_kernel(JoinArgs a) { sum_losses(a, *a.count); }
+__global__ __launch_bounds__(kJoinWaves * 64) void sum_kernel(JoinArgs a) { sum_losses(a, *a.count, *a.count); }
 
 // ---- the gradients ------------------------------------------------------------------
 
@@ -713,17 +728,25 @@ int gockpt_head_loss(const gockpt_head* head, int reduction, float* loss, float*
     t.lse = lse;
     t.logit = logit;
     t.loss = loss;
-    hipLaunchKernelGGL(token_kernel, dim3(1), dim3(kTokenThreads), 0, s, t);
     LossArgs g{};
+    JoinArgs j{};
+    // So few tokens are not numbered: the streaming kernel takes them all, a launch
+    // less (one token of 4096 columns, 32000 classes: 50.3 us, numbered 53.7).
+    const bool few = p.logits.shape == kThin && p.logits.tiles_r > 0 && p.logits.tiles_c > 0;
+    if (few)
+        g.few = j.few = t;
+    else
+        hipLaunchKernelGGL(token_kernel, dim3(1), dim3(kTokenThreads), 0, s, t);
     const Source table = source_of(head->table, ws + p.table, s);
     g.a.r = table.data;
     g.a.r_stride = table.stride;
     if (hidden_in_place(head->hidden)) {
         g.a.c = static_cast<const uint8_t*>(head->hidden.data);
         g.a.c_stride = (head->hidden.rows > 1 ? head->hidden.stride : head->hidden.cols) * 2;
-        g.a.c_rows = t.of_kept;
+        g.a.c_rows = few ? nullptr : t.of_kept;
     } else {
-        launch_rows(head->hidden, t.of_kept, t.count, head->hidden.rows, ws + p.hidden, s);
+        launch_rows(head->hidden, few ? nullptr : t.of_kept, few ? nullptr : t.count, head->hidden.rows, ws + p.hidden,
+                    s);
         g.a.c = ws + p.hidden;
         g.a.c_stride = up(head->hidden.cols, 8) * 2;
     }
@@ -742,7 +765,6 @@ int gockpt_head_loss(const gockpt_head* head, int reduction, float* loss, float*
         else
             start_logits<kFP16>(p.logits.shape, g, s);
     }
-    JoinArgs j{};
     j.part = g.part;
     j.count = t.count;
     j.of_kept = t.of_kept;
@@ -754,12 +776,12 @@ int gockpt_head_loss(const gockpt_head* head, int reduction, float* loss, float*
     j.logit = logit;
     j.loss = loss;
     j.each = reinterpret_cast<float*>(ws + p.each);
-    const bool few = g.a.tiles_r <= kJoinFew;
+    const bool narrow = g.a.tiles_r <= kJoinFew;
     if (t.tokens <= kJoinAlone) {
-        hipLaunchKernelGGL((few ? join_kernel<true, 16> : join_kernel<true, 64>), dim3(1), dim3(kJoinWaves * 64), 0, s, j);
+        hipLaunchKernelGGL((narrow ? join_kernel<true, 16> : join_kernel<true, 64>), dim3(1), dim3(kJoinWaves * 64), 0, s, j);
     } else {
-        const int tokens = few ? 16 : 4;
-        hipLaunchKernelGGL((few ? join_kernel<false, 16> : join_kernel<false, 64>),
+        const int tokens = narrow ? 16 : 4;
+        hipLaunchKernelGGL((narrow ? join_kernel<false, 16> : join_kernel<false, 64>),
                            dim3(std::min((t.tokens + tokens - 1) / tokens, kUnits * 8)), dim3(256), 0, s, j);
         if (loss != nullptr && reduction != GOCKPT_EACH)
             hipLaunchKernelGGL(sum_kernel, dim3(1), dim3(kJoinWaves * 64), 0, s, j);
