@@ -39,7 +39,7 @@ extern "C" {
  * when that is not ignore_id and lies in [first_id, first_id + table.rows), or,
  * with classes > 0, in [0, classes): then the table is this rank's range of so
  * many classes.  Any other token (padding marked by -1, say) is masked: no
- * loss, no gradient, and its hidden row is not read. */
+ * loss, no gradient, and what its hidden row holds does not matter. */
 typedef struct {
     gockpt_matrix hidden, table;
     gockpt_token_ids targets; /* as many as hidden has rows */

@@ -9,8 +9,8 @@
 // one wavefront a token joins them.  The gradients compute the logits again in
 // pieces of the vocabulary whose Z fits the workspace; a piece's Z is read by two
 // products, dW's rows of the piece, which is done, and dX, which is summed in
-// fp32 over the pieces.  Tokens that are masked are left out at the start: the
-// others' numbers are put together, and every kernel works on so many.
+// fp32 over the pieces.  Tokens that are masked are left out at the start (but by
+// the loss of a few): the others are numbered, and every kernel works on so many.
 //
 // Z is rounded to the inputs' 16-bit type, as the matrix cores take it: each
 // term of dX and dW is off by half a step of that type, which the sums average.
