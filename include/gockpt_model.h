@@ -93,7 +93,8 @@ int gockpt_head_grad(const gockpt_head* head, const float* lse, int reduction, c
 /* rows x cols values: each 32 columns of a row (the last block of a row may
  * have fewer) share a scale 2^e, e the least with max |x| <= 127 * 2^e and at
  * least -126; a value is kept as the code nearest to x / 2^e (ties to even) and
- * stands for code * 2^e, which bf16, fp16 and fp32 all hold exactly.  Row r has
+ * stands for code * 2^e, which bf16, fp16 and fp32 all hold exactly (fp16 within
+ * its range: values of another type beyond it are rounded).  Row r has
  * its codes (int8) at codes + r * 32 * blocks, zeros behind its last column, and
  * its scales (e + 127 as a byte) at scales + r * blocks, blocks = ceil(cols /
  * 32).  A block with an inf or NaN has the scale 255 and stands for NaN.  (Where
@@ -120,8 +121,8 @@ int gockpt_linear8(const gockpt_matrix* x, const gockpt_matrix* weight, const go
 /* grad_x = round(grad_out weight), grad_weight = round(grad_out^T kept), with
  * accumulate round(old + it).  Either may be NULL; weight may be NULL without
  * grad_x, keep without grad_weight.  grad_out is of the weight's type, and of
- * bf16 or fp16; the gradients are of any of the three.  Errors: EINVAL, ENOMEM
- * (workspace), EHIP. */
+ * bf16 or fp16, and kept is multiplied in that type; the gradients are of any of
+ * the three.  Errors: EINVAL, ENOMEM (workspace), EHIP. */
 int gockpt_linear8_grad_bytes(const gockpt_matrix* grad_out, const gockpt_matrix* weight, const gockpt_act8* keep,
                               const gockpt_matrix* grad_x, const gockpt_matrix* grad_weight, size_t* bytes);
 int gockpt_linear8_grad(const gockpt_matrix* grad_out, const gockpt_matrix* weight, const gockpt_act8* keep,

@@ -103,15 +103,17 @@ def _differentiable(stream, a, b=None) -> bool:
 
 def _own_rows(t, cols: int, stream):
     """t, or a copy, made on the call's stream, where its rows do not lie at one
-    distance (an expanded or transposed gradient)."""
+    distance, or overlap (an expanded or transposed gradient)."""
     if t.is_contiguous():
         return t
     try:
-        _matrix(t, "", None, cols)
+        _, rows, n, stride, _, _ = MATRIX.unpack(_matrix(t, "", None, cols))
+        if rows <= 1 or stride >= n:
+            return t
     except ValueError:
-        with torch.cuda.stream(stream):
-            return t.contiguous()
-    return t
+        pass
+    with torch.cuda.stream(stream):
+        return t.contiguous()
 
 
 def _check_grad_weight(weight, grad_weight, accumulate, device: int) -> None:
@@ -262,7 +264,8 @@ class Act8:
     """A tensor in 8 bits, in blocks of 32 of its last dimension: ``codes`` (int8,
     rows of whole blocks) times the powers of two of ``scales`` (uint8, the
     exponent + 127; 255: a block with an inf or NaN, which stands for NaN).  What
-    it stands for, bfloat16, float16 and float32 hold exactly."""
+    it stands for, bfloat16, float16 and float32 hold exactly (float16 within its
+    range)."""
 
     __slots__ = ("shape", "dtype", "rows", "cols", "blocks", "buffer", "packed")
 
@@ -383,7 +386,8 @@ def linear8(x, weight, *, grad_weight=None, accumulate: bool = False, stream=Non
 def linear8_grad_weight(grad_out, kept: Act8, grad_weight, *, accumulate: bool = False, stream=None):
     """grad_weight = grad_out.T @ what kept stands for, summed in fp32 and rounded
     once, or with accumulate that added to what grad_weight holds.  grad_out:
-    (*kept.shape[:-1], rows), bfloat16 or float16."""
+    (*kept.shape[:-1], rows), bfloat16 or float16; kept is taken in that type
+    (which for float16 may have less range than what was packed)."""
     if grad_out.shape[:-1] != kept.shape[:-1] or grad_out.dim() == 0:
         raise ValueError(f"grad_out of shape {tuple(grad_out.shape)} for an input of shape {tuple(kept.shape)}")
     if grad_weight.shape != (grad_out.shape[-1], kept.cols):

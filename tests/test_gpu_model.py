@@ -901,6 +901,35 @@ def test_transposed_inputs_on_a_stream():
         assert torch.equal(got, want)
 
 
+def test_rows_that_are_one_row_or_overlap():
+    """Expanded inputs and gradients, and windows of one buffer, are what their copies are."""
+    w, table = randn((72, 48), torch.bfloat16, 1), randn((200, 48), torch.bfloat16, 2)
+    row, buf = randn((1, 48), torch.bfloat16, 3), randn((48 + 29 * 8,), torch.bfloat16, 4)
+    targets = torch.arange(30, device="cuda")
+    for x in (row.expand(30, 48), buf.as_strided((30, 48), (8, 1)), row[None].expand(5, 6, 48)):
+        got = []
+        for rows in (x, x.contiguous()):
+            a, v = rows.detach().requires_grad_(), w.detach().requires_grad_()
+            t = table.detach().requires_grad_()
+            y = g.linear8(a, v)
+            y.reshape(30, 72).sum(0).backward(w[:, 0])
+            up = g.gate8(rows.detach().requires_grad_(), a)
+            up.reshape(30, 48).sum(0).backward(row[0])
+            g.linear_cross_entropy(a, t, targets.view(rows.shape[:-1]), reduction="none").sum().backward()
+            got.append((y.detach(), up.detach(), a.grad, v.grad, t.grad, g.act8_pack(rows).unpack()))
+        for one, other in zip(*got):
+            assert torch.equal(one, other)
+
+
+def test_more_tokens_than_a_block_holds_at_once():
+    hidden, table, targets = head_inputs(40001, 60, 24, "bf16")
+    targets[3::5] = -1
+    targets[17000:18500] = -1
+    head_check(hidden, table, targets, reduction="none")
+    targets[:-1] = -1
+    head_check(hidden, table, targets)
+
+
 def test_head_gradients_that_are_not_wanted():
     hidden, table, targets = head_inputs(50, 300, 64, "bf16")
     both = hidden.detach().requires_grad_(), table.detach().requires_grad_()
