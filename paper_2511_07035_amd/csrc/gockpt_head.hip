@@ -280,10 +280,16 @@ __global__ __launch_bounds__(M::kThreads) void logits_kernel(LossArgs g) {
 #pragma unroll
         for (int i = 0; i < M::kFR; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][e], scale, -from));
-                sum += edge && acc[i][j][e] == -INFINITY ? 0.0f : x;
-            }
+            for (int e = 0; e < 4; ++e)
+                sum += __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][e], scale, -from));
+        if (scale == 0.0f && edge) {  // -inf * 0, where each row that is there counts 1
+            sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < M::kFR; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    sum += acc[i][j][e] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(acc[i][j][e] * scale - from);
+        }
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
         if (lane < 16) waves[wave / M::kWC][(wave % M::kWC * M::kFC + j) * 16 + lane] = float2{most, sum};

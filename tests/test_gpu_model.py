@@ -710,6 +710,14 @@ def test_head_loss_scales(scale):
         head_check(hidden.bfloat16(), table.bfloat16(), targets, reduction="mean", up=scale)
 
 
+def test_head_scale_of_nothing():
+    """All logits 0, whatever the products are."""
+    hidden, table, targets = head_inputs(70, 301, 40, "bf16")
+    targets[::9] = -1
+    loss = head_check(hidden, table, targets, scale=0.0)[0]
+    assert abs(loss.item() - math.log(301)) < 1e-5
+
+
 def test_head_weights_of_very_different_size():
     hidden, table, targets = head_inputs(64, 300, 64, "bf16")
     x, w = hidden.detach().requires_grad_(), table.detach().requires_grad_()
