@@ -97,6 +97,23 @@ __device__ __forceinline__ void see(const TokenArgs& a, int32_t k, int stage) {
     if (k > above) __hip_atomic_fetch_min(entry, k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
+// g of every token but with GOCKPT_EACH, whose largest magnitude is `most`, and
+// what z is scaled by; `all` tokens count.
+__device__ __forceinline__ float factor_of_all(const TokenArgs& a, int32_t all, float most, float& up_by) {
+    float g = 0.0f;
+    if (a.reduction != GOCKPT_EACH) {
+        g = a.grad[0];
+        if (a.reduction == GOCKPT_MEAN) g = g / static_cast<float>(max(all, 1));
+        most = fabsf(g);
+    }
+    // no power of two makes infinities or NaN finite: they go through
+    int q = 0;
+    if (most > 0.0f && most <= 3.402823466e38f) q = max(ilogbf(most), -100);
+    up_by = ldexpf(1.0f, 13 - q);
+    if (threadIdx.x == 0) *a.unscale = ldexpf(1.0f, q - 13);
+    return g;
+}
+
 // One block: each wavefront counts its stretch of tokens, then numbers it from
 // the sum of those before.  A lane holds its first tokens from one pass to the
 // other, all 16384 of a block's.
@@ -145,16 +162,7 @@ __global__ __launch_bounds__(kTokenThreads) void token_kernel(TokenArgs a) {
     }
     float g = 0.0f, up_by = 1.0f;
     if (a.grad != nullptr) {
-        if (!weighted) {
-            g = a.grad[0];
-            if (a.reduction == GOCKPT_MEAN) g = g / static_cast<float>(max(all, 1));
-            most = fabsf(g);
-        }
-        // no power of two makes infinities or NaN finite: they go through
-        int q = 0;
-        if (most > 0.0f && most <= 3.402823466e38f) q = max(ilogbf(most), -100);
-        up_by = ldexpf(1.0f, 13 - q);
-        if (threadIdx.x == 0) *a.unscale = ldexpf(1.0f, q - 13);
+        g = factor_of_all(a, all, most, up_by);
     } else if (a.unscale != nullptr && threadIdx.x == 0) {
         *a.unscale = 1.0f;  // no tokens: the gradients are sums of nothing, times this
     }
@@ -198,13 +206,62 @@ __global__ __launch_bounds__(256) void seen_kernel(TokenArgs a, int stage) {
     if (k < *a.count) see(a, k, stage);
 }
 
+// Up to so many tokens are not numbered, as leaving some out would leave out no
+// tile: the k-th is token k, and of those that do not count nothing is used.  That
+// is a launch less each way, and one more where dX needs no sums joined (96 tokens
+// of 64 columns, 320 classes, both ways: 133 us, numbered 144; one token of 4096
+// columns, 32000 classes, its loss: 50.3, numbered 53.7).
+constexpr int32_t kFew = 256;
+
+// What the gradients take from token_kernel and of the hidden rows, for so few
+// tokens: rows of those that do not count are zeros, so that they add nothing to
+// dW.  The first block also has the tokens' numbers; count[0] is all of them,
+// count[1] as well unless none counts.
+__global__ __launch_bounds__(kFew) void few_kernel(TokenArgs a, const uint8_t* hidden, int64_t stride, int32_t cols,
+                                                   uint8_t* dst) {
+    const int32_t groups = (cols + 7) / 8;
+    for (int32_t at = blockIdx.x * kFew + threadIdx.x; at < groups * a.tokens; at += gridDim.x * kFew) {
+        const int32_t t = at / groups, col = (at - t * groups) * 8;
+        u32x4 w = {0, 0, 0, 0};
+        if (row_of(a, t) != kMasked) w = load8(hidden + t * stride + int64_t{col} * 2, cols - col);
+        *reinterpret_cast<u32x4*>(dst + int64_t{at} * 16) = w;
+    }
+    if (blockIdx.x != 0) return;
+    __shared__ float largest[kFew / 64];
+    const int32_t t = threadIdx.x, row = t < a.tokens ? row_of(a, t) : kMasked;
+    const bool there = row != kMasked, weighted = a.reduction == GOCKPT_EACH;
+    float most = weighted && there ? fabsf(a.grad[t]) : 0.0f;
+    for (int d = 32; d > 0; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
+    if ((t & 63) == 0) largest[t >> 6] = most;
+    const int32_t all = __syncthreads_count(there);
+    for (int w = 0; w < kFew / 64; ++w) most = fmaxf(most, largest[w]);
+    float up_by;
+    const float g = factor_of_all(a, all, most, up_by);
+    if (t == 0) {
+        a.count[0] = a.tokens;
+        a.count[1] = all > 0 ? a.tokens : 0;
+    }
+    if (t < a.tokens) {
+        a.target[t] = row;
+        a.of_token[t] = there ? t : -1;
+        a.base[t] = there ? a.lse_in[t] * static_cast<float>(kLog2e) : 0.0f;
+        a.factor[t] = there ? (weighted ? a.grad[t] : g) * up_by : 0.0f;
+    }
+    if (a.seen == nullptr) return;
+    for (int stage = 0; stage <= kSeen; ++stage) {
+        __threadfence();
+        __syncthreads();
+        if (t < a.tokens) see(a, t, stage);
+    }
+}
+
 // ---- the loss ---------------------------------------------------------------------
 
 struct LossArgs {
     MmaArgs a;       // R: the table, C: the hidden rows that count
     float log2_scale;  // scale log2(e)
     const int32_t* target;
-    TokenArgs few;   // the streaming kernel's: c is the token itself, whether it counts or not
+    TokenArgs few;   // with tokens: c is the token itself, whether it counts or not
     float2* part;    // token k's largest l2 and sum in tile r at k * tiles_r + r
     float* logit;    // l2 of its target
 };
@@ -220,7 +277,8 @@ __device__ __forceinline__ void negate(typename M::Acc& acc) {
 template <class M>
 __global__ __launch_bounds__(M::kThreads) void logits_kernel(LossArgs g) {
     GOCKPT_MMA_LDS(M)
-    const int cn = M::kOneWave ? g.few.tokens : *g.a.cn_dev;
+    const bool few = M::kOneWave || g.few.tokens > 0;
+    const int cn = few ? g.few.tokens : *g.a.cn_dev;
     MmaPlace p;
     if (!mma_place(g.a, cn, M::kBR, M::kBC, p)) return;
     int wants[M::kFC];
@@ -239,7 +297,7 @@ __global__ __launch_bounds__(M::kThreads) void logits_kernel(LossArgs g) {
 #pragma unroll
     for (int j = 0; j < M::kFC; ++j) {
         const int c = M::c_of(p, j);
-        const int want = M::kOneWave ? wants[j] : c < cn ? g.target[c] : -1;
+        const int want = M::kOneWave ? wants[j] : c >= cn ? kMasked : few ? row_of(g.few, c) : g.target[c];
         // most tiles hold the targets of none of their tokens
         if (__any(want >= M::first_r(p) && want < M::first_r(p) + M::kFR * 16)) {
             float l = 0.0f;
@@ -310,7 +368,7 @@ __global__ __launch_bounds__(M::kThreads) void logits_kernel(LossArgs g) {
 struct JoinArgs {
     const float2* part;
     const int32_t *count, *of_kept, *target;
-    TokenArgs few;  // kAlone, with tokens: the k-th is token k itself, whether it counts or not
+    TokenArgs few;  // with tokens: the k-th is token k itself, whether it counts or not
     const float* logit2;
     uint32_t tiles_r;
     int32_t reduction;
@@ -318,14 +376,21 @@ struct JoinArgs {
     float* each;  // the tokens' losses, for their sum
 };
 
-// Up to so many tokens one block joins and adds up.
-constexpr int kJoinWaves = 16, kJoinAlone = 64;
-constexpr uint32_t kJoinFew = 64;  // partials that 16 lanes take at once
+// Up to so many tokens one block joins and adds up; 16 lanes take one where it has
+// few partials (96 tokens of 3: 5 us, in place of two launches of 4 and 2).
+constexpr int kJoinWaves = 16, kJoinAlone = 64, kJoinAloneNarrow = 256;
+constexpr uint32_t kJoinFew = 64;
 
-// The sum of all tokens' losses, in an order that is the same on every call, of
-// which `kept` count.
-__device__ __forceinline__ void sum_losses(const JoinArgs& a, int32_t count, int32_t kept) {
+// The sum of all tokens' losses, in an order that is the same on every call.
+__device__ __forceinline__ void sum_losses(const JoinArgs& a) {
     __shared__ double sums[kJoinWaves];
+    const bool few = a.few.tokens > 0;
+    const int32_t count = few ? a.few.tokens : *a.count;
+    int32_t kept = count;
+    if (few) {
+        const int32_t t = threadIdx.x;
+        kept = __syncthreads_count(t < count && row_of(a.few, t) != kMasked);
+    }
     double total = 0.0;
     for (int32_t k = threadIdx.x; k < count; k += kJoinWaves * 64) total += static_cast<double>(a.each[k]);
     for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d);
@@ -342,7 +407,7 @@ template <bool kAlone, int kLanes>
 __global__ __launch_bounds__(kAlone ? kJoinWaves * 64 : 256) void join_kernel(JoinArgs a) {
     constexpr int kTokens = (kAlone ? kJoinWaves * 64 : 256) / kLanes;  // of a block at once
     const int lane = threadIdx.x % kLanes;
-    const bool few = kAlone && a.few.tokens > 0;
+    const bool few = a.few.tokens > 0;
     const int32_t count = few ? a.few.tokens : *a.count;
     const bool single = a.reduction == GOCKPT_EACH;
     for (int32_t k = blockIdx.x * kTokens + threadIdx.x / kLanes; k < count; k += gridDim.x * kTokens) {
@@ -385,16 +450,12 @@ __global__ __launch_bounds__(kAlone ? kJoinWaves * 64 : 256) void join_kernel(Jo
     if constexpr (kAlone) {
         if (single || a.loss == nullptr) return;
         __threadfence_block();
-        int32_t kept = count;
-        if (few)
-            kept = __syncthreads_count(static_cast<int32_t>(threadIdx.x) < count && row_of(a.few, threadIdx.x) != kMasked);
-        else
-            __syncthreads();
-        sum_losses(a, count, kept);
+        __syncthreads();
+        sum_losses(a);
     }
 }
 
-__global__ __launch_bounds__(kJoinWaves * 64) void sum_kernel(JoinArgs a) { sum_losses(a, *a.count, *a.count); }
+__global__ __launch_bounds__(kJoinWaves * 64) void sum_kernel(JoinArgs a) { sum_losses(a); }
 
 // ---- the gradients ------------------------------------------------------------------
 
@@ -641,7 +702,7 @@ GradPlan plan_grad(const gockpt_head& h, bool by_hidden, bool by_table) {
     p.full = plan_piece(n, std::min(p.piece, rows), cols, by_hidden, by_table, most_hidden);
     p.rest = rest > 0 ? plan_piece(n, rest, cols, by_hidden, by_table, p.full.by_hidden.splits) : p.full;
     p.z_stride = up(p.piece, 64) * 2;
-    p.count = parts.take(4);
+    p.count = parts.take(8);
     p.unscale = parts.take(4);
     p.of_kept = parts.take(n * 4);
     p.target = parts.take(n * 4);
@@ -736,9 +797,7 @@ int gockpt_head_loss(const gockpt_head* head, int reduction, float* loss, float*
     t.loss = loss;
     LossArgs g{};
     JoinArgs j{};
-    // So few tokens are not numbered: the streaming kernel takes them all, a launch
-    // less (one token of 4096 columns, 32000 classes: 50.3 us, numbered 53.7).
-    const bool few = p.logits.shape == kThin && p.logits.tiles_r > 0 && p.logits.tiles_c > 0;
+    const bool few = t.tokens <= kFew && p.logits.tiles_r > 0 && p.logits.tiles_c > 0;
     if (few)
         g.few = j.few = t;
     else
@@ -783,7 +842,7 @@ int gockpt_head_loss(const gockpt_head* head, int reduction, float* loss, float*
     j.loss = loss;
     j.each = reinterpret_cast<float*>(ws + p.each);
     const bool narrow = g.a.tiles_r <= kJoinFew;
-    if (t.tokens <= kJoinAlone) {
+    if (t.tokens <= (narrow ? kJoinAloneNarrow : kJoinAlone)) {
         hipLaunchKernelGGL((narrow ? join_kernel<true, 16> : join_kernel<true, 64>), dim3(1), dim3(kJoinWaves * 64), 0, s, j);
     } else {
         const int tokens = narrow ? 16 : 4;
@@ -844,11 +903,22 @@ int gockpt_head_grad(const gockpt_head* head, const float* lse, int reduction, c
     t.base = reinterpret_cast<float*>(ws + p.base);
     t.factor = reinterpret_cast<float*>(ws + p.factor);
     t.unscale = reinterpret_cast<float*>(ws + p.unscale);
-    hipLaunchKernelGGL(token_kernel, dim3(1), dim3(kTokenThreads), 0, s, t);
-    if (t.seen != nullptr && t.tokens > kSeenAlone)
-        for (int stage = 0; stage <= kSeen; ++stage)
-            hipLaunchKernelGGL(seen_kernel, dim3((t.tokens + 255) / 256), dim3(256), 0, s, t, stage);
-    launch_rows(head->hidden, t.of_kept, t.count, t.tokens, ws + p.hidden, s);
+    const bool few = t.tokens > 0 && t.tokens <= kFew;
+    // dX goes where it belongs at once: c is the token, and there is one sum
+    const bool direct = few && by_hidden && rows > 0 && p.piece >= rows && p.full.by_hidden.splits == 1 &&
+                        p.full.by_hidden.shape != kWide;
+    if (few) {
+        const int64_t pieces = (cols + 7) / 8 * t.tokens;
+        hipLaunchKernelGGL(few_kernel, dim3(std::min<int64_t>((pieces + kFew - 1) / kFew, kUnits * 8)), dim3(kFew), 0, s,
+                           t, static_cast<const uint8_t*>(head->hidden.data), head->hidden.stride * 2,
+                           static_cast<int32_t>(cols), ws + p.hidden);
+    } else {
+        hipLaunchKernelGGL(token_kernel, dim3(1), dim3(kTokenThreads), 0, s, t);
+        if (t.seen != nullptr && t.tokens > kSeenAlone)
+            for (int stage = 0; stage <= kSeen; ++stage)
+                hipLaunchKernelGGL(seen_kernel, dim3((t.tokens + 255) / 256), dim3(256), 0, s, t, stage);
+        launch_rows(head->hidden, t.of_kept, t.count, t.tokens, ws + p.hidden, s);
+    }
     const Source table = source_of(head->table, ws + p.table, s);
     const int64_t hidden_stride = up(cols, 8) * 2;
     const int dtype = head->table.dtype;
@@ -891,8 +961,18 @@ int gockpt_head_grad(const gockpt_head* head, const float* lse, int reduction, c
             a.cn_dev = t.count;
             a.k = static_cast<int32_t>(here);
             StoreArgs o{};
-            o.slices = slices;
-            o.add = first > 0;
+            if (direct) {
+                o.out = static_cast<uint8_t*>(const_cast<void*>(grad_hidden->data));
+                o.stride = (t.tokens > 1 ? grad_hidden->stride : cols) * dtype_bytes(grad_hidden->dtype);
+                o.dtype = grad_hidden->dtype;
+                o.alpha = head->scale;
+                o.beta = t.unscale;
+                o.owner = t.target;
+                o.fix = reinterpret_cast<const float*>(ws + p.lost);
+            } else {
+                o.slices = slices;
+                o.add = first > 0;
+            }
             launch_product(kAcrossAlong, dtype, plan.by_hidden, a, o, s);
         }
         if (by_table) {
@@ -904,7 +984,7 @@ int gockpt_head_grad(const gockpt_head* head, const float* lse, int reduction, c
             a.rn = static_cast<int32_t>(cols);
             a.cn = static_cast<int32_t>(here);
             a.k = t.tokens;
-            a.k_dev = t.count;
+            a.k_dev = few ? t.count + 1 : t.count;
             const int64_t stride = (rows > 1 ? grad_table->stride : cols) * dtype_bytes(grad_table->dtype);
             FinishArgs f{};
             f.out = static_cast<uint8_t*>(const_cast<void*>(grad_table->data)) + first * stride;
@@ -939,7 +1019,7 @@ int gockpt_head_grad(const gockpt_head* head, const float* lse, int reduction, c
             }
         }
     }
-    if (by_hidden) {
+    if (by_hidden && !direct) {
         FinishArgs f{};
         f.slices = slices;
         f.slice_step = int64_t{t.tokens} * cols;

@@ -236,6 +236,8 @@ template <int kT_, int kRLay, int kCLay, int kBR_, int kBC_, int kWR_, int kWC_>
 struct Mma {
     static constexpr int kT = kT_, kBR = kBR_, kBC = kBC_, kWR = kWR_, kWC = kWC_;
     static constexpr bool kBothAcross = kRLay == kAcrossK && kCLay == kAcrossK;
+    // whether StoreArgs' corrections are made; C along k, the widest tiles have no registers for it
+    static constexpr bool kFixes = kBothAcross || (kRLay == kAcrossK && kBR < 256);
     static constexpr int kWaves = kWR * kWC, kThreads = kWaves * 64;
     static constexpr int kFR = kBR / kWR / 16, kFC = kBC / kWC / 16;  // fragments of a wave
     static constexpr int kRBytes = kBR * kStepK * 2, kCBytes = kBC * kStepK * 2;
@@ -432,7 +434,7 @@ struct Stream {
     static constexpr int kTile = 32 * kStepK * 2;
     static constexpr int kRBytes = kWaves * kTile, kCBytes = kWaves * kTile;
     static constexpr bool kOneWave = true;  // the first wavefront has the sum
-    static constexpr bool kBothAcross = false;
+    static constexpr bool kFixes = false;
     using Acc = f32x4[2][2];
 
     struct State {
@@ -585,9 +587,12 @@ struct StoreArgs {
     const float* beta;  // and one on the device (null: 1)
     float* slices;      // not null: fp32 sums instead, slice s at s * cn * rn, unscaled;
     int32_t add;        // added to what is there
-    // not null: fix[k] R(r, k) is added to c's sum, for the k that `seen` names for c
-    // (entry u of c at seen[u * seen_step + first + c], kSeen of them) and whose
-    // owner[k] is first + c; other entries may hold anything.  R lies across k.
+    // Corrections of single terms; R lies across k.  C too, and `seen` not null: fix[k]
+    // R(r, k) is added to c's sum, for the k that `seen` names for c (entry u of c at
+    // seen[u * seen_step + first + c], kSeen of them) and whose owner[k] is first + c;
+    // other entries may hold anything.  C along k, `owner` not null and the tile not
+    // kWide: fix[c] R(r, k) is, with k = owner[c]; of -1 nothing is added, below that
+    // the sum is 0.
     const int32_t* seen;
     int64_t seen_step;
     const int32_t* owner;
@@ -596,29 +601,58 @@ struct StoreArgs {
 };
 constexpr int kSeen = 2;
 
+// In steps over all of a lane's terms, as each step waits for memory: one term after
+// another took 13 us a tile.
 template <class M>
 __device__ __forceinline__ void add_fixes(const MmaArgs& a, const StoreArgs& o, const MmaPlace& p, int cn, int k_all,
                                           typename M::Acc& acc) {
+    constexpr int kTerms = M::kBothAcross ? kSeen : 1;
+    int k[M::kFC][kTerms];
+    float x[M::kFC][kTerms];
 #pragma unroll
     for (int j = 0; j < M::kFC; ++j) {
-        const int c = M::c_of(p, j);
+        const int c = min(M::c_of(p, j), cn - 1);
 #pragma unroll
-        for (int u = 0; u < kSeen; ++u) {
-            const int k = c < cn ? o.seen[u * o.seen_step + o.first + c] : -1;
-            const bool there = k >= 0 && k < k_all && o.owner[k] == o.first + c;
-            if (!__any(there)) continue;
-            const float x = there ? o.fix[k] : 0.0f;
-            const uint8_t* row = a.r + (there ? k : 0) * a.r_stride;
+        for (int u = 0; u < kTerms; ++u)
+            k[j][u] = M::kBothAcross ? o.seen[u * o.seen_step + o.first + c] : o.owner[c];
+    }
+#pragma unroll
+    for (int j = 0; j < M::kFC; ++j) {
+        const int c = min(M::c_of(p, j), cn - 1);
+#pragma unroll
+        for (int u = 0; u < kTerms; ++u) {
+            const bool there = static_cast<uint32_t>(k[j][u]) < static_cast<uint32_t>(k_all);
+            const int of = there ? k[j][u] : 0;
+            x[j][u] = o.fix[M::kBothAcross ? of : c];
+            if (M::kBothAcross ? o.owner[of] != o.first + c || !there : k[j][u] == -1) k[j][u] = -1;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < M::kFC; ++j) {
+        bool some = false;
+#pragma unroll
+        for (int u = 0; u < kTerms; ++u) some = some || k[j][u] != -1;
+        if (!__any(some)) continue;
+        u32x2 w[kTerms][M::kFR];
+#pragma unroll
+        for (int u = 0; u < kTerms; ++u)
 #pragma unroll
             for (int i = 0; i < M::kFR; ++i) {
                 const int r = M::r_of(p, i);
-                if (!there || r >= a.rn) continue;
-                const u32x2 w = *reinterpret_cast<const u32x2*>(row + r * 2);
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    acc[i][j][e] += x * elem_to_f32<M::kT>(w[e / 2] >> (16 * (e & 1)) & 0xffff);
+                w[u][i] = u32x2{0, 0};
+                if (k[j][u] >= 0 && r < a.rn)
+                    w[u][i] = *reinterpret_cast<const u32x2*>(a.r + k[j][u] * a.r_stride + r * 2);
             }
-        }
+#pragma unroll
+        for (int u = 0; u < kTerms; ++u)
+#pragma unroll
+            for (int i = 0; i < M::kFR; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float add = x[j][u] * elem_to_f32<M::kT>(w[u][i][e / 2] >> (16 * (e & 1)) & 0xffff);
+                    // x of what is not there may be anything
+                    acc[i][j][e] = k[j][u] < -1 ? 0.0f : k[j][u] >= 0 ? acc[i][j][e] + add : acc[i][j][e];
+                }
     }
 }
 
@@ -643,6 +677,19 @@ __device__ __forceinline__ void add8(uint8_t* p, const float (&x)[8], int n) {
         for (int i = 0; i < 7; ++i)
             if (i < n) q[i] = static_cast<uint16_t>(pack2<kT>(elem_to_f32<kT>(q[i]) + x[i], 0.0f));
     }
+}
+
+// The n > 0 values of 16 bits at p, of which 8 are taken; zeros behind them.
+__device__ __forceinline__ u32x4 load8(const uint8_t* p, int n) {
+    u32x4 w = {0, 0, 0, 0};
+    if (n >= 8) {
+        w = *reinterpret_cast<const u32x4_any*>(p);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 7; ++i)
+            if (i < n) w[i / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(p)[i]) << (16 * (i & 1));
+    }
+    return w;
 }
 
 // Four values along r.  x is rounded once; with accumulate the sum is.

@@ -17,8 +17,8 @@ __global__ __launch_bounds__(M::kThreads) void product_kernel(MmaArgs a, StoreAr
     const int k = a.k_dev != nullptr ? *a.k_dev : a.k;
     typename M::Acc acc;
     GOCKPT_MMA_RUN(M, a, p, cn, k, acc);
-    if constexpr (M::kBothAcross)
-        if (o.seen != nullptr && p.split == 0) add_fixes<M>(a, o, p, cn, k, acc);
+    if constexpr (M::kFixes)
+        if ((M::kBothAcross ? o.seen : o.owner) != nullptr && p.split == 0) add_fixes<M>(a, o, p, cn, k, acc);
     M::sync();
     store_tile<M>(GOCKPT_MMA_STORE(M), a, o, p, cn, acc);
 }
@@ -97,16 +97,7 @@ __global__ __launch_bounds__(256) void rows_kernel(const uint8_t* src, int64_t s
         const int col = static_cast<int>(at - row * groups) * 8;
         const int64_t from = rows != nullptr ? rows[row] : row;
         const uint8_t* p = src + from * stride + static_cast<int64_t>(col) * 2;
-        u32x4 w = {0, 0, 0, 0};
-        if (col + 8 <= cols) {
-            w = *reinterpret_cast<const u32x4_any*>(p);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 7; ++i)
-                if (col + i < cols)
-                    w[i / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(p)[i]) << (16 * (i & 1));
-        }
-        *reinterpret_cast<u32x4*>(dst + at * 16) = w;
+        *reinterpret_cast<u32x4*>(dst + at * 16) = load8(p, cols - col);
     }
 }
 

@@ -710,6 +710,26 @@ def test_head_loss_scales(scale):
         head_check(hidden.bfloat16(), table.bfloat16(), targets, reduction="mean", up=scale)
 
 
+@pytest.mark.parametrize("vocab", [300, 40000])
+@pytest.mark.parametrize("tokens", [1, 20, 129, 256, 257])
+def test_head_masked_tokens_of_a_table_with_nan(tokens, vocab):
+    """Their loss and gradient are 0 and they add nothing, whatever the table and their rows hold."""
+    hidden, table, targets = head_inputs(tokens, vocab, 40, "bf16")
+    table[7, 3], table[250] = float("nan"), float("inf")
+    hidden[::2] = float("nan")
+    targets[::2] = -1
+    for y in (targets, torch.full_like(targets, -1)):
+        x, w = hidden.detach().requires_grad_(), table.detach().requires_grad_()
+        loss = g.linear_cross_entropy(x, w, y, reduction="none")
+        loss.backward(torch.ones_like(loss))
+        masked = y < 0
+        assert bool((loss[masked] == 0).all()) and bool((x.grad[masked] == 0).all())
+        assert bool(loss[~masked].isnan().all()) and bool(x.grad[~masked].isnan().all())
+        if bool(masked.all()):
+            assert bool((w.grad == 0).all())
+            assert float(g.linear_cross_entropy(x, w, y)) == 0.0
+
+
 def test_head_scale_of_nothing():
     """All logits 0, whatever the products are."""
     hidden, table, targets = head_inputs(70, 301, 40, "bf16")
