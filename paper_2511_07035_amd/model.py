@@ -101,6 +101,17 @@ def _differentiable(stream, a, b=None) -> bool:
     return True
 
 
+def _once(backward):
+    """once_differentiable, whose 5 us are spent only where a graph of the backward
+    is asked for."""
+    guarded = torch.autograd.function.once_differentiable(backward)
+
+    @functools.wraps(backward)
+    def wrapped(ctx, *grads):
+        return (guarded if torch.is_grad_enabled() else backward)(ctx, *grads)
+    return wrapped
+
+
 def _own_rows(t, cols: int, stream):
     """t, or a copy, made on the call's stream, where its rows do not lie at one
     distance, or overlap (an expanded or transposed gradient)."""
@@ -211,7 +222,6 @@ def head_grad(hidden, table, targets, lse, grad, *, scale: float = 1.0, first_id
         raise ValueError("accumulate: into a grad_weight")
     hidden, table = _own_rows(hidden.detach(), table.shape[-1], stream), table.detach()
     device, head = _head(hidden, table, targets, scale, first_id, ignore_id, classes or 0)
-    dim = table.shape[1]
     n = 1 if r != GOCKPT_EACH else targets.numel()
     for t, size, what in ((lse, targets.numel(), "lse"), (grad, n, "grad")):
         _here(t, what, device)
@@ -225,13 +235,18 @@ def head_grad(hidden, table, targets, lse, grad, *, scale: float = 1.0, first_id
         raise ValueError(f"grad_hidden of shape {tuple(grad_hidden.shape)} for hidden of shape {tuple(hidden.shape)}")
     if grad_weight is not None and grad_weight.shape != table.shape:
         raise ValueError(f"grad_weight of shape {tuple(grad_weight.shape)} for a table of shape {tuple(table.shape)}")
-    gx = None if grad_hidden is None else _matrix(grad_hidden, "grad_hidden", device, dim)
-    gw = None if grad_weight is None else _matrix(grad_weight, "grad_weight", device)
-    ws, ptr, size = _workspace(table, "gockpt_head_grad_bytes", (head, gx, gw), stream)
-    _check(_lib().gockpt_head_grad(head, lse.data_ptr(), r, grad.data_ptr(), gx, gw, accumulate, ptr, size,
-                                   _stream(stream, device)), "gockpt_head_grad", None)
+    _head_grad(device, head, table, lse, grad, r, grad_hidden, grad_weight, accumulate, stream)
     _changed(tuple(t for t in (grad_hidden, grad_weight) if t is not None))
     return grad_hidden, grad_weight
+
+
+def _head_grad(device: int, head: bytes, table, lse, grad, reduction: int, grad_hidden, grad_weight, accumulate: bool,
+               stream) -> None:
+    gx = None if grad_hidden is None else _matrix(grad_hidden, "grad_hidden", device, table.shape[1])
+    gw = None if grad_weight is None else _matrix(grad_weight, "grad_weight", device)
+    ws, ptr, size = _workspace(table, "gockpt_head_grad_bytes", (head, gx, gw), stream)
+    _check(_lib().gockpt_head_grad(head, lse.data_ptr(), reduction, grad.data_ptr(), gx, gw, accumulate, ptr, size,
+                                   _stream(stream, device)), "gockpt_head_grad", None)
 
 
 class _LinearCrossEntropy(torch.autograd.Function):
@@ -243,18 +258,20 @@ class _LinearCrossEntropy(torch.autograd.Function):
         return loss
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once
     def backward(ctx, grad):
         hidden, table, targets, lse = ctx.saved_tensors
-        scale, first_id, ignore_id, _ = ctx.args
-        into = None
+        hidden = _own_rows(hidden, table.shape[1], None)
+        device, head = _head(hidden, table, targets, *ctx.args)
+        gx, gw = _empty(hidden, hidden.shape, hidden.dtype, None) if ctx.needs_input_grad[0] else None, None
         if ctx.needs_input_grad[1]:
-            into = torch.empty_like(table, memory_format=torch.contiguous_format) if ctx.into is None else ctx.into
-        gx, _ = head_grad(hidden, table, targets, lse, grad.contiguous(), scale=scale, first_id=first_id,
-                          ignore_id=ignore_id, reduction=("none", "sum", "mean")[ctx.reduction],
-                          grad_hidden=ctx.needs_input_grad[0], grad_weight=into,
-                          accumulate=ctx.accumulate and into is not None)
-        return (gx, into if ctx.into is None else None) + (None,) * 5
+            gw = _empty(table, table.shape, table.dtype, None) if ctx.into is None else ctx.into
+        _head_grad(device, head, table, lse, grad.contiguous(), ctx.reduction, gx, gw,
+                   ctx.accumulate and gw is not None, None)
+        if gw is ctx.into and gw is not None:
+            _changed((gw,))
+            gw = None
+        return gx, gw, None, None, None, None, None
 
 
 # ---- activations in 8 bits -----------------------------------------------------------
@@ -409,7 +426,7 @@ class _Linear8(torch.autograd.Function):
         return out
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once
     def backward(ctx, grad_out):
         weight, _ = ctx.saved_tensors
         gx = gw = None
@@ -474,7 +491,7 @@ class _Gate8(torch.autograd.Function):
         return out
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once
     def backward(ctx, grad_out):
         ctx.saved_tensors  # raises where the graph's buffers have been freed
         device = _here(grad_out, "grad_out")
