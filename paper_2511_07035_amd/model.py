@@ -301,8 +301,7 @@ class Act8:
         else:
             with torch.cuda.stream(stream):
                 self.buffer = torch.empty(n * (GOCKPT_ACT8_BLOCK + 1), dtype=torch.uint8, device=device)
-        at = self.buffer.data_ptr()
-        self.packed = ACT8.pack(at, at + n * GOCKPT_ACT8_BLOCK, rows, cols)
+        self.packed = self._at(self.buffer)
 
     @property
     def codes(self):
@@ -315,11 +314,21 @@ class Act8:
 
     @property
     def nbytes(self) -> int:
-        return self.buffer.numel()
+        return self.rows * self.blocks * (GOCKPT_ACT8_BLOCK + 1)
+
+    def _at(self, buffer) -> bytes:
+        at = buffer.data_ptr()
+        return ACT8.pack(at, at + self.rows * self.blocks * GOCKPT_ACT8_BLOCK, self.rows, self.cols)
 
     def _pack(self, device: int) -> bytes:
         _here(self.buffer, "Act8", device)
         return self.packed
+
+    def _leave(self):
+        """The buffer, for a graph to save: what is left describes it wherever the
+        graph has it, and holds no memory when the graph has let it go."""
+        buffer, self.buffer = self.buffer, None
+        return buffer
 
     def unpack(self, *, out=None, dtype=None, stream=None):
         """What it stands for, in dtype (default: the packed tensor's), or in out."""
@@ -379,7 +388,7 @@ def _linear8_grad(grad_out, weight, kept, grad_x, grad_weight, accumulate, strea
     rows = grad_out.shape[-1]
     grad_out = _own_rows(grad_out, rows, stream)
     args = (_matrix(grad_out, "grad_out", None, rows), None if weight is None else _matrix(weight, "weight", device),
-            None if kept is None else kept._pack(device),
+            kept,
             None if grad_x is None else _matrix(grad_x, "grad_x", device, grad_x.shape[-1]),
             None if grad_weight is None else _matrix(grad_weight, "grad_weight", device))
     ws, ptr, size = _workspace(grad_out, "gockpt_linear8_grad_bytes", args, stream)
@@ -410,7 +419,8 @@ def linear8_grad_weight(grad_out, kept: Act8, grad_weight, *, accumulate: bool =
     if grad_weight.shape != (grad_out.shape[-1], kept.cols):
         raise ValueError(f"grad_weight of shape {tuple(grad_weight.shape)}, expected "
                          f"{(grad_out.shape[-1], kept.cols)}")
-    _linear8_grad(grad_out.detach(), None, kept, None, grad_weight, accumulate, stream)
+    _linear8_grad(grad_out.detach(), None, kept._pack(_here(grad_out, "grad_out")), None, grad_weight, accumulate,
+                  stream)
     return grad_weight
 
 
@@ -419,7 +429,7 @@ class _Linear8(torch.autograd.Function):
     def forward(ctx, x, weight, grad_weight, accumulate):
         out, kept = _linear8(x, weight, ctx.needs_input_grad[1], None)
         # the weight is read again for x's gradient alone
-        ctx.save_for_backward(weight if ctx.needs_input_grad[0] else None, None if kept is None else kept.buffer)
+        ctx.save_for_backward(weight if ctx.needs_input_grad[0] else None, None if kept is None else kept._leave())
         ctx.kept, ctx.into, ctx.accumulate = kept, grad_weight, accumulate
         ctx.x = (x.shape, x.dtype)
         ctx.weight = (weight.shape, weight.dtype)
@@ -428,7 +438,7 @@ class _Linear8(torch.autograd.Function):
     @staticmethod
     @_once
     def backward(ctx, grad_out):
-        weight, _ = ctx.saved_tensors
+        weight, buffer = ctx.saved_tensors
         gx = gw = None
         if ctx.needs_input_grad[0]:
             gx = torch.empty(ctx.x[0], dtype=ctx.x[1], device=grad_out.device)
@@ -436,7 +446,8 @@ class _Linear8(torch.autograd.Function):
             gw = ctx.into
             if gw is None:
                 gw = torch.empty(ctx.weight[0], dtype=ctx.weight[1], device=grad_out.device)
-        _linear8_grad(grad_out, weight, ctx.kept, gx, gw, ctx.accumulate and ctx.into is not None, None)
+        _linear8_grad(grad_out, weight, None if buffer is None else ctx.kept._at(buffer), gx, gw,
+                      ctx.accumulate and ctx.into is not None, None)
         return gx, gw if ctx.into is None else None, None, None
 
 
@@ -486,21 +497,21 @@ class _Gate8(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, factor, kind):
         out, kept = _gate8(x, factor, kind, True, None)
-        ctx.save_for_backward(*(None if k is None else k.buffer for k in kept))
+        ctx.save_for_backward(*(None if k is None else k._leave() for k in kept))
         ctx.kept, ctx.kind = kept, kind
         return out
 
     @staticmethod
     @_once
     def backward(ctx, grad_out):
-        ctx.saved_tensors  # raises where the graph's buffers have been freed
+        buffers = ctx.saved_tensors
         device = _here(grad_out, "grad_out")
         cols = grad_out.shape[-1]
         grad_out = _own_rows(grad_out, cols, None)
         grads = [torch.empty(grad_out.shape, dtype=grad_out.dtype, device=grad_out.device) if needed else None
                  for needed in ctx.needs_input_grad[:2]]
         _check(_lib().gockpt_gate8_grad(ctx.kind, _matrix(grad_out, "grad_out", None, cols),
-                                        *(None if k is None else k._pack(device) for k in ctx.kept),
+                                        *(None if k is None else k._at(b) for k, b in zip(ctx.kept, buffers)),
                                         *(None if g is None else _matrix(g, "", None, cols) for g in grads),
                                         _stream(None, device)), "gockpt_gate8_grad", None)
         return grads[0], grads[1], None

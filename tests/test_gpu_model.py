@@ -359,6 +359,35 @@ def test_linear8_keeps_little_and_only_what_it_needs():
         y.backward(torch.ones_like(y))
 
 
+def test_graphs_let_go_of_what_they_keep():
+    """A result that lives on after the backward holds none of the 8-bit copies, and hooks may move them."""
+    x, w = randn((512, 1024), torch.bfloat16, 1).requires_grad_(), randn((256, 1024), torch.bfloat16, 2).requires_grad_()
+    f = randn((512, 256), torch.bfloat16, 3).requires_grad_()
+
+    def run():
+        x.grad = w.grad = f.grad = None
+        return g.gate8(g.linear8(x, w), f)
+    y = run()
+    y.backward(f.detach())
+    want = x.grad.clone(), w.grad.clone(), f.grad.clone()
+    del y
+    x.grad = w.grad = f.grad = None
+    before = torch.cuda.memory_allocated()
+    y = run()
+    held = torch.cuda.memory_allocated() - before
+    assert held >= 33 * (512 * 1024 + 2 * 512 * 256) // 32
+    y.backward(f.detach())
+    held = torch.cuda.memory_allocated() - before - 2 * (x.numel() + w.numel() + f.numel())
+    assert held <= 2 * y.numel() + 3 * 512, held  # y itself
+    with pytest.raises(RuntimeError):
+        y.backward(f.detach())
+    with torch.autograd.graph.save_on_cpu():
+        y = run()
+    y.backward(f.detach())
+    for got, one in zip((x.grad, w.grad, f.grad), want):
+        assert torch.equal(got, one)
+
+
 def test_linear8_of_infinities():
     x = randn((40, 96), torch.bfloat16, 1)
     x[3, 70] = float("inf")
