@@ -218,13 +218,13 @@ constexpr int32_t kFew = 256;
 // dW.  The first block also has the tokens' numbers; count[0] is all of them,
 // count[1] as well unless none counts.
 __global__ __launch_bounds__(kFew) void few_kernel(TokenArgs a, const uint8_t* hidden, int64_t stride, int32_t cols,
-                                                   uint8_t* dst) {
+                                                   uint8_t* dst, int64_t dst_stride) {
     const int32_t groups = (cols + 7) / 8;
     for (int32_t at = blockIdx.x * kFew + threadIdx.x; at < groups * a.tokens; at += gridDim.x * kFew) {
         const int32_t t = at / groups, col = (at - t * groups) * 8;
         u32x4 w = {0, 0, 0, 0};
         if (row_of(a, t) != kMasked) w = load8(hidden + t * stride + int64_t{col} * 2, cols - col);
-        *reinterpret_cast<u32x4*>(dst + int64_t{at} * 16) = w;
+        *reinterpret_cast<u32x4*>(dst + t * dst_stride + col * 2) = w;
     }
     if (blockIdx.x != 0) return;
     __shared__ float largest[kFew / 64];
@@ -645,7 +645,7 @@ LossPlan plan_loss(const gockpt_head& h) {
     p.part = parts.take(n * p.logits.tiles_r * 8);
     p.logit2 = parts.take(n * 4);
     p.each = parts.take(n * 4);
-    p.hidden = parts.take(hidden_in_place(h.hidden) ? 0 : n * up(h.hidden.cols, 8) * 2);
+    p.hidden = parts.take(hidden_in_place(h.hidden) ? 0 : n * copy_stride(h.hidden.cols) * 2);
     p.table = parts.take(copy_bytes(h.table));
     p.bytes = parts.bytes;
     return p;
@@ -711,7 +711,7 @@ GradPlan plan_grad(const gockpt_head& h, bool by_hidden, bool by_table) {
     p.factor = parts.take(n * 4);
     p.lost = parts.take(n * 4);
     if (by_table) p.seen = parts.take(kSeen * rows * 4);
-    p.hidden = parts.take(n * up(cols, 8) * 2);
+    p.hidden = parts.take(n * copy_stride(cols) * 2);
     p.table = parts.take(copy_bytes(h.table));
     p.z = parts.take(n * p.z_stride);
     if (by_hidden) p.slices_hidden = parts.take(p.full.by_hidden.splits * n * cols * 4);
@@ -813,7 +813,7 @@ int gockpt_head_loss(const gockpt_head* head, int reduction, float* loss, float*
         launch_rows(head->hidden, few ? nullptr : t.of_kept, few ? nullptr : t.count, head->hidden.rows, ws + p.hidden,
                     s);
         g.a.c = ws + p.hidden;
-        g.a.c_stride = up(head->hidden.cols, 8) * 2;
+        g.a.c_stride = copy_stride(head->hidden.cols) * 2;
     }
     g.a.rn = t.rows;
     g.a.cn = t.tokens;
@@ -903,6 +903,7 @@ int gockpt_head_grad(const gockpt_head* head, const float* lse, int reduction, c
     t.base = reinterpret_cast<float*>(ws + p.base);
     t.factor = reinterpret_cast<float*>(ws + p.factor);
     t.unscale = reinterpret_cast<float*>(ws + p.unscale);
+    const int64_t hidden_stride = copy_stride(cols) * 2;
     const bool few = t.tokens > 0 && t.tokens <= kFew;
     // dX goes where it belongs at once: c is the token, and there is one sum
     const bool direct = few && by_hidden && rows > 0 && p.piece >= rows && p.full.by_hidden.splits == 1 &&
@@ -911,7 +912,7 @@ int gockpt_head_grad(const gockpt_head* head, const float* lse, int reduction, c
         const int64_t pieces = (cols + 7) / 8 * t.tokens;
         hipLaunchKernelGGL(few_kernel, dim3(std::min<int64_t>((pieces + kFew - 1) / kFew, kUnits * 8)), dim3(kFew), 0, s,
                            t, static_cast<const uint8_t*>(head->hidden.data), head->hidden.stride * 2,
-                           static_cast<int32_t>(cols), ws + p.hidden);
+                           static_cast<int32_t>(cols), ws + p.hidden, hidden_stride);
     } else {
         hipLaunchKernelGGL(token_kernel, dim3(1), dim3(kTokenThreads), 0, s, t);
         if (t.seen != nullptr && t.tokens > kSeenAlone)
@@ -920,7 +921,6 @@ int gockpt_head_grad(const gockpt_head* head, const float* lse, int reduction, c
         launch_rows(head->hidden, t.of_kept, t.count, t.tokens, ws + p.hidden, s);
     }
     const Source table = source_of(head->table, ws + p.table, s);
-    const int64_t hidden_stride = up(cols, 8) * 2;
     const int dtype = head->table.dtype;
     float* slices = reinterpret_cast<float*>(ws + p.slices_hidden);
     for (int64_t first = 0; first < rows; first += p.piece) {

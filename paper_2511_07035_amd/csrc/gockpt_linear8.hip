@@ -84,7 +84,7 @@ BackwardPlan plan_backward(const gockpt_matrix& g, const gockpt_matrix* w, const
     }
     if (by_weight) {
         p.by_weight = plan_product(kAcrossAcross, keep->cols, g.cols, g.rows, kMostSplits);
-        p.input = parts.take(g.rows * up(keep->cols, 8) * 2);
+        p.input = parts.take(g.rows * copy_stride(keep->cols) * 2);
         p.slices_weight = parts.take(slice_bytes(p.by_weight, keep->cols, g.cols));
     }
     p.bytes = parts.bytes;
@@ -234,7 +234,7 @@ int gockpt_linear8_grad(const gockpt_matrix* grad_out, const gockpt_matrix* weig
         product_into(kAcrossAlong, grad_out->dtype, p.by_x, a, *grad_x, 0, ws + p.slices_x, s);
     }
     if (by_weight) {
-        const gockpt_matrix input{ws + p.input, keep->rows, keep->cols, up(keep->cols, 8), grad_out->dtype, 0};
+        const gockpt_matrix input{ws + p.input, keep->rows, keep->cols, copy_stride(keep->cols), grad_out->dtype, 0};
         rc = gockpt_act8_unpack(keep, &input, stream);
         if (rc != GOCKPT_OK) return rc;
         MmaArgs a{};

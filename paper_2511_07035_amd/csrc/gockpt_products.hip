@@ -86,10 +86,10 @@ __global__ __launch_bounds__(256) void finish_kernel(FinishArgs f) {
 // ---- copies ---------------------------------------------------------------------
 
 // 8 columns a thread: rows that start anywhere become rows of whole 16-byte
-// pieces.  An index past the source's columns is never read.
+// pieces, copy_stride apart.  An index past the source's columns is never read.
 __global__ __launch_bounds__(256) void rows_kernel(const uint8_t* src, int64_t stride, int32_t cols,
                                                    const int32_t* rows, const int32_t* count, int32_t n,
-                                                   uint8_t* dst) {
+                                                   uint8_t* dst, int64_t dst_stride) {
     const int64_t groups = (cols + 7) / 8;
     const int64_t all = groups * (count != nullptr ? *count : n);
     for (int64_t at = blockIdx.x * int64_t{256} + threadIdx.x; at < all; at += gridDim.x * int64_t{256}) {
@@ -97,7 +97,7 @@ __global__ __launch_bounds__(256) void rows_kernel(const uint8_t* src, int64_t s
         const int col = static_cast<int>(at - row * groups) * 8;
         const int64_t from = rows != nullptr ? rows[row] : row;
         const uint8_t* p = src + from * stride + static_cast<int64_t>(col) * 2;
-        *reinterpret_cast<u32x4*>(dst + at * 16) = load8(p, cols - col);
+        *reinterpret_cast<u32x4*>(dst + row * dst_stride + col * 2) = load8(p, cols - col);
     }
 }
 
@@ -118,13 +118,13 @@ void launch_rows(const gockpt_matrix& src, const int32_t* rows, const int32_t* c
     if (items > 0)
         hipLaunchKernelGGL(rows_kernel, dim3(copy_grid(items)), dim3(256), 0, s,
                            static_cast<const uint8_t*>(src.data), src.stride * 2, static_cast<int32_t>(src.cols), rows,
-                           count, static_cast<int32_t>(n), dst);
+                           count, static_cast<int32_t>(n), dst, copy_stride(src.cols) * 2);
 }
 
 Source source_of(const gockpt_matrix& m, uint8_t* copy, hipStream_t s) {
     if (in_place(m)) return {static_cast<const uint8_t*>(m.data), (m.rows > 1 ? m.stride : m.cols) * 2};
     launch_rows(m, nullptr, nullptr, m.rows, copy, s);
-    return {copy, up(m.cols, 8) * 2};
+    return {copy, copy_stride(m.cols) * 2};
 }
 
 namespace {
