@@ -252,7 +252,7 @@ __device__ __forceinline__ void activate(float x, float& y, float& slope) {
 // ---- kernels ----------------------------------------------------------------------
 
 struct PackArgs {
-    Rows x;
+    Rows x, copy;  // copy: of 16-bit x (null: none), whole pieces of 8
     Kept kept;
     int64_t groups;  // of 8 columns, blocks' missing ones among them
     int32_t blocks, cols;
@@ -268,6 +268,9 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(PackArgs a) {
         u32x2 codes;
         const uint32_t scale = encode8<kT>(x, top, codes);
         keep8(a.kept, g, false, codes, scale);
+        if constexpr (kT != kFP32)
+            if (a.copy.p != nullptr && p.n > 0)
+                store8<kT>(a.copy.p + p.row * a.copy.stride + int64_t{p.col} * 2, kLaneCols, false, x);
     }
 }
 
@@ -411,6 +414,17 @@ int check_kind(const char* name, int kind) {
 
 }  // namespace
 
+int pack_and_copy(const char* name, const gockpt_matrix* x, const gockpt_act8* out, uint8_t* copy, hipStream_t s) {
+    int rc = check_model_matrix(name, "x", x, kAnyType);
+    if (rc == GOCKPT_OK) rc = check_act8(name, "out", out, x->rows, x->cols);
+    if (rc != GOCKPT_OK || x->rows == 0 || x->cols == 0) return rc;
+    PackArgs a{rows_of(x), Rows{copy, copy_stride(x->cols) * 2}, kept_of(out), x->rows * blocks_of(x->cols) * 4,
+               blocks_of(x->cols), static_cast<int32_t>(x->cols)};
+    auto kernel = x->dtype == kBF16 ? pack_kernel<kBF16> : x->dtype == kFP16 ? pack_kernel<kFP16> : pack_kernel<kFP32>;
+    hipLaunchKernelGGL(kernel, grid_of(a.groups), dim3(kThreads), 0, s, a);
+    return ops_launched(name);
+}
+
 }  // namespace gockpt
 
 using namespace gockpt;
@@ -418,15 +432,7 @@ using namespace gockpt;
 extern "C" {
 
 int gockpt_act8_pack(const gockpt_matrix* x, const gockpt_act8* out, void* stream) {
-    const char* name = "gockpt_act8_pack";
-    int rc = check_model_matrix(name, "x", x, kAnyType);
-    if (rc == GOCKPT_OK) rc = check_act8(name, "out", out, x->rows, x->cols);
-    if (rc != GOCKPT_OK || x->rows == 0 || x->cols == 0) return rc;
-    PackArgs a{rows_of(x), kept_of(out), x->rows * blocks_of(x->cols) * 4, blocks_of(x->cols),
-               static_cast<int32_t>(x->cols)};
-    auto kernel = x->dtype == kBF16 ? pack_kernel<kBF16> : x->dtype == kFP16 ? pack_kernel<kFP16> : pack_kernel<kFP32>;
-    hipLaunchKernelGGL(kernel, grid_of(a.groups), dim3(kThreads), 0, static_cast<hipStream_t>(stream), a);
-    return ops_launched(name);
+    return pack_and_copy("gockpt_act8_pack", x, out, nullptr, static_cast<hipStream_t>(stream));
 }
 
 int gockpt_act8_unpack(const gockpt_act8* x, const gockpt_matrix* out, void* stream) {
@@ -434,7 +440,7 @@ int gockpt_act8_unpack(const gockpt_act8* x, const gockpt_matrix* out, void* str
     int rc = check_model_matrix(name, "out", out, kAnyType);
     if (rc == GOCKPT_OK) rc = check_act8(name, "x", x, out->rows, out->cols);
     if (rc != GOCKPT_OK || out->rows == 0 || out->cols == 0) return rc;
-    PackArgs a{rows_of(out), kept_of(x), out->rows * blocks_of(out->cols) * 4, blocks_of(out->cols),
+    PackArgs a{rows_of(out), Rows{}, kept_of(x), out->rows * blocks_of(out->cols) * 4, blocks_of(out->cols),
                static_cast<int32_t>(out->cols)};
     auto kernel = out->dtype == kBF16 ? unpack_kernel<kBF16>
                                       : out->dtype == kFP16 ? unpack_kernel<kFP16> : unpack_kernel<kFP32>;

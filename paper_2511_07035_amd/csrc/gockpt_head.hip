@@ -802,7 +802,8 @@ int gockpt_head_loss(const gockpt_head* head, int reduction, float* loss, float*
         g.few = j.few = t;
     else
         hipLaunchKernelGGL(token_kernel, dim3(1), dim3(kTokenThreads), 0, s, t);
-    const Source table = source_of(head->table, ws + p.table, s);
+    Copies copies;
+    const Source table = copies.source_of(head->table, ws + p.table);
     g.a.r = table.data;
     g.a.r_stride = table.stride;
     if (hidden_in_place(head->hidden)) {
@@ -810,11 +811,12 @@ int gockpt_head_loss(const gockpt_head* head, int reduction, float* loss, float*
         g.a.c_stride = (head->hidden.rows > 1 ? head->hidden.stride : head->hidden.cols) * 2;
         g.a.c_rows = few ? nullptr : t.of_kept;
     } else {
-        launch_rows(head->hidden, few ? nullptr : t.of_kept, few ? nullptr : t.count, head->hidden.rows, ws + p.hidden,
-                    s);
-        g.a.c = ws + p.hidden;
-        g.a.c_stride = copy_stride(head->hidden.cols) * 2;
+        const Source hidden = copies.rows_of(head->hidden, few ? nullptr : t.of_kept, few ? nullptr : t.count,
+                                             head->hidden.rows, ws + p.hidden);
+        g.a.c = hidden.data;
+        g.a.c_stride = hidden.stride;
     }
+    copies.launch(s);
     g.a.rn = t.rows;
     g.a.cn = t.tokens;
     g.a.cn_dev = t.count;
@@ -908,6 +910,8 @@ int gockpt_head_grad(const gockpt_head* head, const float* lse, int reduction, c
     // dX goes where it belongs at once: c is the token, and there is one sum
     const bool direct = few && by_hidden && rows > 0 && p.piece >= rows && p.full.by_hidden.splits == 1 &&
                         p.full.by_hidden.shape != kWide;
+    Copies copies;
+    const Source table = copies.source_of(head->table, ws + p.table);
     if (few) {
         const int64_t pieces = (cols + 7) / 8 * t.tokens;
         hipLaunchKernelGGL(few_kernel, dim3(std::min<int64_t>((pieces + kFew - 1) / kFew, kUnits * 8)), dim3(kFew), 0, s,
@@ -918,9 +922,9 @@ int gockpt_head_grad(const gockpt_head* head, const float* lse, int reduction, c
         if (t.seen != nullptr && t.tokens > kSeenAlone)
             for (int stage = 0; stage <= kSeen; ++stage)
                 hipLaunchKernelGGL(seen_kernel, dim3((t.tokens + 255) / 256), dim3(256), 0, s, t, stage);
-        launch_rows(head->hidden, t.of_kept, t.count, t.tokens, ws + p.hidden, s);
+        copies.rows_of(head->hidden, t.of_kept, t.count, t.tokens, ws + p.hidden);
     }
-    const Source table = source_of(head->table, ws + p.table, s);
+    copies.launch(s);
     const int dtype = head->table.dtype;
     float* slices = reinterpret_cast<float*>(ws + p.slices_hidden);
     for (int64_t first = 0; first < rows; first += p.piece) {

@@ -171,13 +171,18 @@ int gockpt_linear8(const gockpt_matrix* x, const gockpt_matrix* weight, const go
     if (rc == GOCKPT_OK) rc = check_workspace(name, workspace, workspace_bytes, p.bytes);
     if (rc != GOCKPT_OK) return rc;
     hipStream_t s = static_cast<hipStream_t>(stream);
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    const bool needed = out->rows > 0 && out->cols > 0;
+    const bool with_keep = keep != nullptr && needed && !in_place(*x);
     if (keep != nullptr) {
-        rc = gockpt_act8_pack(x, keep, stream);
+        rc = pack_and_copy(name, x, keep, with_keep ? ws + p.x : nullptr, s);
         if (rc != GOCKPT_OK) return rc;
     }
-    if (out->rows == 0 || out->cols == 0) return GOCKPT_OK;
-    uint8_t* ws = static_cast<uint8_t*>(workspace);
-    const Source sx = source_of(*x, ws + p.x, s), sw = source_of(*weight, ws + p.weight, s);
+    if (!needed) return GOCKPT_OK;
+    Copies copies;
+    const Source sx = with_keep ? copied(*x, ws + p.x) : copies.source_of(*x, ws + p.x);
+    const Source sw = copies.source_of(*weight, ws + p.weight);
+    copies.launch(s);
     MmaArgs a{};
     a.r = sw.data;
     a.r_stride = sw.stride;
@@ -220,9 +225,11 @@ int gockpt_linear8_grad(const gockpt_matrix* grad_out, const gockpt_matrix* weig
     const bool by_x = grad_x != nullptr && grad_x->rows > 0 && grad_x->cols > 0;
     const bool by_weight = grad_weight != nullptr && grad_weight->rows > 0 && grad_weight->cols > 0;
     if (!by_x && !by_weight) return GOCKPT_OK;
-    const Source sg = source_of(*grad_out, ws + p.grad, s);
+    Copies copies;
+    const Source sg = copies.source_of(*grad_out, ws + p.grad);
+    const Source sw = by_x ? copies.source_of(*weight, ws + p.weight) : Source{};
+    copies.launch(s);
     if (by_x) {
-        const Source sw = source_of(*weight, ws + p.weight, s);
         MmaArgs a{};
         a.r = sw.data;
         a.r_stride = sw.stride;

@@ -53,12 +53,31 @@ struct Source {
     int64_t stride;  // bytes
 };
 inline int64_t copy_bytes(const gockpt_matrix& m) { return in_place(m) ? 0 : m.rows * copy_stride(m.cols) * 2; }
-Source source_of(const gockpt_matrix& m, uint8_t* copy, hipStream_t s);
+inline Source copied(const gockpt_matrix& m, uint8_t* copy) { return {copy, copy_stride(m.cols) * 2}; }
 
-// Row c of dst = row rows[c] of src (null: row c), for c < *count (null: n), as
-// above.
-void launch_rows(const gockpt_matrix& src, const int32_t* rows, const int32_t* count, int64_t n, uint8_t* dst,
-                 hipStream_t s);
+// The copies that a call needs, of at most two matrices, in one launch.
+struct Copies {
+    // Row c of dst = row rows[c] of src (null: row c), for c < *count (null: n).
+    struct One {
+        const uint8_t* src;
+        int64_t stride, dst_stride;
+        const int32_t *rows, *count;
+        uint8_t* dst;
+        int32_t cols, n;
+        uint32_t blocks;
+    } one[2] = {};
+    int many = 0;
+
+    Source source_of(const gockpt_matrix& m, uint8_t* copy) {
+        if (in_place(m)) return {static_cast<const uint8_t*>(m.data), (m.rows > 1 ? m.stride : m.cols) * 2};
+        return rows_of(m, nullptr, nullptr, m.rows, copy);
+    }
+    Source rows_of(const gockpt_matrix& src, const int32_t* rows, const int32_t* count, int64_t n, uint8_t* dst);
+    void launch(hipStream_t s) const;
+};
+
+// gockpt_act8_pack, and x copied as above with it (copy not null: 16-bit x).
+int pack_and_copy(const char* name, const gockpt_matrix* x, const gockpt_act8* out, uint8_t* copy, hipStream_t s);
 
 // The products by how their operands lie (R, C).
 enum ProductKind : int { kAlongAlong = 0, kAcrossAlong = 1, kAcrossAcross = 2 };

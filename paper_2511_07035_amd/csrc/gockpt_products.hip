@@ -87,17 +87,19 @@ __global__ __launch_bounds__(256) void finish_kernel(FinishArgs f) {
 
 // 8 columns a thread: rows that start anywhere become rows of whole 16-byte
 // pieces, copy_stride apart.  An index past the source's columns is never read.
-__global__ __launch_bounds__(256) void rows_kernel(const uint8_t* src, int64_t stride, int32_t cols,
-                                                   const int32_t* rows, const int32_t* count, int32_t n,
-                                                   uint8_t* dst, int64_t dst_stride) {
-    const int64_t groups = (cols + 7) / 8;
-    const int64_t all = groups * (count != nullptr ? *count : n);
-    for (int64_t at = blockIdx.x * int64_t{256} + threadIdx.x; at < all; at += gridDim.x * int64_t{256}) {
+// The first blocks have the first matrix.
+__global__ __launch_bounds__(256) void rows_kernel(Copies c) {
+    const bool second = blockIdx.x >= c.one[0].blocks;
+    const Copies::One& a = c.one[second];
+    const uint32_t block = blockIdx.x - (second ? c.one[0].blocks : 0);
+    const int64_t groups = (a.cols + 7) / 8;
+    const int64_t all = groups * (a.count != nullptr ? *a.count : a.n);
+    for (int64_t at = block * int64_t{256} + threadIdx.x; at < all; at += a.blocks * int64_t{256}) {
         const int64_t row = at / groups;
         const int col = static_cast<int>(at - row * groups) * 8;
-        const int64_t from = rows != nullptr ? rows[row] : row;
-        const uint8_t* p = src + from * stride + static_cast<int64_t>(col) * 2;
-        *reinterpret_cast<u32x4*>(dst + row * dst_stride + col * 2) = load8(p, cols - col);
+        const int64_t from = a.rows != nullptr ? a.rows[row] : row;
+        const uint8_t* p = a.src + from * a.stride + static_cast<int64_t>(col) * 2;
+        *reinterpret_cast<u32x4*>(a.dst + row * a.dst_stride + col * 2) = load8(p, a.cols - col);
     }
 }
 
@@ -112,19 +114,17 @@ void launch_finish(const FinishArgs& f, hipStream_t s) {
     if (items > 0) hipLaunchKernelGGL(finish_kernel, dim3(copy_grid(items)), dim3(256), 0, s, f);
 }
 
-void launch_rows(const gockpt_matrix& src, const int32_t* rows, const int32_t* count, int64_t n, uint8_t* dst,
-                 hipStream_t s) {
+Source Copies::rows_of(const gockpt_matrix& src, const int32_t* rows, const int32_t* count, int64_t n, uint8_t* dst) {
     const int64_t items = (src.cols + 7) / 8 * n;
+    const Source to = copied(src, dst);
     if (items > 0)
-        hipLaunchKernelGGL(rows_kernel, dim3(copy_grid(items)), dim3(256), 0, s,
-                           static_cast<const uint8_t*>(src.data), src.stride * 2, static_cast<int32_t>(src.cols), rows,
-                           count, static_cast<int32_t>(n), dst, copy_stride(src.cols) * 2);
+        one[many++] = {static_cast<const uint8_t*>(src.data), src.stride * 2, to.stride, rows, count, dst,
+                       static_cast<int32_t>(src.cols), static_cast<int32_t>(n), copy_grid(items)};
+    return to;
 }
 
-Source source_of(const gockpt_matrix& m, uint8_t* copy, hipStream_t s) {
-    if (in_place(m)) return {static_cast<const uint8_t*>(m.data), (m.rows > 1 ? m.stride : m.cols) * 2};
-    launch_rows(m, nullptr, nullptr, m.rows, copy, s);
-    return {copy, copy_stride(m.cols) * 2};
+void Copies::launch(hipStream_t s) const {
+    if (many > 0) hipLaunchKernelGGL(rows_kernel, dim3(one[0].blocks + one[1].blocks), dim3(256), 0, s, *this);
 }
 
 namespace {
