@@ -75,26 +75,29 @@ __device__ __forceinline__ int32_t row_of(const TokenArgs& a, int64_t t) {
     return row >= 0 && row < a.rows ? static_cast<int32_t>(row) : kElsewhere;
 }
 
-// Up to so many tokens the block that numbers them also fills `seen` (of 16384 it
-// took 87 us for that, the three launches take 5, 14 and 14: atomics on 16384
-// places of a table that no L2 owns).
-constexpr int32_t kSeenAlone = 1024;
+// Up to so many tokens the block that numbers them also fills `seen` (of 2048 in 9
+// us); two launches do of more (2331 in 10 us, 16384 in 23; the block alone had to
+// store for 20 us and do its atomics for 50).
+constexpr int32_t kSeenAlone = 2048;
 
-// Token k's part in filling `seen`: its row's entries reset; then, for each entry,
-// the least number above the entry before, which is the same whatever the order.
-// Rows that no token has keep what the memory held: a reader asks target whether
-// an entry is true.
-__device__ __forceinline__ void see(const TokenArgs& a, int32_t k, int stage) {
+// A row's entries before any token: rows that no token has keep what the memory
+// held, and a reader asks target whether an entry is true.
+__device__ __forceinline__ void see_none(const TokenArgs& a, int32_t row) {
+    if (a.seen == nullptr || row < 0) return;
+    for (int u = 0; u < kSeen; ++u) a.seen[u * static_cast<int64_t>(a.rows) + row] = INT32_MAX;
+}
+
+// Token k of its row's: the least number stays in the first entry, and each other
+// one, whether it came too late or was there before, goes on to the second, where
+// the least of those stays.  That is the same whatever the order.
+__device__ __forceinline__ void see(const TokenArgs& a, int32_t k) {
+    static_assert(kSeen == 2, "two entries");
     const int32_t row = a.target[k];
     if (row < 0) return;
-    if (stage == 0) {
-        for (int u = 0; u < kSeen; ++u) a.seen[u * static_cast<int64_t>(a.rows) + row] = INT32_MAX;
-        return;
-    }
-    int32_t* const entry = a.seen + (stage - 1) * static_cast<int64_t>(a.rows) + row;
-    const int32_t above =
-        stage > 1 ? __hip_atomic_load(entry - a.rows, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : -1;
-    if (k > above) __hip_atomic_fetch_min(entry, k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const int32_t was = __hip_atomic_fetch_min(a.seen + row, k, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const int32_t other = max(was, k);
+    if (other != INT32_MAX)
+        __hip_atomic_fetch_min(a.seen + a.rows + row, other, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
 // g of every token but with GOCKPT_EACH, whose largest magnitude is `most`, and
@@ -176,6 +179,7 @@ __global__ __launch_bounds__(kTokenThreads) void token_kernel(TokenArgs a) {
         if (there) {
             a.of_kept[k] = static_cast<int32_t>(t);
             a.target[k] = row;
+            if (a.tokens <= kSeenAlone) see_none(a, row);
             if (a.grad != nullptr) {
                 a.base[k] = a.lse_in[t] * static_cast<float>(kLog2e);
                 a.factor[k] = (weighted ? a.grad[t] : g) * up_by;
@@ -193,17 +197,19 @@ __global__ __launch_bounds__(kTokenThreads) void token_kernel(TokenArgs a) {
     for (int64_t at = from + 64 * kHeld; at < to; at += 64)
         number(at + lane, at + lane < to ? row_of(a, at + lane) : kMasked);
     if (a.seen == nullptr || a.tokens > kSeenAlone) return;
-    for (int stage = 0; stage <= kSeen; ++stage) {
-        __threadfence();
-        __syncthreads();
-        for (int32_t k = threadIdx.x; k < all; k += kTokenThreads) see(a, k, stage);
-    }
+    __threadfence();
+    __syncthreads();
+    for (int32_t k = threadIdx.x; k < all; k += kTokenThreads) see(a, k);
 }
 
-// Of more tokens, a launch for each stage.
-__global__ __launch_bounds__(256) void seen_kernel(TokenArgs a, int stage) {
+template <bool kReset>
+__global__ __launch_bounds__(256) void seen_kernel(TokenArgs a) {
     const int32_t k = blockIdx.x * 256 + threadIdx.x;
-    if (k < *a.count) see(a, k, stage);
+    if (k >= *a.count) return;
+    if constexpr (kReset)
+        see_none(a, a.target[k]);
+    else
+        see(a, k);
 }
 
 // Up to so many tokens are not numbered, as leaving some out would leave out no
@@ -246,13 +252,12 @@ __global__ __launch_bounds__(kFew) void few_kernel(TokenArgs a, const uint8_t* h
         a.of_token[t] = there ? t : -1;
         a.base[t] = there ? a.lse_in[t] * static_cast<float>(kLog2e) : 0.0f;
         a.factor[t] = there ? (weighted ? a.grad[t] : g) * up_by : 0.0f;
+        see_none(a, row);
     }
     if (a.seen == nullptr) return;
-    for (int stage = 0; stage <= kSeen; ++stage) {
-        __threadfence();
-        __syncthreads();
-        if (t < a.tokens) see(a, t, stage);
-    }
+    __threadfence();
+    __syncthreads();
+    if (t < a.tokens) see(a, t);
 }
 
 // ---- the loss ---------------------------------------------------------------------
@@ -919,9 +924,11 @@ int gockpt_head_grad(const gockpt_head* head, const float* lse, int reduction, c
                            static_cast<int32_t>(cols), ws + p.hidden, hidden_stride);
     } else {
         hipLaunchKernelGGL(token_kernel, dim3(1), dim3(kTokenThreads), 0, s, t);
-        if (t.seen != nullptr && t.tokens > kSeenAlone)
-            for (int stage = 0; stage <= kSeen; ++stage)
-                hipLaunchKernelGGL(seen_kernel, dim3((t.tokens + 255) / 256), dim3(256), 0, s, t, stage);
+        if (t.seen != nullptr && t.tokens > kSeenAlone) {
+            const dim3 grid((t.tokens + 255) / 256);
+            hipLaunchKernelGGL(seen_kernel<true>, grid, dim3(256), 0, s, t);
+            hipLaunchKernelGGL(seen_kernel<false>, grid, dim3(256), 0, s, t);
+        }
         copies.rows_of(head->hidden, t.of_kept, t.count, t.tokens, ws + p.hidden);
     }
     copies.launch(s);
