@@ -88,6 +88,15 @@ __device__ __forceinline__ T* uniform(T* p) {
     return reinterpret_cast<T*>(static_cast<uint64_t>(hi) << 32 | lo);
 }
 
+// threadIdx.x, of which the compiler does not know that it is what it was before a
+// product: what comes after it computes its addresses then, and the product does
+// not go without their registers.
+__device__ __forceinline__ int this_thread() {
+    int t = threadIdx.x;
+    asm volatile("" : "+v"(t));
+    return t;
+}
+
 // This wave's copies into LDS have landed (vmcnt 0; the builtin tells the
 // compiler too, which else waits again before reads).
 __device__ __forceinline__ void wait_copies() { __builtin_amdgcn_s_waitcnt(0x0f70); }
@@ -415,9 +424,9 @@ struct Mma {
     // The r of this lane's four elements of fragments (i, ..), from the first on,
     // and the c of those of fragments (.., j).
     static __device__ __forceinline__ int r_of(const MmaPlace& p, int i) {
-        return first_r(p) + i * 16 + 4 * ((threadIdx.x & 63) >> 4);
+        return first_r(p) + i * 16 + 4 * ((this_thread() & 63) >> 4);
     }
-    static __device__ __forceinline__ int c_of(const MmaPlace& p, int j) { return first_c(p, j) + (threadIdx.x & 15); }
+    static __device__ __forceinline__ int c_of(const MmaPlace& p, int j) { return first_c(p, j) + (this_thread() & 15); }
 };
 
 // The product of at most 32 c, both operands along k: R is read once, and that is
@@ -766,7 +775,7 @@ struct Store {
     // `rn` r in all; row c at out + c * stride.
     __device__ __forceinline__ void put(const typename M::Acc& acc, int j, uint8_t* out, int64_t stride, int dtype,
                                         bool accumulate, float alpha, int r0, int rn, int c0, int cn) const {
-        const int lane = threadIdx.x & 63, c = lane & 15, up = lane >> 4;
+        const int lane = this_thread() & 63, c = lane & 15, up = lane >> 4;
         if (dtype == kFP32 || accumulate) {
 #pragma unroll
             for (int i = 0; i < M::kFR; ++i)
