@@ -841,6 +841,39 @@ def test_head_in_pieces_of_the_vocabulary(tokens, vocab, dim):
     assert_close(gw, dw, dw_err + rounded(dw, torch.float32), "grad_weight")
 
 
+@pytest.mark.parametrize("tokens", [3, 300])
+def test_head_offsets_beyond_32_bits(tokens):
+    vocab, dim = 280000, 8192
+    table = torch.empty(vocab, dim, dtype=torch.bfloat16, device="cuda").normal_(0.0, 0.02).requires_grad_()
+    hidden = randn((tokens, dim), torch.bfloat16, 2).requires_grad_()
+    targets = torch.arange(tokens, device="cuda") * 7 + (vocab - 7 * tokens)
+    g.linear_cross_entropy(hidden, table, targets, reduction="none").sum().backward()
+    own = torch.arange(tokens, device="cuda")
+    X, parts = hidden.detach().double(), list(range(0, vocab, 10000))
+    logits, d = [], []
+    for a in parts:
+        W = table.detach()[a:a + 10000].double()
+        logits.append(X @ W.t())
+        d.append(2 * U * (dim + 2) * (X.abs() @ W.abs().t()) + 2 * U * logits[-1].abs())
+    logits, d = torch.cat(logits, 1), torch.cat(d, 1)
+    lse = torch.logsumexp(logits, 1)
+    e = d.amax(1) + (300 + 8) * U + 4 * U * (lse.abs() + logits.abs().amax(1))
+    p = torch.exp(logits - lse[:, None])
+    z = p.clone()
+    z[own, targets] -= 1.0
+    z_err = p * (d + e[:, None] + 2.0 ** -22) + 4 * U * z.abs() + H[torch.bfloat16][0] * z.abs() + 2.0 ** -38
+    want, err = torch.zeros_like(X), torch.zeros_like(X)
+    for a in parts:
+        W = table.detach()[a:a + 10000].double()
+        want += z[:, a:a + 10000] @ W
+        err += z_err[:, a:a + 10000] @ W.abs() + 2 * U * (vocab + 8) * (z[:, a:a + 10000].abs() @ W.abs())
+    assert_close(hidden.grad, want, err + rounded(want, torch.bfloat16), "grad_hidden")
+    for rows in (slice(0, 500), slice(vocab - 2500, vocab)):
+        want = z[:, rows].t() @ X
+        err = z_err[:, rows].t() @ X.abs() + 2 * U * (tokens + 4) * (z[:, rows].abs().t() @ X.abs())
+        assert_close(table.grad[rows], want, err + rounded(want, torch.bfloat16), "grad_weight")
+
+
 def test_head_of_ranks_that_split_the_vocabulary():
     hidden, table, targets = head_inputs(90, 1000, 64, "bf16")
     targets[4::9] = -1
