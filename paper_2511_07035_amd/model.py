@@ -284,7 +284,8 @@ class Act8:
     it stands for, bfloat16, float16 and float32 hold exactly (float16 within its
     range)."""
 
-    __slots__ = ("shape", "dtype", "rows", "cols", "blocks", "buffer", "packed")
+    # no address among them: a copy's buffer lies elsewhere
+    __slots__ = ("shape", "dtype", "rows", "cols", "blocks", "buffer")
 
     def __init__(self, shape, dtype, device="cuda", stream=None):
         if len(shape) == 0:
@@ -301,7 +302,6 @@ class Act8:
         else:
             with torch.cuda.stream(stream):
                 self.buffer = torch.empty(n * (GOCKPT_ACT8_BLOCK + 1), dtype=torch.uint8, device=device)
-        self.packed = self._at(self.buffer)
 
     @property
     def codes(self):
@@ -322,7 +322,7 @@ class Act8:
 
     def _pack(self, device: int) -> bytes:
         _here(self.buffer, "Act8", device)
-        return self.packed
+        return self._at(self.buffer)
 
     def _leave(self):
         """The buffer, for a graph to save: what is left describes it wherever the
@@ -378,7 +378,7 @@ def _linear8(x, weight, keep: bool, stream):
     ws, ptr, size = _workspace(weight, "gockpt_linear8_bytes", (mx, mw), stream)
     out = _empty(x, (*x.shape[:-1], rows), x.dtype, stream)
     kept = Act8(x.shape, x.dtype, x.device, stream) if keep else None
-    _check(_lib().gockpt_linear8(mx, mw, _matrix(out, "out", None, rows), None if kept is None else kept.packed,
+    _check(_lib().gockpt_linear8(mx, mw, _matrix(out, "out", None, rows), None if kept is None else kept._at(kept.buffer),
                                  ptr, size, _stream(stream, device)), "gockpt_linear8", None)
     return out, kept
 
@@ -477,7 +477,7 @@ def _gate8(x, factor, kind: int, keep: bool, stream):
     out = _empty(x, x.shape, x.dtype, stream)
     kept = [Act8(x.shape, x.dtype, x.device, stream) if keep and t is not None else None for t in (x, factor)]
     _check(_lib().gockpt_gate8(kind, mx, mf, _matrix(out, "out", None, cols),
-                               *(None if k is None else k.packed for k in kept), _stream(stream, device)),
+                               *(None if k is None else k._at(k.buffer) for k in kept), _stream(stream, device)),
            "gockpt_gate8", None)
     return out, kept
 

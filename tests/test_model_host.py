@@ -286,3 +286,24 @@ def test_copies_are_made_on_the_calls_stream(monkeypatch):
     assert own.is_contiguous() and seen == ["s", "out"]
     rows = torch.zeros(4, 8)[:, :6]
     assert model._own_rows(rows, 6, "s") is rows and len(seen) == 2
+
+
+def test_a_copy_of_8_bits_has_its_own_address():
+    """copy.deepcopy and pickle give a copy another buffer; what the library is given names that one."""
+    import copy
+    import pickle
+
+    import torch
+    a = g.Act8((3, 40), torch.bfloat16, "cpu")
+    a.buffer.copy_(torch.arange(a.nbytes).to(torch.uint8))
+    for b in (copy.deepcopy(a), pickle.loads(pickle.dumps(a)), copy.deepcopy([a, a])[1]):
+        assert b.buffer.data_ptr() != a.buffer.data_ptr() and b.shape == a.shape and b.dtype == a.dtype
+        assert torch.equal(b.codes, a.codes) and torch.equal(b.scales, a.scales)
+        # nothing in it but the buffer says where that lies
+        at = (a.buffer.data_ptr(), a.buffer.data_ptr() + 3 * 64)
+        for name in b.__slots__:
+            held = getattr(b, name)
+            assert not isinstance(held, bytes) or not any(struct.pack("<Q", x) in held for x in at), name
+        assert model.ACT8.unpack(b._at(b.buffer)) == (b.buffer.data_ptr(), b.buffer.data_ptr() + 3 * 64, 3, 40)
+    shallow = copy.copy(a)  # the same memory, as a shallow copy of a tensor is
+    assert shallow.buffer is a.buffer
