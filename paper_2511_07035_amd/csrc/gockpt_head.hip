@@ -542,6 +542,9 @@ void start_logits(int shape, const LossArgs& g, hipStream_t s) {
     using W = Mma<kT, kAlongK, kAlongK, 256, 256, 2, 4>;
     using D = Mma<kT, kAlongK, kAlongK, 128, 128, 2, 2>;
     using T = Stream<kT>;
+    static_assert(W::kThreads == product_threads(kWide) && D::kThreads == product_threads(kMid) &&
+                      T::kThreads == product_threads(kThin),
+                  "what too_many_blocks counts");
     if (shape == kWide)
         hipLaunchKernelGGL(logits_kernel<W>, grid, dim3(W::kThreads), 0, s, g);
     else if (shape == kMid)
@@ -556,6 +559,9 @@ void start_z(int shape, const GradArgs& g, hipStream_t s) {
     using W = Mma<kT, kAlongK, kAlongK, 256, 256, 2, 4>;
     using D = Mma<kT, kAlongK, kAlongK, 128, 128, 2, 2>;
     using T = Stream<kT>;
+    static_assert(W::kThreads == product_threads(kWide) && D::kThreads == product_threads(kMid) &&
+                      T::kThreads == product_threads(kThin),
+                  "what too_many_blocks counts");
     if (shape == kWide)
         hipLaunchKernelGGL(z_kernel<W>, grid, dim3(W::kThreads), 0, s, g);
     else if (shape == kMid)

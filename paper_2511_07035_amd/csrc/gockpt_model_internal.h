@@ -94,9 +94,13 @@ struct ProductPlan {
 // most_splits 1: not split.
 ProductPlan plan_product(int kind, int64_t rn, int64_t cn, int64_t k, int most_splits);
 
-// A grid of that many blocks there is not.
+// Threads of a block of each shape.
+constexpr int product_threads(int shape) { return shape == kWide ? 512 : 256; }
+
+// A launch has fewer than 2^32 threads.
 inline bool too_many_blocks(const ProductPlan& p) {
-    return p.splits > 0 && uint64_t{p.tiles_r} * p.tiles_c > uint64_t{INT32_MAX} / static_cast<uint64_t>(p.splits);
+    const uint64_t most = ((uint64_t{1} << 32) - 1) / static_cast<uint64_t>(product_threads(p.shape));
+    return p.splits > 0 && uint64_t{p.tiles_r} * p.tiles_c > most / static_cast<uint64_t>(p.splits);
 }
 
 // Starts the product of the operands in `a`, which the plan completes.

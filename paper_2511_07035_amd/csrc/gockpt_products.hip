@@ -23,19 +23,20 @@ __global__ __launch_bounds__(M::kThreads) void product_kernel(MmaArgs a, StoreAr
     store_tile<M>(GOCKPT_MMA_STORE(M), a, o, p, cn, acc);
 }
 
-template <class M>
+template <class M, int kShape>
 void start(const MmaArgs& a, const StoreArgs& o, hipStream_t s) {
+    static_assert(M::kThreads == product_threads(kShape), "what too_many_blocks counts");
     hipLaunchKernelGGL(product_kernel<M>, dim3(a.tiles_r * a.tiles_c * a.splits), dim3(M::kThreads), 0, s, a, o);
 }
 
 template <int kT, int kR, int kC>
 void start_shape(int shape, const MmaArgs& a, const StoreArgs& o, hipStream_t s) {
-    if (shape == kWide) return start<Mma<kT, kR, kC, 256, 256, 2, 4>>(a, o, s);
-    if (shape == kMid) return start<Mma<kT, kR, kC, 128, 128, 2, 2>>(a, o, s);
+    if (shape == kWide) return start<Mma<kT, kR, kC, 256, 256, 2, 4>, kWide>(a, o, s);
+    if (shape == kMid) return start<Mma<kT, kR, kC, 128, 128, 2, 2>, kMid>(a, o, s);
     if constexpr (kR == kAlongK)
-        start<Stream<kT>>(a, o, s);
+        start<Stream<kT>, kThin>(a, o, s);
     else if constexpr (kC == kAlongK)
-        start<Mma<kT, kR, kC, 128, 32, 4, 1>>(a, o, s);
+        start<Mma<kT, kR, kC, 128, 32, 4, 1>, kThin>(a, o, s);
 }
 
 template <int kT>

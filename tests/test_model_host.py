@@ -307,3 +307,35 @@ def test_a_copy_of_8_bits_has_its_own_address():
         assert model.ACT8.unpack(b._at(b.buffer)) == (b.buffer.data_ptr(), b.buffer.data_ptr() + 3 * 64, 3, 40)
     shallow = copy.copy(a)  # the same memory, as a shallow copy of a tensor is
     assert shallow.buffer is a.buffer
+
+
+def test_products_of_more_threads_than_a_launch_has_are_refused():
+    """A launch has fewer than 2^32 threads: 2^23 - 1 blocks of 512, a tile of 256 x 256 each."""
+    L = model._lib()
+    for tokens, rows, ok in ((1 << 22, 131072, False), ((1 << 22) - 256, 131072, True), (1 << 22, 131072 - 256, True),
+                             (1 << 23, 65536, False), (1 << 23, 65537, False), (1 << 26, 16384, False)):
+        h = head(M(tokens, 64), M(rows, 64), ids=(P, 1, tokens, tokens, 0, 64, 0))
+        rc, need = size("gockpt_head_loss_bytes", h)
+        assert (rc == 0) == ok and (need > 0) == ok, (tokens, rows, rc)
+        x, w = M(tokens, 64), M(rows, 64)
+        rc8, need8 = size("gockpt_linear8_bytes", x, w)
+        assert (rc8 == 0) == ok, (tokens, rows, rc8)
+        if ok:  # and with too little workspace nothing is launched
+            assert L.gockpt_head_loss(h, 0, P, P, P, P, need - 1, None) == g.GOCKPT_ENOMEM
+            continue
+        assert rc == rc8 == g.GOCKPT_EINVAL and need8 == 0 and "tiles" in said()
+        # before anything is launched
+        assert L.gockpt_head_loss(h, 0, P, P, P, P, 1 << 62, None) == g.GOCKPT_EINVAL and "tiles" in said()
+        assert L.gockpt_linear8(x, w, M(tokens, rows), A(tokens, 64), P, 1 << 62, None) == g.GOCKPT_EINVAL
+        # the same product as an input's gradient, and as a weight's
+        dy, wide = M(tokens, 64), M(64, rows)
+        for args in ((dy, wide, None, M(tokens, rows), None),):
+            assert size("gockpt_linear8_grad_bytes", *args)[0] == g.GOCKPT_EINVAL and "tiles" in said()
+            assert L.gockpt_linear8_grad(*args, 0, P, 1 << 62, None) == g.GOCKPT_EINVAL
+    # the head's gradients take the vocabulary in pieces, whose products are small enough
+    n = 1 << 22
+    h = head(M(n, 64), M(131072, 64), ids=(P, 1, n, n, 0, 64, 0))
+    assert size("gockpt_head_grad_bytes", h, M(n, 64), M(131072, 64))[0] == 0
+    n = 1 << 30  # 2^22 tiles of tokens
+    h = head(M(n, 512), M(131072, 512), ids=(P, 1, n, n, 0, 64, 0))
+    assert size("gockpt_head_grad_bytes", h, M(n, 512), None)[0] == g.GOCKPT_EINVAL and "tiles" in said()
