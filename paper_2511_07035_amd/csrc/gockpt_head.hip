@@ -220,8 +220,8 @@ __global__ __launch_bounds__(256) void seen_kernel(TokenArgs a) {
 constexpr int32_t kFew = 256;
 
 // What the gradients take from token_kernel and of the hidden rows, for so few
-// tokens: rows of those that do not count are zeros, so that they add nothing to
-// dW.  The first block also has the tokens' numbers; count[0] is all of them,
+// tokens: rows of those that do not count are zeros, as z_kernel makes their z, so
+// that they add nothing to dW.  The first block also has the tokens' numbers; count[0] is all of them,
 // count[1] as well unless none counts.
 __global__ __launch_bounds__(kFew) void few_kernel(TokenArgs a, const uint8_t* hidden, int64_t stride, int32_t cols,
                                                    uint8_t* dst, int64_t dst_stride) {
@@ -488,7 +488,7 @@ __global__ __launch_bounds__(M::kThreads) void z_kernel(GradArgs g) {
     for (int j = 0; j < M::kFC; ++j) {
         const int c = min(M::c_of(p, j), cn - 1);
         const float base = g.base[c], factor = g.factor[c];
-        const int want = M::c_of(p, j) < cn ? g.target[c] - g.first : -1;
+        const int row = g.target[c], want = M::c_of(p, j) < cn ? row - g.first : -1;
 #pragma unroll
         for (int i = 0; i < M::kFR; ++i)
 #pragma unroll
@@ -512,6 +512,13 @@ __global__ __launch_bounds__(M::kThreads) void z_kernel(GradArgs g) {
                     }
             }
             if (here) g.lost[c] = lost;
+        }
+        // a token that does not count adds nothing, also where its zeros met infinities
+        if (__any(row == kMasked)) {
+#pragma unroll
+            for (int i = 0; i < M::kFR; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][j][e] = row == kMasked ? 0.0f : acc[i][j][e];
         }
         if (edge) {
 #pragma unroll
