@@ -81,7 +81,10 @@ int gockpt_head_grad_bytes(const gockpt_head* head, const gockpt_matrix* grad_hi
  * accumulate grad_table becomes round(old + its sum).  Logits are computed
  * again in pieces of the vocabulary; z is rounded to the inputs' type, scaled
  * by a power of two so that fp16 keeps what a loss scale lifts, and all sums are
- * fp32.  Errors: EINVAL, ENOMEM (workspace), EHIP. */
+ * fp32.  For grad_hidden with GOCKPT_EACH each token has a power of two of its
+ * own; for grad_table all share one, and in fp16 each z is off by up to 2^-38 of
+ * the largest |g|.
+ * Errors: EINVAL, ENOMEM (workspace), EHIP. */
 int gockpt_head_grad(const gockpt_head* head, const float* lse, int reduction, const float* grad,
                      const gockpt_matrix* grad_hidden, const gockpt_matrix* grad_table, int accumulate,
                      void* workspace, size_t workspace_bytes, void* stream);

@@ -22,7 +22,15 @@
 // dW, where a class that few tokens have has few terms to average.
 // Z is scaled by a power of two, 2^13 / 2^q where 2^q <= max |g| < 2^(q + 1), so
 // that fp16 has probabilities down to 2^-37 and nothing overflows; the products
-// are scaled back in fp32.
+// are scaled back in fp32.  Where each token has a g of its own, fp16 would so keep
+// little or nothing of a token whose g is far below the largest (at 2^-20 of it and
+// 50304 classes alike a row of dX was off by 5e-4, at 2^-24 by up to 0.7 of itself).
+// There dX takes a Z of its own, each token's row lifted by the power of two that
+// its g lacks, which a row of dX is divided by again.  dW sums over the tokens and
+// keeps the one scale: what fp16 lacks there is 2^-38 of the largest g.  Both
+// gradients so take 670 us instead of 600 (2331 x 1160, 32003 classes), as Z is
+// stored twice and in pieces half as large; dX alone, whose one Z is the lifted, 381
+// instead of 378.
 #include "gockpt_mma.h"
 #include "gockpt_model_internal.h"
 
@@ -51,6 +59,7 @@ struct TokenArgs {
     int32_t* seen;      // the first of them that have each row of the table, the second (null: not wanted)
     float* base;        // log2(e) lse of the k-th
     float* factor;      // g 2^(13 - q)
+    float* up;          // what lifts the k-th's row of Z (null: nothing does)
     float* unscale;     // 2^(q - 13)
 };
 
@@ -115,6 +124,13 @@ __device__ __forceinline__ float factor_of_all(const TokenArgs& a, int32_t all, 
     up_by = ldexpf(1.0f, 13 - q);
     if (threadIdx.x == 0) *a.unscale = ldexpf(1.0f, q - 13);
     return g;
+}
+
+// The power of two that lifts a factor of a token to those of the largest g.
+__device__ __forceinline__ float up_of(float factor) {
+    const float x = fabsf(factor);
+    if (!(x > 0.0f && x <= 3.402823466e38f)) return 1.0f;
+    return ldexpf(1.0f, min(max(13 - ilogbf(x), 0), 126));
 }
 
 // One block: each wavefront counts its stretch of tokens, then numbers it from
@@ -182,7 +198,9 @@ __global__ __launch_bounds__(kTokenThreads) void token_kernel(TokenArgs a) {
             if (a.tokens <= kSeenAlone) see_none(a, row);
             if (a.grad != nullptr) {
                 a.base[k] = a.lse_in[t] * static_cast<float>(kLog2e);
-                a.factor[k] = (weighted ? a.grad[t] : g) * up_by;
+                const float factor = (weighted ? a.grad[t] : g) * up_by;
+                a.factor[k] = factor;
+                if (a.up != nullptr) a.up[k] = up_of(factor);
             }
         } else {
             if (a.lse != nullptr) a.lse[t] = 0.0f;
@@ -251,7 +269,9 @@ __global__ __launch_bounds__(kFew) void few_kernel(TokenArgs a, const uint8_t* h
         a.target[t] = row;
         a.of_token[t] = there ? t : -1;
         a.base[t] = there ? a.lse_in[t] * static_cast<float>(kLog2e) : 0.0f;
-        a.factor[t] = there ? (weighted ? a.grad[t] : g) * up_by : 0.0f;
+        const float factor = there ? (weighted ? a.grad[t] : g) * up_by : 0.0f;
+        a.factor[t] = factor;
+        if (a.up != nullptr) a.up[t] = up_of(factor);
         see_none(a, row);
     }
     if (a.seen == nullptr) return;
@@ -473,9 +493,13 @@ struct GradArgs {
     uint8_t* z;      // token k's row at z + k * z_stride
     int64_t z_stride;
     float* lost;     // what rounding took from the target's z
+    // kLifted: the same, each row times up; z null: only these
+    const float* up;
+    uint8_t* lifted;
+    float* lost_lifted;
 };
 
-template <class M>
+template <class M, bool kLifted>
 __global__ __launch_bounds__(M::kThreads) void z_kernel(GradArgs g) {
     GOCKPT_MMA_LDS(M)
     const int cn = *g.a.cn_dev;
@@ -497,7 +521,7 @@ __global__ __launch_bounds__(M::kThreads) void z_kernel(GradArgs g) {
                     __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][e], g.log2_scale, -base)) * factor;
         // most tiles hold the targets of none of their tokens
         if (__any(want >= M::first_r(p) && want < M::first_r(p) + M::kFR * 16)) {
-            float lost = 0.0f;
+            float z = 0.0f;
             bool here = false;
 #pragma unroll
             for (int i = 0; i < M::kFR; ++i) {
@@ -505,13 +529,14 @@ __global__ __launch_bounds__(M::kThreads) void z_kernel(GradArgs g) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     if (at == e) {
-                        const float z = acc[i][j][e] - factor;
+                        z = acc[i][j][e] - factor;
                         acc[i][j][e] = z;
-                        lost = z - elem_to_f32<M::kT>(pack2<M::kT>(z, z) & 0xffff);
                         here = true;
                     }
             }
-            if (here) g.lost[c] = lost;
+            const auto lost_of = [](float x) { return x - elem_to_f32<M::kT>(pack2<M::kT>(x, x) & 0xffff); };
+            if (here) g.lost[c] = lost_of(z);
+            if (kLifted && here) g.lost_lifted[c] = lost_of(z * g.up[c]);
         }
         // a token that does not count adds nothing, also where its zeros met infinities
         if (__any(row == kMasked)) {
@@ -533,9 +558,20 @@ __global__ __launch_bounds__(M::kThreads) void z_kernel(GradArgs g) {
     M::sync();
     const Store<M> store = GOCKPT_MMA_STORE(M);
     const int wide = (g.a.rn + 7) / 8 * 8;  // the products read whole pieces of 8: zeros behind the last row
+    if (!kLifted || g.z != nullptr) {
 #pragma unroll
-    for (int j = 0; j < M::kFC; ++j)
-        store.put(acc, j, g.z, g.z_stride, M::kT, false, 1.0f, M::first_r(p), wide, M::first_c(p, j), cn);
+        for (int j = 0; j < M::kFC; ++j)
+            store.put(acc, j, g.z, g.z_stride, M::kT, false, 1.0f, M::first_r(p), wide, M::first_c(p, j), cn);
+    }
+    if constexpr (kLifted) {
+#pragma unroll
+        for (int j = 0; j < M::kFC; ++j) {
+            const float up = g.up[min(M::c_of(p, j), cn - 1)];
+#pragma unroll
+            for (int i = 0; i < M::kFR; ++i) acc[i][j] *= up;
+            store.put(acc, j, g.lifted, g.z_stride, M::kT, false, 1.0f, M::first_r(p), wide, M::first_c(p, j), cn);
+        }
+    }
 }
 
 // ---- host ---------------------------------------------------------------------------
@@ -560,7 +596,7 @@ void start_logits(int shape, const LossArgs& g, hipStream_t s) {
         hipLaunchKernelGGL(logits_kernel<T>, grid, dim3(T::kThreads), 0, s, g);
 }
 
-template <int kT>
+template <int kT, bool kLifted>
 void start_z(int shape, const GradArgs& g, hipStream_t s) {
     const dim3 grid(g.a.tiles_r * g.a.tiles_c);
     using W = Mma<kT, kAlongK, kAlongK, 256, 256, 2, 4>;
@@ -570,11 +606,11 @@ void start_z(int shape, const GradArgs& g, hipStream_t s) {
                       T::kThreads == product_threads(kThin),
                   "what too_many_blocks counts");
     if (shape == kWide)
-        hipLaunchKernelGGL(z_kernel<W>, grid, dim3(W::kThreads), 0, s, g);
+        hipLaunchKernelGGL((z_kernel<W, kLifted>), grid, dim3(W::kThreads), 0, s, g);
     else if (shape == kMid)
-        hipLaunchKernelGGL(z_kernel<D>, grid, dim3(D::kThreads), 0, s, g);
+        hipLaunchKernelGGL((z_kernel<D, kLifted>), grid, dim3(D::kThreads), 0, s, g);
     else
-        hipLaunchKernelGGL(z_kernel<T>, grid, dim3(T::kThreads), 0, s, g);
+        hipLaunchKernelGGL((z_kernel<T, kLifted>), grid, dim3(T::kThreads), 0, s, g);
 }
 
 void place_tiles(MmaArgs& a, const ProductPlan& p) {
@@ -677,7 +713,8 @@ struct Piece {
 struct GradPlan {
     int64_t piece;   // rows of the table in a piece
     Piece full, rest;
-    size_t count, unscale, of_kept, target, of_token, seen, base, factor, lost, hidden, table, z, slices_hidden, slices_table, bytes;
+    size_t count, unscale, of_kept, target, of_token, seen, base, factor, lost, up, lost_lifted, hidden, table, z, lifted,
+        slices_hidden, slices_table, bytes;
     int64_t z_stride;
 };
 
@@ -689,7 +726,12 @@ Piece plan_piece(int64_t tokens, int64_t rows, int64_t cols, bool by_hidden, boo
     return p;
 }
 
-GradPlan plan_grad(const gockpt_head& h, bool by_hidden, bool by_table) {
+// Whether dX takes a Z of its own.
+bool lifts(const gockpt_head& h, bool by_hidden, int reduction) {
+    return by_hidden && h.hidden.dtype == kFP16 && reduction == GOCKPT_EACH;
+}
+
+GradPlan plan_grad(const gockpt_head& h, bool by_hidden, bool by_table, bool lifted) {
     GradPlan p{};
     Parts parts;
     const int64_t n = h.hidden.rows, rows = h.table.rows, cols = h.table.cols;
@@ -701,7 +743,8 @@ GradPlan plan_grad(const gockpt_head& h, bool by_hidden, bool by_table) {
         return x.z.us + x.by_hidden.us + x.by_table.us +
                (by_hidden ? static_cast<double>(n) * static_cast<double>(cols) * 8.0 / 4.5e6 : 0.0);
     };
-    const int64_t most = std::max<int64_t>(256, kPieceBytes / std::max<int64_t>(1, n * 2) / 256 * 256);
+    const int64_t each = lifted && by_table ? 4 : 2;  // bytes of an element of Z, or of both
+    const int64_t most = std::max<int64_t>(256, kPieceBytes / std::max<int64_t>(1, n * each) / 256 * 256);
     p.piece = std::max<int64_t>(rows, 1);
     if (rows > most) {
         // tiles run in rounds: pieces whose tiles fill them, the rest's too
@@ -728,10 +771,15 @@ GradPlan plan_grad(const gockpt_head& h, bool by_hidden, bool by_table) {
     p.base = parts.take(n * 4);
     p.factor = parts.take(n * 4);
     p.lost = parts.take(n * 4);
+    if (lifted) {
+        p.up = parts.take(n * 4);
+        p.lost_lifted = parts.take(n * 4);
+    }
     if (by_table) p.seen = parts.take(kSeen * rows * 4);
     p.hidden = parts.take(n * copy_stride(cols) * 2);
     p.table = parts.take(copy_bytes(h.table));
     p.z = parts.take(n * p.z_stride);
+    p.lifted = lifted && by_table ? parts.take(n * p.z_stride) : p.z;
     if (by_hidden) p.slices_hidden = parts.take(p.full.by_hidden.splits * n * cols * 4);
     if (by_table) {
         const auto bytes = [&](const ProductPlan& x, int64_t r) { return x.splits > 1 ? x.splits * r * cols * 4 : 0; };
@@ -882,9 +930,18 @@ int gockpt_head_grad_bytes(const gockpt_head* head, const gockpt_matrix* grad_hi
     int rc = check_head(name, head, nullptr);
     if (rc == GOCKPT_OK) rc = check_grads(name, head, grad_hidden, grad_table);
     if (rc != GOCKPT_OK) return rc;
-    const GradPlan p = plan_grad(*head, grad_hidden != nullptr, grad_table != nullptr);
+    // of any reduction
+    const bool by_hidden = grad_hidden != nullptr, by_table = grad_table != nullptr;
+    const bool lifted = lifts(*head, by_hidden, GOCKPT_EACH);
+    const GradPlan p = plan_grad(*head, by_hidden, by_table, lifted);
     rc = check_blocks(name, p);
-    if (rc == GOCKPT_OK) *bytes = p.bytes;
+    size_t most = p.bytes;
+    if (rc == GOCKPT_OK && lifted && p.piece < head->table.rows) {  // in one piece there is more with a Z for dX
+        const GradPlan q = plan_grad(*head, by_hidden, by_table, false);
+        rc = check_blocks(name, q);
+        most = std::max(most, q.bytes);
+    }
+    if (rc == GOCKPT_OK) *bytes = most;
     return rc;
 }
 
@@ -902,7 +959,8 @@ int gockpt_head_grad(const gockpt_head* head, const float* lse, int reduction, c
         if (rc == GOCKPT_OK && reinterpret_cast<uintptr_t>(p) % 4 != 0)
             rc = ops_fail(GOCKPT_EINVAL, "%s: lse or grad is not aligned", name);
     if (rc != GOCKPT_OK) return rc;
-    const GradPlan p = plan_grad(*head, grad_hidden != nullptr, grad_table != nullptr);
+    const bool lifted = lifts(*head, grad_hidden != nullptr, reduction);
+    const GradPlan p = plan_grad(*head, grad_hidden != nullptr, grad_table != nullptr, lifted);
     rc = check_blocks(name, p);
     if (rc == GOCKPT_OK) rc = check_workspace(name, workspace, workspace_bytes, p.bytes);
     if (rc != GOCKPT_OK) return rc;
@@ -922,6 +980,11 @@ int gockpt_head_grad(const gockpt_head* head, const float* lse, int reduction, c
     if (by_table) t.seen = reinterpret_cast<int32_t*>(ws + p.seen);
     t.base = reinterpret_cast<float*>(ws + p.base);
     t.factor = reinterpret_cast<float*>(ws + p.factor);
+    if (lifted) t.up = reinterpret_cast<float*>(ws + p.up);
+    float* const lost = reinterpret_cast<float*>(ws + p.lost);
+    // what dX is made of
+    float* const lost_hidden = lifted ? reinterpret_cast<float*>(ws + p.lost_lifted) : lost;
+    uint8_t* const z_hidden = ws + (lifted ? p.lifted : p.z);
     t.unscale = reinterpret_cast<float*>(ws + p.unscale);
     const int64_t hidden_stride = copy_stride(cols) * 2;
     const bool few = t.tokens > 0 && t.tokens <= kFew;
@@ -966,19 +1029,24 @@ int gockpt_head_grad(const gockpt_head* head, const float* lse, int reduction, c
             g.first = static_cast<int32_t>(first);
             g.base = t.base;
             g.factor = t.factor;
-            g.z = ws + p.z;
+            g.z = lifted && !by_table ? nullptr : ws + p.z;
             g.z_stride = p.z_stride;
-            g.lost = reinterpret_cast<float*>(ws + p.lost);
+            g.lost = lost;
+            g.up = t.up;
+            g.lifted = z_hidden;
+            g.lost_lifted = lost_hidden;
             if (dtype == kBF16)
-                start_z<kBF16>(plan.z.shape, g, s);
+                start_z<kBF16, false>(plan.z.shape, g, s);
+            else if (lifted)
+                start_z<kFP16, true>(plan.z.shape, g, s);
             else
-                start_z<kFP16>(plan.z.shape, g, s);
+                start_z<kFP16, false>(plan.z.shape, g, s);
         }
         if (by_hidden) {
             MmaArgs a{};
             a.r = table.data + first * table.stride;
             a.r_stride = table.stride;
-            a.c = ws + p.z;
+            a.c = z_hidden;
             a.c_stride = p.z_stride;
             a.rn = static_cast<int32_t>(cols);
             a.cn = t.tokens;
@@ -992,7 +1060,8 @@ int gockpt_head_grad(const gockpt_head* head, const float* lse, int reduction, c
                 o.alpha = head->scale;
                 o.beta = t.unscale;
                 o.owner = t.target;
-                o.fix = reinterpret_cast<const float*>(ws + p.lost);
+                o.fix = lost_hidden;
+                o.up = t.up;
             } else {
                 o.slices = slices;
                 o.add = first > 0;
@@ -1021,7 +1090,7 @@ int gockpt_head_grad(const gockpt_head* head, const float* lse, int reduction, c
             o.seen = t.seen;
             o.seen_step = rows;
             o.owner = t.target;
-            o.fix = reinterpret_cast<const float*>(ws + p.lost);
+            o.fix = lost;
             o.first = static_cast<int32_t>(first);
             if (plan.by_table.splits > 1) {
                 o.slices = reinterpret_cast<float*>(ws + p.slices_table);
@@ -1056,7 +1125,8 @@ int gockpt_head_grad(const gockpt_head* head, const float* lse, int reduction, c
         f.dtype = grad_hidden->dtype;
         f.alpha = head->scale;
         f.beta = t.unscale;
-        f.fix = reinterpret_cast<const float*>(ws + p.lost);
+        f.up = t.up;
+        f.fix = lost_hidden;
         f.fix_row = t.target;
         f.fix_from = table.data;
         f.fix_stride = table.stride;

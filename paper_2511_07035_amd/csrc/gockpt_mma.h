@@ -607,6 +607,7 @@ struct StoreArgs {
     const int32_t* owner;
     const float* fix;
     int32_t first;
+    const float* up;  // with these, C along k: c's sum is up[c] times too large, a power of two (null: none is)
 };
 constexpr int kSeen = 2;
 
@@ -662,6 +663,15 @@ __device__ __forceinline__ void add_fixes(const MmaArgs& a, const StoreArgs& o, 
                     // x of what is not there may be anything
                     acc[i][j][e] = k[j][u] < -1 ? 0.0f : k[j][u] >= 0 ? acc[i][j][e] + add : acc[i][j][e];
                 }
+    }
+    if constexpr (!M::kBothAcross) {
+        if (o.up == nullptr) return;
+#pragma unroll
+        for (int j = 0; j < M::kFC; ++j) {
+            const float down = 1.0f / o.up[min(M::c_of(p, j), cn - 1)];
+#pragma unroll
+            for (int i = 0; i < M::kFR; ++i) acc[i][j] *= down;
+        }
     }
 }
 

@@ -126,6 +126,7 @@ struct FinishArgs {
     const uint8_t* fix_from;
     int64_t fix_stride;  // bytes; rows of whole pieces of 8
     int32_t fix_dtype;
+    const float* up;  // row c's sum is up[c] times too large, a power of two (null: none is)
 };
 void launch_finish(const FinishArgs& f, hipStream_t s);
 

@@ -77,7 +77,7 @@ __global__ __launch_bounds__(256) void finish_kernel(FinishArgs f) {
                     sum[i] += x * (f.fix_dtype == kBF16 ? elem_to_f32<kBF16>(b) : elem_to_f32<kFP16>(b));
                 }
             }
-            sum *= alpha;
+            sum *= f.up != nullptr ? alpha / f.up[c] : alpha;
         }
         store4(f.out + row * f.stride + static_cast<int64_t>(col) * dtype_bytes(f.dtype), f.dtype, f.accumulate != 0,
                sum, n);

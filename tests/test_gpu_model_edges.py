@@ -73,3 +73,93 @@ def test_head_masked_tokens_beside_infinities(tokens, vocab, value, dtype):
     want = z.t() @ X
     err = z_err.t() @ X.abs() + 2 * U * (tokens + 2) * (z.abs().t() @ X.abs())
     assert_close(w.grad, want, err + rounded(want, DT[dtype]), "grad_weight")
+
+
+def weighted_grad(tokens, vocab, dim, dtype, weights, mean=0.0, chunk=512):
+    """head_grad of "none" with these weights into fp32, against float64.  Each token's
+    z is held relative to its own weight for grad_hidden, and where fp16 runs out
+    relative to the largest for grad_weight."""
+    t = DT[dtype]
+    hidden, table, targets = head_inputs(tokens, vocab, dim, dtype, sigma=0.02, know=False)
+    table = (table.float() + mean).to(t)
+    hidden *= 0.5
+    targets[::7] = -1
+    weights = weights.float().cuda()
+    lse, _ = g.head_stats(hidden, table, targets)
+    gx, gw = torch.full(hidden.shape, float("nan"), device="cuda"), torch.full(table.shape, float("nan"), device="cuda")
+    g.head_grad(hidden, table, targets, lse, weights, grad_hidden=gx, grad_weight=gw)
+    alone, _ = g.head_grad(hidden, table, targets, lse, weights, grad_hidden=torch.empty_like(gx))
+    W = table.double()
+    counts = targets >= 0
+    most = weights[counts].abs().max().double() if bool(counts.any()) else torch.zeros((), device="cuda").double()
+    want_w, err_w = torch.zeros_like(W), torch.zeros_like(W)
+    out = 2.0 ** -38 if dtype == "fp16" else 0.0
+    for a in range(0, tokens, chunk):
+        X, y, gt = hidden[a:a + chunk].double(), targets[a:a + chunk], weights[a:a + chunk].double()
+        gt = torch.where(y >= 0, gt, torch.zeros_like(gt))
+        logits = X @ W.t()
+        d = 2 * U * (dim + 2) * (X.abs() @ W.abs().t()) + 2 * U * logits.abs()
+        want_lse = torch.logsumexp(logits, 1)
+        e = d.amax(1) + (300 + 8) * U + 4 * U * (want_lse.abs() + logits.abs().amax(1))
+        p = torch.exp(logits - want_lse[:, None])
+        z = p.clone()
+        z[torch.arange(y.numel(), device="cuda"), y.clamp(min=0)] -= 1.0
+        z *= gt[:, None]
+        # the product of the weight and of its scale is exact; a weight in fp32's subnormals is taken as it is
+        z_err = gt.abs()[:, None] * p * (d + e[:, None] + 2.0 ** -22) + (4 * U + H[t][0]) * z.abs()
+        want = z @ W
+        err = (z_err + out * gt.abs()[:, None]) @ W.abs() + 2 * U * (vocab + 8) * (z.abs() @ W.abs())
+        for got, what in ((gx, "with grad_weight"), (alone, "alone")):
+            assert_close(got[a:a + chunk], want, err + rounded(want, torch.float32), f"grad_hidden {what} from {a}: ")
+        want_w += z.t() @ X
+        err_w += (z_err + out * most * (y >= 0)[:, None]).t() @ X.abs() + 2 * U * (tokens + 2) * (z.abs().t() @ X.abs())
+    assert_close(gw, want_w, err_w + rounded(want_w, torch.float32), "grad_weight")
+    return hidden, table, targets, weights, gx
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("mean", [0.0, 0.05])
+@pytest.mark.parametrize("tokens,vocab,dim", [(1, 300, 64), (20, 50304, 64), (64, 50304, 64), (256, 1000, 72),
+                                              (257, 3001, 65), (700, 50304, 40), (3000, 50304, 64)])
+def test_head_weights_far_apart_keep_each_tokens_gradient(tokens, vocab, dim, mean, dtype):
+    """Weights from 2^20 to 2^-20 in one call, some of them 0 or negative: every row of
+    grad_hidden is as good as alone.  The largest case takes the vocabulary in pieces."""
+    k = torch.arange(tokens)
+    weights = torch.exp2(((k * 17) % 41 - 20).double()) * (1.0 + (k % 5) / 8.0) * torch.where(k % 3 == 0, -1.0, 1.0)
+    weights[5::31] = 0.0
+    weighted_grad(tokens, vocab, dim, dtype, weights, mean)
+
+
+@pytest.mark.parametrize("scale", [2.0 ** 90, 2.0 ** -60])
+def test_head_weights_at_the_ends_of_their_type(scale):
+    k = torch.arange(40)
+    weighted_grad(40, 3000, 64, "fp16", torch.exp2((-(k % 25)).double()) * scale, 0.05)
+
+
+def test_head_weights_far_apart_in_16_bits_scale_rows_exactly():
+    """A weight that is a power of two times another scales its row by just that, also
+    from one call to the other and through the loss."""
+    hidden, table, targets = head_inputs(96, 5000, 64, "fp16", sigma=0.02)
+    hidden[48:], targets[48:] = hidden[:48], targets[:48]
+    lse, _ = g.head_stats(hidden, table, targets)
+    weights = torch.ones(96, device="cuda")
+    weights[:48] = 2.0 ** -22
+    gx = torch.empty(96, 64, device="cuda")
+    g.head_grad(hidden, table, targets, lse, weights, grad_hidden=gx, grad_weight=torch.empty(5000, 64, device="cuda"))
+    assert torch.equal(gx[:48] * 2.0 ** 22, gx[48:])
+    x = hidden.detach().requires_grad_()
+    up = weights * 2.0 ** 20  # the smaller ones' rows are within fp16's range too
+    g.linear_cross_entropy(x, table, targets, reduction="none").backward(up)
+    # the same fp32 sums times a power of two, rounded once; those from 65520 on to infinity
+    assert torch.equal(x.grad, (gx * 2.0 ** 20).half())
+    # none has a weight but one; weights that are no numbers stay in their rows
+    weights = torch.zeros(96, device="cuda")
+    weights[9] = 2.0 ** -40
+    gx, _ = g.head_grad(hidden, table, targets, lse, weights, grad_hidden=torch.empty(96, 64, device="cuda"))
+    assert not bool(gx[:9].any()) and not bool(gx[10:].any()) and bool(gx[9].any())
+    for value in (float("inf"), float("nan")):
+        weights = torch.full((96,), 2.0 ** -22, device="cuda")
+        weights[3] = value
+        gx, _ = g.head_grad(hidden, table, targets, lse, weights, grad_hidden=torch.empty(96, 64, device="cuda"))
+        rows = torch.isfinite(gx).all(1)
+        assert not bool(rows[3]) and int((~rows).sum()) == 1
