@@ -139,7 +139,8 @@ int gockpt_linear8_grad(const gockpt_matrix* grad_out, const gockpt_matrix* weig
 #define GOCKPT_GELU_TANH 2 /* x (1 + tanh(sqrt(2 / pi) (x + 0.044715 x^3))) / 2 */
 
 /* out = round(act(x) * factor), or round(act(x)) where factor is NULL; all of
- * one type, any of the three.  keep_x and keep_factor: where x and factor go in
+ * one type, any of the three.  Before it is rounded a 16-bit act(x) is off by up
+ * to 2^-15 of itself, with GOCKPT_GELU_TANH 2^-14 (where it is at least 2^-126).  keep_x and keep_factor: where x and factor go in
  * 8 bits (both NULL: nowhere; keep_factor NULL without a factor).
  * Errors: EINVAL, EHIP. */
 int gockpt_gate8(int kind, const gockpt_matrix* x, const gockpt_matrix* factor, const gockpt_matrix* out,

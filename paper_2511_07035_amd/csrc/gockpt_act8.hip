@@ -186,9 +186,11 @@ __device__ __forceinline__ void restore8(const Kept& k, int64_t group, float (&x
 
 // ---- activations ------------------------------------------------------------------
 
-// exp, and 1 / (1 + exp(-x)).  Outputs of 16 bits take the hardware's exp2 of
-// the rounded product with log2(e), off by |x| 2^-24 relative at most, which is
-// 2^-17 where anything is left of the result; fp32 outputs the library's exp.
+// exp, and 1 / (1 + exp(-x)).  Outputs of 16 bits take the hardware's exp2 of the
+// product with log2(e).  The constant is off by 0.23 2^-24 of itself and the
+// rounding of the product by 2^-24, the result so by 1.23 |x| 2^-24 of itself and by
+// the instruction's own 2^-23: 2^-17 in all where anything is left of the result (|x|
+// up to 88).  fp32 outputs take the library's exp.
 template <int kT>
 __device__ __forceinline__ float exp_of(float x) {
     if constexpr (kT == kFP32)
@@ -206,9 +208,14 @@ __device__ __forceinline__ float sigmoid(float x) {
         return __builtin_amdgcn_rcpf(1.0f + e);
 }
 
-// Phi(x) = (1 + erf(x / sqrt 2)) / 2 and phi(x), its derivative.  16-bit
-// outputs: Abramowitz and Stegun 7.1.26, off by 7.5e-8 at most, which shares
-// its exponential with phi.
+// Phi(x) = (1 + erf(x / sqrt 2)) / 2 and phi(x), its derivative.  16-bit outputs take
+// the tail as exp(-x^2 / 2) / 2 times erfcx(z) = exp(z^2) erfc(z), z = |x| / sqrt 2,
+// which falls as 1 / z: t P(t) with t = 1 / (1 + 0.435 z).  P is of the fifth degree,
+// fitted here to the least largest relative error over 0 <= z <= 10, 2^-17.7 of the
+// tail.  With the exponential's (1.12 x^2 2^-24, its argument's two roundings and the
+// constant's) that is 2^-15 at most wherever the result is a bf16, x > -13.7: far
+// below half a step also in the far tail, where an error that is small against 1 is
+// not small against the result.
 template <int kT>
 __device__ __forceinline__ void normal(float x, float& cdf, float& pdf) {
     const float e = exp_of<kT>(-0.5f * x * x);
@@ -216,11 +223,12 @@ __device__ __forceinline__ void normal(float x, float& cdf, float& pdf) {
     if constexpr (kT == kFP32) {
         cdf = 0.5f * erfcf(-0.707106781186547524401f * x);
     } else {
-        const float t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * 0.707106781186547524401f * fabsf(x));
-        float p = 1.061405429f * t - 1.453152027f;
-        p = p * t + 1.421413741f;
-        p = p * t - 0.284496736f;
-        p = p * t + 0.254829592f;
+        const float t = __builtin_amdgcn_rcpf(1.0f + 0.435f * 0.707106781186547524401f * fabsf(x));
+        float p = 0.3812965552f - 0.1508592834f * t;
+        p = p * t + 0.01285750788f;
+        p = p * t + 0.2734441863f;
+        p = p * t + 0.2373346605f;
+        p = p * t + 0.2459255198f;
         const float tail = 0.5f * p * t * e;
         cdf = x < 0.0f ? tail : 1.0f - tail;
     }

@@ -11,7 +11,7 @@ import paper_2511_07035_amd as g
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from test_gpu_model import DT, H, U, assert_close, head_inputs, kept64, product_error, randn, rounded  # noqa: E402
+from test_gpu_model import DT, H, U, act64, assert_close, head_inputs, kept64, product_error, randn, rounded  # noqa: E402
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
@@ -163,3 +163,29 @@ def test_head_weights_far_apart_in_16_bits_scale_rows_exactly():
         gx, _ = g.head_grad(hidden, table, targets, lse, weights, grad_hidden=torch.empty(96, 64, device="cuda"))
         rows = torch.isfinite(gx).all(1)
         assert not bool(rows[3]) and int((~rows).sum()) == 1
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("kind", ["silu", "gelu", "gelu_tanh"])
+def test_gate8_tails_are_as_good_as_the_middle(kind, dtype):
+    """act(x) and its derivative for negative x, relative to themselves down to where
+    they leave the type: the exponent of a result e^-a is off by a few roundings of a <
+    90, so the result by 2^-15 (gelu_tanh, with seven more roundings in a, 2^-14)."""
+    t = DT[dtype]
+    values = torch.cat([torch.linspace(-14.5, 0, 4001, dtype=torch.float64), torch.linspace(-88, -14.5, 1001).double()])
+    x = values.cuda().to(t).view(-1, 1).contiguous().requires_grad_()  # each in a block of its own
+    y = g.gate8(x, kind=kind)
+    y.backward(torch.ones_like(y))
+    rel = 2.0 ** (-14 if kind == "gelu_tanh" else -15)
+    X = x.detach().double()
+    want, _, _ = act64(X, kind)
+    # e^-a below 2^-126 may be 0, which is x times as much in the result
+    assert_close(y.detach(), want, rel * want.abs() + 2.0 ** -126 * X.abs() + rounded(want, t), "y")
+    K = kept64(x)
+    _, want, parts = act64(K, kind)  # the derivative is a sum: relative to its terms
+    assert_close(x.grad, want, 2 * rel * parts + 61 * 2.0 ** -126 * K.abs() + rounded(want, t), "dx")
+    f = torch.full_like(x, 0.75).detach().requires_grad_()
+    y = g.gate8(x.detach(), f, kind=kind)
+    y.backward(torch.ones_like(y))
+    want = act64(K, kind)[0]
+    assert_close(f.grad, want, rel * want.abs() + 2.0 ** -126 * K.abs() + rounded(want, t), "df")
