@@ -127,6 +127,12 @@ def _own_rows(t, cols: int, stream):
         return t.contiguous()
 
 
+def _refuse_leaf(t, what: str) -> None:
+    """What a call writes, and which no gradient would come of."""
+    if t.requires_grad and torch.is_grad_enabled():
+        raise ValueError(f"{what}: requires a gradient, which the call would not give it")
+
+
 def _check_grad_weight(weight, grad_weight, accumulate, device: int) -> None:
     if grad_weight is None:
         if accumulate:
@@ -235,6 +241,9 @@ def head_grad(hidden, table, targets, lse, grad, *, scale: float = 1.0, first_id
         raise ValueError(f"grad_hidden of shape {tuple(grad_hidden.shape)} for hidden of shape {tuple(hidden.shape)}")
     if grad_weight is not None and grad_weight.shape != table.shape:
         raise ValueError(f"grad_weight of shape {tuple(grad_weight.shape)} for a table of shape {tuple(table.shape)}")
+    for t, what in ((grad_hidden, "grad_hidden"), (grad_weight, "grad_weight")):
+        if t is not None:
+            _refuse_leaf(t, what)
     _head_grad(device, head, table, lse, grad, r, grad_hidden, grad_weight, accumulate, stream)
     _changed(tuple(t for t in (grad_hidden, grad_weight) if t is not None))
     return grad_hidden, grad_weight
@@ -337,8 +346,8 @@ class Act8:
             out = _empty(self.buffer, self.shape, self.dtype if dtype is None else dtype, stream)
         elif out.shape != self.shape or (dtype is not None and out.dtype != dtype):
             raise ValueError(f"out: expected shape {tuple(self.shape)}, got {tuple(out.shape)} of {out.dtype}")
-        elif out.requires_grad and torch.is_grad_enabled():
-            raise ValueError("out: requires a gradient, which the call would not give it")
+        else:
+            _refuse_leaf(out, "out")
         m = _matrix(out, "out", device, self.cols)
         _check(_lib().gockpt_act8_unpack(self._pack(device), m, _stream(stream, device)), "gockpt_act8_unpack", None)
         _changed((out,))
@@ -378,8 +387,9 @@ def _linear8(x, weight, keep: bool, stream):
     ws, ptr, size = _workspace(weight, "gockpt_linear8_bytes", (mx, mw), stream)
     out = _empty(x, (*x.shape[:-1], rows), x.dtype, stream)
     kept = Act8(x.shape, x.dtype, x.device, stream) if keep else None
-    _check(_lib().gockpt_linear8(mx, mw, _matrix(out, "out", None, rows), None if kept is None else kept._at(kept.buffer),
-                                 ptr, size, _stream(stream, device)), "gockpt_linear8", None)
+    _check(_lib().gockpt_linear8(mx, mw, _matrix(out, "out", None, rows),
+                                 None if kept is None else kept._at(kept.buffer), ptr, size,
+                                 _stream(stream, device)), "gockpt_linear8", None)
     return out, kept
 
 
@@ -419,6 +429,7 @@ def linear8_grad_weight(grad_out, kept: Act8, grad_weight, *, accumulate: bool =
     if grad_weight.shape != (grad_out.shape[-1], kept.cols):
         raise ValueError(f"grad_weight of shape {tuple(grad_weight.shape)}, expected "
                          f"{(grad_out.shape[-1], kept.cols)}")
+    _refuse_leaf(grad_weight, "grad_weight")
     _linear8_grad(grad_out.detach(), None, kept._pack(_here(grad_out, "grad_out")), None, grad_weight, accumulate,
                   stream)
     return grad_weight

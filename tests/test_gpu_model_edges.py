@@ -11,7 +11,8 @@ import paper_2511_07035_amd as g
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from test_gpu_model import DT, H, U, act64, assert_close, head_inputs, kept64, product_error, randn, rounded  # noqa: E402
+from test_gpu_model import (DT, H, U, act64, assert_close, head_inputs, kept64,  # noqa: E402
+                            product_error, randn, rounded)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
@@ -189,3 +190,30 @@ def test_gate8_tails_are_as_good_as_the_middle(kind, dtype):
     y.backward(torch.ones_like(y))
     want = act64(K, kind)[0]
     assert_close(f.grad, want, rel * want.abs() + 2.0 ** -126 * K.abs() + rounded(want, t), "df")
+
+
+def test_destinations_that_require_a_gradient_are_refused():
+    hidden, table, targets = head_inputs(40, 100, 64, "bf16")
+    lse, _ = g.head_stats(hidden, table, targets)
+    one, kept = torch.ones(1, device="cuda"), g.act8_pack(hidden)
+    dy = randn((40, 24), torch.bfloat16, 3)
+
+    def made(shape):
+        leaf = torch.full(shape, 5.0, device="cuda", requires_grad=True)
+        return leaf, leaf * 1.0, (leaf * 1.0)[:, :]
+
+    def grads(**into):
+        return g.head_grad(hidden, table, targets, lse, one, reduction="sum", **into)
+
+    for shape, call in (((40, 64), lambda t: grads(grad_hidden=t)), ((100, 64), lambda t: grads(grad_weight=t)),
+                        ((100, 64), lambda t: grads(grad_weight=t, accumulate=True)),
+                        ((24, 64), lambda t: g.linear8_grad_weight(dy, kept, t)),
+                        ((24, 64), lambda t: g.linear8_grad_weight(dy, kept, t, accumulate=True)),
+                        ((40, 64), lambda t: kept.unpack(out=t))):
+        for t in made(shape):
+            with pytest.raises(ValueError, match="requires a gradient"):
+                call(t)
+            assert bool((t == 5.0).all())
+            with torch.no_grad():  # as torch's own writes into a parameter
+                call(t.detach()), call(t)
+            assert not bool((t == 5.0).all())
