@@ -11,8 +11,8 @@ import paper_2511_07035_amd as g
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from test_gpu_model import (DT, H, U, act64, assert_close, head_inputs, kept64,  # noqa: E402
-                            product_error, randn, rounded)
+from test_gpu_model import (DT, H, U, act64, assert_close, head64, head_inputs, kept64,  # noqa: E402
+                            padded, product_error, randn, rounded)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
@@ -217,3 +217,58 @@ def test_destinations_that_require_a_gradient_are_refused():
             with torch.no_grad():  # as torch's own writes into a parameter
                 call(t.detach()), call(t)
             assert not bool((t == 5.0).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("grad", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("tokens,rows,cols", [(1, 8, 8), (70, 33, 50), (300, 520, 264), (3000, 64, 48), (1030, 515, 600)])
+def test_linear8_grad_weight_by_itself(tokens, rows, cols, accumulate, grad, dtype):
+    """Against float64, and the same bits as the layer's backward."""
+    t = DT[dtype]
+    x, w = randn((tokens, cols), t, 1), randn((rows, cols), t, 2, 0.05).requires_grad_()
+    dy, old = randn((tokens, rows), t, 3, 0.1), randn((rows, cols), DT[grad], 4)
+    K = kept64(x)
+    want = dy.double().t() @ K + (old.double() if accumulate else 0.0)
+    # the sum with the old value is rounded to fp32 before its type
+    extra = 2 * U * (want.abs() + old.double().abs())
+    err = product_error(dy.double().t(), K, want, DT[grad], extra)
+    kept = g.act8_pack(x)
+    alone, apart = old.clone(), padded(old.clone(), 3, 5.0)
+    for into in (alone, apart):
+        version = into._version
+        assert g.linear8_grad_weight(dy, kept, into, accumulate=accumulate) is into and into._version > version
+        assert_close(into, want, err, "grad_weight")
+    assert bool((apart._base[:, cols:] == 5.0).all())
+    back = old.clone()
+    g.linear8(x, w, grad_weight=back, accumulate=accumulate).backward(dy)
+    assert torch.equal(alone, back)
+
+
+@pytest.mark.parametrize("reduction", ["mean", "sum", "none"])
+@pytest.mark.parametrize("up", [1e-6, 65536.0, 2.0 ** -60, 2.0 ** 60])
+@pytest.mark.parametrize("tokens,vocab,dim", [(64, 3000, 64), (300, 5000, 33)])
+def test_head_fp16_under_loss_gradients_of_any_size(tokens, vocab, dim, up, reduction):
+    """fp16 inputs: fp32 gradients scale with the loss's, and fp16 ones are those rounded."""
+    hidden, table, targets = head_inputs(tokens, vocab, dim, "fp16")
+    targets[::9] = -1
+    counts = targets >= 0
+    lse, _ = g.head_stats(hidden, table, targets)
+    n = tokens if reduction == "none" else 1
+    grad = torch.full((n,), up, device="cuda")
+    into = [torch.full((tokens, dim), float("nan"), device="cuda"), torch.full((vocab, dim), float("nan"), device="cuda")]
+    g.head_grad(hidden, table, targets, lse, grad, reduction=reduction, grad_hidden=into[0], grad_weight=into[1])
+    X, W, logits, want_lse, d, e = head64(hidden, table, targets, 1.0, counts)
+    gt = counts.double() * float(grad[0]) / (int(counts.sum()) if reduction == "mean" else 1)
+    p = torch.exp(logits - want_lse[:, None])
+    z = p.clone()
+    z[torch.arange(tokens, device="cuda"), targets.clamp(min=0)] -= 1.0
+    z *= gt[:, None]
+    z_err = gt.abs()[:, None] * (p * (d + e[:, None] + 2.0 ** -22) + 2.0 ** -38) + (6 * U + H[torch.float16][0]) * z.abs()
+    for got, a, b, z_, z_e in ((into[0], W, "grad_hidden", z, z_err), (into[1], X, "grad_weight", z.t(), z_err.t())):
+        want = z_ @ a
+        err = z_e @ a.abs() + 2 * U * (z_.shape[1] + 8) * (z_.abs() @ a.abs())
+        assert_close(got, want, err + rounded(want, torch.float32), b)
+    x, w = hidden.detach().requires_grad_(), table.detach().requires_grad_()
+    g.linear_cross_entropy(x, w, targets, reduction=reduction).backward(grad.view(targets.shape if n > 1 else ()))
+    assert torch.equal(x.grad, into[0].half()) and torch.equal(w.grad, into[1].half())
