@@ -1,12 +1,14 @@
 """Edges of the model's operators on the GPU.  Tolerances as in test_gpu_model,
 whose helpers these tests take."""
 import copy
+import ctypes
 import math
 import pickle
 
 import pytest
 
 import paper_2511_07035_amd as g
+from paper_2511_07035_amd import model, ops
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
@@ -272,3 +274,108 @@ def test_head_fp16_under_loss_gradients_of_any_size(tokens, vocab, dim, up, redu
     x, w = hidden.detach().requires_grad_(), table.detach().requires_grad_()
     g.linear_cross_entropy(x, w, targets, reduction=reduction).backward(grad.view(targets.shape if n > 1 else ()))
     assert torch.equal(x.grad, into[0].half()) and torch.equal(w.grad, into[1].half())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+@pytest.mark.parametrize("tokens,vocab,dim", [(5, 300, 33), (200, 1000, 64), (300, 1003, 65), (9000, 30_000, 24)])
+def test_head_grad_stays_within_its_workspace(tokens, vocab, dim, dtype):
+    """The bytes that are told serve every reduction, with either gradient or both; what
+    lies behind them is left alone, and what they held before does not matter."""
+    hidden, table, targets = head_inputs(tokens, vocab, dim, dtype)
+    targets[::5] = -1
+    lse, _ = g.head_stats(hidden, table, targets)
+    head = model._head(hidden, table, targets, 1.0, 0, None, 0)[1]
+    L, stream = model._lib(), torch.cuda.current_stream().cuda_stream
+    weights = torch.exp2((-(torch.arange(tokens, device="cuda") % 23)).float())
+    for by in ((True, True), (True, False), (False, True)):
+        out = [torch.empty(n, dim, device="cuda") if b else None for n, b in zip((tokens, vocab), by)]
+        packed = [None if o is None else ops._matrix(o, "", None) for o in out]
+        need = ctypes.c_size_t()
+        assert L.gockpt_head_grad_bytes(head, *packed, ctypes.byref(need)) == 0
+        ws = torch.empty(need.value + 4096, dtype=torch.uint8, device="cuda")
+        assert ws.data_ptr() % 256 == 0
+        for reduction, grad in ((0, weights), (1, weights[3:4].clone()), (2, weights[:1].clone())):
+            got = []
+            for fill in (0, 0xff):
+                ws.fill_(fill)
+                ws[need.value:] = 0x5a
+                for o in out:
+                    if o is not None:
+                        o.fill_(float("nan"))
+                rc = L.gockpt_head_grad(head, lse.data_ptr(), reduction, grad.data_ptr(), *packed, 0, ws.data_ptr(),
+                                        need.value, stream)
+                assert rc == 0, g.lib().gockpt_last_error(None)
+                assert bool((ws[need.value:] == 0x5a).all())
+                got.append([o.clone() for o in out if o is not None])
+            for a, b in zip(*got):
+                assert torch.equal(a, b) and bool(torch.isfinite(a).all())
+
+
+@pytest.mark.parametrize("tokens", [40, 300])
+def test_head_weights_far_apart_replay_from_a_graph(tokens):
+    """fp16 with a weight for each token, captured: replays with other weights are the eager calls."""
+    hidden, table, targets = head_inputs(tokens, 3000, 64, "fp16")
+    weights, into = torch.ones(tokens, device="cuda"), torch.zeros(3000, 64, device="cuda")
+    x = hidden.detach().requires_grad_()
+    w = table.detach().requires_grad_()
+
+    def run():
+        x.grad = None
+        loss = g.linear_cross_entropy(x, w, targets, reduction="none", grad_weight=into)
+        loss.backward(weights)
+        return x.grad, into
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        for _ in range(2):
+            run()
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = run()
+    for k in range(4):
+        weights.copy_(torch.exp2((-(torch.arange(tokens, device="cuda") * (k + 1) % 25)).float()))
+        targets.copy_(torch.roll(targets, 1))
+        targets[k] = -1
+        for t in captured:
+            t.fill_(float("nan"))
+        graph.replay()
+        got = [t.clone() for t in captured]
+        torch.cuda.synchronize()
+        lse, _ = g.head_stats(hidden, table, targets)
+        want = g.head_grad(hidden, table, targets, lse, weights, grad_weight=torch.zeros_like(into))
+        for a, b in zip(got, want):
+            assert torch.equal(a, b), k
+
+
+def test_head_weights_far_apart_over_ranks():
+    """Ranks that split the vocabulary, in fp16 with a weight for each token: their parts
+    of grad_hidden add up to what one rank has, their rows of grad_weight are its rows."""
+    tokens, vocab, dim = 300, 5000, 64
+    hidden, table, targets = head_inputs(tokens, vocab, dim, "fp16", sigma=0.02)
+    targets[::6] = -1
+    weights = torch.exp2((-(torch.arange(tokens, device="cuda") % 25)).float())
+    lse, _ = g.head_stats(hidden, table, targets)
+    want = g.head_grad(hidden, table, targets, lse, weights, grad_hidden=torch.empty(tokens, dim, device="cuda"),
+                       grad_weight=torch.empty(vocab, dim, device="cuda"))
+    total = torch.zeros(tokens, dim, dtype=torch.float64, device="cuda")
+    size = torch.zeros_like(total)
+    for a, b in ((0, 1700), (1700, 1703), (1703, 5000)):
+        gx, gw = g.head_grad(hidden, table[a:b], targets, lse, weights, first_id=a, classes=vocab,
+                             grad_hidden=torch.empty(tokens, dim, device="cuda"),
+                             grad_weight=torch.empty(b - a, dim, device="cuda"))
+        total += gx
+        # the same terms in another order, and other classes' two first tokens: by the sums' errors and z's halves
+        p = torch.exp(hidden.double() @ table[a:b].double().t() - lse.double()[:, None])
+        size += weights[:, None].double() * (p @ table[a:b].double().abs())
+        z = p * (targets >= 0)[:, None] * weights[:, None]
+        at = (targets >= a) & (targets < b)
+        z[at.nonzero()[:, 0], targets[at] - a] -= weights[at]
+        err = (2.0 ** -11 * z.abs() + 2.0 ** -38).t() @ hidden.double().abs()
+        err += 4 * U * (tokens + 2) * (z.abs().t() @ hidden.double().abs())
+        assert_close(gw, want[1][a:b].double(), 2 * err, f"grad_weight from {a}")
+    own = weights[:, None].double() * table[targets.clamp(min=0)].double().abs()
+    err = 2.0 ** -10 * size + 2.0 ** -37 * weights[:, None].double() * table.double().abs().sum(0)
+    err += 4 * U * (vocab + 8) * (size + own)
+    assert_close(total, want[0].double(), err, "grad_hidden")
