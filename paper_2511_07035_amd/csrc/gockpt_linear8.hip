@@ -1,11 +1,11 @@
 // gockpt_linear8.hip -- the linear layer that keeps its input in 8 bits.
 //
 // The weight's gradient restores the input to its 16-bit type (which holds it
-// exactly) in the workspace and multiplies that: 20 and 367 us for 16384 x 2048
-// values by 8192.  A product that took the codes themselves, widened between
-// global memory and LDS, needed 673 us with the conversion before each tile's
-// barrier and 539 with it between the matrix instructions: each of the 32 tiles
-// along the outputs converts all codes again.
+// exactly) in the workspace and multiplies that: 21 and 373 us for 16384 x 2048
+// values by 8192 (395 among a training step's other products).  A product that took
+// the codes themselves, widened between global memory and LDS, needed 673 us with the
+// conversion before each tile's barrier and 539 with it between the matrix
+// instructions: each of the 32 tiles along the outputs converts all codes again.
 #include "gockpt_mma.h"
 #include "gockpt_model_internal.h"
 

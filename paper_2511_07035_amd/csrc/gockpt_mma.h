@@ -27,10 +27,12 @@
 // Over many tiles of k blocks begin at different ones, and take the rest in turn:
 // blocks that march through k together wait for the same few channels of the
 // caches, which hold one k of all rows.  us, all from the first k and in turn (r x c
-// x k): both along k, 8192 x 8192 x 8192 749 and 724, 16384 x 4096 x 5120 501 and 488;
-// R across, 2048 x 16384 x 8192 393 and 384.  With fewer tiles, and where no operand
-// lies along k, blocks in step share more of the L2: 8192 x 16384 x 2048 398 and 407,
-// 4096 x 16384 x 4096 (R across) 366 and 374, 2048 x 8192 x 16384 (both) 367 and 374.
+// x k): both along k, 8192 x 8192 x 8192 766 and 746, 16384 x 4096 x 5120 511 and 492;
+// R across, 2048 x 16384 x 8192 405 and 385.  With fewer tiles, and where no operand
+// lies along k, blocks in step share more of the L2: 8192 x 16384 x 2048 404 and 415,
+// 4096 x 16384 x 4096 (R across) 388 and 397, 2048 x 8192 x 16384 (both) 374 and 379.
+// (Products one at a time, 20 ms apart.  One after another the card's clock falls,
+// and the long ones take 2 to 20% more, those in turn no less than the others.)
 #pragma once
 
 #include "gockpt_ops_internal.h"

@@ -133,11 +133,11 @@ namespace {
 // Microseconds of so many blocks that take k each.  They run in rounds of as many
 // as fit the device; a tile's time has a fixed part (its first copies, its stores)
 // and a part for each k, which is less where a unit has one block instead of two,
-// or the last round leaves units idle and the others their clock.  Measured
-// (wide, mid): 8192 x 8192 x 8192 (r x c x k, both along k) 728, 958; 8192 x 16384 x
-// 2048 412, 510; 4096 x 2048 x 4096 80, 68; 4096 x 1024 x 4096 76, 46; 256 x 128 x
-// 4096 67, 31; 3088 x 3000 x 1160 36, 45; 2048 x 8192 x 16384 (across) 389, 497; 1160 x
-// 3088 x 3000 (across) 62, 40.  Streamed, 32000 x 1 x 4096: 46.
+// or the last round leaves units idle and the others their clock.  Measured, 20 ms
+// apart (wide, mid): 8192 x 8192 x 8192 (r x c x k, both along k) 746, 960; 8192 x 16384
+// x 2048 406, 515; 4096 x 2048 x 4096 83, 66; 4096 x 1024 x 4096 76, 47; 256 x 128 x
+// 4096 68, 32; 3088 x 3000 x 1160 36, 48; 2048 x 8192 x 16384 (across) 373, 475; 1160 x
+// 3088 x 3000 (across) 59, 37.  Streamed, 32000 x 1 x 4096: 46.
 double blocks_us(int shape, bool streamed, int64_t blocks, double k) {
     const auto over = [](int64_t n, int64_t slots) { return static_cast<double>(n) / static_cast<double>(slots); };
     if (shape == kWide) {

@@ -13,13 +13,14 @@
 Conventions are those of the operators around the step: checks raise ValueError
 or GockptError, all arithmetic runs in the library's kernels, calls are queued on
 the current torch stream, or on ``stream`` where no gradient is needed, and what
-a call writes counts as changed in place.  With ``grad_weight`` (of the weight's
-shape: its part of ``Session.grad``, or an fp32 sum) the backward writes the
-weight's gradient there, or adds to it with ``accumulate``, and returns none for
-it; where the weight requires no gradient, nothing is written.  Each backward
-without ``accumulate`` writes every element: of several calls on one weight in a
-step all but the one whose backward runs first (the last one made) accumulate, or
-the program clears the sum first and all of them do.
+a call writes counts as changed in place and must not overlap what it reads.  With
+``grad_weight`` (of the weight's shape: its part of ``Session.grad``, or an fp32
+sum) the backward writes the weight's gradient there, or adds to it with
+``accumulate``, and returns none for it; where the weight requires no gradient,
+nothing is written.  Each backward without ``accumulate`` writes every element: of
+several calls on one weight in a step all but the one whose backward runs first
+(the last one made) accumulate, or the program clears the sum first and all of
+them do.
 """
 from __future__ import annotations
 
